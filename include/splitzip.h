@@ -451,6 +451,119 @@ int splitzip_variant_compress(const void* d_in, uint64_t n_elems, const splitzip
 int splitzip_variant_decompress(const void* d_comp, size_t comp_bytes, uint64_t n_elems, const splitzip_variant* v,
                                 const splitzip_codebook* cb, void* d_out, splitzip_sizes* d_sizes, void* stream);
 
+/* ---- A KV cache in pages: writing it, reading it, attention over it ------------------------------
+ *
+ * What a serving program does with the caches that the calls above pack for
+ * the way: new tokens are written into the pages -- rounded to FP8 as they
+ * are, if the cache holds FP8 words --, every step attends to what is there,
+ * and sequences are read back as BF16.  The words lie as splitzip_paged
+ * describes them, so splitzip_compress_batch_paged and its reverse move such
+ * caches as they are (the scales, one byte per token and head, travel beside
+ * the streams).
+ *
+ * An FP8 word stands for word * 2^(b - 127), b the scale byte of its token and
+ * head (0 to 254).  splitzip_cache_write takes for b the least value from 0 on
+ * for which the largest finite magnitude of the row fits the format (57344
+ * for E5M2, 448 for E4M3), and rounds x * 2^(127 - b) once, to nearest, ties to
+ * even.  Infinities stay infinities in E5M2 and become NaN in E4M3, which has
+ * none; they and NaN do not count for b.
+ *
+ * Nothing that device memory holds (tables, lengths, starts, paths) leads
+ * outside the buffers that the descriptions give; where it is inconsistent
+ * the results are undefined.  No call allocates, synchronises or reads device
+ * memory from the host; all can be captured into a graph, and replayed with
+ * other tables, lengths and starts in the same buffers. */
+
+/* K and V of one layer.  Token t of a page, head h: d_k + page * page_stride_bytes
+ * + t * token_stride_bytes + h * head_stride_bytes, head_dim words; V in the
+ * same way from d_v (pages of both, or K and V side by side in a page). */
+typedef struct {
+  void* d_k;            /* 16-byte aligned */
+  void* d_v;
+  uint8_t* d_k_scales;  /* FP8: byte [page][head][token of the page], pages scale_page_stride_bytes apart, 8-byte aligned; */
+  uint8_t* d_v_scales;  /* BF16: not looked at */
+  uint32_t dtype;       /* splitzip_dtype of the words */
+  uint32_t kv_heads;
+  uint32_t head_dim;    /* 64, 128 or 256 (others: SPLITZIP_ERR_UNSUPPORTED) */
+  uint32_t page_tokens; /* tokens per page: a power of two, at least 8; without a block table any multiple of 8 */
+  uint32_t n_pages;     /* pages in the pool */
+  uint32_t reserved;    /* 0 */
+  uint64_t page_stride_bytes, token_stride_bytes, head_stride_bytes; /* multiples of 16 */
+  uint64_t scale_page_stride_bytes;                                  /* a multiple of 8 */
+} splitzip_cache;
+
+/* The sequences of a call and the rows it has of each.  Rows d_starts[s] to
+ * d_starts[s + 1] - 1 of the call's tensors belong to sequence s and are the
+ * last ones of the d_lens[s] tokens it has in the cache, this call's included:
+ * row i of T is token d_lens[s] - T + i.  (Write: they are where the rows go.
+ * Attention: they have been written before.  Read: T = d_lens[s] reads a whole
+ * sequence.)  Rows in front of token 0 are not written and read as zeros. */
+typedef struct {
+  const uint32_t* d_block_table; /* n_seqs rows of table_stride page indices (at or above n_pages: clamped to the last page);
+                                    NULL: sequence s is page s of the pool */
+  const int32_t* d_starts;       /* n_seqs + 1, ascending from 0 */
+  const int32_t* d_lens;         /* n_seqs; at most table_stride * page_tokens and 2^30 (clamped) */
+  uint32_t table_stride;
+  uint32_t n_seqs;               /* at most 65535 */
+  uint32_t max_rows;             /* the most rows of a sequence and the longest length: what a launch is cut for.  */
+  uint32_t max_len;              /* Larger ones in device memory are right, and slower. */
+} splitzip_seqs;
+
+/* d_k, d_v: n_rows rows of kv_heads x head_dim BF16 words, k_row_stride and
+ * v_row_stride words apart (multiples of 8), 16-byte aligned.  One launch.
+ * splitzip_cache_write fills the rows' tokens and nothing else of the pool;
+ * splitzip_cache_read rounds word * 2^(b - 127) to BF16. */
+int splitzip_cache_write(const splitzip_cache* cache, const splitzip_seqs* seqs, const void* d_k, uint64_t k_row_stride,
+                         const void* d_v, uint64_t v_row_stride, uint32_t n_rows, void* stream);
+int splitzip_cache_read(const splitzip_cache* cache, const splitzip_seqs* seqs, void* d_k, uint64_t k_row_stride, void* d_v,
+                        uint64_t v_row_stride, uint32_t n_rows, void* stream);
+
+/* What a row sees, and how scores are shaped.  With base = d_lens[s] - T:
+ * tokens below base are seen by all rows of the sequence; token base + j by
+ * row i if bit j % 64 of d_tree[row * tree_words + j / 64] is set (bits the
+ * words do not reach are 0) -- the rows of a tree of drafted tokens see their
+ * ancestors and themselves, those of a prefix one another --, without d_tree
+ * if j <= i.  pos of a row is d_positions[row] (in a tree: base + depth) or,
+ * without, base + i; pos of a token is that of its row, below base its number.
+ * A window w > 0 leaves a row the tokens with pos_row - pos_token < w. */
+typedef struct {
+  float scale;                /* x = scale * (q . k) */
+  float softcap;              /* > 0: x = softcap * tanh(x / softcap); 0: none */
+  const float* d_slopes;      /* q_heads, or NULL: x += slope * (pos_token - pos_row), behind the cap */
+  const uint64_t* d_tree;     /* n_rows x tree_words, 8-byte aligned, or NULL */
+  const int32_t* d_positions; /* n_rows, or NULL */
+  uint32_t tree_words;
+  uint32_t window;
+  uint64_t reserved;          /* 0 */
+} splitzip_attention;
+
+/* Attention of the rows of a step -- one token per sequence, or a tree of
+ * drafted tokens, or a piece of a prompt -- over the cache: out = softmax(x) v,
+ * lse = ln sum e^x (nullable).  d_q and d_out: n_rows rows of q_heads x head_dim
+ * BF16 words (q_heads a multiple of kv_heads; query head h reads head
+ * h / (q_heads / kv_heads) of the cache), strides and alignment as above.
+ * Statistics and sums are held in 32 bits, the weights are rounded to BF16 in
+ * front of the product with V.  A row that sees nothing, or nothing but scores
+ * of minus infinity, gets zeros and lse = -infinity.  What a row does not see does
+ * not touch it, whatever it holds.  d_workspace: the parts of long sequences until they are joined,
+ * splitzip_attention_workspace_bytes (an upper bound for every window; 0 for
+ * arguments that a call refuses), 16-byte aligned, no defined value needed;
+ * calls that share one must not overlap in time.  One launch, or two.  The
+ * result is a pure function of the arguments. */
+size_t splitzip_attention_workspace_bytes(const splitzip_cache* cache, const splitzip_seqs* seqs, uint32_t n_rows, uint32_t q_heads);
+int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* seqs, const splitzip_attention* how, const void* d_q,
+                             uint64_t q_row_stride, void* d_out, uint64_t out_row_stride, float* d_lse, uint32_t n_rows,
+                             uint32_t q_heads, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* The accepted path of a tree of drafted tokens becomes the sequence: in every
+ * one of the n_caches caches (a HOST array, read before the call returns; one
+ * geometry, one table: the layers of a model), token base + d_path[s *
+ * path_stride + i] moves to base + i, scales included.  A path ascends
+ * strictly; its first entry that does not, or is no row of the call (-1), ends
+ * it.  Other tokens stay as they are.  One launch for 64 caches. */
+int splitzip_cache_move(const splitzip_cache* caches, uint32_t n_caches, const splitzip_seqs* seqs, const int32_t* d_path,
+                        uint32_t path_stride, uint32_t n_rows, void* stream);
+
 const char* splitzip_strerror(int err);
 int splitzip_version(void);
 

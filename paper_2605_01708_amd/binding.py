@@ -62,6 +62,23 @@ class _CPaged(C.Structure):
                 ("page_stride_bytes", C.c_uint64), ("offset_bytes", C.c_uint64)]
 
 
+class _CCache(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scales", C.c_void_p), ("d_v_scales", C.c_void_p),
+                ("dtype", C.c_uint32), ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("page_tokens", C.c_uint32),
+                ("n_pages", C.c_uint32), ("reserved", C.c_uint32), ("page_stride_bytes", C.c_uint64),
+                ("token_stride_bytes", C.c_uint64), ("head_stride_bytes", C.c_uint64), ("scale_page_stride_bytes", C.c_uint64)]
+
+
+class _CSeqs(C.Structure):
+    _fields_ = [("d_block_table", C.c_void_p), ("d_starts", C.c_void_p), ("d_lens", C.c_void_p), ("table_stride", C.c_uint32),
+                ("n_seqs", C.c_uint32), ("max_rows", C.c_uint32), ("max_len", C.c_uint32)]
+
+
+class _CAttention(C.Structure):
+    _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("d_slopes", C.c_void_p), ("d_tree", C.c_void_p),
+                ("d_positions", C.c_void_p), ("tree_words", C.c_uint32), ("window", C.c_uint32), ("reserved", C.c_uint64)]
+
+
 class Variant(C.Structure):
     """splitzip_variant: one of the formats of the paper's ablations"""
     _fields_ = [("dtype", C.c_uint32), ("code_bits", C.c_uint32), ("k", C.c_uint32), ("escape_mode", C.c_uint32),
@@ -180,6 +197,16 @@ def lib():
         L.splitzip_variant_compress.argtypes = [vp, u64, vrp, cbp, vp, sz, vp, sz, vp, vp]
         L.splitzip_variant_decompress.restype = i
         L.splitzip_variant_decompress.argtypes = [vp, sz, u64, vrp, cbp, vp, vp, vp]
+        chp, sqp = C.POINTER(_CCache), C.POINTER(_CSeqs)
+        for f in (L.splitzip_cache_write, L.splitzip_cache_read):
+            f.restype = i
+            f.argtypes = [chp, sqp, vp, u64, vp, u64, C.c_uint32, vp]
+        L.splitzip_attention_workspace_bytes.restype = sz
+        L.splitzip_attention_workspace_bytes.argtypes = [chp, sqp, C.c_uint32, C.c_uint32]
+        L.splitzip_cache_attention.restype = i
+        L.splitzip_cache_attention.argtypes = [chp, sqp, C.POINTER(_CAttention), vp, u64, vp, u64, vp, C.c_uint32, C.c_uint32, vp, sz, vp]
+        L.splitzip_cache_move.restype = i
+        L.splitzip_cache_move.argtypes = [chp, C.c_uint32, sqp, vp, C.c_uint32, C.c_uint32, vp]
         L.fast = _short_way(L)
         _lib = L
         _leave_fast_in_a_bad_fork()
@@ -875,3 +902,183 @@ class DecompressBatchPaged:
         _check(lib().splitzip_decompress_batch_paged(self.items, self.n, self.dtype, C.byref(self.paging.c),
                                                      sizes.data_ptr() if sizes is not None else None, _stream_ptr(stream)),
                "splitzip_decompress_batch_paged")
+
+
+# ---- a KV cache in pages: writing, reading, attention over it -----------------------------------------
+
+def _ptr(t: torch.Tensor | None):
+    return None if t is None else t.data_ptr()
+
+
+def _strides(t: torch.Tensor):
+    """a tensor's strides, those of dimensions of one element as in a contiguous tensor (there they may be anything)"""
+    out = list(t.stride())
+    for k in range(t.dim() - 1, -1, -1):
+        if t.shape[k] == 1:
+            out[k] = t.shape[k + 1] * out[k + 1] if k + 1 < t.dim() else 1
+    return tuple(out)
+
+
+class KvCache:
+    """splitzip_cache: K and V of one layer.
+
+    k, v: device tensors [pages, page_tokens, kv_heads, head_dim] of the dtype's words (any 2-byte dtype for BF16, 1-byte for FP8), of
+    the same strides, head_dim contiguous: views into a pool will do.  k_scales, v_scales (FP8): uint8 [pages, kv_heads, page_tokens]
+    with contiguous pages."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, dtype: int, k_scales: torch.Tensor | None = None,
+                 v_scales: torch.Tensor | None = None):
+        if k.dim() != 4 or k.shape != v.shape or _strides(k) != _strides(v) or k.stride(3) != 1:
+            raise ValueError("k and v must be [pages, page_tokens, kv_heads, head_dim] with the same strides and a contiguous head_dim")
+        es = _elem_size(dtype)
+        if k.element_size() != es or v.element_size() != es:
+            raise ValueError("k and v must hold words of the dtype")
+        pages, tokens, heads, dim = k.shape
+        scale_stride = 0
+        if dtype != BF16:
+            if k_scales is None or v_scales is None:
+                raise ValueError("an FP8 cache has scales")
+            for s in (k_scales, v_scales):
+                if (tuple(s.shape) != (pages, heads, tokens) or s.element_size() != 1 or _strides(s)[1:] != (tokens, 1)
+                        or _strides(s)[0] != _strides(k_scales)[0]):
+                    raise ValueError("scales must be bytes [pages, kv_heads, page_tokens] with contiguous pages")
+            scale_stride = _strides(k_scales)[0]
+        self.dtype, self.kv_heads, self.head_dim = dtype, heads, dim
+        self._keep = (k, v, k_scales, v_scales)
+        self.c = _CCache(k.data_ptr(), v.data_ptr(), _ptr(k_scales), _ptr(v_scales), dtype, heads, dim, tokens, pages, 0,
+                         *(x * es for x in _strides(k)[:3]), scale_stride)
+
+    @classmethod
+    def zeros(cls, pages: int, page_tokens: int, kv_heads: int, head_dim: int, dtype: int, device="cuda") -> "KvCache":
+        """A cache of its own memory, zeros."""
+        kv = [torch.zeros((pages, page_tokens, kv_heads, head_dim), dtype=torch.bfloat16 if dtype == BF16 else torch.uint8, device=device) for _ in range(2)]
+        scales = [None if dtype == BF16 else torch.zeros((pages, kv_heads, page_tokens), dtype=torch.uint8, device=device) for _ in range(2)]
+        return cls(*kv, dtype, *scales)
+
+    @property
+    def k(self) -> torch.Tensor:
+        return self._keep[0]
+
+    @property
+    def v(self) -> torch.Tensor:
+        return self._keep[1]
+
+    @property
+    def k_scales(self):
+        return self._keep[2]
+
+    @property
+    def v_scales(self):
+        return self._keep[3]
+
+
+class KvCaches:
+    """The marshalled list of a splitzip_cache_move call: caches of one geometry, the layers of a model."""
+
+    def __init__(self, caches):
+        self.n = len(caches)
+        self._keep = list(caches)
+        self.items = (_CCache * max(self.n, 1))(*[c.c for c in caches])
+
+
+class Sequences:
+    """splitzip_seqs: the sequences of a call and its rows of each.
+
+    block_table: int32 [n_seqs, pages of the longest] on the device (None: sequence s is page s); starts: int32 [n_seqs + 1],
+    lens: int32 [n_seqs], on the device.  max_rows, max_len: the most rows of a sequence and the longest length, which the launches
+    are cut for."""
+
+    def __init__(self, block_table: torch.Tensor | None, starts: torch.Tensor, lens: torch.Tensor, max_rows: int, max_len: int):
+        n = lens.numel()
+        for t in (starts, lens):
+            if t.element_size() != 4 or not t.is_contiguous():
+                raise ValueError("starts and lens must be contiguous tensors of 32-bit integers")
+        if starts.numel() != n + 1:
+            raise ValueError("starts must have an entry more than lens")
+        stride = 0
+        if block_table is not None:
+            if block_table.dim() != 2 or block_table.shape[0] != n or block_table.element_size() != 4 or not block_table.is_contiguous():
+                raise ValueError("block_table must be a contiguous tensor [n_seqs, entries] of 32-bit page indices")
+            stride = block_table.shape[1]
+        self._keep = (block_table, starts, lens)
+        self.c = _CSeqs(_ptr(block_table), starts.data_ptr(), lens.data_ptr(), stride, n, max_rows, max_len)
+
+
+class Attention:
+    """splitzip_attention: what a row sees and how its scores are shaped.
+
+    slopes: float32 [q_heads]; tree: 64-bit words [n_rows, words], bit j of a row for row j of its sequence; positions: int32 [n_rows]
+    (contiguous, on the device)."""
+
+    def __init__(self, scale: float, softcap: float = 0.0, window: int = 0, slopes: torch.Tensor | None = None,
+                 tree: torch.Tensor | None = None, positions: torch.Tensor | None = None):
+        if slopes is not None and (slopes.dtype != torch.float32 or not slopes.is_contiguous()):
+            raise ValueError("slopes must be contiguous float32")
+        if tree is not None and (tree.dim() != 2 or tree.element_size() != 8 or not tree.is_contiguous()):
+            raise ValueError("tree must be a contiguous tensor [n_rows, words] of 64-bit words")
+        if positions is not None and (positions.element_size() != 4 or not positions.is_contiguous()):
+            raise ValueError("positions must be a contiguous tensor of 32-bit integers")
+        self._keep = (slopes, tree, positions)
+        self.c = _CAttention(scale, softcap, _ptr(slopes), _ptr(tree), _ptr(positions), 0 if tree is None else tree.shape[1], window, 0)
+
+
+def _rows(t: torch.Tensor, heads: int, dim: int, what: str) -> int:
+    """words from row to row of a tensor [rows, heads, dim] of BF16 words"""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.element_size() != 2 or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"{what} must be [rows, {heads}, {dim}] of 2-byte words with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+def _write_or_read(f, name, cache: KvCache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor, stream):
+    ks, vs = _rows(k, cache.kv_heads, cache.head_dim, "k"), _rows(v, cache.kv_heads, cache.head_dim, "v")
+    if k.shape[0] != v.shape[0]:
+        raise ValueError("k and v must have the same number of rows")
+    _check(f(C.byref(cache.c), C.byref(seqs.c), k.data_ptr(), ks, v.data_ptr(), vs, k.shape[0], _stream_ptr(stream)), name)
+
+
+def cache_write(k: torch.Tensor, v: torch.Tensor, cache: KvCache, seqs: Sequences, stream=None) -> None:
+    """splitzip_cache_write: the BF16 rows k, v [rows, kv_heads, head_dim] become their sequences' last tokens, quantised if the cache is FP8."""
+    _write_or_read(lib().splitzip_cache_write, "splitzip_cache_write", cache, seqs, k, v, stream)
+
+
+def cache_read(cache: KvCache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+    """splitzip_cache_read: the rows' tokens out of the cache, as BF16, into k, v [rows, kv_heads, head_dim]."""
+    _write_or_read(lib().splitzip_cache_read, "splitzip_cache_read", cache, seqs, k, v, stream)
+
+
+def attention_workspace_bytes(cache: KvCache, seqs: Sequences, n_rows: int, q_heads: int) -> int:
+    return int(lib().splitzip_attention_workspace_bytes(C.byref(cache.c), C.byref(seqs.c), n_rows, q_heads))
+
+
+def attention_workspace(cache: KvCache, seqs: Sequences, n_rows: int, q_heads: int, device="cuda") -> torch.Tensor:
+    """A workspace for cache_attention calls of up to n_rows rows over these sequences; one per stream."""
+    return torch.empty(max(attention_workspace_bytes(cache, seqs, n_rows, q_heads), 16), dtype=torch.uint8, device=device)
+
+
+def cache_attention(q: torch.Tensor, cache: KvCache, seqs: Sequences, out: torch.Tensor, workspace: torch.Tensor, how: Attention,
+                    lse: torch.Tensor | None = None, stream=None) -> None:
+    """splitzip_cache_attention: the BF16 rows q [rows, q_heads, head_dim] against their sequences' tokens, into out; lse float32 [rows, q_heads]."""
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, q_heads, head_dim]")
+    rows, heads = q.shape[0], q.shape[1]
+    qs, os_ = _rows(q, heads, cache.head_dim, "q"), _rows(out, heads, cache.head_dim, "out")
+    if out.shape[0] != rows or (lse is not None and (tuple(lse.shape) != (rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous())):
+        raise ValueError("out must have the rows of q, and lse be contiguous float32 [rows, q_heads]")
+    for t, n, what in zip(how._keep, (heads, rows, rows), ("slopes", "tree", "positions")):
+        if t is not None and t.shape[0] != n:
+            raise ValueError(f"{what} must have {n} entries")
+    _check(lib().splitzip_cache_attention(C.byref(cache.c), C.byref(seqs.c), C.byref(how.c), q.data_ptr(), qs, out.data_ptr(), os_, _ptr(lse),
+                                          rows, heads, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                          _stream_ptr(stream)), "splitzip_cache_attention")
+
+
+def cache_move(caches: KvCaches, seqs: Sequences, path: torch.Tensor, n_rows: int | None = None, stream=None) -> None:
+    """splitzip_cache_move: in all the caches, row path[s, i] of sequence s becomes its token base + i; path int32 [n_seqs, entries], -1 ends a
+    path.  n_rows: rows of the call (all that starts says, if None)."""
+    if path.dim() != 2 or path.shape[0] != seqs.c.n_seqs or path.element_size() != 4 or not path.is_contiguous():
+        raise ValueError("path must be a contiguous tensor [n_seqs, entries] of 32-bit integers")
+    _check(lib().splitzip_cache_move(caches.items, caches.n, C.byref(seqs.c), path.data_ptr(), path.shape[1],
+                                     _MOST_ROWS if n_rows is None else n_rows, _stream_ptr(stream)), "splitzip_cache_move")
+
+
+_MOST_ROWS = 1 << 30

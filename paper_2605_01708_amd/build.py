@@ -10,6 +10,7 @@ import warnings
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "splitzip.hip")
+CACHE_SRC = os.path.join(HERE, "csrc", "cache.hip")
 INC = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libsplitzip.so")
 FAST_SRC = os.path.join(HERE, "csrc", "fastcall.cpp")
@@ -24,7 +25,7 @@ HIPCC_FLAGS = [
 
 def build(verbose: bool = False, extra_flags=()) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, *extra_flags, "-I", INC, SRC, "-o", LIB]
+    cmd = [hipcc, *HIPCC_FLAGS, *extra_flags, "-I", INC, SRC, CACHE_SRC, "-o", LIB]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)

@@ -1,0 +1,321 @@
+// SplitZip for MI355X (gfx950): the cache_ entry points of include/splitzip.h -- a KV cache in pages, quantised as it is
+// written, and attention over it -- and the host side of their kernels.  The kernels live in the headers included below:
+//   common.hpp      byte permutes and vector types shared with the codec
+//   cache.hpp       where the words of a token are; writing, reading back, moving an accepted path
+//   attention.hpp   attention of a step's rows, one token or a tree of drafted ones, over everything cached
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "splitzip.h"
+
+namespace {
+
+#include "common.hpp"
+#include "cache.hpp"
+#include "attention.hpp"
+
+bool aligned16(uint64_t x) { return (x & 15u) == 0; }
+bool aligned16(const void* p) { return aligned16((uint64_t)reinterpret_cast<uintptr_t>(p)); }
+bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
+
+int cu_count() {
+  static int cached[64] = {0};
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+  if (!cached[dev]) {
+    int n = 0;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
+    cached[dev] = n;
+  }
+  return cached[dev];
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? SPLITZIP_OK : SPLITZIP_ERR_HIP; }
+
+constexpr uint64_t kMostTokens = 1u << 30;   // of a sequence: token numbers and the steps past them stay in 31 bits
+constexpr uint32_t kMostSeqs = 65535;        // a dimension of a grid
+
+int words_bytes(uint32_t dtype) { return dtype == SPLITZIP_BF16 ? 2 : 1; }
+
+// a geometry's rules; the addresses of the words are looked at where a call has them
+int check_cache(const splitzip_cache* c, bool pointers) {
+  if (!c || c->dtype > SPLITZIP_FP8_E4M3 || c->reserved) return SPLITZIP_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return SPLITZIP_ERR_UNSUPPORTED;
+  if (!c->kv_heads || !c->n_pages || c->page_tokens < 8 || c->page_tokens > kMostTokens) return SPLITZIP_ERR_INVALID_ARG;
+  if (!aligned16(c->page_stride_bytes) || !aligned16(c->token_stride_bytes) || !aligned16(c->head_stride_bytes)) return SPLITZIP_ERR_INVALID_ARG;
+  const uint64_t row = (uint64_t)c->head_dim * words_bytes(c->dtype);
+  if (c->token_stride_bytes < row || c->head_stride_bytes < row) return SPLITZIP_ERR_INVALID_ARG;
+  if (c->dtype != SPLITZIP_BF16 && (c->scale_page_stride_bytes & 7u || c->page_tokens & 7u)) return SPLITZIP_ERR_INVALID_ARG;
+  if (!pointers) return SPLITZIP_OK;
+  if (!c->d_k || !c->d_v || !aligned16(c->d_k) || !aligned16(c->d_v)) return SPLITZIP_ERR_INVALID_ARG;
+  if (c->dtype != SPLITZIP_BF16 && (!c->d_k_scales || !c->d_v_scales || !aligned(c->d_k_scales, 8) || !aligned(c->d_v_scales, 8))) return SPLITZIP_ERR_INVALID_ARG;
+  return SPLITZIP_OK;
+}
+
+int check_seqs(const splitzip_cache* c, const splitzip_seqs* q) {
+  if (!q) return SPLITZIP_ERR_INVALID_ARG;
+  if (q->n_seqs > kMostSeqs) return SPLITZIP_ERR_UNSUPPORTED;
+  if (q->n_seqs && (!q->d_starts || !q->d_lens || !aligned(q->d_starts, 4) || !aligned(q->d_lens, 4) || !aligned(q->d_block_table, 4))) return SPLITZIP_ERR_INVALID_ARG;
+  if (q->d_block_table) {
+    if (!q->table_stride || (c->page_tokens & (c->page_tokens - 1))) return SPLITZIP_ERR_INVALID_ARG;
+  } else if (q->n_seqs > c->n_pages || c->page_tokens & 7u) {
+    return SPLITZIP_ERR_INVALID_ARG;
+  }
+  return SPLITZIP_OK;
+}
+
+Cache device_cache(const splitzip_cache* c, const splitzip_seqs* q) {
+  Cache d;
+  d.k = static_cast<uint8_t*>(c->d_k);
+  d.v = static_cast<uint8_t*>(c->d_v);
+  d.k_scales = c->dtype == SPLITZIP_BF16 ? nullptr : c->d_k_scales;
+  d.v_scales = c->dtype == SPLITZIP_BF16 ? nullptr : c->d_v_scales;
+  d.page_stride = c->page_stride_bytes;
+  d.token_stride = c->token_stride_bytes;
+  d.head_stride = c->head_stride_bytes;
+  d.scale_page_stride = c->scale_page_stride_bytes;
+  d.page_shift = q->d_block_table ? 31u - (uint32_t)__builtin_clz(c->page_tokens) : 30u;
+  d.n_pages = c->n_pages;
+  d.heads = c->kv_heads;
+  return d;
+}
+
+Seqs device_seqs(const splitzip_cache* c, const splitzip_seqs* q, uint32_t n_rows) {
+  Seqs d;
+  d.table = q->d_block_table;
+  d.starts = q->d_starts;
+  d.lens = q->d_lens;
+  d.table_stride = q->table_stride;
+  d.n_seqs = q->n_seqs;
+  d.n_rows = n_rows;
+  const uint64_t reach = q->d_block_table ? (uint64_t)q->table_stride * c->page_tokens : c->page_tokens;
+  d.capacity = (uint32_t)(reach < kMostTokens ? reach : kMostTokens);
+  return d;
+}
+
+bool rows_ok(const void* p, uint64_t stride, uint64_t elems) {
+  return p && aligned16(p) && stride >= elems && stride % 8 == 0 && stride <= (1ull << 40);
+}
+
+// f<KIND, D>() for the cache's kind and width
+template <template <int, int> class F, typename... A>
+int by_kind(const splitzip_cache* c, A... args) {
+#define SPLITZIP_KIND(K)                                          \
+  if (c->dtype == K) {                                            \
+    if (c->head_dim == 64) return F<K, 64>::run(args...);         \
+    if (c->head_dim == 128) return F<K, 128>::run(args...);       \
+    return F<K, 256>::run(args...);                               \
+  }
+  SPLITZIP_KIND(SPLITZIP_BF16)
+  SPLITZIP_KIND(SPLITZIP_FP8_E5M2)
+  SPLITZIP_KIND(SPLITZIP_FP8_E4M3)
+#undef SPLITZIP_KIND
+  return SPLITZIP_ERR_INVALID_ARG;
+}
+
+template <int KIND, int D>
+struct Write {
+  static int run(dim3 grid, hipStream_t st, const RowsArgs* a) {
+    hipLaunchKernelGGL((cache_write_kernel<KIND, D>), grid, dim3(kThreads), 0, st, *a);
+    return launched();
+  }
+};
+template <int KIND, int D>
+struct Read {
+  static int run(dim3 grid, hipStream_t st, const RowsArgs* a) {
+    hipLaunchKernelGGL((cache_read_kernel<KIND, D>), grid, dim3(kThreads), 0, st, *a);
+    return launched();
+  }
+};
+
+template <template <int, int> class F>
+int rows_call(const splitzip_cache* c, const splitzip_seqs* q, void* d_k, uint64_t k_stride, void* d_v, uint64_t v_stride, uint32_t n_rows, void* stream) {
+  int rc = check_cache(c, true);
+  if (rc == SPLITZIP_OK) rc = check_seqs(c, q);
+  if (rc != SPLITZIP_OK) return rc;
+  const uint64_t elems = (uint64_t)c->kv_heads * c->head_dim;
+  if (!q->n_seqs || !n_rows) return SPLITZIP_OK;
+  if (n_rows > kMostTokens) return SPLITZIP_ERR_UNSUPPORTED;
+  if (!rows_ok(d_k, k_stride, elems) || !rows_ok(d_v, v_stride, elems)) return SPLITZIP_ERR_INVALID_ARG;
+  RowsArgs a;
+  a.cache = device_cache(c, q);
+  a.seqs = device_seqs(c, q, n_rows);
+  a.k = static_cast<uint8_t*>(d_k);
+  a.v = static_cast<uint8_t*>(d_v);
+  a.k_stride = 2 * k_stride;
+  a.v_stride = 2 * v_stride;
+  const uint64_t pairs = (uint64_t)(q->max_rows ? q->max_rows : 1) * c->kv_heads, per = kThreads / (c->head_dim / 8);
+  uint64_t wgs = (pairs + per - 1) / per;
+  const uint64_t most = (uint64_t)cu_count() * 32;
+  if (wgs > most) wgs = most;
+  return by_kind<F>(c, dim3((unsigned)wgs, q->n_seqs), static_cast<hipStream_t>(stream), (const RowsArgs*)&a);
+}
+
+// How an attention call is cut: the rows of a (sequence, head of the cache) into tiles of 16 nt, its tokens into parts.
+struct AttentionPlan {
+  uint32_t nt, row_tiles, parts, part_tokens;
+};
+constexpr uint32_t kLeastPart = 256;   // tokens
+// the tokens that a launch is cut for: a window's, where rows see no more
+uint64_t tokens_planned(const splitzip_seqs* q, uint32_t window) {
+  uint64_t tokens = q->max_len < kMostTokens ? q->max_len : kMostTokens;
+  if (window && (uint64_t)window + q->max_rows + kStep < tokens) tokens = (uint64_t)window + q->max_rows + kStep;
+  return tokens ? tokens : 1;
+}
+AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, uint32_t q_heads, uint64_t tokens) {
+  AttentionPlan p;
+  const uint64_t rows = (uint64_t)(q->max_rows ? q->max_rows : 1) * (q_heads / c->kv_heads);
+  p.nt = rows <= 16 ? 1u : rows <= 32 || c->head_dim == 256 ? 2u : 4u;
+  const uint64_t tiles = (rows + 16 * p.nt - 1) / (16 * p.nt);
+  p.row_tiles = (uint32_t)(tiles < 4096 ? tiles : 4096);
+  // workgroups for the chip eight times over
+  const uint64_t units = (uint64_t)q->n_seqs * c->kv_heads * p.row_tiles, want = (uint64_t)cu_count() * 8;
+  const uint64_t parts = units ? (want + units - 1) / units : 1;
+  uint64_t per = (tokens + parts - 1) / parts;
+  per = (per + 127) / 128 * 128;
+  if (per < kLeastPart) per = kLeastPart;
+  p.part_tokens = (uint32_t)per;
+  p.parts = (uint32_t)((tokens + per - 1) / per);
+  return p;
+}
+// the most parts that a call with these tokens or fewer (a window's) is cut into
+uint64_t most_parts(const splitzip_cache* c, const splitzip_seqs* q, uint32_t q_heads) {
+  const AttentionPlan p = plan_attention(c, q, q_heads, 1);
+  const uint64_t units = (uint64_t)q->n_seqs * c->kv_heads * p.row_tiles, want = (uint64_t)cu_count() * 8;
+  const uint64_t parts = units ? (want + units - 1) / units : 1, least = (tokens_planned(q, 0) + kLeastPart - 1) / kLeastPart;
+  return parts < least ? parts : least;
+}
+
+template <int KIND, int D>
+struct Attend {
+  static int run(dim3 grid, uint32_t nt, hipStream_t st, const AttentionArgs* a) {
+    if constexpr (D == 256) {
+      if (nt == 1) hipLaunchKernelGGL((attention_kernel<KIND, D, 1>), grid, dim3(kThreads), 0, st, *a);
+      else hipLaunchKernelGGL((attention_kernel<KIND, D, 2>), grid, dim3(kThreads), 0, st, *a);
+    } else {
+      if (nt == 1) hipLaunchKernelGGL((attention_kernel<KIND, D, 1>), grid, dim3(kThreads), 0, st, *a);
+      else if (nt == 2) hipLaunchKernelGGL((attention_kernel<KIND, D, 2>), grid, dim3(kThreads), 0, st, *a);
+      else hipLaunchKernelGGL((attention_kernel<KIND, D, 4>), grid, dim3(kThreads), 0, st, *a);
+    }
+    return launched();
+  }
+};
+
+uint64_t workspace_of(uint64_t parts, const splitzip_cache* c, uint32_t n_rows, uint32_t q_heads) {
+  return parts <= 1 ? 0 : (uint64_t)n_rows * q_heads * parts * (c->head_dim + 2) * sizeof(float);
+}
+
+}  // namespace
+
+extern "C" {
+
+int splitzip_cache_write(const splitzip_cache* cache, const splitzip_seqs* seqs, const void* d_k, uint64_t k_row_stride, const void* d_v,
+                         uint64_t v_row_stride, uint32_t n_rows, void* stream) {
+  return rows_call<Write>(cache, seqs, const_cast<void*>(d_k), k_row_stride, const_cast<void*>(d_v), v_row_stride, n_rows, stream);
+}
+
+int splitzip_cache_read(const splitzip_cache* cache, const splitzip_seqs* seqs, void* d_k, uint64_t k_row_stride, void* d_v, uint64_t v_row_stride,
+                        uint32_t n_rows, void* stream) {
+  return rows_call<Read>(cache, seqs, d_k, k_row_stride, d_v, v_row_stride, n_rows, stream);
+}
+
+size_t splitzip_attention_workspace_bytes(const splitzip_cache* cache, const splitzip_seqs* seqs, uint32_t n_rows, uint32_t q_heads) {
+  if (check_cache(cache, false) != SPLITZIP_OK || check_seqs(cache, seqs) != SPLITZIP_OK || !q_heads || q_heads % cache->kv_heads) return 0;
+  return (size_t)workspace_of(most_parts(cache, seqs, q_heads), cache, n_rows, q_heads);
+}
+
+int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* seqs, const splitzip_attention* how, const void* d_q,
+                             uint64_t q_row_stride, void* d_out, uint64_t out_row_stride, float* d_lse, uint32_t n_rows, uint32_t q_heads,
+                             void* d_workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_cache(cache, true);
+  if (rc == SPLITZIP_OK) rc = check_seqs(cache, seqs);
+  if (rc != SPLITZIP_OK) return rc;
+  if (!how || !q_heads || q_heads % cache->kv_heads || !(how->softcap >= 0.0f) || how->reserved) return SPLITZIP_ERR_INVALID_ARG;
+  if (!aligned(how->d_slopes, 4) || !aligned(how->d_tree, 8) || !aligned(how->d_positions, 4) || (how->d_tree && !how->tree_words)) return SPLITZIP_ERR_INVALID_ARG;
+  if (!seqs->n_seqs || !n_rows) return SPLITZIP_OK;
+  const uint64_t elems = (uint64_t)q_heads * cache->head_dim;
+  if (n_rows > kMostTokens || elems * 2 > (1ull << 31)) return SPLITZIP_ERR_UNSUPPORTED;
+  const AttentionPlan p = plan_attention(cache, seqs, q_heads, tokens_planned(seqs, how->window));
+  const uint64_t need = workspace_of(p.parts, cache, n_rows, q_heads);
+  if (workspace_bytes < need) return SPLITZIP_ERR_CAPACITY;
+  if (need && (!d_workspace || !aligned16(d_workspace))) return SPLITZIP_ERR_INVALID_ARG;
+  if (!rows_ok(d_q, q_row_stride, elems) || !rows_ok(d_out, out_row_stride, elems) || !aligned(d_lse, 4)) return SPLITZIP_ERR_INVALID_ARG;
+  const uint64_t units = ((uint64_t)p.parts * seqs->n_seqs * cache->kv_heads + 7) / 8 * 8 * p.row_tiles;
+  if (units >> 31) return SPLITZIP_ERR_UNSUPPORTED;
+  AttentionArgs a;
+  a.cache = device_cache(cache, seqs);
+  a.seqs = device_seqs(cache, seqs, n_rows);
+  a.q = static_cast<const uint8_t*>(d_q);
+  a.out = static_cast<uint8_t*>(d_out);
+  a.lse = d_lse;
+  a.q_stride = 2 * q_row_stride;
+  a.out_stride = 2 * out_row_stride;
+  a.slopes = how->d_slopes;
+  a.tree = how->d_tree;
+  a.positions = how->d_positions;
+  a.part_out = static_cast<float*>(d_workspace);
+  a.part_stat = a.part_out + (uint64_t)n_rows * q_heads * p.parts * cache->head_dim;
+  a.scale = how->scale;
+  a.softcap = how->softcap;
+  a.tree_words = how->tree_words;
+  a.window = how->window;
+  a.group = q_heads / cache->kv_heads;
+  a.parts = p.parts;
+  a.part_tokens = p.part_tokens;
+  a.row_tiles = p.row_tiles;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  rc = by_kind<Attend>(cache, dim3((unsigned)units), p.nt, st, (const AttentionArgs*)&a);
+  if (rc != SPLITZIP_OK || p.parts == 1) return rc;
+  const uint64_t outs = (uint64_t)(seqs->max_rows ? seqs->max_rows : 1) * q_heads;
+  const dim3 grid((unsigned)(outs < 16384 ? (outs + kWaves - 1) / kWaves : 4096), seqs->n_seqs);
+  if (cache->head_dim == 64) hipLaunchKernelGGL(attention_join_kernel<64>, grid, dim3(kThreads), 0, st, a);
+  else if (cache->head_dim == 128) hipLaunchKernelGGL(attention_join_kernel<128>, grid, dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL(attention_join_kernel<256>, grid, dim3(kThreads), 0, st, a);
+  return launched();
+}
+
+int splitzip_cache_move(const splitzip_cache* caches, uint32_t n_caches, const splitzip_seqs* seqs, const int32_t* d_path, uint32_t path_stride,
+                        uint32_t n_rows, void* stream) {
+  if (!n_caches) return SPLITZIP_OK;
+  if (!caches) return SPLITZIP_ERR_INVALID_ARG;
+  for (uint32_t k = 0; k < n_caches; ++k) {
+    const splitzip_cache &c = caches[k], &f = caches[0];
+    const int rc = check_cache(&c, true);
+    if (rc != SPLITZIP_OK) return rc;
+    if (c.dtype != f.dtype || c.kv_heads != f.kv_heads || c.head_dim != f.head_dim || c.page_tokens != f.page_tokens || c.n_pages != f.n_pages ||
+        c.page_stride_bytes != f.page_stride_bytes || c.token_stride_bytes != f.token_stride_bytes || c.head_stride_bytes != f.head_stride_bytes ||
+        (c.dtype != SPLITZIP_BF16 && c.scale_page_stride_bytes != f.scale_page_stride_bytes))
+      return SPLITZIP_ERR_INVALID_ARG;
+  }
+  const int rc = check_seqs(caches, seqs);
+  if (rc != SPLITZIP_OK) return rc;
+  if (!seqs->n_seqs || !path_stride || !n_rows) return SPLITZIP_OK;
+  if (!d_path || !aligned(d_path, 4)) return SPLITZIP_ERR_INVALID_ARG;
+  if (n_rows > kMostTokens || (uint64_t)caches->kv_heads * caches->head_dim > (1u << 28)) return SPLITZIP_ERR_UNSUPPORTED;
+  MoveArgs a;
+  a.cache = device_cache(caches, seqs);
+  a.seqs = device_seqs(caches, seqs, n_rows);
+  a.path = d_path;
+  a.path_stride = path_stride;
+  a.row_bytes = caches->head_dim * (uint32_t)words_bytes(caches->dtype);
+  for (uint32_t at = 0; at < n_caches; at += kMoveMax) {
+    const uint32_t n = n_caches - at < kMoveMax ? n_caches - at : kMoveMax;
+    for (uint32_t k = 0; k < n; ++k) {
+      const Cache d = device_cache(caches + at + k, seqs);
+      a.at[k].k = d.k;
+      a.at[k].v = d.v;
+      a.at[k].k_scales = d.k_scales;
+      a.at[k].v_scales = d.v_scales;
+    }
+    for (uint32_t k = n; k < kMoveMax; ++k) a.at[k].k = a.at[k].v = a.at[k].k_scales = a.at[k].v_scales = nullptr;
+    hipLaunchKernelGGL(cache_move_kernel, dim3(2, seqs->n_seqs, n), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+    const int rl = launched();
+    if (rl != SPLITZIP_OK) return rl;
+  }
+  return SPLITZIP_OK;
+}
+
+}  // extern "C"
