@@ -13,16 +13,23 @@
 // the first product in the layout in which the second takes them: lane group g = l / 16 has tokens 4 g .. 4 g + 3 of a
 // 16-token tile, and with the tile's row m standing for token 8 (m / 4) + m % 4 of the 32 (and + 4 in the second
 // tile) these are tokens 8 g .. 8 g + 7, the lane's eight elements of the second product's K dimension.  No score moves between lanes.
-// Both operands come straight from memory into registers, every byte once: K as rows, V as eight tokens times D / 16
-// elements per lane, transposed in registers by byte permutes.
+// K is loaded as rows, V as eight tokens times a few elements per lane, transposed in registers by byte permutes.  FP8 words become BF16
+// on the way, their scale with them.
 //
-// Statistics, outputs and the sums over waves and over the parts of a long sequence are held in 32 bits.  P goes into the second
-// product as BF16, as V does (relative error 2^-9 per token, as that of the BF16 result); the sum of P is taken before that rounding.
+// The running maximum is one that is at most 2^8 short: it is raised (and what was summed rescaled) only when a score would be
+// beyond that, which a wave finds with one comparison and a ballot; weights up to 256 cost nothing in a floating format.  Statistics,
+// outputs and the sums over waves and over the parts of a long sequence are held in 32 bits.  P goes into the second product as
+// BF16, as V does (relative error 2^-8 per token, as that of the BF16 result); its sum is taken before that rounding, since lse is a
+// result in 32 bits.
+//
+// Two kernels: attention_tokens_kernel for up to 16 rows, whose waves take different tokens (memory's speed is all that
+// counts), and attention_rows_kernel, whose waves take different rows of the same tokens, staged in LDS.
 #ifndef SPLITZIP_ATTENTION_HPP
 #define SPLITZIP_ATTENTION_HPP
 
 constexpr uint32_t kStep = 32;          // tokens of a wave at a time
 constexpr float kLowest = -3.0e38f;     // the running maximum before the first score (finite: differences stay numbers)
+constexpr float kSlack = 8.0f;          // what the running maximum may be short of the largest score, in powers of two
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttentionArgs {
@@ -37,7 +44,8 @@ struct AttentionArgs {
   const int32_t* positions;          // [n_rows] or null: base + row
   float* part_out;                   // [n_rows][q_heads][parts][D]
   float* part_stat;                  // [n_rows][q_heads][parts][2]: maximum (of log2), sum
-  float scale, softcap;
+  float scale, softcap;              // scale >= 0: its sign is in flip_q
+  uint32_t flip_q;                   // 0x80008000: the queries change sign
   uint32_t tree_words, window;       // window 0: none
   uint32_t group, parts, part_tokens, row_tiles;
 };
@@ -67,8 +75,100 @@ __device__ inline uint32_t parts_of(const AttentionArgs& a, const Seq& s, int fi
   return min(max(n, 1u), a.parts);
 }
 
+// What a workgroup is to do: a part of the tokens of a (sequence, head of the cache), and tiles of rows tile0, tile0 + row_tiles, ...
+struct Share {
+  Seq s;
+  uint32_t seq, head, part, n_parts, tile0, rows;   // rows: of the matrix product, the sequence's times the group's query heads
+  int begin, end;
+};
+__device__ inline bool share_of(const AttentionArgs& a, uint32_t lane, Share& w) {
+  // workgroups of the same (part, sequence, head) lie 8 apart, on the same XCD
+  const uint32_t of = blockIdx.x / 8 / a.row_tiles;
+  w.tile0 = blockIdx.x / 8 % a.row_tiles;
+  const uint32_t unit = of * 8 + blockIdx.x % 8, pair = unit / a.cache.heads;
+  w.head = unit % a.cache.heads;
+  w.seq = pair % a.seqs.n_seqs;
+  w.part = pair / a.seqs.n_seqs;
+  if (w.part >= a.parts) return false;
+  w.s = seq_at(a.seqs, w.seq);
+  const int first = first_token(a, w.s, lane);
+  w.n_parts = parts_of(a, w.s, first);
+  if (w.part >= w.n_parts) return false;
+  w.begin = first + (int)(w.part * a.part_tokens);
+  w.end = w.part + 1 < w.n_parts ? w.begin + (int)a.part_tokens : w.s.len;   // the last one goes on to the end
+  w.rows = (uint32_t)w.s.rows * a.group;
+  return true;
+}
+
+// The lane's rows (r0 + 16 n + m of the product) and their operand of the first product.
+template <int KIND, int D, int NT>
+struct Rows {
+  int row[NT], pos[NT];   // row of the sequence (-1: none), its position
+  float slope[NT];        // times log2 e
+  bf16x8 q[NT][D / 32];
+  int64_t low_edge;       // tokens up to here may be out of a row's window
+
+  __device__ void load(const AttentionArgs& a, const Share& w, uint32_t r0, uint32_t m, uint32_t g) {
+    low_edge = -0x7fffffffffffffff;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const uint32_t r = r0 + 16 * n + m;
+      const bool have = r < w.rows;
+      row[n] = have ? (int)(r / a.group) : -1;
+      const uint32_t h = w.head * a.group + (have ? r % a.group : 0);
+      pos[n] = have ? position_of(a, w.s, row[n]) : 0;
+      slope[n] = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
+      if (have && a.window) low_edge = max(low_edge, (int64_t)pos[n] - (int64_t)a.window);
+      const uint8_t* at = a.q + (uint64_t)(uint32_t)(w.s.start + max(row[n], 0)) * a.q_stride + 2 * (uint64_t)h * D;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) {
+        // FP8 rows are loaded 16 bytes, two steps, at a time: the same order here
+        const uint32_t d = KIND == SPLITZIP_BF16 ? 32 * t + 8 * g : 64 * (t / 2) + 16 * g + 8 * (t % 2);
+        u32x4 x = {0, 0, 0, 0};
+        if (have) x = *reinterpret_cast<const u32x4*>(at + 2 * d) ^ a.flip_q;
+        q[n][t] = __builtin_bit_cast(bf16x8, x);
+      }
+    }
+    if (a.window) {
+#pragma unroll
+      for (int o = 8; o > 0; o /= 2) low_edge = max(low_edge, (int64_t)__shfl_xor((long long)low_edge, o));
+    }
+  }
+  // whether every row sees every one of the 32 tokens from t0 on
+  __device__ bool see_all(const Share& w, int t0) const { return t0 + (int)kStep <= min(w.s.base, w.s.len) && (int64_t)t0 > low_edge; }
+  // bit e: row n sees token t8 + e
+  __device__ uint32_t seen(const AttentionArgs& a, const Share& w, int n, int t8) const {
+    if (row[n] < 0) return 0;
+    const int behind = min(max(w.s.len - t8, 0), 8), j0 = t8 - w.s.base;   // j0: the row that token t8 is
+    uint32_t bits = (1u << behind) - 1u;
+    if (j0 > -8) {
+      uint32_t b;
+      if (a.tree) {
+        const uint64_t* words = a.tree + (uint64_t)(uint32_t)(w.s.start + row[n]) * a.tree_words;
+        const uint32_t j = (uint32_t)max(j0, 0), at = j / 64, shift = j % 64;
+        uint64_t x = at < a.tree_words ? words[at] >> shift : 0;
+        if (shift > 56 && at + 1 < a.tree_words) x |= words[at + 1] << (64 - shift);
+        b = (uint32_t)x;
+      } else {
+        b = (1u << min(max(row[n] + 1 - max(j0, 0), 0), 8)) - 1u;
+      }
+      if (j0 < 0) b = b << -j0 | ((1u << -j0) - 1u);   // tokens in front of the call's own: all rows see them
+      bits &= b;
+    }
+    if (a.window) {
+#pragma unroll 1
+      for (int e = 0; e < 8; ++e) {
+        const int j = j0 + e, at = j >= 0 && t8 + e < w.s.len ? position_of(a, w.s, j) : t8 + e;
+        if ((int64_t)pos[n] - (int64_t)at >= (int64_t)a.window) bits &= ~(1u << e);
+      }
+    }
+    return bits;
+  }
+};
+
 // the scores' way into the exponent of two
 __device__ inline float shaped(const AttentionArgs& a, float x, float slope_log2, float far) {
+  x *= a.scale;
   if (a.softcap > 0.0f) {
     // tanh(y) = 1 - 2 / (1 + e^2y): its absolute error of 1e-7 times the cap is one of the exponent
     const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e / a.softcap));
@@ -78,333 +178,553 @@ __device__ inline float shaped(const AttentionArgs& a, float x, float slope_log2
 }
 
 __device__ inline f32x4 mfma(const bf16x8& x, const bf16x8& y, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
+__device__ inline bf16x8 as_bf16(const u32x4& x) { return __builtin_bit_cast(bf16x8, x); }
 
-template <int KIND, int D, int NT>
-__global__ void __launch_bounds__(kThreads) attention_kernel(AttentionArgs a) {
-  constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
-  constexpr int KS = D / 32;     // steps of the first product
-  constexpr int DV = D / 16;     // elements of V per lane and token, and tiles of the second product
-  constexpr int kRow = D + 4;    // floats of a row in LDS
-  __shared__ float lds_out[kWaves * 16 * kRow];
-  __shared__ float lds_stat[kWaves][16][2];
-  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, m = lane % 16, g = lane / 16;
-
-  // workgroups of the same (part, sequence, head) lie 8 apart, on the same XCD
-  const uint32_t of = blockIdx.x / 8 / a.row_tiles, tile0 = blockIdx.x / 8 % a.row_tiles;
-  const uint32_t unit = of * 8 + blockIdx.x % 8;
-  const uint32_t head = unit % a.cache.heads, seq = unit / a.cache.heads % a.seqs.n_seqs, part = unit / a.cache.heads / a.seqs.n_seqs;
-  if (part >= a.parts) return;
-  const Seq s = seq_at(a.seqs, seq);
-  const int first = first_token(a, s, lane);
-  const uint32_t n_parts = parts_of(a, s, first);
-  if (part >= n_parts) return;
-  const int begin = first + (int)(part * a.part_tokens);
-  const int end = part + 1 < n_parts ? begin + (int)a.part_tokens : s.len;   // the last one goes on to the end
-  const uint32_t rows = (uint32_t)s.rows * a.group, q_heads = a.cache.heads * a.group;
-
-  for (uint32_t tile = tile0; tile * 16 * NT < rows; tile += a.row_tiles) {
-    // the lane's rows, and their operand of the first product
-    int row[NT], pos[NT];
-    float slope[NT];
-    bf16x8 q[NT][KS];
-    int64_t low_edge = -0x7fffffffffffffff;   // tokens up to here may be out of a row's window
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const uint32_t r = (tile * NT + n) * 16 + m;
-      const bool have = r < rows;
-      row[n] = have ? (int)(r / a.group) : -1;
-      const uint32_t h = head * a.group + (have ? r % a.group : 0);
-      pos[n] = have ? position_of(a, s, row[n]) : 0;
-      slope[n] = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
-      if (have && a.window) low_edge = max(low_edge, (int64_t)pos[n] - (int64_t)a.window);
-      const uint8_t* at = a.q + (uint64_t)(uint32_t)(s.start + max(row[n], 0)) * a.q_stride + 2 * (uint64_t)h * D;
-#pragma unroll
-      for (int t = 0; t < KS; ++t) {
-        // FP8 rows are loaded 16 bytes, two steps, at a time: the same order here
-        const uint32_t d = KIND == SPLITZIP_BF16 ? 32 * t + 8 * g : 64 * (t / 2) + 16 * g + 8 * (t % 2);
-        u32x4 w = {0, 0, 0, 0};
-        if (have) w = *reinterpret_cast<const u32x4*>(at + 2 * d);
-        q[n][t] = __builtin_bit_cast(bf16x8, w);
-      }
-    }
-    if (a.window) {
-#pragma unroll
-      for (int o = 8; o > 0; o /= 2) low_edge = max(low_edge, (int64_t)__shfl_xor((long long)low_edge, o));
-    }
-
-    f32x4 acc[NT][DV];
-    float top[NT], sum[NT];
+// What a wave has of its rows: outputs (tile j of D / 16: an element per lane and register), the sum of the weights of the lane's own
+// tokens and the running maximum, of powers of two.
+template <int D, int NT>
+struct State {
+  f32x4 acc[NT][D / 16];
+  float sum[NT], top[NT];
+  __device__ void clear() {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       top[n] = kLowest;
       sum[n] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < DV; ++j) acc[n][j] = f32x4{0, 0, 0, 0};
+      for (int j = 0; j < D / 16; ++j) acc[n][j] = f32x4{0, 0, 0, 0};
     }
+  }
 
-    for (int t0 = begin + (int)(wave * kStep); t0 < end; t0 += (int)(kWaves * kStep)) {
-      // tokens 8 (m / 4) + .. for K, 8 g + .. for V; those behind the sequence's end are read at its last eight
-      const uint32_t last8 = (uint32_t)(s.len - 1) & ~7u;
-      const uint32_t k8 = min((uint32_t)t0 + 8 * (m / 4), last8), v8 = min((uint32_t)t0 + 8 * g, last8);
-      const uint32_t k_page = page_of_token(a.cache, a.seqs, seq, k8), k_place = place_of_token(a.cache, a.seqs, k8) + m % 4;
-      const uint32_t v_page = page_of_token(a.cache, a.seqs, seq, v8), v_place = place_of_token(a.cache, a.seqs, v8);
-      const uint8_t* k_at = a.cache.k + word_offset(a.cache, k_page, k_place, head);
-      const uint8_t* v_at = a.cache.v + word_offset(a.cache, v_page, v_place, head);
-
-      f32x4 x[NT][2];
+  // The weights of the lane's eight tokens from their scores x (all: every row sees all of them; else seen).
+  template <int KIND>
+  __device__ void weigh(const AttentionArgs& a, const Share& w, const Rows<KIND, D, NT>& r, const f32x4 (&x)[NT][2], bool all,
+                        const uint32_t (&seen)[NT], int t8, bf16x8 (&p)[NT]) {
+    const bool plain = a.softcap == 0.0f && !a.slopes && a.scale > 0.0f;   // powers of two are the scores times c
+    const float c = plain ? a.scale * kLog2e : 1.0f;
+    float y[NT][8], high[NT];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) x[n][0] = x[n][1] = f32x4{0, 0, 0, 0};
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint8_t* at = k_at + 4 * b * a.cache.token_stride;
-        if constexpr (KIND == SPLITZIP_BF16) {
-#pragma unroll
-          for (int t = 0; t < KS; ++t) {
-            const bf16x8 k = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(at + 2 * (32 * t + 8 * g)));
-#pragma unroll
-            for (int n = 0; n < NT; ++n) x[n][b] = mfma(k, q[n][t], x[n][b]);
-          }
-        } else {
-#pragma unroll
-          for (int t = 0; t < KS; t += 2) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(at + 32 * t + 16 * g);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const u32x4 f = {fp8_pair_to_bf16<KIND, false>(w[2 * u]), fp8_pair_to_bf16<KIND, true>(w[2 * u]),
-                               fp8_pair_to_bf16<KIND, false>(w[2 * u + 1]), fp8_pair_to_bf16<KIND, true>(w[2 * u + 1])};
-#pragma unroll
-              for (int n = 0; n < NT; ++n) x[n][b] = mfma(__builtin_bit_cast(bf16x8, f), q[n][t + u], x[n][b]);
-            }
-          }
-        }
-      }
-      // V: DV elements of each of the eight tokens, as BF16; vt[j]: element j of all eight
-      u32x4 vt[DV];
-      {
-        uint32_t w[8][DV / 2];
+      for (int e = 0; e < 8; ++e) y[n][e] = x[n][e / 4][e % 4];
+      if (!plain) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const uint8_t* at = v_at + e * a.cache.token_stride + ES * DV * m;
-          if constexpr (KIND == SPLITZIP_BF16) {
-            __builtin_memcpy(w[e], __builtin_assume_aligned(at, 2 * DV < 16 ? 2 * DV : 16), 2 * DV);
-          } else {
-            uint32_t raw[DV / 4];
-            __builtin_memcpy(raw, __builtin_assume_aligned(at, DV < 16 ? DV : 16), DV);
-#pragma unroll
-            for (int i = 0; i < DV / 4; ++i) {
-              w[e][2 * i] = fp8_pair_to_bf16<KIND, false>(raw[i]);
-              w[e][2 * i + 1] = fp8_pair_to_bf16<KIND, true>(raw[i]);
-            }
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < DV; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) vt[j][i] = byte_perm(w[2 * i + 1][j / 2], w[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-      }
-      // the scales of the lane's eight tokens
-      u32x2 k_scales = {0, 0}, v_scales = {0, 0};
-      if constexpr (KIND != SPLITZIP_BF16) {
-        const uint64_t scale = scale_offset(a.cache, a.seqs, v_page, v_place, head);
-        k_scales = *reinterpret_cast<const u32x2*>(a.cache.k_scales + scale);
-        v_scales = *reinterpret_cast<const u32x2*>(a.cache.v_scales + scale);
-      }
-
-      const bool all = t0 + (int)kStep <= min(s.base, s.len) && (int64_t)t0 > low_edge;   // every row sees every token
-      uint32_t seen[NT];   // bit e: the lane's row sees the lane's token e
-#pragma unroll
-      for (int n = 0; n < NT; ++n) seen[n] = 0xffu;
-      if (!all) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          seen[n] = 0;
-          for (int e = 0; e < 8; ++e) {
-            const int t = t0 + (int)(8 * g) + e, j = t - s.base;
-            bool ok = row[n] >= 0 && t < s.len;
-            if (ok && j >= 0) {
-              if (a.tree) ok = (uint32_t)j / 64 < a.tree_words && (a.tree[(uint64_t)(uint32_t)(s.start + row[n]) * a.tree_words + (uint32_t)j / 64] >> (j % 64) & 1);
-              else ok = j <= row[n];
-            }
-            if (ok && a.window) ok = (int64_t)pos[n] - (int64_t)(j >= 0 ? position_of(a, s, j) : t) < (int64_t)a.window;
-            seen[n] |= (uint32_t)ok << e;
-          }
-        }
-      }
-
-      bf16x8 p[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float v = x[n][e / 4][e % 4] * a.scale;
-          if constexpr (KIND != SPLITZIP_BF16) v *= two_to((int)(k_scales[e / 4] >> (8 * (e % 4)) & 0xffu));
           float far = 0.0f;
           if (a.slopes) {
-            const int t = t0 + (int)(8 * g) + e, j = t - s.base;
-            const int at = j >= 0 && t < s.len ? position_of(a, s, j) : t;
-            far = (float)(pos[n] - at);
+            const int t = t8 + e, j = t - w.s.base;
+            far = (float)(r.pos[n] - (j >= 0 && t < w.s.len ? position_of(a, w.s, j) : t));
           }
-          v = shaped(a, v, slope[n], far);
-          y[e] = seen[n] >> e & 1 ? v : -__builtin_inff();
+          y[n][e] = shaped(a, y[n][e], r.slope[n], far);
         }
-        float high = y[0];
+      }
+      if (!all) {
 #pragma unroll
-        for (int e = 1; e < 8; ++e) high = fmaxf(high, y[e]);
-        high = fmaxf(high, __shfl_xor(high, 16));
-        high = fmaxf(high, __shfl_xor(high, 32));
-        const float now = fmaxf(top[n], high), less = __builtin_amdgcn_exp2f(top[n] - now);
+        for (int e = 0; e < 8; ++e) y[n][e] = seen[n] >> e & 1 ? y[n][e] : -__builtin_inff();
+      }
+      high[n] = fmaxf(fmaxf(fmaxf(y[n][0], y[n][1]), fmaxf(y[n][2], y[n][3])), fmaxf(fmaxf(y[n][4], y[n][5]), fmaxf(y[n][6], y[n][7]))) * c;
+    }
+    bool raise = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) raise |= high[n] > top[n] + kSlack;
+    if (__ballot(raise)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float h = high[n];
+        h = fmaxf(h, __shfl_xor(h, 16));
+        h = fmaxf(h, __shfl_xor(h, 32));
+        const float now = fmaxf(top[n], h), less = __builtin_amdgcn_exp2f(top[n] - now);
         top[n] = now;
         sum[n] *= less;
 #pragma unroll
-        for (int j = 0; j < DV; ++j) acc[n][j] *= less;
-        float w[8];
+        for (int j = 0; j < D / 16; ++j) acc[n][j] *= less;
+      }
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          w[e] = __builtin_amdgcn_exp2f(y[e] - now);
-          sum[n] += w[e];
-          if constexpr (KIND != SPLITZIP_BF16) w[e] *= two_to((int)(v_scales[e / 4] >> (8 * (e % 4)) & 0xffu));
-          if (!(seen[n] >> e & 1)) w[e] = 0.0f;   // whatever a token's scale holds that the row does not see
+    for (int n = 0; n < NT; ++n) {
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[n][i], c, -top[n]));
+      sum[n] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+      p[n] = as_bf16(u32x4{bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7])});
+    }
+  }
+
+  __device__ float total(int n) const {   // of all the wave's tokens
+    const float x = sum[n] + __shfl_xor(sum[n], 16);
+    return x + __shfl_xor(x, 32);
+  }
+  __device__ void add(int j, const bf16x8& v, const bf16x8 (&p)[NT]) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n][j] = mfma(v, p[n], acc[n][j]);
+  }
+  // The same for 32 tokens, from t0 on, that some row does not see; get(j): operand j of V.  Such a token may hold anything, and 0
+  // times an infinity or a NaN is no 0: tokens with such words are taken out of the product, and added one by one to the rows that see
+  // them, from memory (element(j, i): which element the lane has in acc[n][j][i]).
+  template <int KIND, typename V, typename E>
+  __device__ void add_guarded(const AttentionArgs& a, const Share& w, int t0, const V& get, const E& element, const bf16x8 (&p)[NT],
+                              const uint32_t (&seen)[NT], uint32_t m) {
+    u32x4 high = {0, 0, 0, 0};   // per token: 0x80 where an element's exponent is all ones, in any of the lane's
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      const u32x4 v = get(j);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) high[i] |= ((v[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    }
+    uint32_t odd = 0;   // bit e: token e of the lane's eight
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd |= (high[i] >> 15 & 1u) << (2 * i) | high[i] >> 31 << (2 * i + 1);
+#pragma unroll
+    for (int o = 8; o > 0; o /= 2) odd |= (uint32_t)__shfl_xor((int)odd, o);   // in any element
+    u32x4 keep;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) keep[i] = (odd >> (2 * i) & 1 ? 0u : 0xffffu) | (odd >> (2 * i) & 2 ? 0u : 0xffff0000u);
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) add(j, as_bf16(get(j) & keep), p);
+    if (!__ballot(odd != 0)) return;
+#pragma unroll 1
+    for (uint32_t k = 0; k < kStep; ++k) {
+      if (!((uint32_t)__builtin_amdgcn_readlane((int)odd, (int)(k / 8 * 16)) >> (k % 8) & 1)) continue;
+      const uint32_t t = (uint32_t)t0 + k, page = page_of_token(a.cache, a.seqs, w.seq, t), place = place_of_token(a.cache, a.seqs, t);
+      const uint8_t* at = a.cache.v + word_offset(a.cache, page, place, w.head);
+      uint32_t byte = 0;
+      if constexpr (KIND != SPLITZIP_BF16) byte = a.cache.v_scales[scale_offset(a.cache, a.seqs, page, place, w.head)];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const bool mine = (uint32_t)__shfl((int)seen[n], (int)(k / 8 * 16 + m)) >> (k % 8) & 1;
+        const u32x4 all = __builtin_bit_cast(u32x4, p[n]);
+        const uint32_t pair = k / 2 % 4 == 0 ? all[0] : k / 2 % 4 == 1 ? all[1] : k / 2 % 4 == 2 ? all[2] : all[3];
+        const uint32_t half = (uint32_t)__shfl((int)pair, (int)(k / 8 * 16 + m)) >> (16 * (k % 2)) << 16;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t v;
+            if constexpr (KIND == SPLITZIP_BF16) v = reinterpret_cast<const uint16_t*>(at)[element(j, i)];
+            else v = fp8_pair_to_bf16<KIND, false>(at[element(j, i)], byte);
+            if (mine) acc[n][j][i] = __builtin_fmaf(__uint_as_float(half), __uint_as_float(v << 16), acc[n][j][i]);
+          }
+          asm volatile("" ::: "memory");   // (four loads at a time: a rare way, and registers are what the usual one needs)
         }
-        const u32x4 packed = {bf16_pair(w[0], w[1]), bf16_pair(w[2], w[3]), bf16_pair(w[4], w[5]), bf16_pair(w[6], w[7])};
-        p[n] = __builtin_bit_cast(bf16x8, packed);
+      }
+    }
+  }
+};
+
+// bytes of a pair of tokens' elements 2 i, 2 i + 1 (BF16) into the pair of element 2 i and that of 2 i + 1
+__device__ inline uint32_t evens(uint32_t t0, uint32_t t1) { return byte_perm(t1, t0, 0x05040100u); }
+__device__ inline uint32_t odds(uint32_t t0, uint32_t t1) { return byte_perm(t1, t0, 0x07060302u); }
+// halves of a pair of tokens that are among the sequence's
+__device__ inline uint32_t inside(int t, int len) { return (t < len ? 0xffffu : 0u) | (t + 1 < len ? 0xffff0000u : 0u); }
+
+__device__ inline float lse_of(float top, float total) { return total != 0.0f ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff(); }
+__device__ inline float one_over(float total) { return total != 0.0f ? 1.0f / total : 0.0f; }   // (a NaN is no 0)
+
+// Up to 16 rows: the four waves of a workgroup take every fourth 32 tokens of its part, from memory straight into registers,
+// and their outputs meet in LDS at the end.
+template <int KIND, int D>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == 256 ? 2 : 3))) attention_tokens_kernel(AttentionArgs a) {
+  constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
+  constexpr int KS = D / 32;                // steps of the first product
+  constexpr int DV = D / 16;                // elements of V per lane and token, and tiles of the second product
+  constexpr int KW = KS * ES / 2;           // 16-byte loads of a row of K per lane
+  constexpr int VW = DV * ES / 4;           // registers of a token of V per lane
+  constexpr int kRow = D + 4;               // floats of a row in LDS
+  __shared__ float lds_out[kWaves * 16 * kRow];
+  __shared__ float lds_stat[kWaves][16][2];
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, m = lane % 16, g = lane / 16;
+  Share w;
+  if (!share_of(a, lane, w)) return;
+  const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
+  const uint64_t token = a.cache.token_stride;
+
+  for (uint32_t tile = w.tile0; tile * 16 < w.rows; tile += a.row_tiles) {
+    Rows<KIND, D, 1> r;
+    r.load(a, w, tile * 16, m, g);
+    State<D, 1> st;
+    st.clear();
+    // tokens 8 (m / 4) + .. for K, 8 g + .. for V
+    const auto k_group = [&](int t0) { return min((uint32_t)t0 + 8 * (m / 4), last8); };
+    const auto v_group = [&](int t0) { return min((uint32_t)t0 + 8 * g, last8); };
+    int t0 = w.begin + (int)(wave * kStep);
+    uint32_t k_page = 0, v_page = 0;
+    if (t0 < w.end) {
+      k_page = page_of_token(a.cache, a.seqs, w.seq, k_group(t0));
+      v_page = page_of_token(a.cache, a.seqs, w.seq, v_group(t0));
+    }
+#pragma unroll 1
+    for (; t0 < w.end; t0 += (int)(kWaves * kStep)) {
+      const uint32_t k_place = place_of_token(a.cache, a.seqs, k_group(t0)), v_place = place_of_token(a.cache, a.seqs, v_group(t0));
+      const uint8_t* k_at = a.cache.k + word_offset(a.cache, k_page, k_place + m % 4, w.head);
+      const uint8_t* v_at = a.cache.v + word_offset(a.cache, v_page, v_place, w.head);
+      u32x4 k[2][KW];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < KW; ++i) k[b][i] = *reinterpret_cast<const u32x4*>(k_at + 4 * b * token + 64 * i + 16 * g);
+      uint32_t v[8][VW];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) __builtin_memcpy(v[e], __builtin_assume_aligned(v_at + e * token + 4 * VW * m, VW < 4 ? 4 * VW : 16), 4 * VW);
+      // the scales of the lane's groups
+      u32x2 k_scales = {0, 0}, v_scales = {0, 0};
+      if constexpr (ES == 1) {
+        k_scales = *reinterpret_cast<const u32x2*>(a.cache.k_scales + scale_offset(a.cache, a.seqs, k_page, k_place, w.head));
+        v_scales = *reinterpret_cast<const u32x2*>(a.cache.v_scales + scale_offset(a.cache, a.seqs, v_page, v_place, w.head));
+      }
+      if (t0 + (int)(kWaves * kStep) < w.end) {   // the next pages
+        k_page = page_of_token(a.cache, a.seqs, w.seq, k_group(t0 + (int)(kWaves * kStep)));
+        v_page = page_of_token(a.cache, a.seqs, w.seq, v_group(t0 + (int)(kWaves * kStep)));
       }
 
-      if (!all) {
-        // A token that some row does not see may hold anything, and 0 times an infinity or a NaN is no 0: tokens with such
-        // words are taken out of the product, and added one by one to the rows that see them.
-        const int t8 = t0 + (int)(8 * g);
-        uint32_t odd = 0;   // bit e: token e of the lane's eight has such a word in the lane's columns
+      f32x4 x[1][2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          bool any = false;
+      for (int b = 0; b < 2; ++b) {
+        x[0][b] = f32x4{0, 0, 0, 0};
 #pragma unroll
-          for (int j = 0; j < DV; ++j) any |= (vt[j][e / 2] >> (16 * (e % 2)) & 0x7f80u) == 0x7f80u;
-          odd |= (uint32_t)any << e;
-        }
-#pragma unroll
-        for (int o = 8; o > 0; o /= 2) odd |= (uint32_t)__shfl_xor((int)odd, o);   // all columns of the token
-        uint32_t behind = 0;   // tokens behind the end: nobody's
-#pragma unroll
-        for (int e = 0; e < 8; ++e) behind |= (uint32_t)(t8 + e >= s.len) << e;
-        uint32_t keep[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t out2 = (odd | behind) >> (2 * i);
-          keep[i] = (out2 & 1 ? 0u : 0xffffu) | (out2 & 2 ? 0u : 0xffff0000u);
-        }
-        const uint32_t alone = odd & ~behind;
-        if (__ballot(alone != 0)) {
-          for (uint32_t t = 0; t < kStep; ++t) {
-            if (!((uint32_t)__builtin_amdgcn_readlane((int)alone, (int)(t / 8 * 16)) >> (t % 8) & 1)) continue;
-            u32x4 just;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) just[i] = g == t / 8 && i == (int)(t % 8 / 2) ? (t % 2 ? 0xffff0000u : 0xffffu) : 0u;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const bool mine = (uint32_t)__shfl((int)seen[n], (int)(t / 8 * 16 + m)) >> (t % 8) & 1;
-              // (the row's own weight alone: another token's 0 times this one's infinity is a NaN as well)
-              const bf16x8 only = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, p[n]) & just);
-#pragma unroll
-              for (int j = 0; j < DV; ++j) {
-                const f32x4 c = mfma(__builtin_bit_cast(bf16x8, vt[j] & just), only, f32x4{0, 0, 0, 0});
-                if (mine) acc[n][j] += c;
-              }
-            }
+        for (int t = 0; t < KS; ++t) {
+          if constexpr (ES == 2) {
+            x[0][b] = mfma(as_bf16(k[b][t]), r.q[0][t], x[0][b]);
+          } else {
+            const u32x2 words = {k[b][t / 2][t % 2 * 2], k[b][t / 2][t % 2 * 2 + 1]};
+            x[0][b] = mfma(as_bf16(from_fp8<KIND>(words, k_scales[b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
           }
         }
-#pragma unroll
-        for (int j = 0; j < DV; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) vt[j][i] &= keep[i];
       }
+      const bool all = r.see_all(w, t0);
+      const int t8 = t0 + (int)(8 * g);
+      uint32_t seen[1] = {0xffu};
+      if (!all) seen[0] = r.seen(a, w, 0, t8);
+      bf16x8 p[1];
+      st.weigh(a, w, r, x, all, seen, t8, p);
+      u32x4 vt[DV];   // element j of the eight tokens
 #pragma unroll
-      for (int j = 0; j < DV; ++j)
+      for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[n][j] = mfma(__builtin_bit_cast(bf16x8, vt[j]), p[n], acc[n][j]);
+        for (int j = 0; j < DV; j += 2) {
+          uint32_t w0, w1;
+          if constexpr (ES == 2) {
+            w0 = v[2 * i][j / 2];
+            w1 = v[2 * i + 1][j / 2];
+          } else {
+            const uint32_t b0 = v_scales[i / 2] >> (16 * (i % 2)) & 0xffu, b1 = v_scales[i / 2] >> (16 * (i % 2) + 8) & 0xffu;
+            w0 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[2 * i][j / 4], b0) : fp8_pair_to_bf16<KIND, false>(v[2 * i][j / 4], b0);
+            w1 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[2 * i + 1][j / 4], b1) : fp8_pair_to_bf16<KIND, false>(v[2 * i + 1][j / 4], b1);
+          }
+          vt[j][i] = evens(w0, w1);
+          vt[j + 1][i] = odds(w0, w1);
+        }
+      }
+      if (all) {
+#pragma unroll
+        for (int j = 0; j < DV; ++j) st.add(j, as_bf16(vt[j]), p);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t in = inside(t8 + 2 * i, w.s.len);
+#pragma unroll
+          for (int j = 0; j < DV; ++j) vt[j][i] &= in;
+        }
+        st.template add_guarded<KIND>(a, w, t0, [&](int j) { return vt[j]; }, [&](int j, int i) { return DV * (4 * g + i) + j; }, p, seen, m);
+      }
     }
 
     // the four waves' parts of the tokens together
+    lds_barrier();   // (the tile before this one has been read)
+    const float of_wave = st.total(0);
+    if (g == 0) {
+      lds_stat[wave][m][0] = st.top[0];
+      lds_stat[wave][m][1] = of_wave;
+    }
+    // lane (m, g) has elements DV (4 g + i) + j of row m in acc[j][i]
+    float* mine = lds_out + (wave * 16 + m) * kRow + 4 * DV * g;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      sum[n] += __shfl_xor(sum[n], 16);
-      sum[n] += __shfl_xor(sum[n], 32);
-      __syncthreads();
-      if (g == 0) {
-        lds_stat[wave][m][0] = top[n];
-        lds_stat[wave][m][1] = sum[n];
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < DV; j += 4)
+        *reinterpret_cast<f32x4*>(mine + DV * i + j) = f32x4{st.acc[0][j][i], st.acc[0][j + 1][i], st.acc[0][j + 2][i], st.acc[0][j + 3][i]};
+    lds_barrier();
+    const uint32_t r16 = threadIdx.x / 16, c = threadIdx.x % 16, at = tile * 16 + r16;
+    if (at < w.rows) {
+      float high = lds_stat[0][r16][0], total = 0.0f, o[DV];
+#pragma unroll
+      for (int v = 1; v < kWaves; ++v) high = fmaxf(high, lds_stat[v][r16][0]);
+#pragma unroll
+      for (int j = 0; j < DV; ++j) o[j] = 0.0f;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        const float f = __builtin_amdgcn_exp2f(lds_stat[v][r16][0] - high);
+        total += f * lds_stat[v][r16][1];
+#pragma unroll
+        for (int j = 0; j < DV; ++j) o[j] += f * lds_out[(v * 16 + r16) * kRow + DV * c + j];
       }
-      // lane (m, g) has elements 4 DV g + DV i + j of row m in acc[j][i]
-      float* mine = lds_out + (wave * 16 + m) * kRow + 4 * DV * g;
+      const uint32_t q_heads = a.cache.heads * a.group, h = w.head * a.group + at % a.group;
+      const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(at / a.group));
+      if (w.n_parts == 1) {
+        const float f = one_over(total);
+        uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + DV * c);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < DV; j += 2) *reinterpret_cast<uint32_t*>(to + 2 * j) = bf16_pair(o[j] * f, o[j + 1] * f);
+        if (c == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(high, total);
+      } else {
+        const uint64_t place = (out_row * q_heads + h) * a.parts + w.part;
 #pragma unroll
-        for (int j = 0; j < DV; j += 4) *reinterpret_cast<f32x4*>(mine + DV * i + j) = f32x4{acc[n][j][i], acc[n][j + 1][i], acc[n][j + 2][i], acc[n][j + 3][i]};
-      __syncthreads();
-      const uint32_t r = threadIdx.x / 16, c = threadIdx.x % 16, at = (tile * NT + n) * 16 + r;
-      if (at < rows) {
-        float high = lds_stat[0][r][0], total = 0.0f, o[DV];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) high = fmaxf(high, lds_stat[w][r][0]);
-#pragma unroll
-        for (int j = 0; j < DV; ++j) o[j] = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          const float f = __builtin_amdgcn_exp2f(lds_stat[w][r][0] - high);
-          total += f * lds_stat[w][r][1];
-#pragma unroll
-          for (int j = 0; j < DV; ++j) o[j] += f * lds_out[(w * 16 + r) * kRow + DV * c + j];
-        }
-        const uint32_t i = at / a.group, h = head * a.group + at % a.group;
-        const uint64_t out_row = (uint64_t)(uint32_t)(s.start + (int)i);
-        if (n_parts == 1) {
-          const float f = total != 0.0f ? 1.0f / total : 0.0f;   // (a NaN is no 0)
-          uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + DV * c);
-#pragma unroll
-          for (int j = 0; j < DV; j += 2) *reinterpret_cast<uint32_t*>(to + 2 * j) = bf16_pair(o[j] * f, o[j + 1] * f);
-          if (c == 0 && a.lse) a.lse[out_row * q_heads + h] = total != 0.0f ? (high + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff();
-        } else {
-          const uint64_t place = (out_row * q_heads + h) * a.parts + part;
-#pragma unroll
-          for (int j = 0; j < DV; j += 4) *reinterpret_cast<f32x4*>(a.part_out + place * D + DV * c + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
-          if (c == 0) {
-            a.part_stat[2 * place] = high;
-            a.part_stat[2 * place + 1] = total;
-          }
+        for (int j = 0; j < DV; j += 4) *reinterpret_cast<f32x4*>(a.part_out + place * D + DV * c + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
+        if (c == 0) {
+          a.part_stat[2 * place] = high;
+          a.part_stat[2 * place + 1] = total;
         }
       }
     }
   }
 }
 
-// The parts of a sequence together: a wave per row and query head.
+// More rows: the W waves of a workgroup take 16 NT rows each of the same tokens.  Those are staged in LDS, 32 KB at a time and twice
+// over, as the 32 operands of the matrix instruction that they are (lane after lane, 16 bytes each: written and read without
+// a bank conflict), FP8 words converted and V transposed once for all waves.  Staging is dealt out as four pieces of K and four of V, four
+// operands each; a wave asks for its pieces of the next tokens before it works on these.
+template <int KIND, int D>
+struct Stage {
+  static constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
+  static constexpr int KS = D / 32, DV = D / 16;
+  static constexpr int kTokens = 8192 / D;
+  u32x4 k[2 * ES];      // rows of K: operands 4 s .. 4 s + 3, two of them in 16 bytes of FP8
+  uint32_t v[8][ES];    // four elements of eight tokens
+  u32x2 scales;
+
+  // piece s of K: tiles of 16 tokens and steps, operand f = 4 s + i being step f % KS of tile f / KS
+  __device__ static uint32_t k_group(uint32_t s, uint32_t m) { return 4 * s / KS / 2 * 32 + 8 * (m / 4); }
+  __device__ void load_k(const Cache& c, const Seqs& q, uint32_t page, uint32_t t8, uint32_t head, uint32_t s, uint32_t m, uint32_t g) {
+    const uint32_t place = place_of_token(c, q, t8);
+    const uint8_t* at = c.k + word_offset(c, page, place + m % 4, head) + 16 * g;
+#pragma unroll
+    for (int i = 0; i < 2 * ES; ++i) {
+      const uint32_t f = 4 * s + (ES == 2 ? i : 2 * i);
+      k[i] = *reinterpret_cast<const u32x4*>(at + f / KS % 2 * 4 * c.token_stride + (ES == 2 ? f % KS : f % KS / 2) * 64);
+    }
+    if constexpr (ES == 1) scales = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, q, page, place, head));
+  }
+  __device__ void store_k(u32x4* to, uint32_t s, uint32_t m) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (ES == 2) {
+        to[64 * (4 * s + i)] = k[i];
+      } else {
+        const uint32_t pair = (4 * s + i) / KS % 2 ? scales[1] : scales[0];
+        to[64 * (4 * s + i)] = from_fp8<KIND>(u32x2{k[i / 2][i % 2 * 2], k[i / 2][i % 2 * 2 + 1]}, pair >> (8 * (m % 4)) & 0xffu);
+      }
+    }
+  }
+  // piece s of V: 64 elements (block s % (D / 64)) of 32 tokens; a lane has elements 4 m .. 4 m + 3 of them of tokens 8 g ..
+  __device__ static uint32_t v_group(uint32_t s, uint32_t g) { return s / (D / 64) * 32 + 8 * g; }
+  __device__ void load_v(const Cache& c, const Seqs& q, uint32_t page, uint32_t t8, uint32_t head, uint32_t s, uint32_t m) {
+    const uint32_t place = place_of_token(c, q, t8);
+    const uint8_t* at = c.v + word_offset(c, page, place, head) + ES * (64 * (s % (D / 64)) + 4 * m);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) __builtin_memcpy(v[e], __builtin_assume_aligned(at + e * c.token_stride, 4 * ES), 4 * ES);
+    if constexpr (ES == 1) scales = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, q, page, place, head));
+  }
+  __device__ void store_v(u32x4* to, uint32_t s, int t8, int len, bool inner) const {
+    u32x4 vt[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t x0[2], x1[2];
+      if constexpr (ES == 2) {
+        x0[0] = v[2 * i][0];
+        x0[1] = v[2 * i][1];
+        x1[0] = v[2 * i + 1][0];
+        x1[1] = v[2 * i + 1][1];
+      } else {
+        const uint32_t b0 = scales[i / 2] >> (16 * (i % 2)) & 0xffu, b1 = scales[i / 2] >> (16 * (i % 2) + 8) & 0xffu;
+        x0[0] = fp8_pair_to_bf16<KIND, false>(v[2 * i][0], b0);
+        x0[1] = fp8_pair_to_bf16<KIND, true>(v[2 * i][0], b0);
+        x1[0] = fp8_pair_to_bf16<KIND, false>(v[2 * i + 1][0], b1);
+        x1[1] = fp8_pair_to_bf16<KIND, true>(v[2 * i + 1][0], b1);
+      }
+      const uint32_t in = inner ? 0xffffffffu : inside(t8 + 2 * i, len);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        vt[2 * j][i] = evens(x0[j], x1[j]) & in;
+        vt[2 * j + 1][i] = odds(x0[j], x1[j]) & in;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[64 * (16 + 4 * s + j)] = vt[j];
+  }
+};
+
+template <int KIND, int D, int W, int NT>
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) attention_rows_kernel(AttentionArgs a) {
+  using S = Stage<KIND, D>;
+  constexpr int KS = S::KS, DV = S::DV, kTokens = S::kTokens;
+  constexpr bool kBoth = W == 4;   // a wave stages a piece of K and one of V; else waves 0 .. 3 K, the others V
+  static_assert(W == 4 || W == 8, "four pieces of K and four of V");
+  __shared__ u32x4 lds[2][32 * 64];
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, m = lane % 16, g = lane / 16;
+  Share w;
+  if (!share_of(a, lane, w)) return;
+  const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;
+  const uint32_t piece = wave % 4;
+  const bool of_k = kBoth || wave < 4, of_v = kBoth || wave >= 4;
+
+  for (uint32_t tile = w.tile0; tile * 16 * NT * W < w.rows; tile += a.row_tiles) {
+    const uint32_t r0 = (tile * W + wave) * 16 * NT;
+    const bool active = r0 < w.rows;
+    Rows<KIND, D, NT> r;
+    State<D, NT> st;
+    S sk, sv;
+    const auto k8 = [&](int t0) { return min((uint32_t)t0 + S::k_group(piece, m), last8); };
+    const auto v8 = [&](int t0) { return min((uint32_t)t0 + S::v_group(piece, g), last8); };
+    uint32_t k_page = 0, v_page = 0;
+    const auto ask_pages = [&](int t0) {
+      if (t0 >= w.end) return;
+      if (of_k) k_page = page_of_token(a.cache, a.seqs, w.seq, k8(t0));
+      if (of_v) v_page = page_of_token(a.cache, a.seqs, w.seq, v8(t0));
+    };
+    const auto ask = [&](int t0) {
+      if (t0 >= w.end) return;
+      if (of_k) sk.load_k(a.cache, a.seqs, k_page, k8(t0), w.head, piece, m, g);
+      if (of_v) sv.load_v(a.cache, a.seqs, v_page, v8(t0), w.head, piece, m);
+    };
+    ask_pages(w.begin);
+    ask(w.begin);
+    ask_pages(w.begin + kTokens);
+    r.load(a, w, r0, m, g);
+    st.clear();
+    int buf = 0;
+#pragma unroll 1
+    for (int t0 = w.begin; t0 < w.end; t0 += kTokens, buf ^= 1) {
+      if (of_k) sk.store_k(lds[buf] + lane, piece, m);
+      if (of_v) sv.store_v(lds[buf] + lane, piece, t0 + (int)S::v_group(piece, g), w.s.len, t0 + kTokens <= w.s.len);
+      ask(t0 + kTokens);
+      ask_pages(t0 + 2 * kTokens);
+      lds_barrier();   // one is enough: who writes the other half has passed it, so nobody reads that half any more
+      if (!active) continue;
+      const u32x4* at = lds[buf] + lane;
+#pragma unroll 1
+      for (int u = 0; u < kTokens / (int)kStep; ++u) {
+        const int tu = t0 + u * (int)kStep;
+        if (tu >= w.end) break;
+        f32x4 x[NT][2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) x[n][b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int t = 0; t < KS; ++t) {
+            const bf16x8 k = as_bf16(at[64 * ((2 * u + b) * KS + t)]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) x[n][b] = mfma(k, r.q[n][t], x[n][b]);
+          }
+        }
+        const bool all = r.see_all(w, tu);
+        const int t8 = tu + (int)(8 * g);
+        uint32_t seen[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) seen[n] = all ? 0xffu : r.seen(a, w, n, t8);
+        bf16x8 p[NT];
+        st.weigh(a, w, r, x, all, seen, t8, p);
+          const u32x4* v = at + 64 * (16 + u * DV);
+        if (all) {
+#pragma unroll
+          for (int j = 0; j < DV; ++j) st.add(j, as_bf16(v[64 * j]), p);
+        } else {
+          st.template add_guarded<KIND>(a, w, tu, [&](int j) { return v[64 * j]; },
+                                        [&](int j, int i) { return 64 * (j / 4) + 16 * g + 4 * i + j % 4; }, p, seen, m);
+        }
+      }
+    }
+    lds_barrier();   // the next tile of rows writes where these tokens are
+
+    // lane (m, g) has elements 64 b + 16 g + 4 i + j of row m in acc[4 b + j][i]
+    const uint32_t q_heads = a.cache.heads * a.group;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const uint32_t row = r0 + 16 * n + m;
+      const float total = st.total(n);
+      if (row >= w.rows) continue;
+      const uint32_t h = w.head * a.group + row % a.group;
+      const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(row / a.group));
+      if (w.n_parts == 1) {
+        const float f = one_over(total);
+        uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + 16 * g);
+#pragma unroll
+        for (int b = 0; b < D / 64; ++b) {
+          u32x4 o[2];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            o[i / 2][i % 2 * 2] = bf16_pair(st.acc[n][4 * b][i] * f, st.acc[n][4 * b + 1][i] * f);
+            o[i / 2][i % 2 * 2 + 1] = bf16_pair(st.acc[n][4 * b + 2][i] * f, st.acc[n][4 * b + 3][i] * f);
+          }
+          *reinterpret_cast<u32x4*>(to + 128 * b) = o[0];
+          *reinterpret_cast<u32x4*>(to + 128 * b + 16) = o[1];
+        }
+        if (g == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(st.top[n], total);
+      } else {
+        const uint64_t place = (out_row * q_heads + h) * a.parts + w.part;
+        float* to = a.part_out + place * D + 16 * g;
+#pragma unroll
+        for (int b = 0; b < D / 64; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<f32x4*>(to + 64 * b + 4 * i) = f32x4{st.acc[n][4 * b][i], st.acc[n][4 * b + 1][i], st.acc[n][4 * b + 2][i], st.acc[n][4 * b + 3][i]};
+        if (g == 0) {
+          a.part_stat[2 * place] = st.top[n];
+          a.part_stat[2 * place + 1] = total;
+        }
+      }
+    }
+  }
+}
+
+// The parts of a sequence together: a workgroup per row and query head.  A thread takes four elements of every (1024 / D)-th part.
 template <int D>
 __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs a) {
-  constexpr int PER = D / 64;
+  constexpr uint32_t kAcross = D / 4, kDown = kThreads / kAcross;
+  __shared__ f32x4 lds_out[kThreads];
+  __shared__ float lds_sum[kDown], lds_top[kWaves];
   const uint32_t lane = threadIdx.x % 64, q_heads = a.cache.heads * a.group;
   const Seq s = seq_at(a.seqs, blockIdx.y);
   const uint32_t n_parts = parts_of(a, s, first_token(a, s, lane));
   if (n_parts == 1) return;   // written already
-  for (uint32_t u = blockIdx.x * kWaves + threadIdx.x / 64; u < (uint32_t)s.rows * q_heads; u += gridDim.x * kWaves) {
+  const uint32_t across = threadIdx.x % kAcross, down = threadIdx.x / kAcross;
+  for (uint32_t u = blockIdx.x; u < (uint32_t)s.rows * q_heads; u += gridDim.x) {
     const uint64_t out_row = (uint64_t)(uint32_t)(s.start + (int)(u / q_heads)), h = u % q_heads;
     const uint64_t place = (out_row * q_heads + h) * a.parts;
+    const float* stat = a.part_stat + 2 * place;
+    const float* from = a.part_out + place * D + 4 * across;
     float high = kLowest;
-    for (uint32_t p = 0; p < n_parts; ++p) high = fmaxf(high, a.part_stat[2 * (place + p)]);
-    float total = 0.0f, o[PER] = {};
-    for (uint32_t p = 0; p < n_parts; ++p) {
-      const float f = __builtin_amdgcn_exp2f(a.part_stat[2 * (place + p)] - high);
-      total += f * a.part_stat[2 * (place + p) + 1];
+    for (uint32_t p = threadIdx.x; p < n_parts; p += kThreads) high = fmaxf(high, stat[2 * p]);
 #pragma unroll
-      for (int j = 0; j < PER; ++j) o[j] += f * a.part_out[(place + p) * D + PER * lane + j];
-    }
-    const float f = total != 0.0f ? 1.0f / total : 0.0f;
-    uint8_t* to = a.out + out_row * a.out_stride + 2 * (h * D + PER * lane);
+    for (int o = 32; o > 0; o /= 2) high = fmaxf(high, __shfl_xor(high, o));
+    __syncthreads();   // (the row before this one has been read)
+    if (lane == 0) lds_top[threadIdx.x / 64] = high;
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const __bf16 b = (__bf16)(o[j] * f);
-      *reinterpret_cast<__bf16*>(to + 2 * j) = b;
+    for (int k = 0; k < kWaves; ++k) high = fmaxf(high, lds_top[k]);
+    float total = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+#pragma unroll 4
+    for (uint32_t p = down; p < n_parts; p += kDown) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(from + (uint64_t)p * D);
+      const float f = __builtin_amdgcn_exp2f(stat[2 * p] - high);
+      total += f * stat[2 * p + 1];
+      o += f * x;
     }
-    if (lane == 0 && a.lse) a.lse[out_row * q_heads + h] = total != 0.0f ? (high + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff();
+    lds_out[threadIdx.x] = o;
+    if (across == 0) lds_sum[down] = total;
+    __syncthreads();
+    if (down == 0) {
+#pragma unroll
+      for (uint32_t k = 1; k < kDown; ++k) {
+        o += lds_out[k * kAcross + across];
+        total += lds_sum[k];
+      }
+      const float f = one_over(total);
+      uint32_t* to = reinterpret_cast<uint32_t*>(a.out + out_row * a.out_stride + 2 * (h * D + 4 * across));
+      to[0] = bf16_pair(o[0] * f, o[1] * f);
+      to[1] = bf16_pair(o[2] * f, o[3] * f);
+      if (across == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(high, total);
+    }
   }
 }
 

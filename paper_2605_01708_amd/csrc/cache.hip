@@ -154,9 +154,10 @@ int rows_call(const splitzip_cache* c, const splitzip_seqs* q, void* d_k, uint64
   return by_kind<F>(c, dim3((unsigned)wgs, q->n_seqs), static_cast<hipStream_t>(stream), (const RowsArgs*)&a);
 }
 
-// How an attention call is cut: the rows of a (sequence, head of the cache) into tiles of 16 nt, its tokens into parts.
+// How an attention call is cut: which kernel, the rows of a (sequence, head of the cache) into tiles, its tokens into parts.
 struct AttentionPlan {
-  uint32_t nt, row_tiles, parts, part_tokens;
+  uint32_t waves, nt;   // 0: attention_tokens_kernel; else attention_rows_kernel with so many waves of 16 nt rows
+  uint32_t row_tiles, parts, part_tokens;
 };
 constexpr uint32_t kLeastPart = 256;   // tokens
 // the tokens that a launch is cut for: a window's, where rows see no more
@@ -165,15 +166,25 @@ uint64_t tokens_planned(const splitzip_seqs* q, uint32_t window) {
   if (window && (uint64_t)window + q->max_rows + kStep < tokens) tokens = (uint64_t)window + q->max_rows + kStep;
   return tokens ? tokens : 1;
 }
+// the parts that would fill the chip
+uint64_t parts_wanted(const splitzip_cache* c, const splitzip_seqs* q, const AttentionPlan& p) {
+  const uint64_t units = (uint64_t)q->n_seqs * c->kv_heads * p.row_tiles, want = (uint64_t)cu_count() * (p.waves == 8 ? 2 : 4);
+  return units ? (want + units - 1) / units : 1;
+}
 AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, uint32_t q_heads, uint64_t tokens) {
   AttentionPlan p;
   const uint64_t rows = (uint64_t)(q->max_rows ? q->max_rows : 1) * (q_heads / c->kv_heads);
-  p.nt = rows <= 16 ? 1u : rows <= 32 || c->head_dim == 256 ? 2u : 4u;
-  const uint64_t tiles = (rows + 16 * p.nt - 1) / (16 * p.nt);
+  uint64_t tile = 16;
+  p.waves = 0;
+  p.nt = 1;
+  if (rows > 16) {
+    p.waves = rows <= (c->head_dim == 256 ? 64 : 128) ? 4 : 8;
+    p.nt = rows <= 64 || c->head_dim == 256 ? 1 : 2;
+    tile = 16ull * p.nt * p.waves;
+  }
+  const uint64_t tiles = (rows + tile - 1) / tile;
   p.row_tiles = (uint32_t)(tiles < 4096 ? tiles : 4096);
-  // workgroups for the chip eight times over
-  const uint64_t units = (uint64_t)q->n_seqs * c->kv_heads * p.row_tiles, want = (uint64_t)cu_count() * 8;
-  const uint64_t parts = units ? (want + units - 1) / units : 1;
+  const uint64_t parts = parts_wanted(c, q, p);
   uint64_t per = (tokens + parts - 1) / parts;
   per = (per + 127) / 128 * 128;
   if (per < kLeastPart) per = kLeastPart;
@@ -183,23 +194,20 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
 }
 // the most parts that a call with these tokens or fewer (a window's) is cut into
 uint64_t most_parts(const splitzip_cache* c, const splitzip_seqs* q, uint32_t q_heads) {
-  const AttentionPlan p = plan_attention(c, q, q_heads, 1);
-  const uint64_t units = (uint64_t)q->n_seqs * c->kv_heads * p.row_tiles, want = (uint64_t)cu_count() * 8;
-  const uint64_t parts = units ? (want + units - 1) / units : 1, least = (tokens_planned(q, 0) + kLeastPart - 1) / kLeastPart;
+  const uint64_t parts = parts_wanted(c, q, plan_attention(c, q, q_heads, 1)), least = (tokens_planned(q, 0) + kLeastPart - 1) / kLeastPart;
   return parts < least ? parts : least;
 }
 
 template <int KIND, int D>
 struct Attend {
-  static int run(dim3 grid, uint32_t nt, hipStream_t st, const AttentionArgs* a) {
-    if constexpr (D == 256) {
-      if (nt == 1) hipLaunchKernelGGL((attention_kernel<KIND, D, 1>), grid, dim3(kThreads), 0, st, *a);
-      else hipLaunchKernelGGL((attention_kernel<KIND, D, 2>), grid, dim3(kThreads), 0, st, *a);
-    } else {
-      if (nt == 1) hipLaunchKernelGGL((attention_kernel<KIND, D, 1>), grid, dim3(kThreads), 0, st, *a);
-      else if (nt == 2) hipLaunchKernelGGL((attention_kernel<KIND, D, 2>), grid, dim3(kThreads), 0, st, *a);
-      else hipLaunchKernelGGL((attention_kernel<KIND, D, 4>), grid, dim3(kThreads), 0, st, *a);
-    }
+  template <int W, int NT>
+  static void rows(dim3 grid, hipStream_t st, const AttentionArgs* a) {
+    hipLaunchKernelGGL((attention_rows_kernel<KIND, D, W, NT>), grid, dim3(64 * W), 0, st, *a);
+  }
+  static int run(dim3 grid, uint32_t waves, uint32_t nt, hipStream_t st, const AttentionArgs* a) {
+    if (!waves) hipLaunchKernelGGL((attention_tokens_kernel<KIND, D>), grid, dim3(kThreads), 0, st, *a);
+    else if constexpr (D == 256) waves == 4 ? rows<4, 1>(grid, st, a) : rows<8, 1>(grid, st, a);
+    else nt == 1 ? rows<4, 1>(grid, st, a) : waves == 4 ? rows<4, 2>(grid, st, a) : rows<8, 2>(grid, st, a);
     return launched();
   }
 };
@@ -258,7 +266,8 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   a.positions = how->d_positions;
   a.part_out = static_cast<float*>(d_workspace);
   a.part_stat = a.part_out + (uint64_t)n_rows * q_heads * p.parts * cache->head_dim;
-  a.scale = how->scale;
+  a.scale = how->scale < 0.0f ? -how->scale : how->scale;
+  a.flip_q = how->scale < 0.0f ? 0x80008000u : 0u;
   a.softcap = how->softcap;
   a.tree_words = how->tree_words;
   a.window = how->window;
@@ -267,10 +276,10 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   a.part_tokens = p.part_tokens;
   a.row_tiles = p.row_tiles;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  rc = by_kind<Attend>(cache, dim3((unsigned)units), p.nt, st, (const AttentionArgs*)&a);
+  rc = by_kind<Attend>(cache, dim3((unsigned)units), p.waves, p.nt, st, (const AttentionArgs*)&a);
   if (rc != SPLITZIP_OK || p.parts == 1) return rc;
   const uint64_t outs = (uint64_t)(seqs->max_rows ? seqs->max_rows : 1) * q_heads;
-  const dim3 grid((unsigned)(outs < 16384 ? (outs + kWaves - 1) / kWaves : 4096), seqs->n_seqs);
+  const dim3 grid((unsigned)(outs < 8192 ? outs : 8192), seqs->n_seqs);
   if (cache->head_dim == 64) hipLaunchKernelGGL(attention_join_kernel<64>, grid, dim3(kThreads), 0, st, a);
   else if (cache->head_dim == 128) hipLaunchKernelGGL(attention_join_kernel<128>, grid, dim3(kThreads), 0, st, a);
   else hipLaunchKernelGGL(attention_join_kernel<256>, grid, dim3(kThreads), 0, st, a);

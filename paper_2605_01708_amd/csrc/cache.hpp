@@ -71,7 +71,8 @@ struct RowsArgs {
   uint64_t k_stride, v_stride;   // bytes from row to row
 };
 
-__device__ inline float two_to(int byte) { return __uint_as_float((uint32_t)byte << 23); }   // 2^(byte - 127) for 1..254, 0 for 0
+// waits for the wave's own accesses to LDS, not for its loads from memory, which stay on their way
+__device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // largest finite magnitude of eight BF16 words, as bits (which order as the magnitudes do)
 __device__ inline uint32_t largest8(const u32x4& w) {
@@ -123,12 +124,14 @@ __device__ inline u32x2 to_fp8(const u32x4& w, int byte) {
   return out;
 }
 
-// The words of a pair of bytes (the low or the high two of a register) as BF16, exactly.
+// The words of a pair of bytes (the low or the high two of a register) times 2^(byte - 127), rounded to BF16.  The instruction takes the
+// power from the exponent field of a number in 32 bits (the field 0 stands for 2^-127): the byte, shifted there.  A word has four
+// significant bits at most, so only results below BF16's normal numbers are rounded, once, and those at 2^128 become infinite.
 template <int KIND, bool HIGH>
-__device__ inline uint32_t fp8_pair_to_bf16(uint32_t w) {
+__device__ inline uint32_t fp8_pair_to_bf16(uint32_t w, uint32_t byte) {
   bf16x2 r;
-  if constexpr (KIND == SPLITZIP_FP8_E5M2) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8((int)w, 1.0f, HIGH);
-  else r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, HIGH);
+  if constexpr (KIND == SPLITZIP_FP8_E5M2) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, __uint_as_float(byte << 23), HIGH);
+  else r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, __uint_as_float(byte << 23), HIGH);
   return __builtin_bit_cast(uint32_t, r);
 }
 
@@ -138,19 +141,11 @@ __device__ inline uint32_t bf16_pair(float lo, float hi) {
   return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
 }
 
-// 8 FP8 words times 2^(byte - 127) as BF16: a word has four significant bits at most, so the product is exact in 32 bits,
-// subnormal ones included (2^-143 at the least), and is rounded once.
+// 8 FP8 words times 2^(byte - 127) as BF16
 template <int KIND>
-__device__ inline u32x4 from_fp8(const u32x2& w, int byte) {
-  const int up = byte - 127, half = up / 2;
-  const float a = __uint_as_float((uint32_t)(127 + half) << 23), b = __uint_as_float((uint32_t)(127 + up - half) << 23);
-  u32x4 out;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t p = i & 1 ? fp8_pair_to_bf16<KIND, true>(w[i / 2]) : fp8_pair_to_bf16<KIND, false>(w[i / 2]);
-    out[i] = bf16_pair(__uint_as_float(p << 16) * a * b, __uint_as_float(p & 0xffff0000u) * a * b);
-  }
-  return out;
+__device__ inline u32x4 from_fp8(const u32x2& w, uint32_t byte) {
+  return u32x4{fp8_pair_to_bf16<KIND, false>(w[0], byte), fp8_pair_to_bf16<KIND, true>(w[0], byte), fp8_pair_to_bf16<KIND, false>(w[1], byte),
+               fp8_pair_to_bf16<KIND, true>(w[1], byte)};
 }
 
 // Rows into the cache, and back.  A row of a head is taken by D / 8 lanes, eight elements each; a workgroup belongs to one
