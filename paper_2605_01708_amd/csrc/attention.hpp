@@ -48,6 +48,7 @@ struct AttentionArgs {
   uint32_t flip_q;                   // 0x80008000: the queries change sign
   uint32_t tree_words, window;       // window 0: none
   uint32_t group, parts, part_tokens, row_tiles;
+  uint32_t heads_across;             // heads of the cache that a workgroup takes
 };
 
 __device__ inline int position_of(const AttentionArgs& a, const Seq& s, int i) {
@@ -82,11 +83,11 @@ struct Share {
   int begin, end;
 };
 __device__ inline bool share_of(const AttentionArgs& a, uint32_t lane, Share& w) {
-  // workgroups of the same (part, sequence, head) lie 8 apart, on the same XCD
-  const uint32_t of = blockIdx.x / 8 / a.row_tiles;
+  // workgroups of the same (part, sequence, heads) lie 8 apart, on the same XCD
+  const uint32_t of = blockIdx.x / 8 / a.row_tiles, groups = a.cache.heads / a.heads_across;
   w.tile0 = blockIdx.x / 8 % a.row_tiles;
-  const uint32_t unit = of * 8 + blockIdx.x % 8, pair = unit / a.cache.heads;
-  w.head = unit % a.cache.heads;
+  const uint32_t unit = of * 8 + blockIdx.x % 8, pair = unit / groups;
+  w.head = unit % groups * a.heads_across;
   w.seq = pair % a.seqs.n_seqs;
   w.part = pair / a.seqs.n_seqs;
   if (w.part >= a.parts) return false;
@@ -320,157 +321,238 @@ __device__ inline uint32_t inside(int t, int len) { return (t < len ? 0xffffu : 
 __device__ inline float lse_of(float top, float total) { return total != 0.0f ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff(); }
 __device__ inline float one_over(float total) { return total != 0.0f ? 1.0f / total : 0.0f; }   // (a NaN is no 0)
 
-// Up to 16 rows: the four waves of a workgroup take every fourth 32 tokens of its part, from memory straight into registers,
-// and their outputs meet in LDS at the end.
+// Up to 16 rows: memory's speed is all that counts.  A wave belongs to one head of the cache; the four of a workgroup take four heads of the
+// same tokens (or two heads, or one, and every second or fourth stage of tokens), so that a token's heads, which lie side by
+// side, are read at the same time.  K and V go from memory straight into a piece of LDS of the wave's own, in whole rows (a load of the
+// matrix operand itself would take 16 bytes from each of 16 rows at a time), from there into registers, and while the wave
+// works on those the next tokens are on their way to the same place: no barrier, 128 KB of a CU's LDS in flight.
 template <int KIND, int D>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == 256 ? 2 : 3))) attention_tokens_kernel(AttentionArgs a) {
-  constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
-  constexpr int KS = D / 32;                // steps of the first product
-  constexpr int DV = D / 16;                // elements of V per lane and token, and tiles of the second product
-  constexpr int KW = KS * ES / 2;           // 16-byte loads of a row of K per lane
-  constexpr int VW = DV * ES / 4;           // registers of a token of V per lane
-  constexpr int kRow = D + 4;               // floats of a row in LDS
-  __shared__ float lds_out[kWaves * 16 * kRow];
+struct Stream {
+  static constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
+  static constexpr int kRow = D * ES;                                    // bytes of a token
+  static constexpr int kTokens = 16384 / (2 * kRow) < 32 ? 32 : 16384 / (2 * kRow);   // of a stage
+  static constexpr int kHalf = kTokens * kRow;                           // bytes of K, or V, of a stage
+  static constexpr int kSteps = kTokens / (int)kStep;
+  static constexpr int kUnits = kRow / 16;                               // 16-byte units of a row
+  static constexpr int KS = D / 32, DV = D / 16;
+  static constexpr int KW = KS * ES / 2;                                 // units of a row of K per lane
+  static constexpr int VB = DV * ES;                                     // bytes of a token of V per lane
+  static constexpr int VW = VB / 4;
+
+  // Rows of K lie in the order of the tokens, their units permuted so that the 16 rows of an operand (of the tile's row m: token
+  // 8 (m / 4) + m % 4, the other tile's 4 further) lie in 16 different units of the banks.
+  __device__ static uint32_t k_key(uint32_t token) {
+    const uint32_t mi = token / 8 % 4 * 4 + token % 4;
+    return kUnits >= 16 ? mi : mi / (16 / kUnits);
+  }
+  // Rows of V: those of the second and fourth eight in pairs the other way round where four of them (one of each eight) are read at a time
+  // and a row is half of the banks.
+  __device__ static uint32_t v_row(uint32_t token) { return kUnits == 8 ? token ^ (token / 8 & 1) : token; }
+
+  // asks for the stage from token t0 on; pages: lane l has the page of its 8 l-th token; offsets: bytes from page and place
+  __device__ static void ask(const AttentionArgs& a, const uint8_t* k_base, const uint8_t* v_base, uint32_t pages, int t0, uint32_t last8,
+                             uint8_t* lds, uint32_t lane) {
+#pragma unroll
+    for (int i = 0; i < kHalf / 1024; ++i) {
+      const uint32_t unit = (uint32_t)i * 64 + lane, row = unit / kUnits, at = unit % kUnits;   // where this lane's 16 bytes come to lie
+      // (rows of 128 bytes or more: the eight tokens are the same ones for all lanes)
+      const uint32_t eight = kUnits >= 8 ? (uint32_t)i * 64 / kUnits / 8 : row / 8;
+      uint32_t page;
+      if constexpr (kUnits >= 8) page = (uint32_t)__builtin_amdgcn_readlane((int)pages, i * 64 / kUnits / 8);
+      else page = (uint32_t)__shfl((int)pages, (int)(row / 8));
+      const uint32_t place = place_of_token(a.cache, a.seqs, min((uint32_t)t0 + 8 * eight, last8));
+      const uint64_t from = page * a.cache.page_stride + place * a.cache.token_stride;
+      const uint32_t k_off = row % 8 * (uint32_t)a.cache.token_stride + (at ^ k_key(row)) * 16;
+      const uint32_t v_off = v_row(row) % 8 * (uint32_t)a.cache.token_stride + at * 16;
+      load_to_lds(k_base + from + k_off, lds + i * 1024);
+      load_to_lds(v_base + from + v_off, lds + kHalf + i * 1024);
+    }
+  }
+};
+
+template <int KIND, int D>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Stream<KIND, D>::kHalf > 8192 ? 1 : 2))) attention_tokens_kernel(AttentionArgs a) {
+  using S = Stream<KIND, D>;
+  constexpr int ES = S::ES, KS = S::KS, DV = S::DV, KW = S::KW, VW = S::VW;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds_all[kWaves][2 * S::kHalf];
   __shared__ float lds_stat[kWaves][16][2];
-  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, m = lane % 16, g = lane / 16;
+  const uint32_t lane = threadIdx.x % 64, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), m = lane % 16, g = lane / 16;
   Share w;
   if (!share_of(a, lane, w)) return;
+  const uint32_t hw = a.heads_across, tw = kWaves / hw, turn = wave / hw;   // heads of the workgroup, waves of a head, which of them
+  w.head += wave % hw;
   const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
-  const uint64_t token = a.cache.token_stride;
+  const uint8_t *k_base = a.cache.k + w.head * a.cache.head_stride, *v_base = a.cache.v + w.head * a.cache.head_stride;
+  uint8_t* const mine = lds_all[wave];
+  const int stride = (int)tw * S::kTokens;
 
   for (uint32_t tile = w.tile0; tile * 16 < w.rows; tile += a.row_tiles) {
+    const auto ask_pages = [&](int t0) {
+      return page_of_token(a.cache, a.seqs, w.seq, min((uint32_t)t0 + 8 * (lane % (S::kTokens / 8)), last8));
+    };
+    u32x2 k_scales[S::kSteps], v_scales[S::kSteps];
+    const auto ask_scales = [&](uint32_t pages, int t0) {
+      if constexpr (ES == 1) {
+#pragma unroll
+        for (int u = 0; u < S::kSteps; ++u) {
+          const uint32_t k4 = 4 * u + m / 4, v4 = 4 * u + g;
+          const uint32_t k_place = place_of_token(a.cache, a.seqs, min((uint32_t)t0 + 8 * k4, last8)), v_place = place_of_token(a.cache, a.seqs, min((uint32_t)t0 + 8 * v4, last8));
+          k_scales[u] = *reinterpret_cast<const u32x2*>(a.cache.k_scales + scale_offset(a.cache, a.seqs, (uint32_t)__shfl((int)pages, (int)k4), k_place, w.head));
+          v_scales[u] = *reinterpret_cast<const u32x2*>(a.cache.v_scales + scale_offset(a.cache, a.seqs, (uint32_t)__shfl((int)pages, (int)v4), v_place, w.head));
+        }
+      }
+    };
+    int t0 = w.begin + (int)turn * S::kTokens;
+    uint32_t pages = 0;
+    if (t0 < w.end) {
+      pages = ask_pages(t0);
+      S::ask(a, k_base, v_base, pages, t0, last8, mine, lane);
+      ask_scales(pages, t0);
+      if (t0 + stride < w.end) pages = ask_pages(t0 + stride);
+    }
     Rows<KIND, D, 1> r;
     r.load(a, w, tile * 16, m, g);
     State<D, 1> st;
     st.clear();
-    // tokens 8 (m / 4) + .. for K, 8 g + .. for V
-    const auto k_group = [&](int t0) { return min((uint32_t)t0 + 8 * (m / 4), last8); };
-    const auto v_group = [&](int t0) { return min((uint32_t)t0 + 8 * g, last8); };
-    int t0 = w.begin + (int)(wave * kStep);
-    uint32_t k_page = 0, v_page = 0;
-    if (t0 < w.end) {
-      k_page = page_of_token(a.cache, a.seqs, w.seq, k_group(t0));
-      v_page = page_of_token(a.cache, a.seqs, w.seq, v_group(t0));
-    }
 #pragma unroll 1
-    for (; t0 < w.end; t0 += (int)(kWaves * kStep)) {
-      const uint32_t k_place = place_of_token(a.cache, a.seqs, k_group(t0)), v_place = place_of_token(a.cache, a.seqs, v_group(t0));
-      const uint8_t* k_at = a.cache.k + word_offset(a.cache, k_page, k_place + m % 4, w.head);
-      const uint8_t* v_at = a.cache.v + word_offset(a.cache, v_page, v_place, w.head);
-      u32x4 k[2][KW];
+    for (; t0 < w.end; t0 += stride) {
+      memory_arrived();
+      u32x4 k[S::kSteps][2][KW];
+      uint32_t v[S::kSteps][8][VW];
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int u = 0; u < S::kSteps; ++u) {
 #pragma unroll
-        for (int i = 0; i < KW; ++i) k[b][i] = *reinterpret_cast<const u32x4*>(k_at + 4 * b * token + 64 * i + 16 * g);
-      uint32_t v[8][VW];
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) __builtin_memcpy(v[e], __builtin_assume_aligned(v_at + e * token + 4 * VW * m, VW < 4 ? 4 * VW : 16), 4 * VW);
-      // the scales of the lane's groups
-      u32x2 k_scales = {0, 0}, v_scales = {0, 0};
-      if constexpr (ES == 1) {
-        k_scales = *reinterpret_cast<const u32x2*>(a.cache.k_scales + scale_offset(a.cache, a.seqs, k_page, k_place, w.head));
-        v_scales = *reinterpret_cast<const u32x2*>(a.cache.v_scales + scale_offset(a.cache, a.seqs, v_page, v_place, w.head));
+          for (int i = 0; i < KW; ++i) {
+            const uint32_t token = 32 * u + 8 * (m / 4) + 4 * b + m % 4;
+            k[u][b][i] = *reinterpret_cast<const u32x4*>(mine + token * S::kRow + ((4 * i + g) ^ S::k_key(token)) * 16);
+          }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          __builtin_memcpy(v[u][e], __builtin_assume_aligned(mine + S::kHalf + S::v_row(32 * u + 8 * g + e) * S::kRow + S::VB * m, S::VB < 16 ? S::VB : 16), S::VB);
       }
-      if (t0 + (int)(kWaves * kStep) < w.end) {   // the next pages
-        k_page = page_of_token(a.cache, a.seqs, w.seq, k_group(t0 + (int)(kWaves * kStep)));
-        v_page = page_of_token(a.cache, a.seqs, w.seq, v_group(t0 + (int)(kWaves * kStep)));
+      u32x2 ks[S::kSteps], vs[S::kSteps];
+#pragma unroll
+      for (int u = 0; u < S::kSteps; ++u) {
+        ks[u] = k_scales[u];
+        vs[u] = v_scales[u];
       }
-
-      f32x4 x[1][2];
+      lds_read();   // into registers: the place is free
+      if (t0 + stride < w.end) {
+        S::ask(a, k_base, v_base, pages, t0 + stride, last8, mine, lane);
+        ask_scales(pages, t0 + stride);
+        if (t0 + 2 * stride < w.end) pages = ask_pages(t0 + 2 * stride);
+      }
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        x[0][b] = f32x4{0, 0, 0, 0};
+      for (int u = 0; u < S::kSteps; ++u) {
+        const int tu = t0 + u * (int)kStep;
+        if (tu >= w.end) break;
+        f32x4 x[1][2];
 #pragma unroll
-        for (int t = 0; t < KS; ++t) {
-          if constexpr (ES == 2) {
-            x[0][b] = mfma(as_bf16(k[b][t]), r.q[0][t], x[0][b]);
-          } else {
-            const u32x2 words = {k[b][t / 2][t % 2 * 2], k[b][t / 2][t % 2 * 2 + 1]};
-            x[0][b] = mfma(as_bf16(from_fp8<KIND>(words, k_scales[b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
+        for (int b = 0; b < 2; ++b) {
+          x[0][b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int t = 0; t < KS; ++t) {
+            if constexpr (ES == 2) {
+              x[0][b] = mfma(as_bf16(k[u][b][t]), r.q[0][t], x[0][b]);
+            } else {
+              const u32x2 words = {k[u][b][t / 2][t % 2 * 2], k[u][b][t / 2][t % 2 * 2 + 1]};
+              x[0][b] = mfma(as_bf16(from_fp8<KIND>(words, ks[u][b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
+            }
           }
         }
-      }
-      const bool all = r.see_all(w, t0);
-      const int t8 = t0 + (int)(8 * g);
-      uint32_t seen[1] = {0xffu};
-      if (!all) seen[0] = r.seen(a, w, 0, t8);
-      bf16x8 p[1];
-      st.weigh(a, w, r, x, all, seen, t8, p);
-      u32x4 vt[DV];   // element j of the eight tokens
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int j = 0; j < DV; j += 2) {
-          uint32_t w0, w1;
-          if constexpr (ES == 2) {
-            w0 = v[2 * i][j / 2];
-            w1 = v[2 * i + 1][j / 2];
-          } else {
-            const uint32_t b0 = v_scales[i / 2] >> (16 * (i % 2)) & 0xffu, b1 = v_scales[i / 2] >> (16 * (i % 2) + 8) & 0xffu;
-            w0 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[2 * i][j / 4], b0) : fp8_pair_to_bf16<KIND, false>(v[2 * i][j / 4], b0);
-            w1 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[2 * i + 1][j / 4], b1) : fp8_pair_to_bf16<KIND, false>(v[2 * i + 1][j / 4], b1);
-          }
-          vt[j][i] = evens(w0, w1);
-          vt[j + 1][i] = odds(w0, w1);
-        }
-      }
-      if (all) {
-#pragma unroll
-        for (int j = 0; j < DV; ++j) st.add(j, as_bf16(vt[j]), p);
-      } else {
+        const bool all = r.see_all(w, tu);
+        const int t8 = tu + (int)(8 * g);
+        uint32_t seen[1] = {0xffu};
+        if (!all) seen[0] = r.seen(a, w, 0, t8);
+        bf16x8 p[1];
+        st.weigh(a, w, r, x, all, seen, t8, p);
+        u32x4 vt[DV];   // element j of the eight tokens
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t in = inside(t8 + 2 * i, w.s.len);
 #pragma unroll
-          for (int j = 0; j < DV; ++j) vt[j][i] &= in;
+          for (int j = 0; j < DV; j += 2) {
+            uint32_t w0, w1;
+            if constexpr (ES == 2) {
+              w0 = v[u][2 * i][j / 2];
+              w1 = v[u][2 * i + 1][j / 2];
+            } else {
+              const uint32_t b0 = vs[u][i / 2] >> (16 * (i % 2)) & 0xffu, b1 = vs[u][i / 2] >> (16 * (i % 2) + 8) & 0xffu;
+              w0 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[u][2 * i][j / 4], b0) : fp8_pair_to_bf16<KIND, false>(v[u][2 * i][j / 4], b0);
+              w1 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[u][2 * i + 1][j / 4], b1) : fp8_pair_to_bf16<KIND, false>(v[u][2 * i + 1][j / 4], b1);
+            }
+            vt[j][i] = evens(w0, w1);
+            vt[j + 1][i] = odds(w0, w1);
+          }
         }
-        st.template add_guarded<KIND>(a, w, t0, [&](int j) { return vt[j]; }, [&](int j, int i) { return DV * (4 * g + i) + j; }, p, seen, m);
+        if (all) {
+#pragma unroll
+          for (int j = 0; j < DV; ++j) st.add(j, as_bf16(vt[j]), p);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t in = inside(t8 + 2 * i, w.s.len);
+#pragma unroll
+            for (int j = 0; j < DV; ++j) vt[j][i] &= in;
+          }
+          st.template add_guarded<KIND>(a, w, tu, [&](int j) { return vt[j]; }, [&](int j, int i) { return DV * (4 * g + i) + j; }, p, seen, m);
+        }
       }
     }
 
-    // the four waves' parts of the tokens together
-    lds_barrier();   // (the tile before this one has been read)
-    const float of_wave = st.total(0);
-    if (g == 0) {
-      lds_stat[wave][m][0] = st.top[0];
-      lds_stat[wave][m][1] = of_wave;
-    }
-    // lane (m, g) has elements DV (4 g + i) + j of row m in acc[j][i]
-    float* mine = lds_out + (wave * 16 + m) * kRow + 4 * DV * g;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < DV; j += 4)
-        *reinterpret_cast<f32x4*>(mine + DV * i + j) = f32x4{st.acc[0][j][i], st.acc[0][j + 1][i], st.acc[0][j + 2][i], st.acc[0][j + 3][i]};
-    lds_barrier();
-    const uint32_t r16 = threadIdx.x / 16, c = threadIdx.x % 16, at = tile * 16 + r16;
-    if (at < w.rows) {
-      float high = lds_stat[0][r16][0], total = 0.0f, o[DV];
-#pragma unroll
-      for (int v = 1; v < kWaves; ++v) high = fmaxf(high, lds_stat[v][r16][0]);
-#pragma unroll
-      for (int j = 0; j < DV; ++j) o[j] = 0.0f;
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
-        const float f = __builtin_amdgcn_exp2f(lds_stat[v][r16][0] - high);
-        total += f * lds_stat[v][r16][1];
-#pragma unroll
-        for (int j = 0; j < DV; ++j) o[j] += f * lds_out[(v * 16 + r16) * kRow + DV * c + j];
+    // the waves of a head together, where there are several; lane (m, g) has elements DV (4 g + i) + j of row m in acc[j][i]
+    float total = st.total(0);
+    if (tw > 1) {
+      if (g == 0) {
+        lds_stat[wave][m][0] = st.top[0];
+        lds_stat[wave][m][1] = total;
       }
+      f32x4* out = reinterpret_cast<f32x4*>(mine) + lane;
+#pragma unroll
+      for (int j = 0; j < DV; ++j) out[64 * j] = st.acc[0][j];
+      lds_barrier();
+      if (turn == 0) {
+        float high = st.top[0];
+        for (uint32_t v = 1; v < tw; ++v) high = fmaxf(high, lds_stat[wave + v * hw][m][0]);
+        const float f0 = __builtin_amdgcn_exp2f(st.top[0] - high);
+        st.top[0] = high;
+        total *= f0;
+#pragma unroll
+        for (int j = 0; j < DV; ++j) st.acc[0][j] *= f0;
+        for (uint32_t v = 1; v < tw; ++v) {
+          const float f = __builtin_amdgcn_exp2f(lds_stat[wave + v * hw][m][0] - high);
+          total += f * lds_stat[wave + v * hw][m][1];
+          const f32x4* from = reinterpret_cast<const f32x4*>(lds_all[wave + v * hw]) + lane;
+#pragma unroll
+          for (int j = 0; j < DV; ++j) st.acc[0][j] += f * from[64 * j];
+        }
+      }
+      lds_barrier();   // (the next tile of rows writes there)
+    }
+    const uint32_t at = tile * 16 + m;
+    if (turn == 0 && at < w.rows) {
       const uint32_t q_heads = a.cache.heads * a.group, h = w.head * a.group + at % a.group;
       const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(at / a.group));
       if (w.n_parts == 1) {
         const float f = one_over(total);
-        uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + DV * c);
+        uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + 4 * DV * g);
 #pragma unroll
-        for (int j = 0; j < DV; j += 2) *reinterpret_cast<uint32_t*>(to + 2 * j) = bf16_pair(o[j] * f, o[j + 1] * f);
-        if (c == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(high, total);
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < DV; j += 4)
+            *reinterpret_cast<u32x2*>(to + 2 * (DV * i + j)) = u32x2{bf16_pair(st.acc[0][j][i] * f, st.acc[0][j + 1][i] * f), bf16_pair(st.acc[0][j + 2][i] * f, st.acc[0][j + 3][i] * f)};
+        if (g == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(st.top[0], total);
       } else {
         const uint64_t place = (out_row * q_heads + h) * a.parts + w.part;
+        float* to = a.part_out + place * D + 4 * DV * g;
 #pragma unroll
-        for (int j = 0; j < DV; j += 4) *reinterpret_cast<f32x4*>(a.part_out + place * D + DV * c + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
-        if (c == 0) {
-          a.part_stat[2 * place] = high;
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < DV; j += 4)
+            *reinterpret_cast<f32x4*>(to + DV * i + j) = f32x4{st.acc[0][j][i], st.acc[0][j + 1][i], st.acc[0][j + 2][i], st.acc[0][j + 3][i]};
+        if (g == 0) {
+          a.part_stat[2 * place] = st.top[0];
           a.part_stat[2 * place + 1] = total;
         }
       }

@@ -46,6 +46,7 @@ int check_cache(const splitzip_cache* c, bool pointers) {
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return SPLITZIP_ERR_UNSUPPORTED;
   if (!c->kv_heads || !c->n_pages || c->page_tokens < 8 || c->page_tokens > kMostTokens) return SPLITZIP_ERR_INVALID_ARG;
   if (!aligned16(c->page_stride_bytes) || !aligned16(c->token_stride_bytes) || !aligned16(c->head_stride_bytes)) return SPLITZIP_ERR_INVALID_ARG;
+  if (c->token_stride_bytes > (1ull << 28)) return SPLITZIP_ERR_UNSUPPORTED;   // eight of them are a 32-bit offset
   const uint64_t row = (uint64_t)c->head_dim * words_bytes(c->dtype);
   if (c->token_stride_bytes < row || c->head_stride_bytes < row) return SPLITZIP_ERR_INVALID_ARG;
   if (c->dtype != SPLITZIP_BF16 && (c->scale_page_stride_bytes & 7u || c->page_tokens & 7u)) return SPLITZIP_ERR_INVALID_ARG;
@@ -158,6 +159,7 @@ int rows_call(const splitzip_cache* c, const splitzip_seqs* q, void* d_k, uint64
 struct AttentionPlan {
   uint32_t waves, nt;   // 0: attention_tokens_kernel; else attention_rows_kernel with so many waves of 16 nt rows
   uint32_t row_tiles, parts, part_tokens;
+  uint32_t heads_across;
 };
 constexpr uint32_t kLeastPart = 256;   // tokens
 // the tokens that a launch is cut for: a window's, where rows see no more
@@ -168,7 +170,7 @@ uint64_t tokens_planned(const splitzip_seqs* q, uint32_t window) {
 }
 // the parts that would fill the chip
 uint64_t parts_wanted(const splitzip_cache* c, const splitzip_seqs* q, const AttentionPlan& p) {
-  const uint64_t units = (uint64_t)q->n_seqs * c->kv_heads * p.row_tiles, want = (uint64_t)cu_count() * (p.waves == 8 ? 2 : 4);
+  const uint64_t units = (uint64_t)q->n_seqs * (c->kv_heads / p.heads_across) * p.row_tiles, want = (uint64_t)cu_count() * (p.waves == 8 ? 2 : 4);
   return units ? (want + units - 1) / units : 1;
 }
 AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, uint32_t q_heads, uint64_t tokens) {
@@ -177,6 +179,7 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
   uint64_t tile = 16;
   p.waves = 0;
   p.nt = 1;
+  p.heads_across = rows > 16 ? 1u : c->kv_heads % 4 == 0 ? 4u : c->kv_heads % 2 == 0 ? 2u : 1u;
   if (rows > 16) {
     p.waves = rows <= (c->head_dim == 256 ? 64 : 128) ? 4 : 8;
     p.nt = rows <= 64 || c->head_dim == 256 ? 1 : 2;
@@ -251,7 +254,7 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   if (workspace_bytes < need) return SPLITZIP_ERR_CAPACITY;
   if (need && (!d_workspace || !aligned16(d_workspace))) return SPLITZIP_ERR_INVALID_ARG;
   if (!rows_ok(d_q, q_row_stride, elems) || !rows_ok(d_out, out_row_stride, elems) || !aligned(d_lse, 4)) return SPLITZIP_ERR_INVALID_ARG;
-  const uint64_t units = ((uint64_t)p.parts * seqs->n_seqs * cache->kv_heads + 7) / 8 * 8 * p.row_tiles;
+  const uint64_t units = ((uint64_t)p.parts * seqs->n_seqs * (cache->kv_heads / p.heads_across) + 7) / 8 * 8 * p.row_tiles;
   if (units >> 31) return SPLITZIP_ERR_UNSUPPORTED;
   AttentionArgs a;
   a.cache = device_cache(cache, seqs);
@@ -275,6 +278,7 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   a.parts = p.parts;
   a.part_tokens = p.part_tokens;
   a.row_tiles = p.row_tiles;
+  a.heads_across = p.heads_across;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   rc = by_kind<Attend>(cache, dim3((unsigned)units), p.waves, p.nt, st, (const AttentionArgs*)&a);
   if (rc != SPLITZIP_OK || p.parts == 1) return rc;

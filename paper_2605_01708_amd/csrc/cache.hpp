@@ -64,6 +64,14 @@ __device__ inline uint64_t scale_offset(const Cache& c, const Seqs& q, uint32_t 
   return page * c.scale_page_stride + (uint64_t)head * (q.table ? 1u << c.page_shift : q.capacity) + place;
 }
 
+// 16 bytes per lane from memory straight into LDS: the wave's lanes one behind the other from `to` on, which is the wave's.  They are
+// there when memory_arrived says so.  Streamed: nothing else reads them.
+__device__ inline void load_to_lds(const uint8_t* from, uint8_t* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, kStream);
+}
+__device__ inline void memory_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ inline void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 struct RowsArgs {
   Cache cache;
   Seqs seqs;
