@@ -42,13 +42,16 @@ struct AttentionArgs {
   const float* slopes;               // [q_heads] or null
   const uint64_t* tree;              // [n_rows][tree_words] or null: a chain
   const int32_t* positions;          // [n_rows] or null: base + row
-  float* part_out;                   // [n_rows][q_heads][parts][D]
-  float* part_stat;                  // [n_rows][q_heads][parts][2]: maximum (of log2), sum
+  float* part_out;                   // [workgroup][2][heads_across][kept][D]: parts of sequences that several workgroups share
+  float* part_stat;                  // the same, [2] each: maximum (of log2), sum
   float scale, softcap;              // scale >= 0: its sign is in flip_q
   uint32_t flip_q;                   // 0x80008000: the queries change sign
   uint32_t tree_words, window;       // window 0: none
-  uint32_t group, parts, part_tokens, row_tiles;
+  uint32_t group;                    // query heads per head of the cache
   uint32_t heads_across;             // heads of the cache that a workgroup takes
+  uint32_t tile_rows, row_tiles;     // rows of the product that it takes; tiles of them that are dealt out
+  uint32_t most_rows, kept;          // rows of a sequence that the launch is cut for, and of a tile that a part is kept of
+  uint32_t shares, block_tokens, least_blocks;   // workgroups of the same heads and rows; what is dealt out to them
 };
 
 __device__ inline int position_of(const AttentionArgs& a, const Seq& s, int i) {
@@ -56,50 +59,137 @@ __device__ inline int position_of(const AttentionArgs& a, const Seq& s, int i) {
 }
 
 // The first token that any row of the sequence may see, a multiple of 32: with a window, the one that the row at the lowest
-// position sees.  The parts of a sequence count from it.
-__device__ inline int first_token(const AttentionArgs& a, const Seq& s, uint32_t lane) {
+// position sees.  The sequence's blocks count from it.
+__device__ inline int first_token(const AttentionArgs& a, const Seq& s) {
   if (!a.window) return 0;
   int low = s.base;   // without positions: the first row's
   if (a.positions) {
     low = 0x7fffffff;
-    for (int i = (int)lane; i < s.rows; i += 64) low = min(low, position_of(a, s, i));
-#pragma unroll
-    for (int o = 32; o > 0; o /= 2) low = min(low, __shfl_xor(low, o));
+    for (int i = 0; i < s.rows; ++i) low = min(low, position_of(a, s, i));
   }
   const int64_t first = (int64_t)low - (int64_t)a.window + 1;
   const int64_t most = max(min(s.base, s.len), 0);   // drafted tokens lie where their positions say, not where they are stored
   return (int)(max(min(first, most), (int64_t)0) & ~(int64_t)(kStep - 1));
 }
-
-__device__ inline uint32_t parts_of(const AttentionArgs& a, const Seq& s, int first) {
-  const uint32_t n = ((uint32_t)(s.len - first) + a.part_tokens - 1) / a.part_tokens;
-  return min(max(n, 1u), a.parts);
+// One at least where there are rows: somebody has to write their zeros.
+__device__ inline uint32_t blocks_of(const AttentionArgs& a, const Seq& s, int first) {
+  return s.rows ? max(((uint32_t)(s.len - first) + a.block_tokens - 1) / a.block_tokens, 1u) : 0u;
 }
 
-// What a workgroup is to do: a part of the tokens of a (sequence, head of the cache), and tiles of rows tile0, tile0 + row_tiles, ...
+// The blocks of all sequences, one sequence behind the other, are dealt out evenly to a.shares workgroups (per heads and tile of
+// rows): lengths differ, and a launch that gave every workgroup one part of one sequence would wait for the longest (64 sequences
+// of 700 to 8192 tokens: 221 us that way).  Every wave sums the blocks up for itself.
+struct Blocks {
+  uint32_t total, shares;   // shares: that get something
+
+  __device__ uint32_t begin(uint32_t share) const { return (uint32_t)((uint64_t)share * total / shares); }
+  __device__ uint32_t owner(uint32_t block) const { return (uint32_t)((((uint64_t)block + 1) * shares - 1) / total); }
+  static __device__ uint32_t blocks_of_seq(const AttentionArgs& a, uint32_t seq) {
+    if (seq >= a.seqs.n_seqs) return 0;
+    const Seq s = seq_at(a.seqs, seq);
+    return blocks_of(a, s, first_token(a, s));
+  }
+  __device__ void count(const AttentionArgs& a, uint32_t lane, uint32_t& own) {   // own: of sequence `lane`
+    total = 0;
+    for (uint32_t at = 0; at < a.seqs.n_seqs; at += 64) {
+      const uint32_t n = blocks_of_seq(a, at + lane), sum = wave_last(wave_incl_scan(n));
+      if (at == 0) own = n;
+      total += sum;
+    }
+    shares = min(a.shares, (total + a.least_blocks - 1) / a.least_blocks);
+  }
+  // the sequence that has this block, and the number of its first block
+  __device__ void find(const AttentionArgs& a, uint32_t lane, uint32_t own, uint32_t block, uint32_t& seq, uint32_t& front) const {
+    uint32_t before = 0;
+    for (uint32_t at = 0;; at += 64) {
+      const uint32_t n = at == 0 ? own : blocks_of_seq(a, at + lane), upto = before + wave_incl_scan(n);
+      const uint64_t beyond = __ballot(upto > block);
+      if (beyond) {
+        const int l = __builtin_ctzll(beyond);
+        seq = at + (uint32_t)l;
+        front = (uint32_t)__builtin_amdgcn_readlane((int)(upto - n), l);
+        return;
+      }
+      before = wave_last(upto);
+    }
+  }
+};
+
+// What a workgroup is to do: segment after segment of its blocks, each a piece of one sequence, for heads from `head` on and the rows of
+// tile `tile`.
 struct Share {
   Seq s;
-  uint32_t seq, head, part, n_parts, tile0, rows;   // rows: of the matrix product, the sequence's times the group's query heads
-  int begin, end;
+  uint32_t seq, head, tile, rows;   // rows: of the matrix product, the sequence's times the group's query heads
+  int first, begin, end;            // the sequence's first token, the segment's tokens
+  uint32_t block, blocks, left;     // the segment's first block in the sequence, the sequence's blocks, the workgroup's from here on
+  uint32_t slot, wg;                // where the segment's part is kept
+  bool whole;                       // the segment is all of the sequence: no part
+  int later;                        // segments before this one
+
+  __device__ bool start(const AttentionArgs& a, uint32_t lane) {
+    // workgroups of the same (share, heads) lie 8 apart, on the same XCD
+    wg = blockIdx.x;
+    const uint32_t of = wg / 8 / a.row_tiles, groups = a.cache.heads / a.heads_across;
+    tile = wg / 8 % a.row_tiles;
+    const uint32_t unit = of * 8 + wg % 8, share = unit / groups;
+    head = unit % groups * a.heads_across;
+    Blocks b;
+    uint32_t own = 0;
+    b.count(a, lane, own);
+    if (share >= b.shares) return false;
+    const uint32_t from = b.begin(share);
+    left = b.begin(share + 1) - from;
+    uint32_t front;
+    b.find(a, lane, own, from, seq, front);
+    later = 0;
+    take(a, from - front);
+    return true;
+  }
+  __device__ void take(const AttentionArgs& a, uint32_t at) {
+    seq = (uint32_t)__builtin_amdgcn_readfirstlane((int)seq);
+    s = seq_at(a.seqs, seq);
+    first = first_token(a, s);
+    blocks = blocks_of(a, s, first);
+    rows = (uint32_t)s.rows * a.group;
+    block = at;
+    if (!blocks) return;
+    const uint32_t mine = min(blocks - at, left);
+    begin = first + (int)(at * a.block_tokens);
+    end = at + mine < blocks ? begin + (int)(mine * a.block_tokens) : s.len;
+    whole = at == 0 && mine == blocks;
+    slot = later ? 1u : 0u;
+  }
+  // to the next segment
+  __device__ bool next(const AttentionArgs& a) {
+    left -= min(blocks - block, left);
+    ++later;
+    do {
+      if (!left) return false;
+      ++seq;
+      take(a, 0);
+    } while (!blocks);
+    return true;
+  }
+  // The segment's first tile of rows, false if there is none, and the next one.  A sequence with more rows than the launch was cut for is taken
+  // as a whole by the workgroups that have its first block, every row_tiles-th tile by each: nothing of it needs a place to be kept in.
+  __device__ bool first_rows(const AttentionArgs& a) {
+    tile = wg / 8 % a.row_tiles;
+    if (rows > a.most_rows) {
+      if (block) return false;
+      begin = first;
+      end = s.len;
+      whole = true;
+    }
+    return (uint64_t)tile * a.tile_rows < rows;
+  }
+  __device__ bool more_rows(const AttentionArgs& a) {
+    tile += a.row_tiles;
+    return (uint64_t)tile * a.tile_rows < rows;   // (up to most_rows there are no more than row_tiles)
+  }
+  __device__ uint64_t place(const AttentionArgs& a, uint32_t head_of_group, uint32_t row) const {
+    return (((uint64_t)wg * 2 + slot) * a.heads_across + head_of_group) * a.kept + row;
+  }
 };
-__device__ inline bool share_of(const AttentionArgs& a, uint32_t lane, Share& w) {
-  // workgroups of the same (part, sequence, heads) lie 8 apart, on the same XCD
-  const uint32_t of = blockIdx.x / 8 / a.row_tiles, groups = a.cache.heads / a.heads_across;
-  w.tile0 = blockIdx.x / 8 % a.row_tiles;
-  const uint32_t unit = of * 8 + blockIdx.x % 8, pair = unit / groups;
-  w.head = unit % groups * a.heads_across;
-  w.seq = pair % a.seqs.n_seqs;
-  w.part = pair / a.seqs.n_seqs;
-  if (w.part >= a.parts) return false;
-  w.s = seq_at(a.seqs, w.seq);
-  const int first = first_token(a, w.s, lane);
-  w.n_parts = parts_of(a, w.s, first);
-  if (w.part >= w.n_parts) return false;
-  w.begin = first + (int)(w.part * a.part_tokens);
-  w.end = w.part + 1 < w.n_parts ? w.begin + (int)a.part_tokens : w.s.len;   // the last one goes on to the end
-  w.rows = (uint32_t)w.s.rows * a.group;
-  return true;
-}
 
 // The lane's rows (r0 + 16 n + m of the product) and their operand of the first product.
 template <int KIND, int D, int NT>
@@ -378,15 +468,17 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
   __shared__ float lds_stat[kWaves][16][2];
   const uint32_t lane = threadIdx.x % 64, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), m = lane % 16, g = lane / 16;
   Share w;
-  if (!share_of(a, lane, w)) return;
+  if (!w.start(a, lane)) return;
   const uint32_t hw = a.heads_across, tw = kWaves / hw, turn = wave / hw;   // heads of the workgroup, waves of a head, which of them
   w.head += wave % hw;
-  const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
   const uint8_t *k_base = a.cache.k + w.head * a.cache.head_stride, *v_base = a.cache.v + w.head * a.cache.head_stride;
   uint8_t* const mine = lds_all[wave];
   const int stride = (int)tw * S::kTokens;
 
-  for (uint32_t tile = w.tile0; tile * 16 < w.rows; tile += a.row_tiles) {
+  do {
+    if (!w.first_rows(a)) continue;
+    do {
+    const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
     const auto ask_pages = [&](int t0) {
       return page_of_token(a.cache, a.seqs, w.seq, min((uint32_t)t0 + 8 * (lane % (S::kTokens / 8)), last8));
     };
@@ -411,7 +503,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
       if (t0 + stride < w.end) pages = ask_pages(t0 + stride);
     }
     Rows<KIND, D, 1> r;
-    r.load(a, w, tile * 16, m, g);
+    r.load(a, w, w.tile * 16, m, g);
     State<D, 1> st;
     st.clear();
 #pragma unroll 1
@@ -530,11 +622,11 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
       }
       lds_barrier();   // (the next tile of rows writes there)
     }
-    const uint32_t at = tile * 16 + m;
+    const uint32_t at = w.tile * 16 + m;
     if (turn == 0 && at < w.rows) {
       const uint32_t q_heads = a.cache.heads * a.group, h = w.head * a.group + at % a.group;
       const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(at / a.group));
-      if (w.n_parts == 1) {
+      if (w.whole) {
         const float f = one_over(total);
         uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + 4 * DV * g);
 #pragma unroll
@@ -544,7 +636,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
             *reinterpret_cast<u32x2*>(to + 2 * (DV * i + j)) = u32x2{bf16_pair(st.acc[0][j][i] * f, st.acc[0][j + 1][i] * f), bf16_pair(st.acc[0][j + 2][i] * f, st.acc[0][j + 3][i] * f)};
         if (g == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(st.top[0], total);
       } else {
-        const uint64_t place = (out_row * q_heads + h) * a.parts + w.part;
+        const uint64_t place = w.place(a, wave % hw, m);
         float* to = a.part_out + place * D + 4 * DV * g;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -557,7 +649,8 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
         }
       }
     }
-  }
+    } while (w.more_rows(a));
+  } while (w.next(a));
 }
 
 // More rows: the W waves of a workgroup take 16 NT rows each of the same tokens.  Those are staged in LDS, 32 KB at a time and twice
@@ -643,13 +736,15 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
   __shared__ u32x4 lds[2][32 * 64];
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, m = lane % 16, g = lane / 16;
   Share w;
-  if (!share_of(a, lane, w)) return;
-  const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;
+  if (!w.start(a, lane)) return;
   const uint32_t piece = wave % 4;
   const bool of_k = kBoth || wave < 4, of_v = kBoth || wave >= 4;
 
-  for (uint32_t tile = w.tile0; tile * 16 * NT * W < w.rows; tile += a.row_tiles) {
-    const uint32_t r0 = (tile * W + wave) * 16 * NT;
+  do {
+    if (!w.first_rows(a)) continue;
+    do {
+    const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;
+    const uint32_t r0 = (w.tile * W + wave) * 16 * NT;
     const bool active = r0 < w.rows;
     Rows<KIND, D, NT> r;
     State<D, NT> st;
@@ -726,7 +821,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
       if (row >= w.rows) continue;
       const uint32_t h = w.head * a.group + row % a.group;
       const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(row / a.group));
-      if (w.n_parts == 1) {
+      if (w.whole) {
         const float f = one_over(total);
         uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + 16 * g);
 #pragma unroll
@@ -742,7 +837,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
         }
         if (g == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(st.top[n], total);
       } else {
-        const uint64_t place = (out_row * q_heads + h) * a.parts + w.part;
+        const uint64_t place = w.place(a, 0, wave * 16 * NT + 16 * n + m);
         float* to = a.part_out + place * D + 16 * g;
 #pragma unroll
         for (int b = 0; b < D / 64; ++b)
@@ -755,58 +850,95 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
         }
       }
     }
-  }
+    } while (w.more_rows(a));
+  } while (w.next(a));
 }
 
-// The parts of a sequence together: a workgroup per row and query head.  A thread takes four elements of every (1024 / D)-th part.
+// The parts of a sequence together.  D / 4 threads have a row and query head, four elements each: where the parts are few, as many rows
+// as that leaves room for go through a workgroup at a time, otherwise all its threads take every (1024 / D)-th part of one.
+constexpr uint32_t kFewParts = 8;
 template <int D>
 __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs a) {
   constexpr uint32_t kAcross = D / 4, kDown = kThreads / kAcross;
   __shared__ f32x4 lds_out[kThreads];
   __shared__ float lds_sum[kDown], lds_top[kWaves];
-  const uint32_t lane = threadIdx.x % 64, q_heads = a.cache.heads * a.group;
+  const uint32_t lane = threadIdx.x % 64, q_heads = a.cache.heads * a.group, groups = a.cache.heads / a.heads_across;
   const Seq s = seq_at(a.seqs, blockIdx.y);
-  const uint32_t n_parts = parts_of(a, s, first_token(a, s, lane));
-  if (n_parts == 1) return;   // written already
+  const uint32_t blocks = blocks_of(a, s, first_token(a, s));
+  if (blocks < 2 || (uint64_t)s.rows * a.group > a.most_rows) return;   // written already
+  Blocks b;
+  uint32_t own = 0, front = 0;
+  b.count(a, lane, own);
+  for (uint32_t at = 0; at < blockIdx.y; at += 64) {
+    const uint32_t n = at == 0 ? own : Blocks::blocks_of_seq(a, at + lane);
+    front += wave_last(wave_incl_scan(at + lane < blockIdx.y ? n : 0));
+  }
+  const uint32_t share0 = b.owner(front), n_parts = b.owner(front + blocks - 1) + 1 - share0;
+  if (n_parts == 1) return;
+  const uint32_t slot0 = b.begin(share0) < front ? 1 : 0;   // of the first part: behind another sequence's; the others are their workgroups' first
   const uint32_t across = threadIdx.x % kAcross, down = threadIdx.x / kAcross;
-  for (uint32_t u = blockIdx.x; u < (uint32_t)s.rows * q_heads; u += gridDim.x) {
+  const bool few = n_parts <= kFewParts;
+  const uint32_t outs = (uint32_t)s.rows * q_heads, step = few ? kDown : 1;
+  for (uint32_t u0 = blockIdx.x * step; u0 < outs; u0 += gridDim.x * step) {
+    const uint32_t u = min(u0 + (few ? down : 0), outs - 1);
     const uint64_t out_row = (uint64_t)(uint32_t)(s.start + (int)(u / q_heads)), h = u % q_heads;
-    const uint64_t place = (out_row * q_heads + h) * a.parts;
-    const float* stat = a.part_stat + 2 * place;
-    const float* from = a.part_out + place * D + 4 * across;
-    float high = kLowest;
-    for (uint32_t p = threadIdx.x; p < n_parts; p += kThreads) high = fmaxf(high, stat[2 * p]);
-#pragma unroll
-    for (int o = 32; o > 0; o /= 2) high = fmaxf(high, __shfl_xor(high, o));
-    __syncthreads();   // (the row before this one has been read)
-    if (lane == 0) lds_top[threadIdx.x / 64] = high;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) high = fmaxf(high, lds_top[k]);
-    float total = 0.0f;
+    const uint32_t head = (uint32_t)h / a.group, r = u / q_heads * a.group + (uint32_t)h % a.group, tile = r / a.tile_rows;
+    const auto place = [&](uint32_t p) {
+      const uint32_t unit = (share0 + p) * groups + head / a.heads_across;
+      const uint64_t wg = ((uint64_t)(unit / 8) * a.row_tiles + tile) * 8 + unit % 8;
+      return ((wg * 2 + (p ? 0 : slot0)) * a.heads_across + head % a.heads_across) * a.kept + r % a.tile_rows;
+    };
+    float high = kLowest, total = 0.0f;
     f32x4 o = {0, 0, 0, 0};
-#pragma unroll 4
-    for (uint32_t p = down; p < n_parts; p += kDown) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(from + (uint64_t)p * D);
-      const float f = __builtin_amdgcn_exp2f(stat[2 * p] - high);
-      total += f * stat[2 * p + 1];
-      o += f * x;
-    }
-    lds_out[threadIdx.x] = o;
-    if (across == 0) lds_sum[down] = total;
-    __syncthreads();
-    if (down == 0) {
+    if (few) {
+      f32x4 x[kFewParts];
+      float top[kFewParts], sum[kFewParts];
 #pragma unroll
+      for (uint32_t p = 0; p < kFewParts; ++p) {
+        const uint64_t at = place(min(p, n_parts - 1));
+        x[p] = *reinterpret_cast<const f32x4*>(a.part_out + at * D + 4 * across);
+        top[p] = a.part_stat[2 * at];
+        sum[p] = p < n_parts ? a.part_stat[2 * at + 1] : 0.0f;
+      }
+#pragma unroll
+      for (uint32_t p = 0; p < kFewParts; ++p) high = fmaxf(high, top[p]);
+#pragma unroll
+      for (uint32_t p = 0; p < kFewParts; ++p) {
+        const float f = __builtin_amdgcn_exp2f(top[p] - high);
+        if (p < n_parts) {
+          total += f * sum[p];
+          o += f * x[p];
+        }
+      }
+    } else {
+      for (uint32_t p = threadIdx.x; p < n_parts; p += kThreads) high = fmaxf(high, a.part_stat[2 * place(p)]);
+#pragma unroll
+      for (int k = 32; k > 0; k /= 2) high = fmaxf(high, __shfl_xor(high, k));
+      __syncthreads();   // (the row before this one has been read)
+      if (lane == 0) lds_top[threadIdx.x / 64] = high;
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) high = fmaxf(high, lds_top[k]);
+#pragma unroll 4
+      for (uint32_t p = down; p < n_parts; p += kDown) {
+        const uint64_t at = place(p);
+        const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_out + at * D + 4 * across);
+        const float f = __builtin_amdgcn_exp2f(a.part_stat[2 * at] - high);
+        total += f * a.part_stat[2 * at + 1];
+        o += f * x;
+      }
+      lds_out[threadIdx.x] = o;
+      if (across == 0) lds_sum[down] = total;
+      __syncthreads();
+      if (down != 0) continue;
       for (uint32_t k = 1; k < kDown; ++k) {
         o += lds_out[k * kAcross + across];
         total += lds_sum[k];
       }
-      const float f = one_over(total);
-      uint32_t* to = reinterpret_cast<uint32_t*>(a.out + out_row * a.out_stride + 2 * (h * D + 4 * across));
-      to[0] = bf16_pair(o[0] * f, o[1] * f);
-      to[1] = bf16_pair(o[2] * f, o[3] * f);
-      if (across == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(high, total);
     }
+    const float f = one_over(total);
+    *reinterpret_cast<u32x2*>(a.out + out_row * a.out_stride + 2 * (h * D + 4 * across)) = u32x2{bf16_pair(o[0] * f, o[1] * f), bf16_pair(o[2] * f, o[3] * f)};
+    if (across == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(high, total);
   }
 }
 

@@ -155,50 +155,46 @@ int rows_call(const splitzip_cache* c, const splitzip_seqs* q, void* d_k, uint64
   return by_kind<F>(c, dim3((unsigned)wgs, q->n_seqs), static_cast<hipStream_t>(stream), (const RowsArgs*)&a);
 }
 
-// How an attention call is cut: which kernel, the rows of a (sequence, head of the cache) into tiles, its tokens into parts.
+// How an attention call is cut: which kernel, the rows of a (sequence, head of the cache) into tiles, the tokens of all sequences
+// into blocks and these into shares.
 struct AttentionPlan {
-  uint32_t waves, nt;   // 0: attention_tokens_kernel; else attention_rows_kernel with so many waves of 16 nt rows
-  uint32_t row_tiles, parts, part_tokens;
-  uint32_t heads_across;
+  uint32_t waves, nt;   // waves 0: attention_tokens_kernel; else attention_rows_kernel with so many waves of 16 nt rows
+  uint32_t heads_across, tile_rows, row_tiles, most_rows, kept;
+  uint32_t shares, block_tokens, least_blocks;
+  uint32_t wgs;
 };
-constexpr uint32_t kLeastPart = 256;   // tokens
-// the tokens that a launch is cut for: a window's, where rows see no more
-uint64_t tokens_planned(const splitzip_seqs* q, uint32_t window) {
-  uint64_t tokens = q->max_len < kMostTokens ? q->max_len : kMostTokens;
-  if (window && (uint64_t)window + q->max_rows + kStep < tokens) tokens = (uint64_t)window + q->max_rows + kStep;
-  return tokens ? tokens : 1;
-}
-// the parts that would fill the chip
-uint64_t parts_wanted(const splitzip_cache* c, const splitzip_seqs* q, const AttentionPlan& p) {
-  const uint64_t units = (uint64_t)q->n_seqs * (c->kv_heads / p.heads_across) * p.row_tiles, want = (uint64_t)cu_count() * (p.waves == 8 ? 2 : 4);
-  return units ? (want + units - 1) / units : 1;
-}
-AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, uint32_t q_heads, uint64_t tokens) {
+AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, uint32_t q_heads) {
   AttentionPlan p;
   const uint64_t rows = (uint64_t)(q->max_rows ? q->max_rows : 1) * (q_heads / c->kv_heads);
-  uint64_t tile = 16;
   p.waves = 0;
   p.nt = 1;
+  p.tile_rows = 16;
   p.heads_across = rows > 16 ? 1u : c->kv_heads % 4 == 0 ? 4u : c->kv_heads % 2 == 0 ? 2u : 1u;
   if (rows > 16) {
     p.waves = rows <= (c->head_dim == 256 ? 64 : 128) ? 4 : 8;
     p.nt = rows <= 64 || c->head_dim == 256 ? 1 : 2;
-    tile = 16ull * p.nt * p.waves;
+    p.tile_rows = 16 * p.nt * p.waves;
   }
-  const uint64_t tiles = (rows + tile - 1) / tile;
-  p.row_tiles = (uint32_t)(tiles < 4096 ? tiles : 4096);
-  const uint64_t parts = parts_wanted(c, q, p);
-  uint64_t per = (tokens + parts - 1) / parts;
-  per = (per + 127) / 128 * 128;
-  if (per < kLeastPart) per = kLeastPart;
-  p.part_tokens = (uint32_t)per;
-  p.parts = (uint32_t)((tokens + per - 1) / per);
+  const uint64_t tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+  p.row_tiles = (uint32_t)(tiles < 1024 ? tiles : 1024);
+  p.most_rows = (uint32_t)(rows < (uint64_t)p.row_tiles * p.tile_rows ? rows : (uint64_t)p.row_tiles * p.tile_rows);
+  p.kept = (uint32_t)(rows < p.tile_rows ? rows : p.tile_rows);
+  // as many workgroups as the chip holds at a time (two of 64 KB of LDS per CU; one of eight waves)
+  const uint64_t groups = (uint64_t)(c->kv_heads / p.heads_across) * p.row_tiles, slots = (uint64_t)cu_count() * (p.waves == 8 || (p.waves == 0 && c->dtype == SPLITZIP_BF16 && c->head_dim == 256) ? 1 : 2);
+  uint64_t shares = (slots + groups - 1) / groups;
+  // a block: what the waves of a head stage at a time
+  const uint32_t staged = 8192u / (c->head_dim * (p.waves ? 1 : words_bytes(c->dtype)));
+  p.block_tokens = p.waves ? staged : (staged < 32 ? 32 : staged) * (kWaves / p.heads_across);
+  // (a sum of blocks is kept in 32 bits)
+  const uint64_t most = (uint64_t)q->n_seqs * (q->d_block_table ? (uint64_t)q->table_stride * c->page_tokens : c->page_tokens);
+  while (most / p.block_tokens + q->n_seqs > (1ull << 31) && p.block_tokens < (1u << 30)) p.block_tokens *= 2;
+  p.least_blocks = p.waves ? 4 : 1;
+  const uint64_t some = ((uint64_t)q->n_seqs * (q->max_len < kMostTokens ? q->max_len : kMostTokens) + p.block_tokens - 1) / p.block_tokens + q->n_seqs;   // blocks, by what the call says
+  if (shares > (some + p.least_blocks - 1) / p.least_blocks) shares = (some + p.least_blocks - 1) / p.least_blocks;
+  if (shares < 1) shares = 1;
+  p.shares = (uint32_t)shares;
+  p.wgs = (uint32_t)((shares * (c->kv_heads / p.heads_across) + 7) / 8 * 8 * p.row_tiles);
   return p;
-}
-// the most parts that a call with these tokens or fewer (a window's) is cut into
-uint64_t most_parts(const splitzip_cache* c, const splitzip_seqs* q, uint32_t q_heads) {
-  const uint64_t parts = parts_wanted(c, q, plan_attention(c, q, q_heads, 1)), least = (tokens_planned(q, 0) + kLeastPart - 1) / kLeastPart;
-  return parts < least ? parts : least;
 }
 
 template <int KIND, int D>
@@ -215,9 +211,8 @@ struct Attend {
   }
 };
 
-uint64_t workspace_of(uint64_t parts, const splitzip_cache* c, uint32_t n_rows, uint32_t q_heads) {
-  return parts <= 1 ? 0 : (uint64_t)n_rows * q_heads * parts * (c->head_dim + 2) * sizeof(float);
-}
+uint64_t parts_of(const AttentionPlan& p) { return (uint64_t)p.wgs * 2 * p.heads_across * p.kept; }
+uint64_t workspace_of(const AttentionPlan& p, const splitzip_cache* c) { return p.shares <= 1 ? 0 : parts_of(p) * (c->head_dim + 2) * sizeof(float); }
 
 }  // namespace
 
@@ -235,7 +230,7 @@ int splitzip_cache_read(const splitzip_cache* cache, const splitzip_seqs* seqs, 
 
 size_t splitzip_attention_workspace_bytes(const splitzip_cache* cache, const splitzip_seqs* seqs, uint32_t n_rows, uint32_t q_heads) {
   if (check_cache(cache, false) != SPLITZIP_OK || check_seqs(cache, seqs) != SPLITZIP_OK || !q_heads || q_heads % cache->kv_heads) return 0;
-  return (size_t)workspace_of(most_parts(cache, seqs, q_heads), cache, n_rows, q_heads);
+  return n_rows ? (size_t)workspace_of(plan_attention(cache, seqs, q_heads), cache) : 0;
 }
 
 int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* seqs, const splitzip_attention* how, const void* d_q,
@@ -249,13 +244,11 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   if (!seqs->n_seqs || !n_rows) return SPLITZIP_OK;
   const uint64_t elems = (uint64_t)q_heads * cache->head_dim;
   if (n_rows > kMostTokens || elems * 2 > (1ull << 31)) return SPLITZIP_ERR_UNSUPPORTED;
-  const AttentionPlan p = plan_attention(cache, seqs, q_heads, tokens_planned(seqs, how->window));
-  const uint64_t need = workspace_of(p.parts, cache, n_rows, q_heads);
+  const AttentionPlan p = plan_attention(cache, seqs, q_heads);
+  const uint64_t need = workspace_of(p, cache);
   if (workspace_bytes < need) return SPLITZIP_ERR_CAPACITY;
   if (need && (!d_workspace || !aligned16(d_workspace))) return SPLITZIP_ERR_INVALID_ARG;
   if (!rows_ok(d_q, q_row_stride, elems) || !rows_ok(d_out, out_row_stride, elems) || !aligned(d_lse, 4)) return SPLITZIP_ERR_INVALID_ARG;
-  const uint64_t units = ((uint64_t)p.parts * seqs->n_seqs * (cache->kv_heads / p.heads_across) + 7) / 8 * 8 * p.row_tiles;
-  if (units >> 31) return SPLITZIP_ERR_UNSUPPORTED;
   AttentionArgs a;
   a.cache = device_cache(cache, seqs);
   a.seqs = device_seqs(cache, seqs, n_rows);
@@ -268,22 +261,28 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   a.tree = how->d_tree;
   a.positions = how->d_positions;
   a.part_out = static_cast<float*>(d_workspace);
-  a.part_stat = a.part_out + (uint64_t)n_rows * q_heads * p.parts * cache->head_dim;
+  a.part_stat = a.part_out + parts_of(p) * cache->head_dim;
   a.scale = how->scale < 0.0f ? -how->scale : how->scale;
   a.flip_q = how->scale < 0.0f ? 0x80008000u : 0u;
   a.softcap = how->softcap;
   a.tree_words = how->tree_words;
   a.window = how->window;
   a.group = q_heads / cache->kv_heads;
-  a.parts = p.parts;
-  a.part_tokens = p.part_tokens;
-  a.row_tiles = p.row_tiles;
   a.heads_across = p.heads_across;
+  a.tile_rows = p.tile_rows;
+  a.row_tiles = p.row_tiles;
+  a.most_rows = p.most_rows;
+  a.kept = p.kept;
+  a.shares = p.shares;
+  a.block_tokens = p.block_tokens;
+  a.least_blocks = p.least_blocks;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  rc = by_kind<Attend>(cache, dim3((unsigned)units), p.waves, p.nt, st, (const AttentionArgs*)&a);
-  if (rc != SPLITZIP_OK || p.parts == 1) return rc;
+  rc = by_kind<Attend>(cache, dim3(p.wgs), p.waves, p.nt, st, (const AttentionArgs*)&a);
+  if (rc != SPLITZIP_OK || p.shares == 1) return rc;
   const uint64_t outs = (uint64_t)(seqs->max_rows ? seqs->max_rows : 1) * q_heads;
-  const dim3 grid((unsigned)(outs < 8192 ? outs : 8192), seqs->n_seqs);
+  // up to 16 rows in a workgroup at a time, as many workgroups as the chip holds several times over
+  const uint64_t most = (uint64_t)cu_count() * 16 / seqs->n_seqs + 1;
+  const dim3 grid((unsigned)(outs < most ? outs : most), seqs->n_seqs);
   if (cache->head_dim == 64) hipLaunchKernelGGL(attention_join_kernel<64>, grid, dim3(kThreads), 0, st, a);
   else if (cache->head_dim == 128) hipLaunchKernelGGL(attention_join_kernel<128>, grid, dim3(kThreads), 0, st, a);
   else hipLaunchKernelGGL(attention_join_kernel<256>, grid, dim3(kThreads), 0, st, a);
