@@ -54,6 +54,16 @@ struct AttentionArgs {
   uint32_t shares, block_tokens, least_blocks;   // workgroups of the same heads and rows; what is dealt out to them
 };
 
+// The arguments once more, where they are needed now and then: read again from where the launch left them, rather than kept in
+// scalar registers (or, those used up, in lanes of vector registers) through loops that do not need them.
+__device__ inline AttentionArgs args_again() {
+  uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  AttentionArgs a;
+  __builtin_memcpy(&a, (const void*)(const __attribute__((address_space(4))) void*)at, sizeof a);
+  return a;
+}
+
 __device__ inline int position_of(const AttentionArgs& a, const Seq& s, int i) {
   return a.positions ? a.positions[s.start + i] : s.base + i;
 }
@@ -126,7 +136,8 @@ struct Share {
   bool whole;                       // the segment is all of the sequence: no part
   int later;                        // segments before this one
 
-  __device__ bool start(const AttentionArgs& a, uint32_t lane) {
+  __device__ bool start(uint32_t lane) {
+    const AttentionArgs a = args_again();
     // workgroups of the same (share, heads) lie 8 apart, on the same XCD
     wg = blockIdx.x;
     const uint32_t of = wg / 8 / a.row_tiles, groups = a.cache.heads / a.heads_across;
@@ -160,7 +171,8 @@ struct Share {
     slot = later ? 1u : 0u;
   }
   // to the next segment
-  __device__ bool next(const AttentionArgs& a) {
+  __device__ bool next() {
+    const AttentionArgs a = args_again();
     left -= min(blocks - block, left);
     ++later;
     do {
@@ -172,7 +184,8 @@ struct Share {
   }
   // The segment's first tile of rows, false if there is none, and the next one.  A sequence with more rows than the launch was cut for is taken
   // as a whole by the workgroups that have its first block, every row_tiles-th tile by each: nothing of it needs a place to be kept in.
-  __device__ bool first_rows(const AttentionArgs& a) {
+  __device__ bool first_rows() {
+    const AttentionArgs a = args_again();
     tile = wg / 8 % a.row_tiles;
     if (rows > a.most_rows) {
       if (block) return false;
@@ -182,7 +195,8 @@ struct Share {
     }
     return (uint64_t)tile * a.tile_rows < rows;
   }
-  __device__ bool more_rows(const AttentionArgs& a) {
+  __device__ bool more_rows() {
+    const AttentionArgs a = args_again();
     tile += a.row_tiles;
     return (uint64_t)tile * a.tile_rows < rows;   // (up to most_rows there are no more than row_tiles)
   }
@@ -199,7 +213,8 @@ struct Rows {
   bf16x8 q[NT][D / 32];
   int64_t low_edge;       // tokens up to here may be out of a row's window
 
-  __device__ void load(const AttentionArgs& a, const Share& w, uint32_t r0, uint32_t m, uint32_t g) {
+  __device__ void load(const Share& w, uint32_t r0, uint32_t m, uint32_t g) {
+    const AttentionArgs a = args_again();
     low_edge = -0x7fffffffffffffff;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -228,7 +243,8 @@ struct Rows {
   // whether every row sees every one of the 32 tokens from t0 on
   __device__ bool see_all(const Share& w, int t0) const { return t0 + (int)kStep <= min(w.s.base, w.s.len) && (int64_t)t0 > low_edge; }
   // bit e: row n sees token t8 + e
-  __device__ uint32_t seen(const AttentionArgs& a, const Share& w, int n, int t8) const {
+  __device__ uint32_t seen(const Share& w, int n, int t8) const {
+    const AttentionArgs a = args_again();
     if (row[n] < 0) return 0;
     const int behind = min(max(w.s.len - t8, 0), 8), j0 = t8 - w.s.base;   // j0: the row that token t8 is
     uint32_t bits = (1u << behind) - 1u;
@@ -268,6 +284,9 @@ __device__ inline float shaped(const AttentionArgs& a, float x, float slope_log2
   return x * kLog2e - slope_log2 * far;
 }
 
+// what the scores times it are powers of two; 0 where they are capped or biased
+__device__ inline float plain_scale(const AttentionArgs& a) { return a.softcap == 0.0f && !a.slopes ? a.scale * kLog2e : 0.0f; }
+
 __device__ inline f32x4 mfma(const bf16x8& x, const bf16x8& y, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
 __device__ inline bf16x8 as_bf16(const u32x4& x) { return __builtin_bit_cast(bf16x8, x); }
 
@@ -287,18 +306,20 @@ struct State {
     }
   }
 
-  // The weights of the lane's eight tokens from their scores x (all: every row sees all of them; else seen).
+  // The weights of the lane's eight tokens from their scores x (all: every row sees all of them; else seen).  c: powers of two are the scores
+  // times c; 0: the scores have a shape.
   template <int KIND>
-  __device__ void weigh(const AttentionArgs& a, const Share& w, const Rows<KIND, D, NT>& r, const f32x4 (&x)[NT][2], bool all,
+  __device__ void weigh(float c, const Share& w, const Rows<KIND, D, NT>& r, const f32x4 (&x)[NT][2], bool all,
                         const uint32_t (&seen)[NT], int t8, bf16x8 (&p)[NT]) {
-    const bool plain = a.softcap == 0.0f && !a.slopes && a.scale > 0.0f;   // powers of two are the scores times c
-    const float c = plain ? a.scale * kLog2e : 1.0f;
+    const bool plain = c > 0.0f;
+    if (!plain) c = 1.0f;
     float y[NT][8], high[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[n][e] = x[n][e / 4][e % 4];
       if (!plain) {
+        const AttentionArgs a = args_again();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float far = 0.0f;
@@ -353,7 +374,7 @@ struct State {
   // times an infinity or a NaN is no 0: tokens with such words are taken out of the product, and added one by one to the rows that see
   // them, from memory (element(j, i): which element the lane has in acc[n][j][i]).
   template <int KIND, typename V, typename E>
-  __device__ void add_guarded(const AttentionArgs& a, const Share& w, int t0, const V& get, const E& element, const bf16x8 (&p)[NT],
+  __device__ void add_guarded(const Share& w, int t0, const V& get, const E& element, const bf16x8 (&p)[NT],
                               const uint32_t (&seen)[NT], uint32_t m) {
     u32x4 high = {0, 0, 0, 0};   // per token: 0x80 where an element's exponent is all ones, in any of the lane's
 #pragma unroll
@@ -373,13 +394,15 @@ struct State {
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) add(j, as_bf16(get(j) & keep), p);
     if (!__ballot(odd != 0)) return;
+    const AttentionArgs a = args_again();
+    const Pages pages(a.cache, a.seqs, w.seq);
 #pragma unroll 1
     for (uint32_t k = 0; k < kStep; ++k) {
       if (!((uint32_t)__builtin_amdgcn_readlane((int)odd, (int)(k / 8 * 16)) >> (k % 8) & 1)) continue;
-      const uint32_t t = (uint32_t)t0 + k, page = page_of_token(a.cache, a.seqs, w.seq, t), place = place_of_token(a.cache, a.seqs, t);
-      const uint8_t* at = a.cache.v + word_offset(a.cache, page, place, w.head);
+      const uint32_t t = (uint32_t)t0 + k, page = pages.page(t), place = pages.place(t);
+      const uint8_t* at = a.cache.v + token_offset(a.cache, page, place) + w.head * a.cache.head_stride;
       uint32_t byte = 0;
-      if constexpr (KIND != SPLITZIP_BF16) byte = a.cache.v_scales[scale_offset(a.cache, a.seqs, page, place, w.head)];
+      if constexpr (KIND != SPLITZIP_BF16) byte = a.cache.v_scales[scale_offset(a.cache, page, place, w.head)];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const bool mine = (uint32_t)__shfl((int)seen[n], (int)(k / 8 * 16 + m)) >> (k % 8) & 1;
@@ -440,8 +463,8 @@ struct Stream {
   __device__ static uint32_t v_row(uint32_t token) { return kUnits == 8 ? token ^ (token / 8 & 1) : token; }
 
   // asks for the stage from token t0 on; pages: lane l has the page of its 8 l-th token; offsets: bytes from page and place
-  __device__ static void ask(const AttentionArgs& a, const uint8_t* k_base, const uint8_t* v_base, uint32_t pages, int t0, uint32_t last8,
-                             uint8_t* lds, uint32_t lane) {
+  __device__ static void ask(const Cache& c, const Pages& at_pages, const uint8_t* k_base, const uint8_t* v_base, uint32_t pages, int t0,
+                             uint32_t last8, uint8_t* lds, uint32_t lane) {
 #pragma unroll
     for (int i = 0; i < kHalf / 1024; ++i) {
       const uint32_t unit = (uint32_t)i * 64 + lane, row = unit / kUnits, at = unit % kUnits;   // where this lane's 16 bytes come to lie
@@ -450,10 +473,9 @@ struct Stream {
       uint32_t page;
       if constexpr (kUnits >= 8) page = (uint32_t)__builtin_amdgcn_readlane((int)pages, i * 64 / kUnits / 8);
       else page = (uint32_t)__shfl((int)pages, (int)(row / 8));
-      const uint32_t place = place_of_token(a.cache, a.seqs, min((uint32_t)t0 + 8 * eight, last8));
-      const uint64_t from = page * a.cache.page_stride + place * a.cache.token_stride;
-      const uint32_t k_off = row % 8 * (uint32_t)a.cache.token_stride + (at ^ k_key(row)) * 16;
-      const uint32_t v_off = v_row(row) % 8 * (uint32_t)a.cache.token_stride + at * 16;
+      const uint64_t from = token_offset(c, page, at_pages.place(min((uint32_t)t0 + 8 * eight, last8)));
+      const uint32_t k_off = row % 8 * c.token_stride + (at ^ k_key(row)) * 16;
+      const uint32_t v_off = v_row(row) % 8 * c.token_stride + at * 16;
       load_to_lds(k_base + from + k_off, lds + i * 1024);
       load_to_lds(v_base + from + v_off, lds + kHalf + i * 1024);
     }
@@ -461,36 +483,37 @@ struct Stream {
 };
 
 template <int KIND, int D>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Stream<KIND, D>::kHalf > 8192 ? 1 : 2))) attention_tokens_kernel(AttentionArgs a) {
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Stream<KIND, D>::kHalf > 8192 ? 1 : 2))) attention_tokens_kernel(AttentionArgs args) {
   using S = Stream<KIND, D>;
   constexpr int ES = S::ES, KS = S::KS, DV = S::DV, KW = S::KW, VW = S::VW;
   __shared__ __attribute__((aligned(1024))) uint8_t lds_all[kWaves][2 * S::kHalf];
   __shared__ float lds_stat[kWaves][16][2];
   const uint32_t lane = threadIdx.x % 64, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), m = lane % 16, g = lane / 16;
   Share w;
-  if (!w.start(a, lane)) return;
-  const uint32_t hw = a.heads_across, tw = kWaves / hw, turn = wave / hw;   // heads of the workgroup, waves of a head, which of them
+  if (!w.start(lane)) return;
+  const Cache c = args.cache;
+  const float plain = plain_scale(args);
+  const uint32_t hw = args.heads_across, tw = kWaves / hw, turn = wave / hw;   // heads of the workgroup, waves of a head, which of them
   w.head += wave % hw;
-  const uint8_t *k_base = a.cache.k + w.head * a.cache.head_stride, *v_base = a.cache.v + w.head * a.cache.head_stride;
+  const uint8_t *k_base = c.k + w.head * c.head_stride, *v_base = c.v + w.head * c.head_stride;
   uint8_t* const mine = lds_all[wave];
   const int stride = (int)tw * S::kTokens;
 
   do {
-    if (!w.first_rows(a)) continue;
+    if (!w.first_rows()) continue;
     do {
     const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
-    const auto ask_pages = [&](int t0) {
-      return page_of_token(a.cache, a.seqs, w.seq, min((uint32_t)t0 + 8 * (lane % (S::kTokens / 8)), last8));
-    };
+    const Pages at_pages(c, args.seqs, w.seq);
+    const auto ask_pages = [&](int t0) { return at_pages.page(min((uint32_t)t0 + 8 * (lane % (S::kTokens / 8)), last8)); };
     u32x2 k_scales[S::kSteps], v_scales[S::kSteps];
     const auto ask_scales = [&](uint32_t pages, int t0) {
       if constexpr (ES == 1) {
 #pragma unroll
         for (int u = 0; u < S::kSteps; ++u) {
           const uint32_t k4 = 4 * u + m / 4, v4 = 4 * u + g;
-          const uint32_t k_place = place_of_token(a.cache, a.seqs, min((uint32_t)t0 + 8 * k4, last8)), v_place = place_of_token(a.cache, a.seqs, min((uint32_t)t0 + 8 * v4, last8));
-          k_scales[u] = *reinterpret_cast<const u32x2*>(a.cache.k_scales + scale_offset(a.cache, a.seqs, (uint32_t)__shfl((int)pages, (int)k4), k_place, w.head));
-          v_scales[u] = *reinterpret_cast<const u32x2*>(a.cache.v_scales + scale_offset(a.cache, a.seqs, (uint32_t)__shfl((int)pages, (int)v4), v_place, w.head));
+          const uint32_t k_place = at_pages.place(min((uint32_t)t0 + 8 * k4, last8)), v_place = at_pages.place(min((uint32_t)t0 + 8 * v4, last8));
+          k_scales[u] = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, (uint32_t)__shfl((int)pages, (int)k4), k_place, w.head));
+          v_scales[u] = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, (uint32_t)__shfl((int)pages, (int)v4), v_place, w.head));
         }
       }
     };
@@ -498,12 +521,12 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
     uint32_t pages = 0;
     if (t0 < w.end) {
       pages = ask_pages(t0);
-      S::ask(a, k_base, v_base, pages, t0, last8, mine, lane);
+      S::ask(c, at_pages, k_base, v_base, pages, t0, last8, mine, lane);
       ask_scales(pages, t0);
       if (t0 + stride < w.end) pages = ask_pages(t0 + stride);
     }
     Rows<KIND, D, 1> r;
-    r.load(a, w, w.tile * 16, m, g);
+    r.load(w, w.tile * 16, m, g);
     State<D, 1> st;
     st.clear();
 #pragma unroll 1
@@ -532,7 +555,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
       }
       lds_read();   // into registers: the place is free
       if (t0 + stride < w.end) {
-        S::ask(a, k_base, v_base, pages, t0 + stride, last8, mine, lane);
+        S::ask(c, at_pages, k_base, v_base, pages, t0 + stride, last8, mine, lane);
         ask_scales(pages, t0 + stride);
         if (t0 + 2 * stride < w.end) pages = ask_pages(t0 + 2 * stride);
       }
@@ -557,9 +580,9 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
         const bool all = r.see_all(w, tu);
         const int t8 = tu + (int)(8 * g);
         uint32_t seen[1] = {0xffu};
-        if (!all) seen[0] = r.seen(a, w, 0, t8);
+        if (!all) seen[0] = r.seen(w, 0, t8);
         bf16x8 p[1];
-        st.weigh(a, w, r, x, all, seen, t8, p);
+        st.weigh(plain, w, r, x, all, seen, t8, p);
         u32x4 vt[DV];   // element j of the eight tokens
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -588,7 +611,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
 #pragma unroll
             for (int j = 0; j < DV; ++j) vt[j][i] &= in;
           }
-          st.template add_guarded<KIND>(a, w, tu, [&](int j) { return vt[j]; }, [&](int j, int i) { return DV * (4 * g + i) + j; }, p, seen, m);
+          st.template add_guarded<KIND>(w, tu, [&](int j) { return vt[j]; }, [&](int j, int i) { return DV * (4 * g + i) + j; }, p, seen, m);
         }
       }
     }
@@ -624,6 +647,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
     }
     const uint32_t at = w.tile * 16 + m;
     if (turn == 0 && at < w.rows) {
+      const AttentionArgs a = args_again();
       const uint32_t q_heads = a.cache.heads * a.group, h = w.head * a.group + at % a.group;
       const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(at / a.group));
       if (w.whole) {
@@ -649,8 +673,8 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
         }
       }
     }
-    } while (w.more_rows(a));
-  } while (w.next(a));
+    } while (w.more_rows());
+  } while (w.next());
 }
 
 // More rows: the W waves of a workgroup take 16 NT rows each of the same tokens.  Those are staged in LDS, 32 KB at a time and twice
@@ -668,15 +692,15 @@ struct Stage {
 
   // piece s of K: tiles of 16 tokens and steps, operand f = 4 s + i being step f % KS of tile f / KS
   __device__ static uint32_t k_group(uint32_t s, uint32_t m) { return 4 * s / KS / 2 * 32 + 8 * (m / 4); }
-  __device__ void load_k(const Cache& c, const Seqs& q, uint32_t page, uint32_t t8, uint32_t head, uint32_t s, uint32_t m, uint32_t g) {
-    const uint32_t place = place_of_token(c, q, t8);
-    const uint8_t* at = c.k + word_offset(c, page, place + m % 4, head) + 16 * g;
+  // (base: of the head, the lane's token of eight and its 16 bytes)
+  __device__ void load_k(const Cache& c, const uint8_t* base, uint32_t page, uint32_t place, uint32_t head, uint32_t s) {
+    const uint8_t* at = base + token_offset(c, page, place);
 #pragma unroll
     for (int i = 0; i < 2 * ES; ++i) {
       const uint32_t f = 4 * s + (ES == 2 ? i : 2 * i);
-      k[i] = *reinterpret_cast<const u32x4*>(at + f / KS % 2 * 4 * c.token_stride + (ES == 2 ? f % KS : f % KS / 2) * 64);
+      k[i] = *reinterpret_cast<const u32x4*>(at + (uint64_t)(f / KS % 2 * 4) * c.token_stride + (ES == 2 ? f % KS : f % KS / 2) * 64);
     }
-    if constexpr (ES == 1) scales = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, q, page, place, head));
+    if constexpr (ES == 1) scales = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, page, place, head));
   }
   __device__ void store_k(u32x4* to, uint32_t s, uint32_t m) const {
 #pragma unroll
@@ -691,12 +715,11 @@ struct Stage {
   }
   // piece s of V: 64 elements (block s % (D / 64)) of 32 tokens; a lane has elements 4 m .. 4 m + 3 of them of tokens 8 g ..
   __device__ static uint32_t v_group(uint32_t s, uint32_t g) { return s / (D / 64) * 32 + 8 * g; }
-  __device__ void load_v(const Cache& c, const Seqs& q, uint32_t page, uint32_t t8, uint32_t head, uint32_t s, uint32_t m) {
-    const uint32_t place = place_of_token(c, q, t8);
-    const uint8_t* at = c.v + word_offset(c, page, place, head) + ES * (64 * (s % (D / 64)) + 4 * m);
+  __device__ void load_v(const Cache& c, const uint8_t* base, uint32_t page, uint32_t place, uint32_t head, uint32_t s, uint32_t m) {
+    const uint8_t* at = base + token_offset(c, page, place) + ES * (64 * (s % (D / 64)) + 4 * m);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) __builtin_memcpy(v[e], __builtin_assume_aligned(at + e * c.token_stride, 4 * ES), 4 * ES);
-    if constexpr (ES == 1) scales = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, q, page, place, head));
+    for (int e = 0; e < 8; ++e) __builtin_memcpy(v[e], __builtin_assume_aligned(at + (uint64_t)e * c.token_stride, 4 * ES), 4 * ES);
+    if constexpr (ES == 1) scales = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, page, place, head));
   }
   __device__ void store_v(u32x4* to, uint32_t s, int t8, int len, bool inner) const {
     u32x4 vt[4];
@@ -728,7 +751,7 @@ struct Stage {
 };
 
 template <int KIND, int D, int W, int NT>
-__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) attention_rows_kernel(AttentionArgs a) {
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) attention_rows_kernel(AttentionArgs args) {
   using S = Stage<KIND, D>;
   constexpr int KS = S::KS, DV = S::DV, kTokens = S::kTokens;
   constexpr bool kBoth = W == 4;   // a wave stages a piece of K and one of V; else waves 0 .. 3 K, the others V
@@ -736,14 +759,18 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
   __shared__ u32x4 lds[2][32 * 64];
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, m = lane % 16, g = lane / 16;
   Share w;
-  if (!w.start(a, lane)) return;
+  if (!w.start(lane)) return;
+  const Cache c = args.cache;
+  const float plain = plain_scale(args);
+  const uint8_t *k_base = c.k + w.head * c.head_stride + (uint64_t)(m % 4) * c.token_stride + 16 * g, *v_base = c.v + w.head * c.head_stride;
   const uint32_t piece = wave % 4;
   const bool of_k = kBoth || wave < 4, of_v = kBoth || wave >= 4;
 
   do {
-    if (!w.first_rows(a)) continue;
+    if (!w.first_rows()) continue;
     do {
     const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;
+    const Pages at_pages(c, args.seqs, w.seq);
     const uint32_t r0 = (w.tile * W + wave) * 16 * NT;
     const bool active = r0 < w.rows;
     Rows<KIND, D, NT> r;
@@ -754,18 +781,18 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
     uint32_t k_page = 0, v_page = 0;
     const auto ask_pages = [&](int t0) {
       if (t0 >= w.end) return;
-      if (of_k) k_page = page_of_token(a.cache, a.seqs, w.seq, k8(t0));
-      if (of_v) v_page = page_of_token(a.cache, a.seqs, w.seq, v8(t0));
+      if (of_k) k_page = at_pages.page(k8(t0));
+      if (of_v) v_page = at_pages.page(v8(t0));
     };
     const auto ask = [&](int t0) {
       if (t0 >= w.end) return;
-      if (of_k) sk.load_k(a.cache, a.seqs, k_page, k8(t0), w.head, piece, m, g);
-      if (of_v) sv.load_v(a.cache, a.seqs, v_page, v8(t0), w.head, piece, m);
+      if (of_k) sk.load_k(c, k_base, k_page, at_pages.place(k8(t0)), w.head, piece);
+      if (of_v) sv.load_v(c, v_base, v_page, at_pages.place(v8(t0)), w.head, piece, m);
     };
     ask_pages(w.begin);
     ask(w.begin);
     ask_pages(w.begin + kTokens);
-    r.load(a, w, r0, m, g);
+    r.load(w, r0, m, g);
     st.clear();
     int buf = 0;
 #pragma unroll 1
@@ -797,15 +824,15 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
         const int t8 = tu + (int)(8 * g);
         uint32_t seen[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) seen[n] = all ? 0xffu : r.seen(a, w, n, t8);
+        for (int n = 0; n < NT; ++n) seen[n] = all ? 0xffu : r.seen(w, n, t8);
         bf16x8 p[NT];
-        st.weigh(a, w, r, x, all, seen, t8, p);
+        st.weigh(plain, w, r, x, all, seen, t8, p);
           const u32x4* v = at + 64 * (16 + u * DV);
         if (all) {
 #pragma unroll
           for (int j = 0; j < DV; ++j) st.add(j, as_bf16(v[64 * j]), p);
         } else {
-          st.template add_guarded<KIND>(a, w, tu, [&](int j) { return v[64 * j]; },
+          st.template add_guarded<KIND>(w, tu, [&](int j) { return v[64 * j]; },
                                         [&](int j, int i) { return 64 * (j / 4) + 16 * g + 4 * i + j % 4; }, p, seen, m);
         }
       }
@@ -813,6 +840,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
     lds_barrier();   // the next tile of rows writes where these tokens are
 
     // lane (m, g) has elements 64 b + 16 g + 4 i + j of row m in acc[4 b + j][i]
+    const AttentionArgs a = args_again();
     const uint32_t q_heads = a.cache.heads * a.group;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -850,8 +878,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
         }
       }
     }
-    } while (w.more_rows(a));
-  } while (w.next(a));
+    } while (w.more_rows());
+  } while (w.next());
 }
 
 // The parts of a sequence together.  D / 4 threads have a row and query head, four elements each: where the parts are few, as many rows

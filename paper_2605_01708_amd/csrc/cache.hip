@@ -46,7 +46,8 @@ int check_cache(const splitzip_cache* c, bool pointers) {
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return SPLITZIP_ERR_UNSUPPORTED;
   if (!c->kv_heads || !c->n_pages || c->page_tokens < 8 || c->page_tokens > kMostTokens) return SPLITZIP_ERR_INVALID_ARG;
   if (!aligned16(c->page_stride_bytes) || !aligned16(c->token_stride_bytes) || !aligned16(c->head_stride_bytes)) return SPLITZIP_ERR_INVALID_ARG;
-  if (c->token_stride_bytes > (1ull << 28)) return SPLITZIP_ERR_UNSUPPORTED;   // eight of them are a 32-bit offset
+  // eight tokens are a 32-bit offset, and so is a page
+  if (c->token_stride_bytes > (1ull << 28) || c->page_stride_bytes >> 32 || c->scale_page_stride_bytes >> 32) return SPLITZIP_ERR_UNSUPPORTED;
   const uint64_t row = (uint64_t)c->head_dim * words_bytes(c->dtype);
   if (c->token_stride_bytes < row || c->head_stride_bytes < row) return SPLITZIP_ERR_INVALID_ARG;
   if (c->dtype != SPLITZIP_BF16 && (c->scale_page_stride_bytes & 7u || c->page_tokens & 7u)) return SPLITZIP_ERR_INVALID_ARG;
@@ -74,12 +75,13 @@ Cache device_cache(const splitzip_cache* c, const splitzip_seqs* q) {
   d.v = static_cast<uint8_t*>(c->d_v);
   d.k_scales = c->dtype == SPLITZIP_BF16 ? nullptr : c->d_k_scales;
   d.v_scales = c->dtype == SPLITZIP_BF16 ? nullptr : c->d_v_scales;
-  d.page_stride = c->page_stride_bytes;
-  d.token_stride = c->token_stride_bytes;
   d.head_stride = c->head_stride_bytes;
-  d.scale_page_stride = c->scale_page_stride_bytes;
+  d.page_stride = (uint32_t)c->page_stride_bytes;
+  d.token_stride = (uint32_t)c->token_stride_bytes;
+  d.scale_page_stride = (uint32_t)c->scale_page_stride_bytes;
   d.page_shift = q->d_block_table ? 31u - (uint32_t)__builtin_clz(c->page_tokens) : 30u;
-  d.n_pages = c->n_pages;
+  d.page_tokens = c->page_tokens;
+  d.last_page = c->n_pages - 1;
   d.heads = c->kv_heads;
   return d;
 }

@@ -20,9 +20,11 @@ constexpr int kTopE5m2 = 15, kTopE4m3 = 8;
 struct Cache {
   uint8_t *k, *v;
   uint8_t *k_scales, *v_scales;
-  uint64_t page_stride, token_stride, head_stride, scale_page_stride;   // bytes
+  uint64_t head_stride;                                 // bytes
+  uint32_t page_stride, token_stride, scale_page_stride;   // bytes: a product with a 32-bit number is one instruction
   uint32_t page_shift;   // log2 of the tokens per page, at least 3: eight tokens in a row from a multiple of eight share a page
-  uint32_t n_pages, heads;
+  uint32_t page_tokens;
+  uint32_t last_page, heads;
 };
 
 // sequences: rows [starts[s], starts[s + 1]) of this call's tensors are the last tokens of the lens[s] that s has in the cache
@@ -47,21 +49,24 @@ __device__ inline Seq seq_at(const Seqs& q, uint32_t s) {
   return r;
 }
 
-// pool page of token t of sequence s (t below the sequence's length)
-__device__ inline uint32_t page_of_token(const Cache& c, const Seqs& q, uint32_t s, uint32_t t) {
-  const uint32_t page = q.table ? q.table[(uint64_t)s * q.table_stride + (t >> c.page_shift)] : s;
-  return page < c.n_pages ? page : c.n_pages - 1;   // a bad table entry never leaves the pool
-}
-__device__ inline uint32_t place_of_token(const Cache& c, const Seqs& q, uint32_t t) {
-  return q.table ? t & ((1u << c.page_shift) - 1u) : t;
-}
-// byte of the first word of a token and head; the same offset in K and V
-__device__ inline uint64_t word_offset(const Cache& c, uint32_t page, uint32_t place, uint32_t head) {
-  return page * c.page_stride + place * c.token_stride + head * c.head_stride;
+// where a sequence's tokens are
+struct Pages {
+  const uint32_t* row;     // of the table, or null
+  uint32_t seq, shift, mask, last;
+  __device__ Pages() {}
+  __device__ Pages(const Cache& c, const Seqs& q, uint32_t s)
+      : row(q.table ? q.table + (uint64_t)s * q.table_stride : nullptr), seq(s), shift(c.page_shift), mask(q.table ? c.page_tokens - 1 : ~0u), last(c.last_page) {}
+  // of token t, below the sequence's length: the page in the pool (a bad table entry never leaves it), the place in the page
+  __device__ uint32_t page(uint32_t t) const { return row ? min(row[t >> shift], last) : seq; }
+  __device__ uint32_t place(uint32_t t) const { return t & mask; }
+};
+// byte of a token's words, heads apart; the same offset in K and V
+__device__ inline uint64_t token_offset(const Cache& c, uint32_t page, uint32_t place) {
+  return (uint64_t)page * c.page_stride + (uint64_t)place * c.token_stride;
 }
 // byte of its scale: [heads][tokens of a page], so that the scales of eight tokens of a head are one load
-__device__ inline uint64_t scale_offset(const Cache& c, const Seqs& q, uint32_t page, uint32_t place, uint32_t head) {
-  return page * c.scale_page_stride + (uint64_t)head * (q.table ? 1u << c.page_shift : q.capacity) + place;
+__device__ inline uint64_t scale_offset(const Cache& c, uint32_t page, uint32_t place, uint32_t head) {
+  return (uint64_t)page * c.scale_page_stride + (uint64_t)head * c.page_tokens + place;
 }
 
 // 16 bytes per lane from memory straight into LDS: the wave's lanes one behind the other from `to` on, which is the wave's.  They are
@@ -145,8 +150,8 @@ __device__ inline uint32_t fp8_pair_to_bf16(uint32_t w, uint32_t byte) {
 
 // nearest BF16, ties to even
 __device__ inline uint32_t bf16_pair(float lo, float hi) {
-  const __bf16 a = (__bf16)lo, b = (__bf16)hi;
-  return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
 
 // 8 FP8 words times 2^(byte - 127) as BF16
@@ -162,6 +167,7 @@ template <int KIND, int D>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(RowsArgs a) {
   constexpr int kLanes = D / 8, kPairs = kThreads / kLanes;
   const Seq s = seq_at(a.seqs, blockIdx.y);
+  const Pages at_pages(a.cache, a.seqs, blockIdx.y);
   const uint32_t lane = threadIdx.x % kLanes, pairs = (uint32_t)s.rows * a.cache.heads;
   for (uint32_t p = blockIdx.x * kPairs + threadIdx.x / kLanes; p < pairs; p += gridDim.x * kPairs) {
     const uint32_t i = p / a.cache.heads, head = p - i * a.cache.heads;
@@ -169,8 +175,8 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(RowsArgs a) {
     if (t < 0) continue;
     const uint64_t row = (uint64_t)(uint32_t)(s.start + (int)i), at = 2 * (head * D + lane * 8);
     const u32x4 k = *reinterpret_cast<const u32x4*>(a.k + row * a.k_stride + at), v = *reinterpret_cast<const u32x4*>(a.v + row * a.v_stride + at);
-    const uint32_t page = page_of_token(a.cache, a.seqs, blockIdx.y, (uint32_t)t), place = place_of_token(a.cache, a.seqs, (uint32_t)t);
-    const uint64_t word = word_offset(a.cache, page, place, head);
+    const uint32_t page = at_pages.page((uint32_t)t), place = at_pages.place((uint32_t)t);
+    const uint64_t word = token_offset(a.cache, page, place) + head * a.cache.head_stride;
     if constexpr (KIND == SPLITZIP_BF16) {
       *reinterpret_cast<u32x4*>(a.cache.k + word + lane * 16) = k;
       *reinterpret_cast<u32x4*>(a.cache.v + word + lane * 16) = v;
@@ -186,7 +192,7 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(RowsArgs a) {
       *reinterpret_cast<u32x2*>(a.cache.k + word + lane * 8) = to_fp8<KIND>(k, bk);
       *reinterpret_cast<u32x2*>(a.cache.v + word + lane * 8) = to_fp8<KIND>(v, bv);
       if (lane == 0) {
-        const uint64_t scale = scale_offset(a.cache, a.seqs, page, place, head);
+        const uint64_t scale = scale_offset(a.cache, page, place, head);
         a.cache.k_scales[scale] = (uint8_t)bk;
         a.cache.v_scales[scale] = (uint8_t)bv;
       }
@@ -198,6 +204,7 @@ template <int KIND, int D>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(RowsArgs a) {
   constexpr int kLanes = D / 8, kPairs = kThreads / kLanes;
   const Seq s = seq_at(a.seqs, blockIdx.y);
+  const Pages at_pages(a.cache, a.seqs, blockIdx.y);
   const uint32_t lane = threadIdx.x % kLanes, pairs = (uint32_t)s.rows * a.cache.heads;
   for (uint32_t p = blockIdx.x * kPairs + threadIdx.x / kLanes; p < pairs; p += gridDim.x * kPairs) {
     const uint32_t i = p / a.cache.heads, head = p - i * a.cache.heads;
@@ -205,13 +212,13 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(RowsArgs a) {
     const uint64_t row = (uint64_t)(uint32_t)(s.start + (int)i), at = 2 * (head * D + lane * 8);
     u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};   // a row in front of the sequence's first token
     if (t >= 0) {
-      const uint32_t page = page_of_token(a.cache, a.seqs, blockIdx.y, (uint32_t)t), place = place_of_token(a.cache, a.seqs, (uint32_t)t);
-      const uint64_t word = word_offset(a.cache, page, place, head);
+      const uint32_t page = at_pages.page((uint32_t)t), place = at_pages.place((uint32_t)t);
+      const uint64_t word = token_offset(a.cache, page, place) + head * a.cache.head_stride;
       if constexpr (KIND == SPLITZIP_BF16) {
         k = *reinterpret_cast<const u32x4*>(a.cache.k + word + lane * 16);
         v = *reinterpret_cast<const u32x4*>(a.cache.v + word + lane * 16);
       } else {
-        const uint64_t scale = scale_offset(a.cache, a.seqs, page, place, head);
+        const uint64_t scale = scale_offset(a.cache, page, place, head);
         k = from_fp8<KIND>(*reinterpret_cast<const u32x2*>(a.cache.k + word + lane * 8), a.cache.k_scales[scale]);
         v = from_fp8<KIND>(*reinterpret_cast<const u32x2*>(a.cache.v + word + lane * 8), a.cache.v_scales[scale]);
       }
@@ -235,6 +242,7 @@ struct MoveArgs {
 };
 __global__ void __launch_bounds__(kThreads) cache_move_kernel(MoveArgs a) {
   const Seq s = seq_at(a.seqs, blockIdx.y);
+  const Pages at_pages(a.cache, a.seqs, blockIdx.y);
   const auto& at = a.at[blockIdx.z];
   uint8_t* const words = blockIdx.x ? at.v : at.k;
   uint8_t* const scales = blockIdx.x ? at.v_scales : at.k_scales;
@@ -250,12 +258,12 @@ __global__ void __launch_bounds__(kThreads) cache_move_kernel(MoveArgs a) {
       before = from;
       const int t = s.base + from, to = s.base + (int)i;
       if (from == (int)i || to < 0) continue;
-      const uint32_t p0 = page_of_token(a.cache, a.seqs, blockIdx.y, (uint32_t)t), l0 = place_of_token(a.cache, a.seqs, (uint32_t)t);
-      const uint32_t p1 = page_of_token(a.cache, a.seqs, blockIdx.y, (uint32_t)to), l1 = place_of_token(a.cache, a.seqs, (uint32_t)to);
+      const uint32_t p0 = at_pages.page((uint32_t)t), l0 = at_pages.place((uint32_t)t), p1 = at_pages.page((uint32_t)to), l1 = at_pages.place((uint32_t)to);
       if (is_word)
-        *reinterpret_cast<u32x4*>(words + word_offset(a.cache, p1, l1, head) + piece * 16) = *reinterpret_cast<const u32x4*>(words + word_offset(a.cache, p0, l0, head) + piece * 16);
+        *reinterpret_cast<u32x4*>(words + token_offset(a.cache, p1, l1) + head * a.cache.head_stride + piece * 16) =
+            *reinterpret_cast<const u32x4*>(words + token_offset(a.cache, p0, l0) + head * a.cache.head_stride + piece * 16);
       else
-        scales[scale_offset(a.cache, a.seqs, p1, l1, head)] = scales[scale_offset(a.cache, a.seqs, p0, l0, head)];
+        scales[scale_offset(a.cache, p1, l1, head)] = scales[scale_offset(a.cache, p0, l0, head)];
     }
   }
 }
