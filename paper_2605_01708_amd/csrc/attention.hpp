@@ -208,23 +208,27 @@ struct Share {
 // The lane's rows (r0 + 16 n + m of the product) and their operand of the first product.
 template <int KIND, int D, int NT>
 struct Rows {
-  int row[NT], pos[NT];   // row of the sequence (-1: none), its position
-  float slope[NT];        // times log2 e
+  int row[NT], slot[NT];  // row of the sequence (-1: none), query head of the group
+  int low_edge;           // tokens up to here may be out of the window of a row of the workgroup's tile
   bf16x8 q[NT][D / 32];
-  int64_t low_edge;       // tokens up to here may be out of a row's window
 
   __device__ void load(const Share& w, uint32_t r0, uint32_t m, uint32_t g) {
     const AttentionArgs a = args_again();
-    low_edge = -0x7fffffffffffffff;
+    low_edge = -1;
+    if (a.window) {
+      for (uint32_t r = w.tile * a.tile_rows + 16 * g + m; r < min((w.tile + 1) * a.tile_rows, w.rows); r += 64)
+        low_edge = max(low_edge, (int)min((int64_t)position_of(a, w.s, (int)(r / a.group)) - (int64_t)a.window, (int64_t)w.s.len));
+#pragma unroll
+      for (int o = 32; o > 0; o /= 2) low_edge = max(low_edge, __shfl_xor(low_edge, o));
+    }
+    low_edge = __builtin_amdgcn_readfirstlane(low_edge);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const uint32_t r = r0 + 16 * n + m;
       const bool have = r < w.rows;
       row[n] = have ? (int)(r / a.group) : -1;
-      const uint32_t h = w.head * a.group + (have ? r % a.group : 0);
-      pos[n] = have ? position_of(a, w.s, row[n]) : 0;
-      slope[n] = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
-      if (have && a.window) low_edge = max(low_edge, (int64_t)pos[n] - (int64_t)a.window);
+      slot[n] = have ? (int)(r % a.group) : 0;
+      const uint32_t h = w.head * a.group + (uint32_t)slot[n];
       const uint8_t* at = a.q + (uint64_t)(uint32_t)(w.s.start + max(row[n], 0)) * a.q_stride + 2 * (uint64_t)h * D;
 #pragma unroll
       for (int t = 0; t < D / 32; ++t) {
@@ -235,13 +239,10 @@ struct Rows {
         q[n][t] = __builtin_bit_cast(bf16x8, x);
       }
     }
-    if (a.window) {
-#pragma unroll
-      for (int o = 8; o > 0; o /= 2) low_edge = max(low_edge, (int64_t)__shfl_xor((long long)low_edge, o));
-    }
   }
-  // whether every row sees every one of the 32 tokens from t0 on
-  __device__ bool see_all(const Share& w, int t0) const { return t0 + (int)kStep <= min(w.s.base, w.s.len) && (int64_t)t0 > low_edge; }
+  // whether every row of the tile sees every one of the tokens from t0 on
+  __device__ bool see_all(const Share& w, int t0, int tokens) const { return t0 + tokens <= min(w.s.base, w.s.len) && t0 > low_edge; }
+  __device__ float slope(const AttentionArgs& a, const Share& w, int n) const { return a.slopes[w.head * a.group + slot[n]] * kLog2e; }
   // bit e: row n sees token t8 + e
   __device__ uint32_t seen(const Share& w, int n, int t8) const {
     const AttentionArgs a = args_again();
@@ -263,10 +264,11 @@ struct Rows {
       bits &= b;
     }
     if (a.window) {
+      const int pos = position_of(a, w.s, row[n]);
 #pragma unroll 1
       for (int e = 0; e < 8; ++e) {
         const int j = j0 + e, at = j >= 0 && t8 + e < w.s.len ? position_of(a, w.s, j) : t8 + e;
-        if ((int64_t)pos[n] - (int64_t)at >= (int64_t)a.window) bits &= ~(1u << e);
+        if ((int64_t)pos - (int64_t)at >= (int64_t)a.window) bits &= ~(1u << e);
       }
     }
     return bits;
@@ -284,11 +286,11 @@ __device__ inline float shaped(const AttentionArgs& a, float x, float slope_log2
   return x * kLog2e - slope_log2 * far;
 }
 
-// what the scores times it are powers of two; 0 where they are capped or biased
-__device__ inline float plain_scale(const AttentionArgs& a) { return a.softcap == 0.0f && !a.slopes ? a.scale * kLog2e : 0.0f; }
-
 __device__ inline f32x4 mfma(const bf16x8& x, const bf16x8& y, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
 __device__ inline bf16x8 as_bf16(const u32x4& x) { return __builtin_bit_cast(bf16x8, x); }
+
+// Nothing is fetched ahead across this: on the ways that are rarely taken, registers count, which the usual way needs.
+__device__ inline void one_at_a_time() { asm volatile("" ::: "memory"); }
 
 // What a wave has of its rows: outputs (tile j of D / 16: an element per lane and register), the sum of the weights of the lane's own
 // tokens and the running maximum, of powers of two.
@@ -306,40 +308,45 @@ struct State {
     }
   }
 
-  // The weights of the lane's eight tokens from their scores x (all: every row sees all of them; else seen).  c: powers of two are the scores
-  // times c; 0: the scores have a shape.
+  // Scores x of the 32 tokens from t0 on (the lane's eight from t0 + 8 g on), as they come out of the product:
+  // capped and biased, in powers of two
   template <int KIND>
-  __device__ void weigh(float c, const Share& w, const Rows<KIND, D, NT>& r, const f32x4 (&x)[NT][2], bool all,
-                        const uint32_t (&seen)[NT], int t8, bf16x8 (&p)[NT]) {
-    const bool plain = c > 0.0f;
-    if (!plain) c = 1.0f;
-    float y[NT][8], high[NT];
+  static __device__ void shape(const Share& w, const Rows<KIND, D, NT>& r, f32x4 (&x)[NT][2], int t8) {
+    const AttentionArgs a = args_again();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+      const int pos = a.slopes && r.row[n] >= 0 ? position_of(a, w.s, r.row[n]) : 0;
+      const float slope = a.slopes && r.row[n] >= 0 ? r.slope(a, w, n) : 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[n][e] = x[n][e / 4][e % 4];
-      if (!plain) {
-        const AttentionArgs a = args_again();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float far = 0.0f;
-          if (a.slopes) {
-            const int t = t8 + e, j = t - w.s.base;
-            far = (float)(r.pos[n] - (j >= 0 && t < w.s.len ? position_of(a, w.s, j) : t));
-          }
-          y[n][e] = shaped(a, y[n][e], r.slope[n], far);
+      for (int e = 0; e < 8; ++e) {
+        float far = 0.0f;
+        if (a.slopes) {
+          const int t = t8 + e, j = t - w.s.base;
+          far = (float)(pos - (j >= 0 && t < w.s.len ? position_of(a, w.s, j) : t));
         }
+        x[n][e / 4][e % 4] = shaped(a, x[n][e / 4][e % 4], slope, far);
       }
-      if (!all) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[n][e] = seen[n] >> e & 1 ? y[n][e] : -__builtin_inff();
-      }
-      high[n] = fmaxf(fmaxf(fmaxf(y[n][0], y[n][1]), fmaxf(y[n][2], y[n][3])), fmaxf(fmaxf(y[n][4], y[n][5]), fmaxf(y[n][6], y[n][7]))) * c;
     }
-    bool raise = false;
+  }
+  // without the tokens that a row does not see
+  template <int KIND>
+  static __device__ void mask(const Share& w, const Rows<KIND, D, NT>& r, f32x4 (&x)[NT][2], int t8) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) raise |= high[n] > top[n] + kSlack;
-    if (__ballot(raise)) {
+    for (int n = 0; n < NT; ++n) {
+      const uint32_t seen = r.seen(w, n, t8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[n][e / 4][e % 4] = seen >> e & 1 ? x[n][e / 4][e % 4] : -__builtin_inff();
+    }
+  }
+  static __device__ float highest(const f32x4 (&x)[2]) {
+    return fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+  }
+  // The running maximum, raised if need be; high: the lane's highest score of the tokens to come, in powers of two.
+  __device__ void raise(const float (&high)[NT]) {
+    bool need = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) need |= high[n] > top[n] + kSlack;
+    if (__builtin_expect(__ballot(need) != 0, 0)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float h = high[n];
@@ -352,11 +359,14 @@ struct State {
         for (int j = 0; j < D / 16; ++j) acc[n][j] *= less;
       }
     }
+  }
+  // The weights of the lane's eight tokens and their sum; powers of two are the scores times c.
+  __device__ void weigh(float c, const f32x4 (&x)[NT][2], bf16x8 (&p)[NT]) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       float e[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[n][i], c, -top[n]));
+      for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i / 4][i % 4], c, -top[n]));
       sum[n] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
       p[n] = as_bf16(u32x4{bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7])});
     }
@@ -370,55 +380,36 @@ struct State {
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n][j] = mfma(v, p[n], acc[n][j]);
   }
-  // The same for 32 tokens, from t0 on, that some row does not see; get(j): operand j of V.  Such a token may hold anything, and 0
-  // times an infinity or a NaN is no 0: tokens with such words are taken out of the product, and added one by one to the rows that see
-  // them, from memory (element(j, i): which element the lane has in acc[n][j][i]).
-  template <int KIND, typename V, typename E>
-  __device__ void add_guarded(const Share& w, int t0, const V& get, const E& element, const bf16x8 (&p)[NT],
-                              const uint32_t (&seen)[NT], uint32_t m) {
-    u32x4 high = {0, 0, 0, 0};   // per token: 0x80 where an element's exponent is all ones, in any of the lane's
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) {
-      const u32x4 v = get(j);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) high[i] |= ((v[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-    }
-    uint32_t odd = 0;   // bit e: token e of the lane's eight
-#pragma unroll
-    for (int i = 0; i < 4; ++i) odd |= (high[i] >> 15 & 1u) << (2 * i) | high[i] >> 31 << (2 * i + 1);
-#pragma unroll
-    for (int o = 8; o > 0; o /= 2) odd |= (uint32_t)__shfl_xor((int)odd, o);   // in any element
-    u32x4 keep;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) keep[i] = (odd >> (2 * i) & 1 ? 0u : 0xffffu) | (odd >> (2 * i) & 2 ? 0u : 0xffff0000u);
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) add(j, as_bf16(get(j) & keep), p);
-    if (!__ballot(odd != 0)) return;
+  // A token that some row does not see may hold anything, and 0 times an infinity or a NaN is no 0: where there are such tokens, V goes
+  // into the product without these words (finite_only), and what rows do see of them is added here, from memory, when the
+  // tokens from `begin` to `end` are done, which went in `step` at a time.  (A weight that is not 0 does not change what is added.)  element(j, i): which element the lane has in acc[n][j][i].
+  template <int KIND, typename E>
+  __device__ void add_odd(const Share& w, const Rows<KIND, D, NT>& r, int begin, int end, int step, const E& element) {
     const AttentionArgs a = args_again();
     const Pages pages(a.cache, a.seqs, w.seq);
 #pragma unroll 1
-    for (uint32_t k = 0; k < kStep; ++k) {
-      if (!((uint32_t)__builtin_amdgcn_readlane((int)odd, (int)(k / 8 * 16)) >> (k % 8) & 1)) continue;
-      const uint32_t t = (uint32_t)t0 + k, page = pages.page(t), place = pages.place(t);
-      const uint8_t* at = a.cache.v + token_offset(a.cache, page, place) + w.head * a.cache.head_stride;
-      uint32_t byte = 0;
-      if constexpr (KIND != SPLITZIP_BF16) byte = a.cache.v_scales[scale_offset(a.cache, page, place, w.head)];
+    for (int t0 = begin; t0 < end; t0 += step) {
+      if (r.see_all(w, t0, step)) continue;
+#pragma unroll 1
+      for (int t = t0; t < min(t0 + step, min(end, w.s.len)); ++t) {
+        const uint32_t page = pages.page((uint32_t)t), place = pages.place((uint32_t)t);
+        const uint8_t* at = a.cache.v + token_offset(a.cache, page, place) + w.head * a.cache.head_stride;
+        uint32_t byte = 0;
+        if constexpr (KIND != SPLITZIP_BF16) byte = a.cache.v_scales[scale_offset(a.cache, page, place, w.head)];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const bool mine = (uint32_t)__shfl((int)seen[n], (int)(k / 8 * 16 + m)) >> (k % 8) & 1;
-        const u32x4 all = __builtin_bit_cast(u32x4, p[n]);
-        const uint32_t pair = k / 2 % 4 == 0 ? all[0] : k / 2 % 4 == 1 ? all[1] : k / 2 % 4 == 2 ? all[2] : all[3];
-        const uint32_t half = (uint32_t)__shfl((int)pair, (int)(k / 8 * 16 + m)) >> (16 * (k % 2)) << 16;
+        for (int n = 0; n < NT; ++n) {
+          const bool mine = r.seen(w, n, t & ~7) >> (t & 7) & 1;
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
+          for (int j = 0; j < D / 16; ++j) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t v;
-            if constexpr (KIND == SPLITZIP_BF16) v = reinterpret_cast<const uint16_t*>(at)[element(j, i)];
-            else v = fp8_pair_to_bf16<KIND, false>(at[element(j, i)], byte);
-            if (mine) acc[n][j][i] = __builtin_fmaf(__uint_as_float(half), __uint_as_float(v << 16), acc[n][j][i]);
+            for (int i = 0; i < 4; ++i) {
+              uint32_t v;
+              if constexpr (KIND == SPLITZIP_BF16) v = reinterpret_cast<const uint16_t*>(at)[element(j, i)];
+              else v = fp8_pair_to_bf16<KIND, false>(at[element(j, i)], byte) & 0xffffu;
+              acc[n][j][i] += mine && (v & 0x7f80u) == 0x7f80u ? __uint_as_float(v << 16) : 0.0f;
+            }
+            one_at_a_time();
           }
-          asm volatile("" ::: "memory");   // (four loads at a time: a rare way, and registers are what the usual one needs)
         }
       }
     }
@@ -430,6 +421,22 @@ __device__ inline uint32_t evens(uint32_t t0, uint32_t t1) { return byte_perm(t1
 __device__ inline uint32_t odds(uint32_t t0, uint32_t t1) { return byte_perm(t1, t0, 0x07060302u); }
 // halves of a pair of tokens that are among the sequence's
 __device__ inline uint32_t inside(int t, int len) { return (t < len ? 0xffffu : 0u) | (t + 1 < len ? 0xffff0000u : 0u); }
+// zeros for the infinities and NaN of N registers of V (element j of the eight tokens from t8 on in vt[j]); whether a token of the sequence had one
+template <int N>
+__device__ inline bool finite_only(u32x4 (&vt)[N], int t8, int len) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t in = inside(t8 + 2 * i, len);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const uint32_t odd = ((vt[j][i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // an exponent of ones carries into the sign's place
+      vt[j][i] &= ~(odd - (odd >> 15) | odd);
+      any |= odd & in;
+    }
+  }
+  return any != 0;
+}
 
 __device__ inline float lse_of(float top, float total) { return total != 0.0f ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff(); }
 __device__ inline float one_over(float total) { return total != 0.0f ? 1.0f / total : 0.0f; }   // (a NaN is no 0)
@@ -482,7 +489,7 @@ struct Stream {
   }
 };
 
-template <int KIND, int D>
+template <int KIND, int D, bool PLAIN>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Stream<KIND, D>::kHalf > 8192 ? 1 : 2))) attention_tokens_kernel(AttentionArgs args) {
   using S = Stream<KIND, D>;
   constexpr int ES = S::ES, KS = S::KS, DV = S::DV, KW = S::KW, VW = S::VW;
@@ -492,7 +499,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
   Share w;
   if (!w.start(lane)) return;
   const Cache c = args.cache;
-  const float plain = plain_scale(args);
+  const float scale = PLAIN ? args.scale * kLog2e : 1.0f;   // PLAIN: scores without cap and bias, their powers of two the products times this
   const uint32_t hw = args.heads_across, tw = kWaves / hw, turn = wave / hw;   // heads of the workgroup, waves of a head, which of them
   w.head += wave % hw;
   const uint8_t *k_base = c.k + w.head * c.head_stride, *v_base = c.v + w.head * c.head_stride;
@@ -529,6 +536,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
     r.load(w, w.tile * 16, m, g);
     State<D, 1> st;
     st.clear();
+    bool odd = false;   // words of V were left out
 #pragma unroll 1
     for (; t0 < w.end; t0 += stride) {
       memory_arrived();
@@ -577,12 +585,13 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
             }
           }
         }
-        const bool all = r.see_all(w, tu);
+        const bool all = r.see_all(w, tu, (int)kStep);
         const int t8 = tu + (int)(8 * g);
-        uint32_t seen[1] = {0xffu};
-        if (!all) seen[0] = r.seen(w, 0, t8);
+        if constexpr (!PLAIN) st.shape(w, r, x, t8);
+        if (__builtin_expect(!all, 0)) st.mask(w, r, x, t8);
+        st.raise({st.highest(x[0]) * scale});
         bf16x8 p[1];
-        st.weigh(plain, w, r, x, all, seen, t8, p);
+        st.weigh(scale, x, p);
         u32x4 vt[DV];   // element j of the eight tokens
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -601,19 +610,14 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
             vt[j + 1][i] = odds(w0, w1);
           }
         }
-        if (all) {
+        if (__builtin_expect(!all, 0)) odd |= finite_only(vt, t8, w.s.len);
 #pragma unroll
-          for (int j = 0; j < DV; ++j) st.add(j, as_bf16(vt[j]), p);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t in = inside(t8 + 2 * i, w.s.len);
-#pragma unroll
-            for (int j = 0; j < DV; ++j) vt[j][i] &= in;
-          }
-          st.template add_guarded<KIND>(w, tu, [&](int j) { return vt[j]; }, [&](int j, int i) { return DV * (4 * g + i) + j; }, p, seen, m);
-        }
+        for (int j = 0; j < DV; ++j) st.add(j, as_bf16(vt[j]), p);
       }
+    }
+    if (__builtin_expect(__ballot(odd) != 0, 0)) {
+      const auto element = [&](int j, int i) { return DV * (4 * g + i) + j; };
+      for (int t = w.begin + (int)turn * S::kTokens; t < w.end; t += stride) st.add_odd(w, r, t, min(t + S::kTokens, w.end), (int)kStep, element);
     }
 
     // the waves of a head together, where there are several; lane (m, g) has elements DV (4 g + i) + j of row m in acc[j][i]
@@ -677,20 +681,22 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
   } while (w.next());
 }
 
-// More rows: the W waves of a workgroup take 16 NT rows each of the same tokens.  Those are staged in LDS, 32 KB at a time and twice
-// over, as the 32 operands of the matrix instruction that they are (lane after lane, 16 bytes each: written and read without
-// a bank conflict), FP8 words converted and V transposed once for all waves.  Staging is dealt out as four pieces of K and four of V, four
-// operands each; a wave asks for its pieces of the next tokens before it works on these.
-template <int KIND, int D>
+// More rows: the W waves of a workgroup take 16 NT rows each of the same tokens.  Those are staged in LDS, 4 KB per wave at a time, as the
+// operands of the matrix instruction that they are (lane after lane, 16 bytes each: written and read without a bank
+// conflict), FP8 words converted and V transposed once for all waves.  Half of the waves stage four operands of K each, the others
+// four of V; a wave asks for its piece of the next stage before it works on this one, which is written in the other half of LDS: one
+// barrier a stage, since who writes a half has passed the barrier behind which nobody reads it.
+template <int KIND, int D, int W>
 struct Stage {
   static constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
   static constexpr int KS = D / 32, DV = D / 16;
-  static constexpr int kTokens = 8192 / D;
-  u32x4 k[2 * ES];      // rows of K: operands 4 s .. 4 s + 3, two of them in 16 bytes of FP8
-  uint32_t v[8][ES];    // four elements of eight tokens
+  static constexpr int kTokens = W * 1024 / D, kUnits = kTokens / (int)kStep;
+  static constexpr int kV = 2 * W;   // operands of K, and of V behind them
+  static_assert(kTokens >= (int)kStep, "a stage has 32 tokens at least");
+  uint32_t w[8 * ES];   // K: 16-byte runs of rows, operands 4 s .. 4 s + 3 (two of them in 16 bytes of FP8); V: four elements of eight tokens
   u32x2 scales;
 
-  // piece s of K: tiles of 16 tokens and steps, operand f = 4 s + i being step f % KS of tile f / KS
+  // piece s of K: operand f = 4 s + i is step f % KS of the tile f / KS of 16 tokens
   __device__ static uint32_t k_group(uint32_t s, uint32_t m) { return 4 * s / KS / 2 * 32 + 8 * (m / 4); }
   // (base: of the head, the lane's token of eight and its 16 bytes)
   __device__ void load_k(const Cache& c, const uint8_t* base, uint32_t page, uint32_t place, uint32_t head, uint32_t s) {
@@ -698,7 +704,9 @@ struct Stage {
 #pragma unroll
     for (int i = 0; i < 2 * ES; ++i) {
       const uint32_t f = 4 * s + (ES == 2 ? i : 2 * i);
-      k[i] = *reinterpret_cast<const u32x4*>(at + (uint64_t)(f / KS % 2 * 4) * c.token_stride + (ES == 2 ? f % KS : f % KS / 2) * 64);
+      const u32x4 x = *reinterpret_cast<const u32x4*>(at + (uint64_t)(f / KS % 2 * 4) * c.token_stride + (ES == 2 ? f % KS : f % KS / 2) * 64);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
     }
     if constexpr (ES == 1) scales = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, page, place, head));
   }
@@ -706,178 +714,195 @@ struct Stage {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (ES == 2) {
-        to[64 * (4 * s + i)] = k[i];
+        to[64 * i] = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
       } else {
         const uint32_t pair = (4 * s + i) / KS % 2 ? scales[1] : scales[0];
-        to[64 * (4 * s + i)] = from_fp8<KIND>(u32x2{k[i / 2][i % 2 * 2], k[i / 2][i % 2 * 2 + 1]}, pair >> (8 * (m % 4)) & 0xffu);
+        to[64 * i] = from_fp8<KIND>(u32x2{w[2 * i], w[2 * i + 1]}, pair >> (8 * (m % 4)) & 0xffu);
       }
     }
   }
   // piece s of V: 64 elements (block s % (D / 64)) of 32 tokens; a lane has elements 4 m .. 4 m + 3 of them of tokens 8 g ..
   __device__ static uint32_t v_group(uint32_t s, uint32_t g) { return s / (D / 64) * 32 + 8 * g; }
-  __device__ void load_v(const Cache& c, const uint8_t* base, uint32_t page, uint32_t place, uint32_t head, uint32_t s, uint32_t m) {
-    const uint8_t* at = base + token_offset(c, page, place) + ES * (64 * (s % (D / 64)) + 4 * m);
+  __device__ void load_v(const Cache& c, const uint8_t* base, uint32_t page, uint32_t place, uint32_t head) {
+    const uint8_t* at = base + token_offset(c, page, place);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) __builtin_memcpy(v[e], __builtin_assume_aligned(at + (uint64_t)e * c.token_stride, 4 * ES), 4 * ES);
+    for (int e = 0; e < 8; ++e) __builtin_memcpy(w + ES * e, __builtin_assume_aligned(at + (uint64_t)e * c.token_stride, 4 * ES), 4 * ES);
     if constexpr (ES == 1) scales = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, page, place, head));
   }
-  __device__ void store_v(u32x4* to, uint32_t s, int t8, int len, bool inner) const {
+  // guarded: without infinities and NaN; true if there were some
+  __device__ bool store_v(u32x4* to, bool guarded, int t8, int len) const {
     u32x4 vt[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t x0[2], x1[2];
       if constexpr (ES == 2) {
-        x0[0] = v[2 * i][0];
-        x0[1] = v[2 * i][1];
-        x1[0] = v[2 * i + 1][0];
-        x1[1] = v[2 * i + 1][1];
+        x0[0] = w[4 * i];
+        x0[1] = w[4 * i + 1];
+        x1[0] = w[4 * i + 2];
+        x1[1] = w[4 * i + 3];
       } else {
         const uint32_t b0 = scales[i / 2] >> (16 * (i % 2)) & 0xffu, b1 = scales[i / 2] >> (16 * (i % 2) + 8) & 0xffu;
-        x0[0] = fp8_pair_to_bf16<KIND, false>(v[2 * i][0], b0);
-        x0[1] = fp8_pair_to_bf16<KIND, true>(v[2 * i][0], b0);
-        x1[0] = fp8_pair_to_bf16<KIND, false>(v[2 * i + 1][0], b1);
-        x1[1] = fp8_pair_to_bf16<KIND, true>(v[2 * i + 1][0], b1);
+        x0[0] = fp8_pair_to_bf16<KIND, false>(w[2 * i], b0);
+        x0[1] = fp8_pair_to_bf16<KIND, true>(w[2 * i], b0);
+        x1[0] = fp8_pair_to_bf16<KIND, false>(w[2 * i + 1], b1);
+        x1[1] = fp8_pair_to_bf16<KIND, true>(w[2 * i + 1], b1);
       }
-      const uint32_t in = inner ? 0xffffffffu : inside(t8 + 2 * i, len);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        vt[2 * j][i] = evens(x0[j], x1[j]) & in;
-        vt[2 * j + 1][i] = odds(x0[j], x1[j]) & in;
+        vt[2 * j][i] = evens(x0[j], x1[j]);
+        vt[2 * j + 1][i] = odds(x0[j], x1[j]);
       }
     }
+    bool odd = false;
+    if (__builtin_expect(guarded, 0)) odd = finite_only(vt, t8, len);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) to[64 * (16 + 4 * s + j)] = vt[j];
+    for (int j = 0; j < 4; ++j) to[64 * j] = vt[j];
+    return odd;
   }
 };
 
-template <int KIND, int D, int W, int NT>
-__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) attention_rows_kernel(AttentionArgs args) {
-  using S = Stage<KIND, D>;
-  constexpr int KS = S::KS, DV = S::DV, kTokens = S::kTokens;
-  constexpr bool kBoth = W == 4;   // a wave stages a piece of K and one of V; else waves 0 .. 3 K, the others V
-  static_assert(W == 4 || W == 8, "four pieces of K and four of V");
-  __shared__ u32x4 lds[2][32 * 64];
-  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, m = lane % 16, g = lane / 16;
+template <int KIND, int D, int W, int NT, bool PLAIN>
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 4 && NT == 1 ? 3 : 2))) attention_rows_kernel(AttentionArgs args) {
+  using S = Stage<KIND, D, W>;
+  constexpr int KS = S::KS, DV = S::DV, kTokens = S::kTokens, kUnits = S::kUnits;
+  __shared__ u32x4 lds[2][W * 4 * 64];
+  __shared__ uint32_t lds_odd;   // words of V were left out
+  const uint32_t lane = threadIdx.x % 64, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), m = lane % 16, g = lane / 16;
   Share w;
   if (!w.start(lane)) return;
   const Cache c = args.cache;
-  const float plain = plain_scale(args);
-  const uint8_t *k_base = c.k + w.head * c.head_stride + (uint64_t)(m % 4) * c.token_stride + 16 * g, *v_base = c.v + w.head * c.head_stride;
-  const uint32_t piece = wave % 4;
-  const bool of_k = kBoth || wave < 4, of_v = kBoth || wave >= 4;
+  const float scale = PLAIN ? args.scale * kLog2e : 1.0f;
+  const bool of_k = wave < W / 2;
+  const uint32_t piece = wave % (W / 2);
+  const uint8_t* const base = of_k ? c.k + w.head * c.head_stride + (uint64_t)(m % 4) * c.token_stride + 16 * g
+                                   : c.v + w.head * c.head_stride + S::ES * (64 * (piece % (D / 64)) + 4 * m);
+  const uint32_t group = of_k ? S::k_group(piece, m) : S::v_group(piece, g);   // the lane's eight tokens of a stage
+  if (threadIdx.x == 0) lds_odd = 0;
+  lds_barrier();
 
   do {
     if (!w.first_rows()) continue;
     do {
-    const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;
-    const Pages at_pages(c, args.seqs, w.seq);
-    const uint32_t r0 = (w.tile * W + wave) * 16 * NT;
-    const bool active = r0 < w.rows;
-    Rows<KIND, D, NT> r;
-    State<D, NT> st;
-    S sk, sv;
-    const auto k8 = [&](int t0) { return min((uint32_t)t0 + S::k_group(piece, m), last8); };
-    const auto v8 = [&](int t0) { return min((uint32_t)t0 + S::v_group(piece, g), last8); };
-    uint32_t k_page = 0, v_page = 0;
-    const auto ask_pages = [&](int t0) {
-      if (t0 >= w.end) return;
-      if (of_k) k_page = at_pages.page(k8(t0));
-      if (of_v) v_page = at_pages.page(v8(t0));
-    };
-    const auto ask = [&](int t0) {
-      if (t0 >= w.end) return;
-      if (of_k) sk.load_k(c, k_base, k_page, at_pages.place(k8(t0)), w.head, piece);
-      if (of_v) sv.load_v(c, v_base, v_page, at_pages.place(v8(t0)), w.head, piece, m);
-    };
-    ask_pages(w.begin);
-    ask(w.begin);
-    ask_pages(w.begin + kTokens);
-    r.load(w, r0, m, g);
-    st.clear();
-    int buf = 0;
-#pragma unroll 1
-    for (int t0 = w.begin; t0 < w.end; t0 += kTokens, buf ^= 1) {
-      if (of_k) sk.store_k(lds[buf] + lane, piece, m);
-      if (of_v) sv.store_v(lds[buf] + lane, piece, t0 + (int)S::v_group(piece, g), w.s.len, t0 + kTokens <= w.s.len);
-      ask(t0 + kTokens);
-      ask_pages(t0 + 2 * kTokens);
-      lds_barrier();   // one is enough: who writes the other half has passed it, so nobody reads that half any more
-      if (!active) continue;
-      const u32x4* at = lds[buf] + lane;
-#pragma unroll 1
-      for (int u = 0; u < kTokens / (int)kStep; ++u) {
-        const int tu = t0 + u * (int)kStep;
-        if (tu >= w.end) break;
-        f32x4 x[NT][2];
+      const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
+      const Pages at_pages(c, args.seqs, w.seq);
+      const uint32_t r0 = (w.tile * W + wave) * 16 * NT;
+      const bool active = r0 < w.rows;
+      Rows<KIND, D, NT> r;
+      State<D, NT> st;
+      S stage;
+      uint32_t page = 0;
+      const auto ask_page = [&](int t0) {
+        if (t0 < w.end) page = at_pages.page(min((uint32_t)t0 + group, last8));
+      };
+      const auto ask = [&](int t0) {
+        if (t0 >= w.end) return;
+        const uint32_t place = at_pages.place(min((uint32_t)t0 + group, last8));
+        if (of_k) stage.load_k(c, base, page, place, w.head, piece);
+        else stage.load_v(c, base, page, place, w.head);
+      };
+      const auto store = [&](int t0, int buf) {
+        if (t0 >= w.end) return;
+        u32x4* to = lds[buf] + 64 * (of_k ? 4 * piece : S::kV + 4 * piece) + lane;
+        if (of_k) stage.store_k(to, piece, m);
+        else if (__builtin_expect(stage.store_v(to, !r.see_all(w, t0, kTokens), t0 + (int)group, w.s.len), 0)) lds_odd = 1;
+      };
+      // the scores of 32 tokens, unit u of a stage
+      const auto scores = [&](f32x4 (&x)[NT][2], const u32x4* at) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) x[n][b] = f32x4{0, 0, 0, 0};
 #pragma unroll
           for (int t = 0; t < KS; ++t) {
-            const bf16x8 k = as_bf16(at[64 * ((2 * u + b) * KS + t)]);
+            const bf16x8 k = as_bf16(at[64 * (b * KS + t)]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) x[n][b] = mfma(k, r.q[n][t], x[n][b]);
           }
         }
-        const bool all = r.see_all(w, tu);
-        const int t8 = tu + (int)(8 * g);
-        uint32_t seen[NT];
+      };
+      ask_page(w.begin);
+      ask(w.begin);
+      ask_page(w.begin + kTokens);
+      r.load(w, r0, m, g);
+      st.clear();
+      int buf = 0;
+#pragma unroll 1
+      for (int t0 = w.begin; t0 < w.end; t0 += kTokens, buf ^= 1) {
+        store(t0, buf);
+        ask(t0 + kTokens);
+        ask_page(t0 + 2 * kTokens);
+        lds_barrier();
+        if (!active) continue;
+        const u32x4* const at = lds[buf] + lane;
+        // all units of the stage at a time, so that there is one question about the maximum, and enough to do between its answers
+        const bool all = r.see_all(w, t0, kTokens);
+        f32x4 x[kUnits][NT][2];
+        float high[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) seen[n] = all ? 0xffu : r.seen(w, n, t8);
-        bf16x8 p[NT];
-        st.weigh(plain, w, r, x, all, seen, t8, p);
-          const u32x4* v = at + 64 * (16 + u * DV);
-        if (all) {
+        for (int u = 0; u < kUnits; ++u) {
+          const int t8 = t0 + u * (int)kStep + (int)(8 * g);
+          scores(x[u], at + 64 * 2 * KS * u);
+          if constexpr (!PLAIN) st.shape(w, r, x[u], t8);
+          if (__builtin_expect(!all, 0)) st.mask(w, r, x[u], t8);
+        }
 #pragma unroll
-          for (int j = 0; j < DV; ++j) st.add(j, as_bf16(v[64 * j]), p);
-        } else {
-          st.template add_guarded<KIND>(w, tu, [&](int j) { return v[64 * j]; },
-                                        [&](int j, int i) { return 64 * (j / 4) + 16 * g + 4 * i + j % 4; }, p, seen, m);
+        for (int n = 0; n < NT; ++n) {
+          high[n] = st.highest(x[0][n]);
+#pragma unroll
+          for (int u = 1; u < kUnits; ++u) high[n] = fmaxf(high[n], st.highest(x[u][n]));
+          high[n] *= scale;
+        }
+        st.raise(high);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+          bf16x8 p[NT];
+          st.weigh(scale, x[u], p);
+#pragma unroll
+          for (int j = 0; j < DV; ++j) st.add(j, as_bf16(at[64 * (S::kV + u * DV + j)]), p);
         }
       }
-    }
-    lds_barrier();   // the next tile of rows writes where these tokens are
+      lds_barrier();   // the next tile of rows writes where these tokens are
+      if (__builtin_expect(lds_odd, 0)) st.add_odd(w, r, w.begin, w.end, kTokens, [&](int j, int i) { return 64 * (j / 4) + 16 * g + 4 * i + j % 4; });
 
-    // lane (m, g) has elements 64 b + 16 g + 4 i + j of row m in acc[4 b + j][i]
-    const AttentionArgs a = args_again();
-    const uint32_t q_heads = a.cache.heads * a.group;
+      // lane (m, g) has elements 64 b + 16 g + 4 i + j of row m in acc[4 b + j][i]
+      const AttentionArgs a = args_again();
+      const uint32_t q_heads = a.cache.heads * a.group;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const uint32_t row = r0 + 16 * n + m;
-      const float total = st.total(n);
-      if (row >= w.rows) continue;
-      const uint32_t h = w.head * a.group + row % a.group;
-      const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(row / a.group));
-      if (w.whole) {
-        const float f = one_over(total);
-        uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + 16 * g);
+      for (int n = 0; n < NT; ++n) {
+        const uint32_t row = r0 + 16 * n + m;
+        const float total = st.total(n);
+        if (row >= w.rows) continue;
+        const uint32_t h = w.head * a.group + row % a.group;
+        const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(row / a.group));
+        if (w.whole) {
+          const float f = one_over(total);
+          uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + 16 * g);
 #pragma unroll
-        for (int b = 0; b < D / 64; ++b) {
-          u32x4 o[2];
+          for (int b = 0; b < D / 64; ++b) {
+            u32x4 o[2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            o[i / 2][i % 2 * 2] = bf16_pair(st.acc[n][4 * b][i] * f, st.acc[n][4 * b + 1][i] * f);
-            o[i / 2][i % 2 * 2 + 1] = bf16_pair(st.acc[n][4 * b + 2][i] * f, st.acc[n][4 * b + 3][i] * f);
+            for (int i = 0; i < 4; ++i) {
+              o[i / 2][i % 2 * 2] = bf16_pair(st.acc[n][4 * b][i] * f, st.acc[n][4 * b + 1][i] * f);
+              o[i / 2][i % 2 * 2 + 1] = bf16_pair(st.acc[n][4 * b + 2][i] * f, st.acc[n][4 * b + 3][i] * f);
+            }
+            *reinterpret_cast<u32x4*>(to + 128 * b) = o[0];
+            *reinterpret_cast<u32x4*>(to + 128 * b + 16) = o[1];
           }
-          *reinterpret_cast<u32x4*>(to + 128 * b) = o[0];
-          *reinterpret_cast<u32x4*>(to + 128 * b + 16) = o[1];
-        }
-        if (g == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(st.top[n], total);
-      } else {
-        const uint64_t place = w.place(a, 0, wave * 16 * NT + 16 * n + m);
-        float* to = a.part_out + place * D + 16 * g;
+          if (g == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(st.top[n], total);
+        } else {
+          const uint64_t place = w.place(a, 0, wave * 16 * NT + 16 * n + m);
+          float* to = a.part_out + place * D + 16 * g;
 #pragma unroll
-        for (int b = 0; b < D / 64; ++b)
+          for (int b = 0; b < D / 64; ++b)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<f32x4*>(to + 64 * b + 4 * i) = f32x4{st.acc[n][4 * b][i], st.acc[n][4 * b + 1][i], st.acc[n][4 * b + 2][i], st.acc[n][4 * b + 3][i]};
-        if (g == 0) {
-          a.part_stat[2 * place] = st.top[n];
-          a.part_stat[2 * place + 1] = total;
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<f32x4*>(to + 64 * b + 4 * i) = f32x4{st.acc[n][4 * b][i], st.acc[n][4 * b + 1][i], st.acc[n][4 * b + 2][i], st.acc[n][4 * b + 3][i]};
+          if (g == 0) {
+            a.part_stat[2 * place] = st.top[n];
+            a.part_stat[2 * place + 1] = total;
+          }
         }
       }
-    }
     } while (w.more_rows());
   } while (w.next());
 }

@@ -173,7 +173,7 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
   p.tile_rows = 16;
   p.heads_across = rows > 16 ? 1u : c->kv_heads % 4 == 0 ? 4u : c->kv_heads % 2 == 0 ? 2u : 1u;
   if (rows > 16) {
-    p.waves = rows <= (c->head_dim == 256 ? 64 : 128) ? 4 : 8;
+    p.waves = rows > 128 || c->head_dim == 256 ? 8 : 4;
     p.nt = rows <= 64 || c->head_dim == 256 ? 1 : 2;
     p.tile_rows = 16 * p.nt * p.waves;
   }
@@ -182,15 +182,15 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
   p.most_rows = (uint32_t)(rows < (uint64_t)p.row_tiles * p.tile_rows ? rows : (uint64_t)p.row_tiles * p.tile_rows);
   p.kept = (uint32_t)(rows < p.tile_rows ? rows : p.tile_rows);
   // as many workgroups as the chip holds at a time (two of 64 KB of LDS per CU; one of eight waves)
-  const uint64_t groups = (uint64_t)(c->kv_heads / p.heads_across) * p.row_tiles, slots = (uint64_t)cu_count() * (p.waves == 8 || (p.waves == 0 && c->dtype == SPLITZIP_BF16 && c->head_dim == 256) ? 1 : 2);
+  const uint64_t groups = (uint64_t)(c->kv_heads / p.heads_across) * p.row_tiles, slots = (uint64_t)cu_count() * (p.waves == 8 || (p.waves == 0 && c->dtype == SPLITZIP_BF16 && c->head_dim == 256) ? 1 : p.waves == 4 && p.nt == 1 ? 3 : 2);
   uint64_t shares = (slots + groups - 1) / groups;
   // a block: what the waves of a head stage at a time
-  const uint32_t staged = 8192u / (c->head_dim * (p.waves ? 1 : words_bytes(c->dtype)));
+  const uint32_t staged = p.waves ? p.waves * 1024u / c->head_dim : 8192u / (c->head_dim * words_bytes(c->dtype));
   p.block_tokens = p.waves ? staged : (staged < 32 ? 32 : staged) * (kWaves / p.heads_across);
   // (a sum of blocks is kept in 32 bits)
   const uint64_t most = (uint64_t)q->n_seqs * (q->d_block_table ? (uint64_t)q->table_stride * c->page_tokens : c->page_tokens);
   while (most / p.block_tokens + q->n_seqs > (1ull << 31) && p.block_tokens < (1u << 30)) p.block_tokens *= 2;
-  p.least_blocks = p.waves ? 4 : 1;
+  p.least_blocks = p.waves ? 256 / p.block_tokens : 1;
   const uint64_t some = ((uint64_t)q->n_seqs * (q->max_len < kMostTokens ? q->max_len : kMostTokens) + p.block_tokens - 1) / p.block_tokens + q->n_seqs;   // blocks, by what the call says
   if (shares > (some + p.least_blocks - 1) / p.least_blocks) shares = (some + p.least_blocks - 1) / p.least_blocks;
   if (shares < 1) shares = 1;
@@ -201,14 +201,20 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
 
 template <int KIND, int D>
 struct Attend {
-  template <int W, int NT>
+  template <int W, int NT, bool PLAIN>
   static void rows(dim3 grid, hipStream_t st, const AttentionArgs* a) {
-    hipLaunchKernelGGL((attention_rows_kernel<KIND, D, W, NT>), grid, dim3(64 * W), 0, st, *a);
+    hipLaunchKernelGGL((attention_rows_kernel<KIND, D, W, NT, PLAIN>), grid, dim3(64 * W), 0, st, *a);
+  }
+  template <bool PLAIN>
+  static void any(dim3 grid, uint32_t waves, uint32_t nt, hipStream_t st, const AttentionArgs* a) {
+    if (!waves) hipLaunchKernelGGL((attention_tokens_kernel<KIND, D, PLAIN>), grid, dim3(kThreads), 0, st, *a);
+    else if constexpr (D == 256) rows<8, 1, PLAIN>(grid, st, a);
+    else nt == 1 ? rows<4, 1, PLAIN>(grid, st, a) : waves == 4 ? rows<4, 2, PLAIN>(grid, st, a) : rows<8, 2, PLAIN>(grid, st, a);
   }
   static int run(dim3 grid, uint32_t waves, uint32_t nt, hipStream_t st, const AttentionArgs* a) {
-    if (!waves) hipLaunchKernelGGL((attention_tokens_kernel<KIND, D>), grid, dim3(kThreads), 0, st, *a);
-    else if constexpr (D == 256) waves == 4 ? rows<4, 1>(grid, st, a) : rows<8, 1>(grid, st, a);
-    else nt == 1 ? rows<4, 1>(grid, st, a) : waves == 4 ? rows<4, 2>(grid, st, a) : rows<8, 2>(grid, st, a);
+    // (a scale of 0 times an infinity that is not seen would be a NaN: not plain)
+    if (a->softcap == 0.0f && !a->slopes && a->scale > 0.0f) any<true>(grid, waves, nt, st, a);
+    else any<false>(grid, waves, nt, st, a);
     return launched();
   }
 };
