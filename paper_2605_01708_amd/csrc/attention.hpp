@@ -286,6 +286,9 @@ __device__ inline float shaped(const AttentionArgs& a, float x, float slope_log2
   return x * kLog2e - slope_log2 * far;
 }
 
+// the larger of two, the other one of a NaN: one instruction, where fmaxf is two, since it makes its operands' NaN quiet
+__device__ inline float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, __builtin_inff()); }
+
 __device__ inline f32x4 mfma(const bf16x8& x, const bf16x8& y, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
 __device__ inline bf16x8 as_bf16(const u32x4& x) { return __builtin_bit_cast(bf16x8, x); }
 
@@ -339,7 +342,7 @@ struct State {
     }
   }
   static __device__ float highest(const f32x4 (&x)[2]) {
-    return fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+    return larger(larger(larger(x[0][0], x[0][1]), larger(x[0][2], x[0][3])), larger(larger(x[1][0], x[1][1]), larger(x[1][2], x[1][3])));
   }
   // The running maximum, raised if need be; high: the lane's highest score of the tokens to come, in powers of two.
   __device__ void raise(const float (&high)[NT]) {
@@ -469,7 +472,7 @@ struct Stream {
   // and a row is half of the banks.
   __device__ static uint32_t v_row(uint32_t token) { return kUnits == 8 ? token ^ (token / 8 & 1) : token; }
 
-  // asks for the stage from token t0 on; pages: lane l has the page of its 8 l-th token; offsets: bytes from page and place
+  // asks for the stage from token t0 on; pages: lane l has the page of its 8 l-th token
   __device__ static void ask(const Cache& c, const Pages& at_pages, const uint8_t* k_base, const uint8_t* v_base, uint32_t pages, int t0,
                              uint32_t last8, uint8_t* lds, uint32_t lane) {
 #pragma unroll
@@ -511,7 +514,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
     do {
     const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
     const Pages at_pages(c, args.seqs, w.seq);
-    const auto ask_pages = [&](int t0) { return at_pages.page(min((uint32_t)t0 + 8 * (lane % (S::kTokens / 8)), last8)); };
+    const auto ask_pages = [&](int t0) { return at_pages.entry(min((uint32_t)t0 + 8 * (lane % (S::kTokens / 8)), last8)); };
     u32x2 k_scales[S::kSteps], v_scales[S::kSteps];
     const auto ask_scales = [&](uint32_t pages, int t0) {
       if constexpr (ES == 1) {
@@ -528,6 +531,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
     uint32_t pages = 0;
     if (t0 < w.end) {
       pages = ask_pages(t0);
+      pages = at_pages.clamped(pages);
       S::ask(c, at_pages, k_base, v_base, pages, t0, last8, mine, lane);
       ask_scales(pages, t0);
       if (t0 + stride < w.end) pages = ask_pages(t0 + stride);
@@ -563,6 +567,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
       }
       lds_read();   // into registers: the place is free
       if (t0 + stride < w.end) {
+        pages = at_pages.clamped(pages);
         S::ask(c, at_pages, k_base, v_base, pages, t0 + stride, last8, mine, lane);
         ask_scales(pages, t0 + stride);
         if (t0 + 2 * stride < w.end) pages = ask_pages(t0 + 2 * stride);
@@ -792,13 +797,14 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
       S stage;
       uint32_t page = 0;
       const auto ask_page = [&](int t0) {
-        if (t0 < w.end) page = at_pages.page(min((uint32_t)t0 + group, last8));
+        if (t0 < w.end) page = at_pages.entry(min((uint32_t)t0 + group, last8));
       };
       const auto ask = [&](int t0) {
         if (t0 >= w.end) return;
         const uint32_t place = at_pages.place(min((uint32_t)t0 + group, last8));
-        if (of_k) stage.load_k(c, base, page, place, w.head, piece);
-        else stage.load_v(c, base, page, place, w.head);
+        const uint32_t in_pool = at_pages.clamped(page);
+        if (of_k) stage.load_k(c, base, in_pool, place, w.head, piece);
+        else stage.load_v(c, base, in_pool, place, w.head);
       };
       const auto store = [&](int t0, int buf) {
         if (t0 >= w.end) return;
@@ -849,7 +855,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
         for (int n = 0; n < NT; ++n) {
           high[n] = st.highest(x[0][n]);
 #pragma unroll
-          for (int u = 1; u < kUnits; ++u) high[n] = fmaxf(high[n], st.highest(x[u][n]));
+          for (int u = 1; u < kUnits; ++u) high[n] = larger(high[n], st.highest(x[u][n]));
           high[n] *= scale;
         }
         st.raise(high);

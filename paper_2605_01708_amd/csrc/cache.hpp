@@ -57,7 +57,11 @@ struct Pages {
   __device__ Pages(const Cache& c, const Seqs& q, uint32_t s)
       : row(q.table ? q.table + (uint64_t)s * q.table_stride : nullptr), seq(s), shift(c.page_shift), mask(q.table ? c.page_tokens - 1 : ~0u), last(c.last_page) {}
   // of token t, below the sequence's length: the page in the pool (a bad table entry never leaves it), the place in the page
-  __device__ uint32_t page(uint32_t t) const { return row ? min(row[t >> shift], last) : seq; }
+  __device__ uint32_t page(uint32_t t) const { return clamped(entry(t)); }
+  // the same in two steps: a loop that asks for the entry well ahead must not touch it before it is needed, or it waits for
+  // everything that it has asked for before
+  __device__ uint32_t entry(uint32_t t) const { return row ? row[t >> shift] : seq; }
+  __device__ uint32_t clamped(uint32_t entry) const { return min(entry, last); }
   __device__ uint32_t place(uint32_t t) const { return t & mask; }
 };
 // byte of a token's words, heads apart; the same offset in K and V
