@@ -90,23 +90,29 @@ __device__ inline uint32_t blocks_of(const AttentionArgs& a, const Seq& s, int f
 // rows): lengths differ, and a launch that gave every workgroup one part of one sequence would wait for the longest (64 sequences
 // of 700 to 8192 tokens: 221 us that way).  Every wave sums the blocks up for itself.
 struct Blocks {
-  uint32_t total, shares;   // shares: that get something
+  uint32_t shares;     // that get something
+  uint32_t each, odd;  // blocks of each, the first `odd` of them one more
 
-  __device__ uint32_t begin(uint32_t share) const { return (uint32_t)((uint64_t)share * total / shares); }
-  __device__ uint32_t owner(uint32_t block) const { return (uint32_t)((((uint64_t)block + 1) * shares - 1) / total); }
+  __device__ uint32_t begin(uint32_t share) const { return share * each + min(share, odd); }
+  __device__ uint32_t owner(uint32_t block) const {
+    const uint32_t longer = odd * (each + 1);
+    return block < longer ? block / (each + 1) : odd + (block - longer) / each;
+  }
   static __device__ uint32_t blocks_of_seq(const AttentionArgs& a, uint32_t seq) {
     if (seq >= a.seqs.n_seqs) return 0;
     const Seq s = seq_at(a.seqs, seq);
     return blocks_of(a, s, first_token(a, s));
   }
   __device__ void count(const AttentionArgs& a, uint32_t lane, uint32_t& own) {   // own: of sequence `lane`
-    total = 0;
+    uint32_t total = 0;
     for (uint32_t at = 0; at < a.seqs.n_seqs; at += 64) {
       const uint32_t n = blocks_of_seq(a, at + lane), sum = wave_last(wave_incl_scan(n));
       if (at == 0) own = n;
       total += sum;
     }
     shares = min(a.shares, (total + a.least_blocks - 1) / a.least_blocks);
+    each = total / max(shares, 1u);
+    odd = total - each * shares;
   }
   // the sequence that has this block, and the number of its first block
   __device__ void find(const AttentionArgs& a, uint32_t lane, uint32_t own, uint32_t block, uint32_t& seq, uint32_t& front) const {
@@ -918,7 +924,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
 
 // The parts of a sequence together.  D / 4 threads have a row and query head, four elements each: where the parts are few, as many rows
 // as that leaves room for go through a workgroup at a time, otherwise all its threads take every (1024 / D)-th part of one.
-constexpr uint32_t kFewParts = 8;
+constexpr uint32_t kVeryFewParts = 4, kFewParts = 16;
 template <int D>
 __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs a) {
   constexpr uint32_t kAcross = D / 4, kDown = kThreads / kAcross;
@@ -953,25 +959,30 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs 
     float high = kLowest, total = 0.0f;
     f32x4 o = {0, 0, 0, 0};
     if (few) {
-      f32x4 x[kFewParts];
-      float top[kFewParts], sum[kFewParts];
+      const auto all_of = [&](auto most) {
+        constexpr uint32_t N = decltype(most)::value;
+        f32x4 x[N];
+        float top[N], sum[N];
 #pragma unroll
-      for (uint32_t p = 0; p < kFewParts; ++p) {
-        const uint64_t at = place(min(p, n_parts - 1));
-        x[p] = *reinterpret_cast<const f32x4*>(a.part_out + at * D + 4 * across);
-        top[p] = a.part_stat[2 * at];
-        sum[p] = p < n_parts ? a.part_stat[2 * at + 1] : 0.0f;
-      }
-#pragma unroll
-      for (uint32_t p = 0; p < kFewParts; ++p) high = fmaxf(high, top[p]);
-#pragma unroll
-      for (uint32_t p = 0; p < kFewParts; ++p) {
-        const float f = __builtin_amdgcn_exp2f(top[p] - high);
-        if (p < n_parts) {
-          total += f * sum[p];
-          o += f * x[p];
+        for (uint32_t p = 0; p < N; ++p) {   // (the last one again where there are no more: a load behind a condition would wait for those before it)
+          const uint64_t at = place(min(p, n_parts - 1));
+          x[p] = *reinterpret_cast<const f32x4*>(a.part_out + at * D + 4 * across);
+          top[p] = a.part_stat[2 * at];
+          sum[p] = a.part_stat[2 * at + 1];
         }
-      }
+#pragma unroll
+        for (uint32_t p = 0; p < N; ++p) high = fmaxf(high, top[p]);
+#pragma unroll
+        for (uint32_t p = 0; p < N; ++p) {
+          if (p < n_parts) {
+            const float f = __builtin_amdgcn_exp2f(top[p] - high);
+            total += f * sum[p];
+            o += f * x[p];
+          }
+        }
+      };
+      if (n_parts <= kVeryFewParts) all_of(std::integral_constant<uint32_t, kVeryFewParts>());
+      else all_of(std::integral_constant<uint32_t, kFewParts>());
     } else {
       for (uint32_t p = threadIdx.x; p < n_parts; p += kThreads) high = fmaxf(high, a.part_stat[2 * place(p)]);
 #pragma unroll

@@ -288,9 +288,11 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   rc = by_kind<Attend>(cache, dim3(p.wgs), p.waves, p.nt, st, (const AttentionArgs*)&a);
   if (rc != SPLITZIP_OK || p.shares == 1) return rc;
   const uint64_t outs = (uint64_t)(seqs->max_rows ? seqs->max_rows : 1) * q_heads;
-  // up to 16 rows in a workgroup at a time, as many workgroups as the chip holds several times over
-  const uint64_t most = (uint64_t)cu_count() * 16 / seqs->n_seqs + 1;
-  const dim3 grid((unsigned)(outs < most ? outs : most), seqs->n_seqs);
+  // a workgroup for each row and head, or, since it takes 256 threads' worth of rows at a time where parts are few, for so many of them
+  const uint64_t at_a_time = 4 * kThreads / cache->head_dim, few = (outs + at_a_time - 1) / at_a_time, held = (uint64_t)cu_count() * 8 / seqs->n_seqs + 1;
+  const uint64_t each = outs < (uint64_t)cu_count() / seqs->n_seqs ? outs : (uint64_t)cu_count() / seqs->n_seqs;
+  const uint64_t wgs = few < held ? few : held;
+  const dim3 grid((unsigned)(wgs > each ? wgs : each), seqs->n_seqs);
   if (cache->head_dim == 64) hipLaunchKernelGGL(attention_join_kernel<64>, grid, dim3(kThreads), 0, st, a);
   else if (cache->head_dim == 128) hipLaunchKernelGGL(attention_join_kernel<128>, grid, dim3(kThreads), 0, st, a);
   else hipLaunchKernelGGL(attention_join_kernel<256>, grid, dim3(kThreads), 0, st, a);
