@@ -79,6 +79,11 @@ class _CAttention(C.Structure):
                 ("d_positions", C.c_void_p), ("tree_words", C.c_uint32), ("window", C.c_uint32), ("reserved", C.c_uint64)]
 
 
+class _CAttentionOf(_CAttention):
+    """and how many entries its slopes, tree and positions have (-1: none), which the calls compare with their tensors"""
+    _fields_ = [("heads", C.c_int64), ("tree_rows", C.c_int64), ("position_rows", C.c_int64)]
+
+
 class Variant(C.Structure):
     """splitzip_variant: one of the formats of the paper's ablations"""
     _fields_ = [("dtype", C.c_uint32), ("code_bits", C.c_uint32), ("k", C.c_uint32), ("escape_mode", C.c_uint32),
@@ -217,7 +222,7 @@ def _short_way(L):
     """The functions of _fastcall, or, where it is not built or built for another Python or torch, none that take a call."""
     try:
         from . import _fastcall   # torch's own libraries are loaded by now
-        return types.SimpleNamespace(**_fastcall.bind(L._handle, _CCodebook, Variant, _CPaged, torch.__version__))
+        return types.SimpleNamespace(**_fastcall.bind(L._handle, _CCodebook, Variant, _CPaged, _CCache, _CSeqs, _CAttentionOf, torch.__version__))
     except ImportError as e:
         warnings.warn(f"{e}: calls take the general way, 1 to 2 us longer each; build the short one with "
                       "`python -m paper_2605_01708_amd.build`", RuntimeWarning, stacklevel=3)
@@ -1019,7 +1024,8 @@ class Attention:
         if positions is not None and (positions.element_size() != 4 or not positions.is_contiguous()):
             raise ValueError("positions must be a contiguous tensor of 32-bit integers")
         self._keep = (slopes, tree, positions)
-        self.c = _CAttention(scale, softcap, _ptr(slopes), _ptr(tree), _ptr(positions), 0 if tree is None else tree.shape[1], window, 0)
+        self.c = _CAttentionOf(scale, softcap, _ptr(slopes), _ptr(tree), _ptr(positions), 0 if tree is None else tree.shape[1], window, 0,
+                               *(-1 if t is None else t.shape[0] for t in self._keep))
 
 
 def _rows(t: torch.Tensor, heads: int, dim: int, what: str) -> int:
@@ -1029,7 +1035,8 @@ def _rows(t: torch.Tensor, heads: int, dim: int, what: str) -> int:
     return t.stride(0) if t.shape[0] > 1 else heads * dim
 
 
-def _write_or_read(f, name, cache: KvCache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor, stream):
+def _write_or_read(name, cache: KvCache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor, stream):
+    f = getattr(lib(), name)
     ks, vs = _rows(k, cache.kv_heads, cache.head_dim, "k"), _rows(v, cache.kv_heads, cache.head_dim, "v")
     if k.shape[0] != v.shape[0]:
         raise ValueError("k and v must have the same number of rows")
@@ -1038,12 +1045,18 @@ def _write_or_read(f, name, cache: KvCache, seqs: Sequences, k: torch.Tensor, v:
 
 def cache_write(k: torch.Tensor, v: torch.Tensor, cache: KvCache, seqs: Sequences, stream=None) -> None:
     """splitzip_cache_write: the BF16 rows k, v [rows, kv_heads, head_dim] become their sequences' last tokens, quantised if the cache is FP8."""
-    _write_or_read(lib().splitzip_cache_write, "splitzip_cache_write", cache, seqs, k, v, stream)
+    rc = (_lib or lib()).fast.splitzip_cache_write(cache.c, seqs.c, k, v, None if stream is None else _handle(stream))
+    if rc != _NOT_TAKEN:
+        return _check(rc, "splitzip_cache_write") if rc else None
+    _write_or_read("splitzip_cache_write", cache, seqs, k, v, stream)
 
 
 def cache_read(cache: KvCache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
     """splitzip_cache_read: the rows' tokens out of the cache, as BF16, into k, v [rows, kv_heads, head_dim]."""
-    _write_or_read(lib().splitzip_cache_read, "splitzip_cache_read", cache, seqs, k, v, stream)
+    rc = (_lib or lib()).fast.splitzip_cache_read(cache.c, seqs.c, k, v, None if stream is None else _handle(stream))
+    if rc != _NOT_TAKEN:
+        return _check(rc, "splitzip_cache_read") if rc else None
+    _write_or_read("splitzip_cache_read", cache, seqs, k, v, stream)
 
 
 def attention_workspace_bytes(cache: KvCache, seqs: Sequences, n_rows: int, q_heads: int) -> int:
@@ -1058,6 +1071,9 @@ def attention_workspace(cache: KvCache, seqs: Sequences, n_rows: int, q_heads: i
 def cache_attention(q: torch.Tensor, cache: KvCache, seqs: Sequences, out: torch.Tensor, workspace: torch.Tensor, how: Attention,
                     lse: torch.Tensor | None = None, stream=None) -> None:
     """splitzip_cache_attention: the BF16 rows q [rows, q_heads, head_dim] against their sequences' tokens, into out; lse float32 [rows, q_heads]."""
+    rc = (_lib or lib()).fast.splitzip_cache_attention(cache.c, seqs.c, how.c, q, out, lse, workspace, None, None if stream is None else _handle(stream))
+    if rc != _NOT_TAKEN:
+        return _check(rc, "splitzip_cache_attention") if rc else None
     if q.dim() != 3:
         raise ValueError("q must be [rows, q_heads, head_dim]")
     rows, heads = q.shape[0], q.shape[1]
@@ -1075,6 +1091,10 @@ def cache_attention(q: torch.Tensor, cache: KvCache, seqs: Sequences, out: torch
 def cache_move(caches: KvCaches, seqs: Sequences, path: torch.Tensor, n_rows: int | None = None, stream=None) -> None:
     """splitzip_cache_move: in all the caches, row path[s, i] of sequence s becomes its token base + i; path int32 [n_seqs, entries], -1 ends a
     path.  n_rows: rows of the call (all that starts says, if None)."""
+    rc = (_lib or lib()).fast.splitzip_cache_move(caches.items, caches.n, seqs.c, path, _MOST_ROWS if n_rows is None else n_rows,
+                                                  None if stream is None else _handle(stream))
+    if rc != _NOT_TAKEN:
+        return _check(rc, "splitzip_cache_move") if rc else None
     if path.dim() != 2 or path.shape[0] != seqs.c.n_seqs or path.element_size() != 4 or not path.is_contiguous():
         raise ValueError("path must be a contiguous tensor [n_seqs, entries] of 32-bit integers")
     _check(lib().splitzip_cache_move(caches.items, caches.n, C.byref(seqs.c), path.data_ptr(), path.shape[1],

@@ -165,6 +165,9 @@ struct AttentionPlan {
   uint32_t shares, block_tokens, least_blocks;
   uint32_t wgs;
 };
+// Sequences of up to so many stages are not cut: what their parts would gain, a little over 1 us a stage, the launch that joins them
+// costs (5 us).
+constexpr uint32_t kUncutStages = 4;
 AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, uint32_t q_heads) {
   AttentionPlan p;
   const uint64_t rows = (uint64_t)(q->max_rows ? q->max_rows : 1) * (q_heads / c->kv_heads);
@@ -190,9 +193,14 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
   // (a sum of blocks is kept in 32 bits)
   const uint64_t most = (uint64_t)q->n_seqs * (q->d_block_table ? (uint64_t)q->table_stride * c->page_tokens : c->page_tokens);
   while (most / p.block_tokens + q->n_seqs > (1ull << 31) && p.block_tokens < (1u << 30)) p.block_tokens *= 2;
-  p.least_blocks = p.waves ? 256 / p.block_tokens : 1;
-  const uint64_t some = ((uint64_t)q->n_seqs * (q->max_len < kMostTokens ? q->max_len : kMostTokens) + p.block_tokens - 1) / p.block_tokens + q->n_seqs;   // blocks, by what the call says
-  if (shares > (some + p.least_blocks - 1) / p.least_blocks) shares = (some + p.least_blocks - 1) / p.least_blocks;
+  p.least_blocks = p.waves && p.block_tokens < 256 ? 256 / p.block_tokens : 1;
+  const uint64_t longest = q->max_len < kMostTokens ? q->max_len : kMostTokens;
+  if (longest <= (uint64_t)kUncutStages * p.block_tokens) {   // every sequence is a block
+    p.block_tokens = (uint32_t)kMostTokens;
+    p.least_blocks = 1;
+  }
+  const uint64_t blocks = q->n_seqs * (longest ? (longest + p.block_tokens - 1) / p.block_tokens : 1);   // by what the call says
+  if (shares > (blocks + p.least_blocks - 1) / p.least_blocks) shares = (blocks + p.least_blocks - 1) / p.least_blocks;
   if (shares < 1) shares = 1;
   p.shares = (uint32_t)shares;
   p.wgs = (uint32_t)((shares * (c->kv_heads / p.heads_across) + 7) / 8 * 8 * p.row_tiles);
@@ -220,7 +228,9 @@ struct Attend {
 };
 
 uint64_t parts_of(const AttentionPlan& p) { return (uint64_t)p.wgs * 2 * p.heads_across * p.kept; }
-uint64_t workspace_of(const AttentionPlan& p, const splitzip_cache* c) { return p.shares <= 1 ? 0 : parts_of(p) * (c->head_dim + 2) * sizeof(float); }
+// whether a sequence may be taken by several workgroups
+bool cuts(const AttentionPlan& p) { return p.shares > 1 && p.block_tokens < kMostTokens; }
+uint64_t workspace_of(const AttentionPlan& p, const splitzip_cache* c) { return !cuts(p) ? 0 : parts_of(p) * (c->head_dim + 2) * sizeof(float); }
 
 }  // namespace
 
@@ -286,7 +296,7 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   a.least_blocks = p.least_blocks;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   rc = by_kind<Attend>(cache, dim3(p.wgs), p.waves, p.nt, st, (const AttentionArgs*)&a);
-  if (rc != SPLITZIP_OK || p.shares == 1) return rc;
+  if (rc != SPLITZIP_OK || !cuts(p)) return rc;
   const uint64_t outs = (uint64_t)(seqs->max_rows ? seqs->max_rows : 1) * q_heads;
   // a workgroup for each row and head, or, since it takes 256 threads' worth of rows at a time where parts are few, for so many of them
   const uint64_t at_a_time = 4 * kThreads / cache->head_dim, few = (outs + at_a_time - 1) / at_a_time, held = (uint64_t)cu_count() * 8 / seqs->n_seqs + 1;

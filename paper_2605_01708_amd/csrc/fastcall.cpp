@@ -26,7 +26,7 @@
 namespace {
 
 constexpr int kNotTaken = 1;
-constexpr int kMost = 12;   // arguments of an entry point, at most
+constexpr int kMost = 16;   // arguments of an entry point, at most
 
 // the library's function called with its own types, from as many 64-bit words
 template <typename A>
@@ -57,17 +57,25 @@ struct Caller<int(A...)> {
 //   A  a ctypes array of items: its address                G  a page geometry: its address
 //   C  a codebook: its dtype and its address               K  a codebook: its address alone
 //   V  a format of the variants: its address
+//   c  a cache's description: its address                 q  that of the sequences        h  that of an attention
+//   X  rows of the cache's heads, a tensor [rows, heads, head_dim] of 2-byte words: address, words from row to row
+//   Q  rows of query heads, the same                      O  as many of the same heads, to be written
+//   L  a float32 tensor [rows, query heads], or None: its address
+//   n  no argument: the rows of the tensors above         e  no argument: their query heads
+//   T  a path, a tensor [sequences, entries] of 32-bit integers: address, entries
 //   S  a stream's handle, or None: the current one
 constexpr bool in(const char* set, char c) { return *set && (*set == c || in(set + 1, c)); }
-constexpr int count(const char* spec, const char* twice) { return *spec ? (in(twice, *spec) ? 2 : 1) + count(spec + 1, twice) : 0; }
-constexpr bool known(const char* spec) { return !*spec || (in("WPZzRYINDAGCKVS", *spec) && known(spec + 1)); }
+constexpr int count(const char* spec, const char* twice, const char* never = "") {
+  return *spec ? (in(twice, *spec) ? 2 : in(never, *spec) ? 0 : 1) + count(spec + 1, twice, never) : 0;
+}
+constexpr bool known(const char* spec) { return !*spec || (in("WPZzRYINDAGCKVScqhXQOLneT", *spec) && known(spec + 1)); }
 struct Entry {
   const char* name;
   const char* spec;
   int n_words, n_args;   // of the library's function, of Python's
   int (*call)(void*, const uint64_t*);
 };
-#define ENTRY(NAME, SPEC) {#NAME, SPEC, Caller<decltype(NAME)>::kArgs, count(SPEC, "R"), &Caller<decltype(NAME)>::call}
+#define ENTRY(NAME, SPEC) {#NAME, SPEC, Caller<decltype(NAME)>::kArgs, count(SPEC, "R", "ne"), &Caller<decltype(NAME)>::call}
 constexpr Entry kEntries[] = {
     ENTRY(splitzip_compress, "WCRPIZS"),
     ENTRY(splitzip_decompress, "PINCYzS"),
@@ -87,16 +95,30 @@ constexpr Entry kEntries[] = {
     ENTRY(splitzip_calibrate_batch_device, "AIIPPS"),
     ENTRY(splitzip_variant_compress, "WVKRRZS"),
     ENTRY(splitzip_variant_decompress, "PINVKYzS"),
+    ENTRY(splitzip_cache_write, "cqXXnS"),
+    ENTRY(splitzip_cache_read, "cqXXnS"),
+    ENTRY(splitzip_cache_attention, "cqhQOLneRS"),
+    ENTRY(splitzip_cache_move, "AIqTIS"),
 };
 #undef ENTRY
 constexpr bool fit(size_t k) {
-  return k == 0 || (known(kEntries[k - 1].spec) && count(kEntries[k - 1].spec, "WRC") == kEntries[k - 1].n_words && fit(k - 1));
+  return k == 0 || (known(kEntries[k - 1].spec) && count(kEntries[k - 1].spec, "WRCXQOT") == kEntries[k - 1].n_words && fit(k - 1));
 }
 static_assert(fit(sizeof kEntries / sizeof kEntries[0]), "a letter for every argument of the library's functions");
 
 // the binding's ctypes structures, as bind was given them
 struct Types {
-  PyObject *codebook, *variant, *paged;
+  PyObject *codebook, *variant, *paged, *cache, *seqs, *attention;
+  template <typename F>
+  void each(F f) const {
+    for (PyObject* t : {codebook, variant, paged, cache, seqs, attention}) f(t);
+  }
+};
+// the binding's description of an attention goes on behind the library's: how many entries its slopes, its tree and its positions have,
+// -1 where there are none
+struct Attention {
+  splitzip_attention how;
+  int64_t heads, tree_rows, position_rows;
 };
 struct Bound {
   void* fn;
@@ -138,6 +160,13 @@ struct Views {
 };
 int64_t bytes_per_word(uint64_t dtype) { return dtype == SPLITZIP_BF16 ? 2 : 1; }
 
+// rows of heads of 2-byte words, one behind the other in a row; words from row to row
+bool rows_of(const at::Tensor* t, int64_t heads, int64_t dim, uint64_t* stride) {
+  if (!t || t->dim() != 3 || t->size(1) != heads || t->size(2) != dim || t->element_size() != 2 || t->stride(2) != 1 || (heads > 1 && t->stride(1) != dim)) return false;
+  *stride = static_cast<uint64_t>(t->size(0) > 1 ? t->stride(0) : heads * dim);
+  return true;
+}
+
 // false if an argument is not of the plain form: nothing has been done then
 bool run(const Bound& b, PyObject* const* a, Py_ssize_t n_args, int* rc) {
   if (n_args != b.entry->n_args || at::impl::torch_function_mode_enabled()) return false;
@@ -146,9 +175,17 @@ bool run(const Bound& b, PyObject* const* a, Py_ssize_t n_args, int* rc) {
   int n = 0;
   int64_t word_size = 0, expected = 0;   // bytes of a word, of the tensor and by the dtype
   uint64_t elems = 0, v = 0;
+  const splitzip_cache* cache = nullptr;
+  const splitzip_seqs* seqs = nullptr;
+  const Attention* how = nullptr;
+  int64_t rows = -1, heads = 0;   // of the tensors of rows
   const auto word = [&](uint64_t x) { w[n++] = x; };
   const auto address = [](const void* p) { return static_cast<uint64_t>(reinterpret_cast<uintptr_t>(p)); };
   for (const char* s = b.entry->spec; *s; ++s) {
+    if (*s == 'n' || *s == 'e') {
+      word(static_cast<uint64_t>(*s == 'n' ? rows : heads));
+      continue;
+    }
     PyObject* o = *a++;
     switch (*s) {
       case 'W': {
@@ -227,6 +264,55 @@ bool run(const Bound& b, PyObject* const* a, Py_ssize_t n_args, int* rc) {
         word(address(f));
         break;
       }
+      case 'c': {
+        cache = static_cast<const splitzip_cache*>(views.of(o, b.types.cache, sizeof(splitzip_cache)));
+        if (!cache) return false;
+        word(address(cache));
+        break;
+      }
+      case 'q': {
+        seqs = static_cast<const splitzip_seqs*>(views.of(o, b.types.seqs, sizeof(splitzip_seqs)));
+        if (!seqs) return false;
+        word(address(seqs));
+        break;
+      }
+      case 'h': {
+        how = static_cast<const Attention*>(views.of(o, b.types.attention, sizeof(Attention)));
+        if (!how) return false;
+        word(address(how));
+        break;
+      }
+      case 'X':
+      case 'Q':
+      case 'O': {
+        const at::Tensor* t = tensor(o);
+        if (*s == 'X') heads = cache->kv_heads;
+        else if (*s == 'Q' && t && t->dim() == 3) heads = t->size(1);
+        if (!rows_of(t, heads, cache->head_dim, &v) || (rows >= 0 && t->size(0) != rows)) return false;
+        rows = t->size(0);
+        if (*s == 'Q' && ((how->heads >= 0 && how->heads != heads) || (how->tree_rows >= 0 && how->tree_rows != rows) ||
+                          (how->position_rows >= 0 && how->position_rows != rows))) return false;
+        word(address(t->data_ptr()));
+        word(v);
+        break;
+      }
+      case 'L': {
+        if (o == Py_None) {
+          word(0);
+          break;
+        }
+        const at::Tensor* t = tensor(o);
+        if (!t || t->scalar_type() != at::kFloat || t->dim() != 2 || t->size(0) != rows || t->size(1) != heads || !t->is_contiguous()) return false;
+        word(address(t->data_ptr()));
+        break;
+      }
+      case 'T': {
+        const at::Tensor* t = tensor(o);
+        if (!t || t->dim() != 2 || t->element_size() != 4 || !t->is_contiguous() || t->size(0) != static_cast<int64_t>(seqs->n_seqs)) return false;
+        word(address(t->data_ptr()));
+        word(static_cast<uint64_t>(t->size(1)));
+        break;
+      }
       case 'S':
         if (o == Py_None) v = address(c10::hip::getCurrentHIPStream().stream());
         else if (!integer(o, &v)) return false;
@@ -257,20 +343,19 @@ PyMethodDef kFastcall = {"fastcall", reinterpret_cast<PyCFunction>(reinterpret_c
 
 void forget(PyObject* capsule) {
   Bound* b = static_cast<Bound*>(PyCapsule_GetPointer(capsule, nullptr));
-  Py_DECREF(b->types.codebook);
-  Py_DECREF(b->types.variant);
-  Py_DECREF(b->types.paged);
+  b->types.each([](PyObject* t) { Py_DECREF(t); });
   delete b;
 }
 
-// bind(handle, codebook, variant, paged, torch): the entry points of the library that ctypes holds by this handle, name ->
+// bind(handle, codebook, variant, paged, cache, seqs, attention, torch): the entry points of the library that ctypes holds by this handle, name ->
 // function, for the binding's structures of these types; an ImportError if the torch of this version is not the one that
 // this was built for (torch's headers read the fields of its tensors)
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject* handle = nullptr;
   Types types;
   const char* torch_version = nullptr;
-  if (!PyArg_ParseTuple(args, "OOOOs", &handle, &types.codebook, &types.variant, &types.paged, &torch_version)) return nullptr;
+  if (!PyArg_ParseTuple(args, "OOOOOOOs", &handle, &types.codebook, &types.variant, &types.paged, &types.cache, &types.seqs, &types.attention, &torch_version))
+    return nullptr;
   if (strcmp(torch_version, BUILT_FOR_TORCH) != 0) {
     PyErr_Format(PyExc_ImportError, "_fastcall was built for torch %s, this is %s", BUILT_FOR_TORCH, torch_version);
     return nullptr;
@@ -289,9 +374,7 @@ PyObject* bind(PyObject*, PyObject* args) {
     Bound* b = new Bound{fn, &e, types};
     PyObject* capsule = PyCapsule_New(b, nullptr, nullptr);
     if (capsule) {
-      Py_INCREF(types.codebook);
-      Py_INCREF(types.variant);
-      Py_INCREF(types.paged);
+      types.each([](PyObject* t) { Py_INCREF(t); });
       PyCapsule_SetDestructor(capsule, forget);
     } else {
       delete b;
@@ -308,7 +391,7 @@ PyObject* bind(PyObject*, PyObject* args) {
   return out;
 }
 
-PyMethodDef kMethods[] = {{"bind", bind, METH_VARARGS, "bind(handle, codebook, variant, paged, torch): {name: function} for a libsplitzip.so that is loaded"}, {nullptr, nullptr, 0, nullptr}};
+PyMethodDef kMethods[] = {{"bind", bind, METH_VARARGS, "bind(handle, codebook, variant, paged, cache, seqs, attention, torch): {name: function} for a libsplitzip.so that is loaded"}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

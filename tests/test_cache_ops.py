@@ -523,6 +523,64 @@ def test_long_sequences_in_parts(kind):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 7, 40])
+def test_many_sequences(rows):
+    """more than 64 sequences: their blocks are summed up 64 at a time, and a workgroup takes several of them"""
+    rng = np.random.default_rng(rows)
+    lens = [int(x) for x in rng.integers(0, 90, 150)] + [900, 0, 500]
+    T = [min(rows, n) if k % 5 else 0 for k, n in enumerate(lens)]
+    w = World(sz.FP8_E5M2, lens, T, 1, 64, 16, seed=rows)
+    q, qd = queries(w, 2)
+    want = attend(w, q, 0.1)
+    close(*run(w, qd, sz.Attention(0.1)), want)
+    w.seqs = sz.Sequences(*w.dev, max_rows=rows, max_len=60)          # cut for short sequences: every one as a whole
+    close(*run(w, qd, sz.Attention(0.1)), want)
+
+
+@pytest.mark.gpu
+def test_the_short_way_and_the_general_way(monkeypatch):
+    """what lib().fast takes gives the bits that the ctypes calls give, and what it does not take is refused or taken by them"""
+    w = World(sz.FP8_E4M3, [300, 70], [3, 3], 2, 128, 16, seed=30)
+    q, qd = queries(w, 4)
+    path = torch.tensor([[0, 2], [1, -1]], dtype=torch.int32, device="cuda")
+    new = torch.randn(2, w.n_rows, 2, 128, device="cuda").to(torch.bfloat16)
+    tree = torch.tensor([1, 3, 7, 1, 2, 4], device="cuda")[:, None].contiguous()
+
+    def all_calls():
+        sz.cache_write(new[0], new[1], w.cache, w.seqs)
+        out, lse = run(w, qd, sz.Attention(0.1, tree=tree))
+        back = torch.zeros_like(new)
+        sz.cache_read(w.cache, w.seqs, back[0], back[1])
+        sz.cache_move(sz.KvCaches([w.cache]), w.seqs, path)
+        return out, lse, back, w.cache.k.clone(), w.scales.clone()
+
+    L, before, scales = sz.lib(), w.pool.clone(), w.scales.clone()
+    taken = []
+    for name in ("splitzip_cache_write", "splitzip_cache_read", "splitzip_cache_attention", "splitzip_cache_move"):
+        f = getattr(L.fast, name)
+        monkeypatch.setattr(L.fast, name, lambda *a, f=f: taken.append(f(*a)) or taken[-1])
+    first = all_calls()
+    assert taken == [0, 0, 0, 0]
+    for name in ("splitzip_cache_write", "splitzip_cache_read", "splitzip_cache_attention", "splitzip_cache_move"):
+        monkeypatch.setattr(L.fast, name, lambda *a: 1)
+    w.pool.copy_(before)
+    w.scales.copy_(scales)
+    for a, b in zip(first, all_calls()):
+        assert torch.equal(a, b)
+
+
+def test_other_forms_are_left_to_the_general_way():
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype)   # noqa: E731
+    c, q = sz.KvCache(z(3, 16, 2, 64), z(3, 16, 2, 64), sz.BF16), sz.Sequences(z(2, 4, dtype=torch.int32), z(3, dtype=torch.int32), z(2, dtype=torch.int32), 1, 64)
+    f, x, how = sz.lib().fast, z(2, 2, 64), sz.Attention(1.0)
+    assert f.splitzip_cache_write(c.c, q.c, x, x, 0) == 1                 # tensors in host memory
+    assert f.splitzip_cache_write(q.c, c.c, x, x, 0) == 1                 # another structure
+    assert f.splitzip_cache_attention(c.c, q.c, how.c, x, x, None, x, None, 0) == 1
+    assert f.splitzip_cache_attention(c.c, q.c, _CAttention(), x, x, None, x, None, 0) == 1
+    assert f.splitzip_cache_move(sz.KvCaches([c]).items, 1, q.c, x, 1, 0) == 1
+
+
+@pytest.mark.gpu
 def test_positions_that_are_far_from_the_slots():
     """positions are the caller's: far below the slots they lie in, or above, with a window that then sees much or nothing"""
     w = World(sz.BF16, [1200, 1200, 1200], [3, 3, 3], 1, 64, 16, seed=12)
