@@ -37,6 +37,7 @@ int launched() { return hipGetLastError() == hipSuccess ? SPLITZIP_OK : SPLITZIP
 
 constexpr uint64_t kMostTokens = 1u << 30;   // of a sequence: token numbers and the steps past them stay in 31 bits
 constexpr uint32_t kMostSeqs = 65535;        // a dimension of a grid
+constexpr uint64_t kHalfCache = 128ull << 20, kBeyondCache = 320ull << 20;   // bytes that a call moves (figures at the kernels)
 
 int words_bytes(uint32_t dtype) { return dtype == SPLITZIP_BF16 ? 2 : 1; }
 
@@ -121,15 +122,18 @@ int by_kind(const splitzip_cache* c, A... args) {
 
 template <int KIND, int D>
 struct Write {
-  static int run(dim3 grid, hipStream_t st, const RowsArgs* a) {
-    hipLaunchKernelGGL((cache_write_kernel<KIND, D>), grid, dim3(kThreads), 0, st, *a);
+  static int run(dim3 grid, uint64_t bytes, hipStream_t st, const RowsArgs* a) {
+    if (bytes < kHalfCache) hipLaunchKernelGGL((cache_write_kernel<KIND, D, kCached>), grid, dim3(kThreads), 0, st, *a);
+    else hipLaunchKernelGGL((cache_write_kernel<KIND, D, kStreamLoads>), grid, dim3(kThreads), 0, st, *a);
     return launched();
   }
 };
 template <int KIND, int D>
 struct Read {
-  static int run(dim3 grid, hipStream_t st, const RowsArgs* a) {
-    hipLaunchKernelGGL((cache_read_kernel<KIND, D>), grid, dim3(kThreads), 0, st, *a);
+  static int run(dim3 grid, uint64_t bytes, hipStream_t st, const RowsArgs* a) {
+    if (bytes < kHalfCache) hipLaunchKernelGGL((cache_read_kernel<KIND, D, kCached>), grid, dim3(kThreads), 0, st, *a);
+    else if (bytes < kBeyondCache) hipLaunchKernelGGL((cache_read_kernel<KIND, D, kStreamLoads>), grid, dim3(kThreads), 0, st, *a);
+    else hipLaunchKernelGGL((cache_read_kernel<KIND, D, kStreamBoth>), grid, dim3(kThreads), 0, st, *a);
     return launched();
   }
 };
@@ -150,11 +154,12 @@ int rows_call(const splitzip_cache* c, const splitzip_seqs* q, void* d_k, uint64
   a.v = static_cast<uint8_t*>(d_v);
   a.k_stride = 2 * k_stride;
   a.v_stride = 2 * v_stride;
-  const uint64_t pairs = (uint64_t)(q->max_rows ? q->max_rows : 1) * c->kv_heads, per = kThreads / (c->head_dim / 8);
+  const uint64_t pairs = (uint64_t)(q->max_rows ? q->max_rows : 1) * c->kv_heads, per = (uint64_t)kAtOnce * kThreads / (c->head_dim / 8);
   uint64_t wgs = (pairs + per - 1) / per;
   const uint64_t most = (uint64_t)cu_count() * 32;
   if (wgs > most) wgs = most;
-  return by_kind<F>(c, dim3((unsigned)wgs, q->n_seqs), static_cast<hipStream_t>(stream), (const RowsArgs*)&a);
+  const uint64_t bytes = 2 * n_rows * elems * (2 + words_bytes(c->dtype));
+  return by_kind<F>(c, dim3((unsigned)wgs, q->n_seqs), bytes, static_cast<hipStream_t>(stream), (const RowsArgs*)&a);
 }
 
 // How an attention call is cut: which kernel, the rows of a (sequence, head of the cache) into tiles, the tokens of all sequences
@@ -343,7 +348,7 @@ int splitzip_cache_move(const splitzip_cache* caches, uint32_t n_caches, const s
       a.at[k].v_scales = d.v_scales;
     }
     for (uint32_t k = n; k < kMoveMax; ++k) a.at[k].k = a.at[k].v = a.at[k].k_scales = a.at[k].v_scales = nullptr;
-    hipLaunchKernelGGL(cache_move_kernel, dim3(2, seqs->n_seqs, n), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(cache_move_kernel, dim3(seqs->n_seqs, n), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
     const int rl = launched();
     if (rl != SPLITZIP_OK) return rl;
   }

@@ -166,76 +166,144 @@ __device__ inline u32x4 from_fp8(const u32x2& w, uint32_t byte) {
 }
 
 // Rows into the cache, and back.  A row of a head is taken by D / 8 lanes, eight elements each; a workgroup belongs to one
-// sequence (blockIdx.y) and takes its (row, head) pairs in turn, K and V of a pair together.
-template <int KIND, int D>
+// sequence (blockIdx.y) and takes kAtOnce (row, head) pairs per lane at a time, K and V of a pair together: all of their words are asked for before
+// the first is used.
+//
+// Bound by memory.  Calls that move more than half of the last-level cache (256 MB) read past it, and reads of the largest write past it:
+//   us a call, ordinary / streamed loads / streamed stores too      8192     16 384      32 768      65 536 tokens of 8 x 128
+//   write E4M3                                                11.4 / 11.9   19.4 / 20.8   40.5 / 36.0   79.8 / 69.6
+//   read E5M2                                      9.5 / 11.8 / 10.9   16.6 / 18.8 / 20.0   40.9 / 33.2 / 37.5   79.2 / 75.7 / 72.8
+//   read BF16                                     11.5 / 15.0 / 13.0   22.5 / 24.4 / 24.8   53.5 / 43.1 / 47.4   104 / 102 / 92
+// (32 768 tokens written: 201 MB at 5.6 TB/s, BF16 6.5; read: 6.1 and 6.2).  Two pairs at a time 36.0 and 41.4 (write, E4M3 and BF16), one 38.1
+// and 42.5, four 37.2 and 41.6.
+constexpr int kAtOnce = 2;
+enum { kCached = 0, kStreamLoads = 1, kStreamBoth = 2 };
+template <int MODE, typename T>
+__device__ inline T ld_row(const uint8_t* p) {
+  if constexpr (MODE == kCached) return *reinterpret_cast<const T*>(p);
+  else return ld_stream(reinterpret_cast<const T*>(p));
+}
+template <int D>
+struct Pairs {
+  static constexpr uint32_t kLanes = D / 8, kOfWg = kThreads / kLanes, kStepPairs = kOfWg * kAtOnce;
+  Seq s;
+  Pages pages;
+  uint32_t n;          // (row, head) pairs of the sequence
+  uint32_t row[kAtOnce], heads[kAtOnce];   // of the call's tensors, of the cache
+  int token[kAtOnce];  // below zero: nowhere
+  __device__ Pairs(const RowsArgs& a) : s(seq_at(a.seqs, blockIdx.y)), pages(a.cache, a.seqs, blockIdx.y), n((uint32_t)s.rows * a.cache.heads) {}
+  // pair j of those from p0 on; false if there is none (then it is the last one once more: what is loaded for it is there, and no load
+  // stands behind a condition)
+  __device__ bool at(const RowsArgs& a, uint32_t p0, int j) {
+    const uint32_t p = p0 + (uint32_t)j * kOfWg + threadIdx.x / kLanes, q = min(p, n - 1), i = q / a.cache.heads;
+    row[j] = (uint32_t)s.start + i;
+    heads[j] = q - i * a.cache.heads;
+    token[j] = s.base + (int)i;
+    return p < n;
+  }
+};
+
+template <int KIND, int D, int MODE>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(RowsArgs a) {
-  constexpr int kLanes = D / 8, kPairs = kThreads / kLanes;
-  const Seq s = seq_at(a.seqs, blockIdx.y);
-  const Pages at_pages(a.cache, a.seqs, blockIdx.y);
-  const uint32_t lane = threadIdx.x % kLanes, pairs = (uint32_t)s.rows * a.cache.heads;
-  for (uint32_t p = blockIdx.x * kPairs + threadIdx.x / kLanes; p < pairs; p += gridDim.x * kPairs) {
-    const uint32_t i = p / a.cache.heads, head = p - i * a.cache.heads;
-    const int t = s.base + (int)i;
-    if (t < 0) continue;
-    const uint64_t row = (uint64_t)(uint32_t)(s.start + (int)i), at = 2 * (head * D + lane * 8);
-    const u32x4 k = *reinterpret_cast<const u32x4*>(a.k + row * a.k_stride + at), v = *reinterpret_cast<const u32x4*>(a.v + row * a.v_stride + at);
-    const uint32_t page = at_pages.page((uint32_t)t), place = at_pages.place((uint32_t)t);
-    const uint64_t word = token_offset(a.cache, page, place) + head * a.cache.head_stride;
-    if constexpr (KIND == SPLITZIP_BF16) {
-      *reinterpret_cast<u32x4*>(a.cache.k + word + lane * 16) = k;
-      *reinterpret_cast<u32x4*>(a.cache.v + word + lane * 16) = v;
-    } else {
-      uint32_t mk = largest8(k), mv = largest8(v);
+  Pairs<D> p(a);
+  const uint32_t lane = threadIdx.x % Pairs<D>::kLanes;
+  for (uint32_t p0 = blockIdx.x * Pairs<D>::kStepPairs; p0 < p.n; p0 += gridDim.x * Pairs<D>::kStepPairs) {
+    bool have[kAtOnce];
+    u32x4 k[kAtOnce], v[kAtOnce];
+    uint32_t page[kAtOnce];
 #pragma unroll
-      for (int o = kLanes / 2; o > 0; o /= 2) {
-        mk = max(mk, (uint32_t)__shfl_xor((int)mk, o));
-        mv = max(mv, (uint32_t)__shfl_xor((int)mv, o));
-      }
-      constexpr int kTop = KIND == SPLITZIP_FP8_E5M2 ? kTopE5m2 : kTopE4m3;
-      const int bk = scale_byte<kTop>(mk), bv = scale_byte<kTop>(mv);
-      *reinterpret_cast<u32x2*>(a.cache.k + word + lane * 8) = to_fp8<KIND>(k, bk);
-      *reinterpret_cast<u32x2*>(a.cache.v + word + lane * 8) = to_fp8<KIND>(v, bv);
-      if (lane == 0) {
-        const uint64_t scale = scale_offset(a.cache, page, place, head);
-        a.cache.k_scales[scale] = (uint8_t)bk;
-        a.cache.v_scales[scale] = (uint8_t)bv;
+    for (int j = 0; j < kAtOnce; ++j) {
+      have[j] = p.at(a, p0, j) && p.token[j] >= 0;
+      const uint32_t at = 2 * (p.heads[j] * D + lane * 8);
+      page[j] = p.pages.entry((uint32_t)max(p.token[j], 0));
+      k[j] = ld_row<MODE, u32x4>(a.k + p.row[j] * a.k_stride + at);
+      v[j] = ld_row<MODE, u32x4>(a.v + p.row[j] * a.v_stride + at);
+    }
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      if (!have[j]) continue;
+      const uint32_t in = p.pages.clamped(page[j]), place = p.pages.place((uint32_t)p.token[j]);
+      const uint64_t word = token_offset(a.cache, in, place) + p.heads[j] * a.cache.head_stride;
+      if constexpr (KIND == SPLITZIP_BF16) {
+        *reinterpret_cast<u32x4*>(a.cache.k + word + lane * 16) = k[j];
+        *reinterpret_cast<u32x4*>(a.cache.v + word + lane * 16) = v[j];
+      } else {
+        uint32_t mk = largest8(k[j]), mv = largest8(v[j]);
+#pragma unroll
+        for (int o = Pairs<D>::kLanes / 2; o > 0; o /= 2) {
+          mk = max(mk, (uint32_t)__shfl_xor((int)mk, o));
+          mv = max(mv, (uint32_t)__shfl_xor((int)mv, o));
+        }
+        constexpr int kTop = KIND == SPLITZIP_FP8_E5M2 ? kTopE5m2 : kTopE4m3;
+        const int bk = scale_byte<kTop>(mk), bv = scale_byte<kTop>(mv);
+        *reinterpret_cast<u32x2*>(a.cache.k + word + lane * 8) = to_fp8<KIND>(k[j], bk);
+        *reinterpret_cast<u32x2*>(a.cache.v + word + lane * 8) = to_fp8<KIND>(v[j], bv);
+        if (lane == 0) {
+          const uint64_t scale = scale_offset(a.cache, in, place, p.heads[j]);
+          a.cache.k_scales[scale] = (uint8_t)bk;
+          a.cache.v_scales[scale] = (uint8_t)bv;
+        }
       }
     }
   }
 }
 
-template <int KIND, int D>
+template <int KIND, int D, int MODE>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(RowsArgs a) {
-  constexpr int kLanes = D / 8, kPairs = kThreads / kLanes;
-  const Seq s = seq_at(a.seqs, blockIdx.y);
-  const Pages at_pages(a.cache, a.seqs, blockIdx.y);
-  const uint32_t lane = threadIdx.x % kLanes, pairs = (uint32_t)s.rows * a.cache.heads;
-  for (uint32_t p = blockIdx.x * kPairs + threadIdx.x / kLanes; p < pairs; p += gridDim.x * kPairs) {
-    const uint32_t i = p / a.cache.heads, head = p - i * a.cache.heads;
-    const int t = s.base + (int)i;
-    const uint64_t row = (uint64_t)(uint32_t)(s.start + (int)i), at = 2 * (head * D + lane * 8);
-    u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};   // a row in front of the sequence's first token
-    if (t >= 0) {
-      const uint32_t page = at_pages.page((uint32_t)t), place = at_pages.place((uint32_t)t);
-      const uint64_t word = token_offset(a.cache, page, place) + head * a.cache.head_stride;
-      if constexpr (KIND == SPLITZIP_BF16) {
-        k = *reinterpret_cast<const u32x4*>(a.cache.k + word + lane * 16);
-        v = *reinterpret_cast<const u32x4*>(a.cache.v + word + lane * 16);
-      } else {
-        const uint64_t scale = scale_offset(a.cache, page, place, head);
-        k = from_fp8<KIND>(*reinterpret_cast<const u32x2*>(a.cache.k + word + lane * 8), a.cache.k_scales[scale]);
-        v = from_fp8<KIND>(*reinterpret_cast<const u32x2*>(a.cache.v + word + lane * 8), a.cache.v_scales[scale]);
+  constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
+  typedef typename std::conditional<ES == 2, u32x4, u32x2>::type Words;
+  Pairs<D> p(a);
+  const uint32_t lane = threadIdx.x % Pairs<D>::kLanes;
+  for (uint32_t p0 = blockIdx.x * Pairs<D>::kStepPairs; p0 < p.n; p0 += gridDim.x * Pairs<D>::kStepPairs) {
+    bool have[kAtOnce];
+    Words k[kAtOnce], v[kAtOnce];
+    uint32_t page[kAtOnce], bk[kAtOnce], bv[kAtOnce];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      have[j] = p.at(a, p0, j);
+      page[j] = p.pages.entry((uint32_t)max(p.token[j], 0));
+    }
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      const uint32_t in = p.pages.clamped(page[j]), place = p.pages.place((uint32_t)max(p.token[j], 0));
+      const uint64_t word = token_offset(a.cache, in, place) + p.heads[j] * a.cache.head_stride + lane * 8 * ES;
+      k[j] = ld_row<MODE, Words>(a.cache.k + word);
+      v[j] = ld_row<MODE, Words>(a.cache.v + word);
+      if constexpr (ES == 1) {
+        const uint64_t scale = scale_offset(a.cache, in, place, p.heads[j]);
+        bk[j] = a.cache.k_scales[scale];
+        bv[j] = a.cache.v_scales[scale];
       }
     }
-    *reinterpret_cast<u32x4*>(a.k + row * a.k_stride + at) = k;
-    *reinterpret_cast<u32x4*>(a.v + row * a.v_stride + at) = v;
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      if (!have[j]) continue;
+      const uint32_t at = 2 * (p.heads[j] * D + lane * 8);
+      u32x4 ko, vo;
+      if constexpr (ES == 2) {
+        ko = k[j];
+        vo = v[j];
+      } else {
+        ko = from_fp8<KIND>(k[j], bk[j]);
+        vo = from_fp8<KIND>(v[j], bv[j]);
+      }
+      if (p.token[j] < 0) ko = vo = u32x4{0, 0, 0, 0};   // a row in front of the sequence's first token
+      u32x4 *const k_to = reinterpret_cast<u32x4*>(a.k + p.row[j] * a.k_stride + at), *const v_to = reinterpret_cast<u32x4*>(a.v + p.row[j] * a.v_stride + at);
+      if constexpr (MODE == kStreamBoth) {
+        st_stream(k_to, ko);
+        st_stream(v_to, vo);
+      } else {
+        *k_to = ko;
+        *v_to = vo;
+      }
+    }
   }
 }
 
 // The accepted path of a tree of drafted tokens: token base + path[i] becomes token base + i.  A path ascends strictly, so
-// path[i] >= i: a token is never written before the ones behind it on the path have been read, as long as every byte of it is
-// read and written in the path's order by one thread -- which is what a thread does with its 16 bytes (or its scale) of
-// every token.  Entries that do not ascend, or are no rows of the call, end the path.
+// path[i] >= i, and token i is not among the sources behind the i-th: a thread that reads and writes its 16 bytes (or its scale) of
+// the tokens in the path's order, or reads those of several before it writes them, never reads what it has written.
+// Entries that do not ascend, or are no rows of the call, end the path.
 constexpr uint32_t kMoveMax = 64;   // caches of a launch
 struct MoveArgs {
   Cache cache;             // the geometry all of them share
@@ -244,31 +312,68 @@ struct MoveArgs {
   uint32_t path_stride, row_bytes;   // entries per sequence; bytes of a token and head
   struct { uint8_t *k, *v, *k_scales, *v_scales; } at[kMoveMax];
 };
+// Bound by latency: the starts, the path, the table and the tokens are asked for one behind the other, each of them once for 64 entries of
+// the path (a lane each) or eight tokens (a register each).  48 paths of up to 6 tokens in 32 layers of E5M2: XXX us.
 __global__ void __launch_bounds__(kThreads) cache_move_kernel(MoveArgs a) {
-  const Seq s = seq_at(a.seqs, blockIdx.y);
-  const Pages at_pages(a.cache, a.seqs, blockIdx.y);
-  const auto& at = a.at[blockIdx.z];
-  uint8_t* const words = blockIdx.x ? at.v : at.k;
-  uint8_t* const scales = blockIdx.x ? at.v_scales : at.k_scales;
-  const uint32_t per_head = a.row_bytes / 16, pieces = per_head * a.cache.heads, of_scales = scales ? a.cache.heads : 0;
-  const int32_t* path = a.path + (uint64_t)blockIdx.y * a.path_stride;
-  for (uint32_t u = threadIdx.x; u < pieces + of_scales; u += kThreads) {
-    const bool is_word = u < pieces;
-    const uint32_t head = is_word ? u / per_head : u - pieces, piece = is_word ? u - head * per_head : 0;
-    int before = -1;
-    for (uint32_t i = 0; i < a.path_stride; ++i) {
-      const int from = path[i];
-      if (from <= before || from >= s.rows) break;
-      before = from;
-      const int t = s.base + from, to = s.base + (int)i;
-      if (from == (int)i || to < 0) continue;
-      const uint32_t p0 = at_pages.page((uint32_t)t), l0 = at_pages.place((uint32_t)t), p1 = at_pages.page((uint32_t)to), l1 = at_pages.place((uint32_t)to);
-      if (is_word)
-        *reinterpret_cast<u32x4*>(words + token_offset(a.cache, p1, l1) + head * a.cache.head_stride + piece * 16) =
-            *reinterpret_cast<const u32x4*>(words + token_offset(a.cache, p0, l0) + head * a.cache.head_stride + piece * 16);
-      else
-        scales[scale_offset(a.cache, p1, l1, head)] = scales[scale_offset(a.cache, p0, l0, head)];
+  constexpr uint32_t kHeld = 8;
+  const uint32_t lane = threadIdx.x % 64;
+  const int32_t* path = a.path + (uint64_t)blockIdx.x * a.path_stride;
+  const Seq s = seq_at(a.seqs, blockIdx.x);
+  const Pages at_pages(a.cache, a.seqs, blockIdx.x);
+  const auto& at = a.at[blockIdx.y];
+  const uint32_t per_head = a.row_bytes / 16, pieces = per_head * a.cache.heads, each = pieces + (at.k_scales ? a.cache.heads : 0);   // of K, and of V
+  int before = -1;
+  for (uint32_t i0 = 0; i0 < a.path_stride; i0 += 64) {
+    // the entries of the path that are part of it, a lane each
+    const uint32_t i = i0 + lane;
+    const int from = i < a.path_stride ? path[i] : -1, last = (int)lane_before((uint32_t)from, (uint32_t)before);
+    const uint64_t ends = ~__ballot(from > last && from < s.rows);
+    const uint32_t n = ends ? (uint32_t)__builtin_ctzll(ends) : 64;
+    const uint32_t t = (uint32_t)max(s.base + from, 0), to = (uint32_t)max(s.base + (int)i, 0);
+    const bool moves = lane < n && from != (int)i && s.base + (int)i >= 0;
+    uint32_t p0 = 0, p1 = 0;
+    if (moves) {
+      p0 = at_pages.entry(t);
+      p1 = at_pages.entry(to);
     }
+    p0 = at_pages.clamped(p0);
+    p1 = at_pages.clamped(p1);
+    const uint32_t l0 = at_pages.place(t), l1 = at_pages.place(to);
+    for (uint32_t u = threadIdx.x; u < 2 * each; u += kThreads) {
+      const bool of_v = u >= each, is_word = u - (of_v ? each : 0) < pieces;
+      const uint32_t w = u - (of_v ? each : 0), head = is_word ? w / per_head : w - pieces;
+      uint8_t* const words = (of_v ? at.v : at.k) + head * a.cache.head_stride + (is_word ? w - head * per_head : 0) * 16;
+      uint8_t* const scales = of_v ? at.v_scales : at.k_scales;
+      for (uint64_t left = __ballot(moves); left;) {
+        u32x4 x[kHeld];
+        uint64_t dst[kHeld];
+        uint32_t held = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < kHeld; ++j) {
+          if (!left) break;
+          const int l = __builtin_ctzll(left);
+          left &= left - 1;
+          const uint32_t sp = (uint32_t)__builtin_amdgcn_readlane((int)p0, l), sl = (uint32_t)__builtin_amdgcn_readlane((int)l0, l);
+          const uint32_t dp = (uint32_t)__builtin_amdgcn_readlane((int)p1, l), dl = (uint32_t)__builtin_amdgcn_readlane((int)l1, l);
+          if (is_word) {
+            x[j] = *reinterpret_cast<const u32x4*>(words + token_offset(a.cache, sp, sl));
+            dst[j] = token_offset(a.cache, dp, dl);
+          } else {
+            x[j][0] = scales[scale_offset(a.cache, sp, sl, head)];
+            dst[j] = scale_offset(a.cache, dp, dl, head);
+          }
+          held = j + 1;
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kHeld; ++j) {
+          if (j >= held) break;
+          if (is_word) *reinterpret_cast<u32x4*>(words + dst[j]) = x[j];
+          else scales[dst[j]] = (uint8_t)x[j][0];
+        }
+      }
+    }
+    if (n < 64) break;
+    before = __builtin_amdgcn_readlane(from, 63);
   }
 }
 
