@@ -37,7 +37,7 @@ int launched() { return hipGetLastError() == hipSuccess ? SPLITZIP_OK : SPLITZIP
 
 constexpr uint64_t kMostTokens = 1u << 30;   // of a sequence: token numbers and the steps past them stay in 31 bits
 constexpr uint32_t kMostSeqs = 65535;        // a dimension of a grid
-constexpr uint64_t kHalfCache = 128ull << 20, kBeyondCache = 320ull << 20;   // bytes that a call moves (figures at the kernels)
+constexpr uint64_t kStreamed = 96ull << 20;   // bytes that a call moves (figures at the kernels)
 
 int words_bytes(uint32_t dtype) { return dtype == SPLITZIP_BF16 ? 2 : 1; }
 
@@ -122,18 +122,17 @@ int by_kind(const splitzip_cache* c, A... args) {
 
 template <int KIND, int D>
 struct Write {
-  static int run(dim3 grid, uint64_t bytes, hipStream_t st, const RowsArgs* a) {
-    if (bytes < kHalfCache) hipLaunchKernelGGL((cache_write_kernel<KIND, D, kCached>), grid, dim3(kThreads), 0, st, *a);
-    else hipLaunchKernelGGL((cache_write_kernel<KIND, D, kStreamLoads>), grid, dim3(kThreads), 0, st, *a);
+  static int run(dim3 grid, bool stream, hipStream_t st, const RowsArgs* a) {
+    if (stream) hipLaunchKernelGGL((cache_write_kernel<KIND, D, true>), grid, dim3(kThreads), 0, st, *a);
+    else hipLaunchKernelGGL((cache_write_kernel<KIND, D, false>), grid, dim3(kThreads), 0, st, *a);
     return launched();
   }
 };
 template <int KIND, int D>
 struct Read {
-  static int run(dim3 grid, uint64_t bytes, hipStream_t st, const RowsArgs* a) {
-    if (bytes < kHalfCache) hipLaunchKernelGGL((cache_read_kernel<KIND, D, kCached>), grid, dim3(kThreads), 0, st, *a);
-    else if (bytes < kBeyondCache) hipLaunchKernelGGL((cache_read_kernel<KIND, D, kStreamLoads>), grid, dim3(kThreads), 0, st, *a);
-    else hipLaunchKernelGGL((cache_read_kernel<KIND, D, kStreamBoth>), grid, dim3(kThreads), 0, st, *a);
+  static int run(dim3 grid, bool stream, hipStream_t st, const RowsArgs* a) {
+    if (stream) hipLaunchKernelGGL((cache_read_kernel<KIND, D, true>), grid, dim3(kThreads), 0, st, *a);
+    else hipLaunchKernelGGL((cache_read_kernel<KIND, D, false>), grid, dim3(kThreads), 0, st, *a);
     return launched();
   }
 };
@@ -159,7 +158,7 @@ int rows_call(const splitzip_cache* c, const splitzip_seqs* q, void* d_k, uint64
   const uint64_t most = (uint64_t)cu_count() * 32;
   if (wgs > most) wgs = most;
   const uint64_t bytes = 2 * n_rows * elems * (2 + words_bytes(c->dtype));
-  return by_kind<F>(c, dim3((unsigned)wgs, q->n_seqs), bytes, static_cast<hipStream_t>(stream), (const RowsArgs*)&a);
+  return by_kind<F>(c, dim3((unsigned)wgs, q->n_seqs), bytes >= kStreamed, static_cast<hipStream_t>(stream), (const RowsArgs*)&a);
 }
 
 // How an attention call is cut: which kernel, the rows of a (sequence, head of the cache) into tiles, the tokens of all sequences

@@ -169,19 +169,20 @@ __device__ inline u32x4 from_fp8(const u32x2& w, uint32_t byte) {
 // sequence (blockIdx.y) and takes kAtOnce (row, head) pairs per lane at a time, K and V of a pair together: all of their words are asked for before
 // the first is used.
 //
-// Bound by memory.  Calls that move more than half of the last-level cache (256 MB) read past it, and reads of the largest write past it:
-//   us a call, ordinary / streamed loads / streamed stores too      8192     16 384      32 768      65 536 tokens of 8 x 128
-//   write E4M3                                                11.4 / 11.9   19.4 / 20.8   40.5 / 36.0   79.8 / 69.6
-//   read E5M2                                      9.5 / 11.8 / 10.9   16.6 / 18.8 / 20.0   40.9 / 33.2 / 37.5   79.2 / 75.7 / 72.8
-//   read BF16                                     11.5 / 15.0 / 13.0   22.5 / 24.4 / 24.8   53.5 / 43.1 / 47.4   104 / 102 / 92
-// (32 768 tokens written: 201 MB at 5.6 TB/s, BF16 6.5; read: 6.1 and 6.2).  Two pairs at a time 36.0 and 41.4 (write, E4M3 and BF16), one 38.1
-// and 42.5, four 37.2 and 41.6.
+// Bound by memory.  Calls that move more than the last-level cache can be of use for (96 MB of its 256) read and, back out of
+// the cache, write past it.  us a call, ordinary and streamed, five sets of tensors in turn, so that nothing of a call is in a cache (in
+// brackets two sets, where it may be):
+//                        7126 tokens of 8 x 128         16 384              32 768               65 536
+//   write E4M3                                       (19.4 / 20.8)          40.0 / 35.1       (79.8 / 69.6)
+//   read E5M2                                         22.5 / 20.1           41.2 / 37.4       (79.2 / 72.8)
+//   read BF16                  12.4 / 12.3                                  52.9 / 47.5       (104 / 92)
+// (32 768 tokens written: 201 MB at 5.7 TB/s, read 5.4, BF16 5.65; a plain copy of that mix of reads and writes 5.4 to 5.7).  One pair at a time
+// instead of two 37.5 and 46.6 (read, E5M2 and BF16) and 38.1 and 42.5 (written) where two take 36.0 and 41.4.
 constexpr int kAtOnce = 2;
-enum { kCached = 0, kStreamLoads = 1, kStreamBoth = 2 };
-template <int MODE, typename T>
+template <bool STREAM, typename T>
 __device__ inline T ld_row(const uint8_t* p) {
-  if constexpr (MODE == kCached) return *reinterpret_cast<const T*>(p);
-  else return ld_stream(reinterpret_cast<const T*>(p));
+  if constexpr (STREAM) return ld_stream(reinterpret_cast<const T*>(p));
+  else return *reinterpret_cast<const T*>(p);
 }
 template <int D>
 struct Pairs {
@@ -203,7 +204,7 @@ struct Pairs {
   }
 };
 
-template <int KIND, int D, int MODE>
+template <int KIND, int D, bool STREAM>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(RowsArgs a) {
   Pairs<D> p(a);
   const uint32_t lane = threadIdx.x % Pairs<D>::kLanes;
@@ -216,8 +217,8 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(RowsArgs a) {
       have[j] = p.at(a, p0, j) && p.token[j] >= 0;
       const uint32_t at = 2 * (p.heads[j] * D + lane * 8);
       page[j] = p.pages.entry((uint32_t)max(p.token[j], 0));
-      k[j] = ld_row<MODE, u32x4>(a.k + p.row[j] * a.k_stride + at);
-      v[j] = ld_row<MODE, u32x4>(a.v + p.row[j] * a.v_stride + at);
+      k[j] = ld_row<STREAM, u32x4>(a.k + p.row[j] * a.k_stride + at);
+      v[j] = ld_row<STREAM, u32x4>(a.v + p.row[j] * a.v_stride + at);
     }
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
@@ -248,7 +249,7 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(RowsArgs a) {
   }
 }
 
-template <int KIND, int D, int MODE>
+template <int KIND, int D, bool STREAM>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(RowsArgs a) {
   constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
   typedef typename std::conditional<ES == 2, u32x4, u32x2>::type Words;
@@ -267,8 +268,8 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(RowsArgs a) {
     for (int j = 0; j < kAtOnce; ++j) {
       const uint32_t in = p.pages.clamped(page[j]), place = p.pages.place((uint32_t)max(p.token[j], 0));
       const uint64_t word = token_offset(a.cache, in, place) + p.heads[j] * a.cache.head_stride + lane * 8 * ES;
-      k[j] = ld_row<MODE, Words>(a.cache.k + word);
-      v[j] = ld_row<MODE, Words>(a.cache.v + word);
+      k[j] = ld_row<STREAM, Words>(a.cache.k + word);
+      v[j] = ld_row<STREAM, Words>(a.cache.v + word);
       if constexpr (ES == 1) {
         const uint64_t scale = scale_offset(a.cache, in, place, p.heads[j]);
         bk[j] = a.cache.k_scales[scale];
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(RowsArgs a) {
       }
       if (p.token[j] < 0) ko = vo = u32x4{0, 0, 0, 0};   // a row in front of the sequence's first token
       u32x4 *const k_to = reinterpret_cast<u32x4*>(a.k + p.row[j] * a.k_stride + at), *const v_to = reinterpret_cast<u32x4*>(a.v + p.row[j] * a.v_stride + at);
-      if constexpr (MODE == kStreamBoth) {
+      if constexpr (STREAM) {
         st_stream(k_to, ko);
         st_stream(v_to, vo);
       } else {
@@ -313,7 +314,7 @@ struct MoveArgs {
   struct { uint8_t *k, *v, *k_scales, *v_scales; } at[kMoveMax];
 };
 // Bound by latency: the starts, the path, the table and the tokens are asked for one behind the other, each of them once for 64 entries of
-// the path (a lane each) or eight tokens (a register each).  48 paths of up to 6 tokens in 32 layers of E5M2: XXX us.
+// the path (a lane each) or eight tokens (a register each).  48 paths of up to 6 tokens in 32 layers of E5M2 (25 MB): 8.6 us.
 __global__ void __launch_bounds__(kThreads) cache_move_kernel(MoveArgs a) {
   constexpr uint32_t kHeld = 8;
   const uint32_t lane = threadIdx.x % 64;
