@@ -98,36 +98,44 @@ struct Blocks {
     const uint32_t longer = odd * (each + 1);
     return block < longer ? block / (each + 1) : odd + (block - longer) / each;
   }
-  static __device__ uint32_t blocks_of_seq(const AttentionArgs& a, uint32_t seq) {
+  // blocks of sequence seq, and the sequence, a lane each
+  static __device__ uint32_t blocks_of_seq(const AttentionArgs& a, uint32_t seq, Seq& s) {
     if (seq >= a.seqs.n_seqs) return 0;
-    const Seq s = seq_at(a.seqs, seq);
+    s = seq_at(a.seqs, seq);
     return blocks_of(a, s, first_token(a, s));
   }
-  __device__ void count(const AttentionArgs& a, uint32_t lane, uint32_t& own) {   // own: of sequence `lane`
-    uint32_t total = 0;
-    for (uint32_t at = 0; at < a.seqs.n_seqs; at += 64) {
-      const uint32_t n = blocks_of_seq(a, at + lane), sum = wave_last(wave_incl_scan(n));
-      if (at == 0) own = n;
-      total += sum;
+  // own, own_seq: of sequence `lane`
+  __device__ void count(const AttentionArgs& a, uint32_t lane, uint32_t& own, Seq& own_seq) {
+    own_seq = Seq{0, 0, 0, 0};
+    own = blocks_of_seq(a, lane, own_seq);
+    uint32_t total = wave_last(wave_incl_scan(own));
+    for (uint32_t at = 64; at < a.seqs.n_seqs; at += 64) {
+      Seq s;
+      total += wave_last(wave_incl_scan(blocks_of_seq(a, at + lane, s)));
     }
     shares = min(a.shares, (total + a.least_blocks - 1) / a.least_blocks);
     each = total / max(shares, 1u);
     odd = total - each * shares;
   }
   // the sequence that has this block, and the number of its first block
-  __device__ void find(const AttentionArgs& a, uint32_t lane, uint32_t own, uint32_t block, uint32_t& seq, uint32_t& front) const {
+  __device__ void find(const AttentionArgs& a, uint32_t lane, uint32_t own, const Seq& own_seq, uint32_t block, uint32_t& seq, uint32_t& front, Seq& s) const {
     uint32_t before = 0;
     for (uint32_t at = 0;; at += 64) {
-      const uint32_t n = at == 0 ? own : blocks_of_seq(a, at + lane), upto = before + wave_incl_scan(n);
+      Seq mine = own_seq;
+      const uint32_t n = at == 0 ? own : blocks_of_seq(a, at + lane, mine), upto = before + wave_incl_scan(n);
       const uint64_t beyond = __ballot(upto > block);
       if (beyond) {
         const int l = __builtin_ctzll(beyond);
         seq = at + (uint32_t)l;
         front = (uint32_t)__builtin_amdgcn_readlane((int)(upto - n), l);
+        s = of_lane(mine, l);
         return;
       }
       before = wave_last(upto);
     }
+  }
+  static __device__ Seq of_lane(const Seq& s, int l) {
+    return Seq{__builtin_amdgcn_readlane(s.start, l), __builtin_amdgcn_readlane(s.rows, l), __builtin_amdgcn_readlane(s.len, l), __builtin_amdgcn_readlane(s.base, l)};
   }
 };
 
@@ -151,20 +159,18 @@ struct Share {
     const uint32_t unit = of * 8 + wg % 8, share = unit / groups;
     head = unit % groups * a.heads_across;
     Blocks b;
-    uint32_t own = 0;
-    b.count(a, lane, own);
+    Seq own_seq;
+    uint32_t own, front;
+    b.count(a, lane, own, own_seq);
     if (share >= b.shares) return false;
     const uint32_t from = b.begin(share);
     left = b.begin(share + 1) - from;
-    uint32_t front;
-    b.find(a, lane, own, from, seq, front);
+    b.find(a, lane, own, own_seq, from, seq, front, s);
     later = 0;
     take(a, from - front);
     return true;
   }
   __device__ void take(const AttentionArgs& a, uint32_t at) {
-    seq = (uint32_t)__builtin_amdgcn_readfirstlane((int)seq);
-    s = seq_at(a.seqs, seq);
     first = first_token(a, s);
     blocks = blocks_of(a, s, first);
     rows = (uint32_t)s.rows * a.group;
@@ -183,7 +189,8 @@ struct Share {
     ++later;
     do {
       if (!left) return false;
-      ++seq;
+      seq = (uint32_t)__builtin_amdgcn_readfirstlane((int)(seq + 1));
+      s = seq_at(a.seqs, seq);
       take(a, 0);
     } while (!blocks);
     return true;
@@ -931,16 +938,18 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs 
   __shared__ f32x4 lds_out[kThreads];
   __shared__ float lds_sum[kDown], lds_top[kWaves];
   const uint32_t lane = threadIdx.x % 64, q_heads = a.cache.heads * a.group, groups = a.cache.heads / a.heads_across;
-  const Seq s = seq_at(a.seqs, blockIdx.y);
-  const uint32_t blocks = blocks_of(a, s, first_token(a, s));
-  if (blocks < 2 || (uint64_t)s.rows * a.group > a.most_rows) return;   // written already
   Blocks b;
-  uint32_t own = 0, front = 0;
-  b.count(a, lane, own);
+  Seq own_seq;
+  uint32_t own, front = 0;
+  b.count(a, lane, own, own_seq);
   for (uint32_t at = 0; at < blockIdx.y; at += 64) {
-    const uint32_t n = at == 0 ? own : Blocks::blocks_of_seq(a, at + lane);
+    Seq other;
+    const uint32_t n = at == 0 ? own : Blocks::blocks_of_seq(a, at + lane, other);
     front += wave_last(wave_incl_scan(at + lane < blockIdx.y ? n : 0));
   }
+  const Seq s = blockIdx.y < 64 ? Blocks::of_lane(own_seq, (int)blockIdx.y) : seq_at(a.seqs, blockIdx.y);
+  const uint32_t blocks = blocks_of(a, s, first_token(a, s));
+  if (blocks < 2 || (uint64_t)s.rows * a.group > a.most_rows) return;   // written already
   const uint32_t share0 = b.owner(front), n_parts = b.owner(front + blocks - 1) + 1 - share0;
   if (n_parts == 1) return;
   const uint32_t slot0 = b.begin(share0) < front ? 1 : 0;   // of the first part: behind another sequence's; the others are their workgroups' first
