@@ -221,7 +221,7 @@ struct Share {
 // The lane's rows (r0 + 16 n + m of the product) and their operand of the first product.
 template <int KIND, int D, int NT>
 struct Rows {
-  int row[NT], slot[NT];  // row of the sequence (-1: none), query head of the group
+  int row[NT];            // row of the sequence (-1: none)
   int low_edge;           // tokens up to here may be out of the window of a row of the workgroup's tile
   bf16x8 q[NT][D / 32];
 
@@ -240,8 +240,7 @@ struct Rows {
       const uint32_t r = r0 + 16 * n + m;
       const bool have = r < w.rows;
       row[n] = have ? (int)(r / a.group) : -1;
-      slot[n] = have ? (int)(r % a.group) : 0;
-      const uint32_t h = w.head * a.group + (uint32_t)slot[n];
+      const uint32_t h = w.head * a.group + (have ? r % a.group : 0);
       const uint8_t* at = a.q + (uint64_t)(uint32_t)(w.s.start + max(row[n], 0)) * a.q_stride + 2 * (uint64_t)h * D;
 #pragma unroll
       for (int t = 0; t < D / 32; ++t) {
@@ -255,7 +254,6 @@ struct Rows {
   }
   // whether every row of the tile sees every one of the tokens from t0 on
   __device__ bool see_all(const Share& w, int t0, int tokens) const { return t0 + tokens <= min(w.s.base, w.s.len) && t0 > low_edge; }
-  __device__ float slope(const AttentionArgs& a, const Share& w, int n) const { return a.slopes[w.head * a.group + slot[n]] * kLog2e; }
   // bit e: row n sees token t8 + e
   __device__ uint32_t seen(const Share& w, int n, int t8) const {
     const AttentionArgs a = args_again();
@@ -285,6 +283,22 @@ struct Rows {
       }
     }
     return bits;
+  }
+};
+
+// What the scores of the lane's rows are shaped with.  Loaded once: a load in the loop would wait for all that the loop has asked for ahead.
+template <int NT>
+struct Bias {
+  float slope[NT];   // times log2 e; 0: no bias
+  int pos[NT];
+  __device__ void load(const Share& w, const int (&row)[NT], uint32_t r0, uint32_t m) {
+    const AttentionArgs a = args_again();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const bool have = a.slopes && row[n] >= 0;
+      slope[n] = have ? a.slopes[w.head * a.group + (r0 + 16 * n + m) % a.group] * kLog2e : 0.0f;
+      pos[n] = have ? position_of(a, w.s, row[n]) : 0;
+    }
   }
 };
 
@@ -326,22 +340,24 @@ struct State {
 
   // Scores x of the 32 tokens from t0 on (the lane's eight from t0 + 8 g on), as they come out of the product:
   // capped and biased, in powers of two
-  template <int KIND>
-  static __device__ void shape(const Share& w, const Rows<KIND, D, NT>& r, f32x4 (&x)[NT][2], int t8) {
+  static __device__ void shape(const Share& w, const Bias<NT>& bias, f32x4 (&x)[NT][2], int t8) {
     const AttentionArgs a = args_again();
+    int at[8];   // positions of the lane's tokens
+    if (a.slopes) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) at[e] = t8 + e;
+      if (__builtin_expect(__ballot(t8 + 7 >= w.s.base) != 0, 0)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int j = t8 + e - w.s.base;
+          if (j >= 0 && t8 + e < w.s.len) at[e] = position_of(a, w.s, j);
+        }
+      }
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int pos = a.slopes && r.row[n] >= 0 ? position_of(a, w.s, r.row[n]) : 0;
-      const float slope = a.slopes && r.row[n] >= 0 ? r.slope(a, w, n) : 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float far = 0.0f;
-        if (a.slopes) {
-          const int t = t8 + e, j = t - w.s.base;
-          far = (float)(pos - (j >= 0 && t < w.s.len ? position_of(a, w.s, j) : t));
-        }
-        x[n][e / 4][e % 4] = shaped(a, x[n][e / 4][e % 4], slope, far);
-      }
+      for (int e = 0; e < 8; ++e) x[n][e / 4][e % 4] = shaped(a, x[n][e / 4][e % 4], bias.slope[n], a.slopes ? (float)(bias.pos[n] - at[e]) : 0.0f);
     }
   }
   // without the tokens that a row does not see
@@ -551,6 +567,8 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
     }
     Rows<KIND, D, 1> r;
     r.load(w, w.tile * 16, m, g);
+    Bias<1> bias;
+    if constexpr (!PLAIN) bias.load(w, r.row, w.tile * 16, m);
     State<D, 1> st;
     st.clear();
     bool odd = false;   // words of V were left out
@@ -605,7 +623,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
         }
         const bool all = r.see_all(w, tu, (int)kStep);
         const int t8 = tu + (int)(8 * g);
-        if constexpr (!PLAIN) st.shape(w, r, x, t8);
+        if constexpr (!PLAIN) st.shape(w, bias, x, t8);
         if (__builtin_expect(!all, 0)) st.mask(w, r, x, t8);
         st.raise({st.highest(x[0]) * scale});
         bf16x8 p[1];
@@ -846,6 +864,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
       ask(w.begin);
       ask_page(w.begin + kTokens);
       r.load(w, r0, m, g);
+      Bias<NT> bias;
+      if constexpr (!PLAIN) bias.load(w, r.row, r0, m);
       st.clear();
       int buf = 0;
 #pragma unroll 1
@@ -864,7 +884,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
         for (int u = 0; u < kUnits; ++u) {
           const int t8 = t0 + u * (int)kStep + (int)(8 * g);
           scores(x[u], at + 64 * 2 * KS * u);
-          if constexpr (!PLAIN) st.shape(w, r, x[u], t8);
+          if constexpr (!PLAIN) st.shape(w, bias, x[u], t8);
           if (__builtin_expect(!all, 0)) st.mask(w, r, x[u], t8);
         }
 #pragma unroll
@@ -931,7 +951,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
 
 // The parts of a sequence together.  D / 4 threads have a row and query head, four elements each: where the parts are few, as many rows
 // as that leaves room for go through a workgroup at a time, otherwise all its threads take every (1024 / D)-th part of one.
-constexpr uint32_t kVeryFewParts = 4, kFewParts = 16;
+constexpr uint32_t kVeryFewParts = 4, kAtOnceParts = 16, kFewParts = 48;
 template <int D>
 __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs a) {
   constexpr uint32_t kAcross = D / 4, kDown = kThreads / kAcross;
@@ -954,8 +974,9 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs 
   if (n_parts == 1) return;
   const uint32_t slot0 = b.begin(share0) < front ? 1 : 0;   // of the first part: behind another sequence's; the others are their workgroups' first
   const uint32_t across = threadIdx.x % kAcross, down = threadIdx.x / kAcross;
-  const bool few = n_parts <= kFewParts;
-  const uint32_t outs = (uint32_t)s.rows * q_heads, step = few ? kDown : 1;
+  const uint32_t outs = (uint32_t)s.rows * q_heads;
+  const bool few = n_parts <= kAtOnceParts || (n_parts <= kFewParts && outs > gridDim.x);   // (with a workgroup for each, all of its threads)
+  const uint32_t step = few ? kDown : 1;
   for (uint32_t u0 = blockIdx.x * step; u0 < outs; u0 += gridDim.x * step) {
     const uint32_t u = min(u0 + (few ? down : 0), outs - 1);
     const uint64_t out_row = (uint64_t)(uint32_t)(s.start + (int)(u / q_heads)), h = u % q_heads;
@@ -968,30 +989,38 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs 
     float high = kLowest, total = 0.0f;
     f32x4 o = {0, 0, 0, 0};
     if (few) {
-      const auto all_of = [&](auto most) {
+      const auto add_parts = [&](auto most, uint32_t p0) {
         constexpr uint32_t N = decltype(most)::value;
         f32x4 x[N];
         float top[N], sum[N];
 #pragma unroll
         for (uint32_t p = 0; p < N; ++p) {   // (the last one again where there are no more: a load behind a condition would wait for those before it)
-          const uint64_t at = place(min(p, n_parts - 1));
+          const uint64_t at = place(min(p0 + p, n_parts - 1));
           x[p] = *reinterpret_cast<const f32x4*>(a.part_out + at * D + 4 * across);
           top[p] = a.part_stat[2 * at];
           sum[p] = a.part_stat[2 * at + 1];
         }
+        float now = high;
 #pragma unroll
-        for (uint32_t p = 0; p < N; ++p) high = fmaxf(high, top[p]);
+        for (uint32_t p = 0; p < N; ++p) now = fmaxf(now, top[p]);
+        const float less = __builtin_amdgcn_exp2f(high - now);
+        high = now;
+        total *= less;
+        o *= less;
 #pragma unroll
         for (uint32_t p = 0; p < N; ++p) {
-          if (p < n_parts) {
+          if (p0 + p < n_parts) {
             const float f = __builtin_amdgcn_exp2f(top[p] - high);
             total += f * sum[p];
             o += f * x[p];
           }
         }
       };
-      if (n_parts <= kVeryFewParts) all_of(std::integral_constant<uint32_t, kVeryFewParts>());
-      else all_of(std::integral_constant<uint32_t, kFewParts>());
+      if (n_parts <= kVeryFewParts) {
+        add_parts(std::integral_constant<uint32_t, kVeryFewParts>(), 0);
+      } else {
+        for (uint32_t p0 = 0; p0 < n_parts; p0 += kAtOnceParts) add_parts(std::integral_constant<uint32_t, kAtOnceParts>(), p0);
+      }
     } else {
       for (uint32_t p = threadIdx.x; p < n_parts; p += kThreads) high = fmaxf(high, a.part_stat[2 * place(p)]);
 #pragma unroll
