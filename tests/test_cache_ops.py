@@ -729,3 +729,14 @@ def test_move(kind, layers, layout):
     for (k, v, b), (k1, v1, b1) in zip(tensors, want):
         assert torch.equal(k.cpu(), k1) and torch.equal(v.cpu(), v1)
         assert b is None or torch.equal(b.cpu(), b1)
+
+
+@pytest.mark.gpu
+def test_a_step_with_drafts_and_the_way_of_the_cache():
+    """write, attention, move, compress, decompress and read as a program uses them (paper_2605_01708_amd.tree_decode)"""
+    from paper_2605_01708_amd import tree_decode
+
+    outs, lens, ratio, same = tree_decode.step(tokens=300, sequences=3, layers=2, drafts=13)
+    assert same and ratio > 1.0
+    assert lens == [303, 266, 229]
+    assert all(torch.isfinite(o).all() and o.shape == (39, 32, 128) for o in outs)
