@@ -213,6 +213,19 @@ struct Share {
     tile += a.row_tiles;
     return (uint64_t)tile * a.tile_rows < rows;   // (up to most_rows there are no more than row_tiles)
   }
+  // The segment's tokens that rows of the tile may see: without a tree, none behind the tile's last row; with a window and no positions, none
+  // in front of the first row's, in whole stages of `step` tokens from the segment's begin (so that the last one ends where the segment
+  // does).  2048 rows of a prompt under a window of 256: 181 us over all of their tokens, 38 so.
+  __device__ void tokens(int& from, int& to, int step) const {
+    const AttentionArgs a = args_again();
+    from = begin;
+    to = end;
+    if (!a.tree) to = min(to, s.base + (int)((min((tile + 1) * a.tile_rows, rows) - 1) / a.group) + 1);
+    if (a.window && !a.positions) {
+      const int64_t lowest = (int64_t)s.base + tile * a.tile_rows / a.group - (int64_t)a.window + 1;
+      if (lowest > from) from += (int)(min(lowest, (int64_t)end) - from) & ~(step - 1);
+    }
+  }
   __device__ uint64_t place(const AttentionArgs& a, uint32_t head_of_group, uint32_t row) const {
     return (((uint64_t)wg * 2 + slot) * a.heads_across + head_of_group) * a.kept + row;
   }
@@ -302,13 +315,20 @@ struct Bias {
   }
 };
 
+constexpr float kSmallCap = 128.0f;
 // the scores' way into the exponent of two
 __device__ inline float shaped(const AttentionArgs& a, float x, float slope_log2, float far) {
   x *= a.scale;
   if (a.softcap > 0.0f) {
     // tanh(y) = 1 - 2 / (1 + e^2y): its absolute error of 1e-7 times the cap is one of the exponent
     const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e / a.softcap));
-    x = a.softcap - (2.0f * a.softcap) * __builtin_amdgcn_rcpf(1.0f + e);
+    const float capped = a.softcap - (2.0f * a.softcap) * __builtin_amdgcn_rcpf(1.0f + e);
+    if (__builtin_expect(a.softcap > kSmallCap, 0)) {   // ... which wide caps make large: there, the series where y is below a quarter
+      const float y = x * __builtin_amdgcn_rcpf(a.softcap), t = y * y;
+      x = t < 0.0625f ? x * (1.0f - t * (1.0f / 3.0f - t * (2.0f / 15.0f - t * (17.0f / 315.0f)))) : capped;
+    } else {
+      x = capped;
+    }
   }
   return x * kLog2e - slope_log2 * far;
 }
@@ -541,178 +561,178 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
   do {
     if (!w.first_rows()) continue;
     do {
-    const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
-    const Pages at_pages(c, args.seqs, w.seq);
-    const auto ask_pages = [&](int t0) { return at_pages.entry(min((uint32_t)t0 + 8 * (lane % (S::kTokens / 8)), last8)); };
-    u32x2 k_scales[S::kSteps], v_scales[S::kSteps];
-    const auto ask_scales = [&](uint32_t pages, int t0) {
-      if constexpr (ES == 1) {
-#pragma unroll
-        for (int u = 0; u < S::kSteps; ++u) {
-          const uint32_t k4 = 4 * u + m / 4, v4 = 4 * u + g;
-          const uint32_t k_place = at_pages.place(min((uint32_t)t0 + 8 * k4, last8)), v_place = at_pages.place(min((uint32_t)t0 + 8 * v4, last8));
-          k_scales[u] = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, (uint32_t)__shfl((int)pages, (int)k4), k_place, w.head));
-          v_scales[u] = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, (uint32_t)__shfl((int)pages, (int)v4), v_place, w.head));
-        }
-      }
-    };
-    int t0 = w.begin + (int)turn * S::kTokens;
-    uint32_t pages = 0;
-    if (t0 < w.end) {
-      pages = ask_pages(t0);
-      pages = at_pages.clamped(pages);
-      S::ask(c, at_pages, k_base, v_base, pages, t0, last8, mine, lane);
-      ask_scales(pages, t0);
-      if (t0 + stride < w.end) pages = ask_pages(t0 + stride);
-    }
-    Rows<KIND, D, 1> r;
-    r.load(w, w.tile * 16, m, g);
-    Bias<1> bias;
-    if constexpr (!PLAIN) bias.load(w, r.row, w.tile * 16, m);
-    State<D, 1> st;
-    st.clear();
-    bool odd = false;   // words of V were left out
-#pragma unroll 1
-    for (; t0 < w.end; t0 += stride) {
-      memory_arrived();
-      u32x4 k[S::kSteps][2][KW];
-      uint32_t v[S::kSteps][8][VW];
-#pragma unroll
-      for (int u = 0; u < S::kSteps; ++u) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int i = 0; i < KW; ++i) {
-            const uint32_t token = 32 * u + 8 * (m / 4) + 4 * b + m % 4;
-            k[u][b][i] = *reinterpret_cast<const u32x4*>(mine + token * S::kRow + ((4 * i + g) ^ S::k_key(token)) * 16);
+      const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
+      const Pages at_pages(c, args.seqs, w.seq);
+      const auto ask_pages = [&](int t0) { return at_pages.entry(min((uint32_t)t0 + 8 * (lane % (S::kTokens / 8)), last8)); };
+      u32x2 k_scales[S::kSteps], v_scales[S::kSteps];
+      const auto ask_scales = [&](uint32_t pages, int t0) {
+        if constexpr (ES == 1) {
+  #pragma unroll
+          for (int u = 0; u < S::kSteps; ++u) {
+            const uint32_t k4 = 4 * u + m / 4, v4 = 4 * u + g;
+            const uint32_t k_place = at_pages.place(min((uint32_t)t0 + 8 * k4, last8)), v_place = at_pages.place(min((uint32_t)t0 + 8 * v4, last8));
+            k_scales[u] = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, (uint32_t)__shfl((int)pages, (int)k4), k_place, w.head));
+            v_scales[u] = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, (uint32_t)__shfl((int)pages, (int)v4), v_place, w.head));
           }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          __builtin_memcpy(v[u][e], __builtin_assume_aligned(mine + S::kHalf + S::v_row(32 * u + 8 * g + e) * S::kRow + S::VB * m, S::VB < 16 ? S::VB : 16), S::VB);
-      }
-      u32x2 ks[S::kSteps], vs[S::kSteps];
-#pragma unroll
-      for (int u = 0; u < S::kSteps; ++u) {
-        ks[u] = k_scales[u];
-        vs[u] = v_scales[u];
-      }
-      lds_read();   // into registers: the place is free
-      if (t0 + stride < w.end) {
+        }
+      };
+      int t0 = w.begin + (int)turn * S::kTokens;
+      uint32_t pages = 0;
+      if (t0 < w.end) {
+        pages = ask_pages(t0);
         pages = at_pages.clamped(pages);
-        S::ask(c, at_pages, k_base, v_base, pages, t0 + stride, last8, mine, lane);
-        ask_scales(pages, t0 + stride);
-        if (t0 + 2 * stride < w.end) pages = ask_pages(t0 + 2 * stride);
+        S::ask(c, at_pages, k_base, v_base, pages, t0, last8, mine, lane);
+        ask_scales(pages, t0);
+        if (t0 + stride < w.end) pages = ask_pages(t0 + stride);
       }
-#pragma unroll
-      for (int u = 0; u < S::kSteps; ++u) {
-        const int tu = t0 + u * (int)kStep;
-        if (tu >= w.end) break;
-        f32x4 x[1][2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          x[0][b] = f32x4{0, 0, 0, 0};
-#pragma unroll
-          for (int t = 0; t < KS; ++t) {
-            if constexpr (ES == 2) {
-              x[0][b] = mfma(as_bf16(k[u][b][t]), r.q[0][t], x[0][b]);
-            } else {
-              const u32x2 words = {k[u][b][t / 2][t % 2 * 2], k[u][b][t / 2][t % 2 * 2 + 1]};
-              x[0][b] = mfma(as_bf16(from_fp8<KIND>(words, ks[u][b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
+      Rows<KIND, D, 1> r;
+      r.load(w, w.tile * 16, m, g);
+      Bias<1> bias;
+      if constexpr (!PLAIN) bias.load(w, r.row, w.tile * 16, m);
+      State<D, 1> st;
+      st.clear();
+      bool odd = false;   // words of V were left out
+  #pragma unroll 1
+      for (; t0 < w.end; t0 += stride) {
+        memory_arrived();
+        u32x4 k[S::kSteps][2][KW];
+        uint32_t v[S::kSteps][8][VW];
+  #pragma unroll
+        for (int u = 0; u < S::kSteps; ++u) {
+  #pragma unroll
+          for (int b = 0; b < 2; ++b)
+  #pragma unroll
+            for (int i = 0; i < KW; ++i) {
+              const uint32_t token = 32 * u + 8 * (m / 4) + 4 * b + m % 4;
+              k[u][b][i] = *reinterpret_cast<const u32x4*>(mine + token * S::kRow + ((4 * i + g) ^ S::k_key(token)) * 16);
+            }
+  #pragma unroll
+          for (int e = 0; e < 8; ++e)
+            __builtin_memcpy(v[u][e], __builtin_assume_aligned(mine + S::kHalf + S::v_row(32 * u + 8 * g + e) * S::kRow + S::VB * m, S::VB < 16 ? S::VB : 16), S::VB);
+        }
+        u32x2 ks[S::kSteps], vs[S::kSteps];
+  #pragma unroll
+        for (int u = 0; u < S::kSteps; ++u) {
+          ks[u] = k_scales[u];
+          vs[u] = v_scales[u];
+        }
+        lds_read();   // into registers: the place is free
+        if (t0 + stride < w.end) {
+          pages = at_pages.clamped(pages);
+          S::ask(c, at_pages, k_base, v_base, pages, t0 + stride, last8, mine, lane);
+          ask_scales(pages, t0 + stride);
+          if (t0 + 2 * stride < w.end) pages = ask_pages(t0 + 2 * stride);
+        }
+  #pragma unroll
+        for (int u = 0; u < S::kSteps; ++u) {
+          const int tu = t0 + u * (int)kStep;
+          if (tu >= w.end) break;
+          f32x4 x[1][2];
+  #pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            x[0][b] = f32x4{0, 0, 0, 0};
+  #pragma unroll
+            for (int t = 0; t < KS; ++t) {
+              if constexpr (ES == 2) {
+                x[0][b] = mfma(as_bf16(k[u][b][t]), r.q[0][t], x[0][b]);
+              } else {
+                const u32x2 words = {k[u][b][t / 2][t % 2 * 2], k[u][b][t / 2][t % 2 * 2 + 1]};
+                x[0][b] = mfma(as_bf16(from_fp8<KIND>(words, ks[u][b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
+              }
             }
           }
-        }
-        const bool all = r.see_all(w, tu, (int)kStep);
-        const int t8 = tu + (int)(8 * g);
-        if constexpr (!PLAIN) st.shape(w, bias, x, t8);
-        if (__builtin_expect(!all, 0)) st.mask(w, r, x, t8);
-        st.raise({st.highest(x[0]) * scale});
-        bf16x8 p[1];
-        st.weigh(scale, x, p);
-        u32x4 vt[DV];   // element j of the eight tokens
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-          for (int j = 0; j < DV; j += 2) {
-            uint32_t w0, w1;
-            if constexpr (ES == 2) {
-              w0 = v[u][2 * i][j / 2];
-              w1 = v[u][2 * i + 1][j / 2];
-            } else {
-              const uint32_t b0 = vs[u][i / 2] >> (16 * (i % 2)) & 0xffu, b1 = vs[u][i / 2] >> (16 * (i % 2) + 8) & 0xffu;
-              w0 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[u][2 * i][j / 4], b0) : fp8_pair_to_bf16<KIND, false>(v[u][2 * i][j / 4], b0);
-              w1 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[u][2 * i + 1][j / 4], b1) : fp8_pair_to_bf16<KIND, false>(v[u][2 * i + 1][j / 4], b1);
+          const bool all = r.see_all(w, tu, (int)kStep);
+          const int t8 = tu + (int)(8 * g);
+          if constexpr (!PLAIN) st.shape(w, bias, x, t8);
+          if (__builtin_expect(!all, 0)) st.mask(w, r, x, t8);
+          st.raise({st.highest(x[0]) * scale});
+          bf16x8 p[1];
+          st.weigh(scale, x, p);
+          u32x4 vt[DV];   // element j of the eight tokens
+  #pragma unroll
+          for (int i = 0; i < 4; ++i) {
+  #pragma unroll
+            for (int j = 0; j < DV; j += 2) {
+              uint32_t w0, w1;
+              if constexpr (ES == 2) {
+                w0 = v[u][2 * i][j / 2];
+                w1 = v[u][2 * i + 1][j / 2];
+              } else {
+                const uint32_t b0 = vs[u][i / 2] >> (16 * (i % 2)) & 0xffu, b1 = vs[u][i / 2] >> (16 * (i % 2) + 8) & 0xffu;
+                w0 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[u][2 * i][j / 4], b0) : fp8_pair_to_bf16<KIND, false>(v[u][2 * i][j / 4], b0);
+                w1 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[u][2 * i + 1][j / 4], b1) : fp8_pair_to_bf16<KIND, false>(v[u][2 * i + 1][j / 4], b1);
+              }
+              vt[j][i] = evens(w0, w1);
+              vt[j + 1][i] = odds(w0, w1);
             }
-            vt[j][i] = evens(w0, w1);
-            vt[j + 1][i] = odds(w0, w1);
           }
+          if (__builtin_expect(!all, 0)) odd |= finite_only(vt, t8, w.s.len);
+  #pragma unroll
+          for (int j = 0; j < DV; ++j) st.add(j, as_bf16(vt[j]), p);
         }
-        if (__builtin_expect(!all, 0)) odd |= finite_only(vt, t8, w.s.len);
-#pragma unroll
-        for (int j = 0; j < DV; ++j) st.add(j, as_bf16(vt[j]), p);
       }
-    }
-    if (__builtin_expect(__ballot(odd) != 0, 0)) {
-      const auto element = [&](int j, int i) { return DV * (4 * g + i) + j; };
-      for (int t = w.begin + (int)turn * S::kTokens; t < w.end; t += stride) st.add_odd(w, r, t, min(t + S::kTokens, w.end), (int)kStep, element);
-    }
+      if (__builtin_expect(__ballot(odd) != 0, 0)) {
+        const auto element = [&](int j, int i) { return DV * (4 * g + i) + j; };
+        for (int t = w.begin + (int)turn * S::kTokens; t < w.end; t += stride) st.add_odd(w, r, t, min(t + S::kTokens, w.end), (int)kStep, element);
+      }
 
-    // the waves of a head together, where there are several; lane (m, g) has elements DV (4 g + i) + j of row m in acc[j][i]
-    float total = st.total(0);
-    if (tw > 1) {
-      if (g == 0) {
-        lds_stat[wave][m][0] = st.top[0];
-        lds_stat[wave][m][1] = total;
-      }
-      f32x4* out = reinterpret_cast<f32x4*>(mine) + lane;
-#pragma unroll
-      for (int j = 0; j < DV; ++j) out[64 * j] = st.acc[0][j];
-      lds_barrier();
-      if (turn == 0) {
-        float high = st.top[0];
-        for (uint32_t v = 1; v < tw; ++v) high = fmaxf(high, lds_stat[wave + v * hw][m][0]);
-        const float f0 = __builtin_amdgcn_exp2f(st.top[0] - high);
-        st.top[0] = high;
-        total *= f0;
-#pragma unroll
-        for (int j = 0; j < DV; ++j) st.acc[0][j] *= f0;
-        for (uint32_t v = 1; v < tw; ++v) {
-          const float f = __builtin_amdgcn_exp2f(lds_stat[wave + v * hw][m][0] - high);
-          total += f * lds_stat[wave + v * hw][m][1];
-          const f32x4* from = reinterpret_cast<const f32x4*>(lds_all[wave + v * hw]) + lane;
-#pragma unroll
-          for (int j = 0; j < DV; ++j) st.acc[0][j] += f * from[64 * j];
-        }
-      }
-      lds_barrier();   // (the next tile of rows writes there)
-    }
-    const uint32_t at = w.tile * 16 + m;
-    if (turn == 0 && at < w.rows) {
-      const AttentionArgs a = args_again();
-      const uint32_t q_heads = a.cache.heads * a.group, h = w.head * a.group + at % a.group;
-      const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(at / a.group));
-      if (w.whole) {
-        const float f = one_over(total);
-        uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + 4 * DV * g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < DV; j += 4)
-            *reinterpret_cast<u32x2*>(to + 2 * (DV * i + j)) = u32x2{bf16_pair(st.acc[0][j][i] * f, st.acc[0][j + 1][i] * f), bf16_pair(st.acc[0][j + 2][i] * f, st.acc[0][j + 3][i] * f)};
-        if (g == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(st.top[0], total);
-      } else {
-        const uint64_t place = w.place(a, wave % hw, m);
-        float* to = a.part_out + place * D + 4 * DV * g;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < DV; j += 4)
-            *reinterpret_cast<f32x4*>(to + DV * i + j) = f32x4{st.acc[0][j][i], st.acc[0][j + 1][i], st.acc[0][j + 2][i], st.acc[0][j + 3][i]};
+      // the waves of a head together, where there are several; lane (m, g) has elements DV (4 g + i) + j of row m in acc[j][i]
+      float total = st.total(0);
+      if (tw > 1) {
         if (g == 0) {
-          a.part_stat[2 * place] = st.top[0];
-          a.part_stat[2 * place + 1] = total;
+          lds_stat[wave][m][0] = st.top[0];
+          lds_stat[wave][m][1] = total;
+        }
+        f32x4* out = reinterpret_cast<f32x4*>(mine) + lane;
+  #pragma unroll
+        for (int j = 0; j < DV; ++j) out[64 * j] = st.acc[0][j];
+        lds_barrier();
+        if (turn == 0) {
+          float high = st.top[0];
+          for (uint32_t v = 1; v < tw; ++v) high = fmaxf(high, lds_stat[wave + v * hw][m][0]);
+          const float f0 = __builtin_amdgcn_exp2f(st.top[0] - high);
+          st.top[0] = high;
+          total *= f0;
+  #pragma unroll
+          for (int j = 0; j < DV; ++j) st.acc[0][j] *= f0;
+          for (uint32_t v = 1; v < tw; ++v) {
+            const float f = __builtin_amdgcn_exp2f(lds_stat[wave + v * hw][m][0] - high);
+            total += f * lds_stat[wave + v * hw][m][1];
+            const f32x4* from = reinterpret_cast<const f32x4*>(lds_all[wave + v * hw]) + lane;
+  #pragma unroll
+            for (int j = 0; j < DV; ++j) st.acc[0][j] += f * from[64 * j];
+          }
+        }
+        lds_barrier();   // (the next tile of rows writes there)
+      }
+      const uint32_t at = w.tile * 16 + m;
+      if (turn == 0 && at < w.rows) {
+        const AttentionArgs a = args_again();
+        const uint32_t q_heads = a.cache.heads * a.group, h = w.head * a.group + at % a.group;
+        const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(at / a.group));
+        if (w.whole) {
+          const float f = one_over(total);
+          uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + 4 * DV * g);
+  #pragma unroll
+          for (int i = 0; i < 4; ++i)
+  #pragma unroll
+            for (int j = 0; j < DV; j += 4)
+              *reinterpret_cast<u32x2*>(to + 2 * (DV * i + j)) = u32x2{bf16_pair(st.acc[0][j][i] * f, st.acc[0][j + 1][i] * f), bf16_pair(st.acc[0][j + 2][i] * f, st.acc[0][j + 3][i] * f)};
+          if (g == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(st.top[0], total);
+        } else {
+          const uint64_t place = w.place(a, wave % hw, m);
+          float* to = a.part_out + place * D + 4 * DV * g;
+  #pragma unroll
+          for (int i = 0; i < 4; ++i)
+  #pragma unroll
+            for (int j = 0; j < DV; j += 4)
+              *reinterpret_cast<f32x4*>(to + DV * i + j) = f32x4{st.acc[0][j][i], st.acc[0][j + 1][i], st.acc[0][j + 2][i], st.acc[0][j + 3][i]};
+          if (g == 0) {
+            a.part_stat[2 * place] = st.top[0];
+            a.part_stat[2 * place + 1] = total;
+          }
         }
       }
-    }
     } while (w.more_rows());
   } while (w.next());
 }
@@ -822,6 +842,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
   do {
     if (!w.first_rows()) continue;
     do {
+      int from, to;
+      w.tokens(from, to, kTokens);
       const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
       const Pages at_pages(c, args.seqs, w.seq);
       const uint32_t r0 = (w.tile * W + wave) * 16 * NT;
@@ -831,17 +853,17 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
       S stage;
       uint32_t page = 0;
       const auto ask_page = [&](int t0) {
-        if (t0 < w.end) page = at_pages.entry(min((uint32_t)t0 + group, last8));
+        if (t0 < to) page = at_pages.entry(min((uint32_t)t0 + group, last8));
       };
       const auto ask = [&](int t0) {
-        if (t0 >= w.end) return;
+        if (t0 >= to) return;
         const uint32_t place = at_pages.place(min((uint32_t)t0 + group, last8));
         const uint32_t in_pool = at_pages.clamped(page);
         if (of_k) stage.load_k(c, base, in_pool, place, w.head, piece);
         else stage.load_v(c, base, in_pool, place, w.head);
       };
       const auto store = [&](int t0, int buf) {
-        if (t0 >= w.end) return;
+        if (t0 >= to) return;
         u32x4* to = lds[buf] + 64 * (of_k ? 4 * piece : S::kV + 4 * piece) + lane;
         if (of_k) stage.store_k(to, piece, m);
         else if (__builtin_expect(stage.store_v(to, !r.see_all(w, t0, kTokens), t0 + (int)group, w.s.len), 0)) lds_odd = 1;
@@ -860,16 +882,16 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
           }
         }
       };
-      ask_page(w.begin);
-      ask(w.begin);
-      ask_page(w.begin + kTokens);
+      ask_page(from);
+      ask(from);
+      ask_page(from + kTokens);
       r.load(w, r0, m, g);
       Bias<NT> bias;
       if constexpr (!PLAIN) bias.load(w, r.row, r0, m);
       st.clear();
       int buf = 0;
 #pragma unroll 1
-      for (int t0 = w.begin; t0 < w.end; t0 += kTokens, buf ^= 1) {
+      for (int t0 = from; t0 < to; t0 += kTokens, buf ^= 1) {
         store(t0, buf);
         ask(t0 + kTokens);
         ask_page(t0 + 2 * kTokens);
@@ -904,7 +926,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
         }
       }
       lds_barrier();   // the next tile of rows writes where these tokens are
-      if (__builtin_expect(lds_odd, 0)) st.add_odd(w, r, w.begin, w.end, kTokens, [&](int j, int i) { return 64 * (j / 4) + 16 * g + 4 * i + j % 4; });
+      if (__builtin_expect(lds_odd, 0)) st.add_odd(w, r, from, to, kTokens, [&](int j, int i) { return 64 * (j / 4) + 16 * g + 4 * i + j % 4; });
 
       // lane (m, g) has elements 64 b + 16 g + 4 i + j of row m in acc[4 b + j][i]
       const AttentionArgs a = args_again();

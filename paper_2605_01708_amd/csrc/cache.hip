@@ -3,6 +3,7 @@
 //   common.hpp      byte permutes and vector types shared with the codec
 //   cache.hpp       where the words of a token are; writing, reading back, moving an accepted path
 //   attention.hpp   attention of a step's rows, one token or a tree of drafted ones, over everything cached
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -261,7 +262,7 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   int rc = check_cache(cache, true);
   if (rc == SPLITZIP_OK) rc = check_seqs(cache, seqs);
   if (rc != SPLITZIP_OK) return rc;
-  if (!how || !q_heads || q_heads % cache->kv_heads || !(how->softcap >= 0.0f) || how->reserved) return SPLITZIP_ERR_INVALID_ARG;
+  if (!how || !q_heads || q_heads % cache->kv_heads || !(how->softcap == 0.0f || (how->softcap >= FLT_MIN && how->softcap <= FLT_MAX)) || how->reserved) return SPLITZIP_ERR_INVALID_ARG;
   if (!aligned(how->d_slopes, 4) || !aligned(how->d_tree, 8) || !aligned(how->d_positions, 4) || (how->d_tree && !how->tree_words)) return SPLITZIP_ERR_INVALID_ARG;
   if (!seqs->n_seqs || !n_rows) return SPLITZIP_OK;
   const uint64_t elems = (uint64_t)q_heads * cache->head_dim;

@@ -740,3 +740,104 @@ def test_a_step_with_drafts_and_the_way_of_the_cache():
     assert same and ratio > 1.0
     assert lens == [303, 266, 229]
     assert all(torch.isfinite(o).all() and o.shape == (39, 32, 128) for o in outs)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,dim", [(sz.BF16, 128), (sz.FP8_E5M2, 64), (sz.FP8_E4M3, 256)])
+@pytest.mark.parametrize("window", [0, 100])
+def test_pieces_of_prompts(kind, dim, window):
+    """several tiles of rows, each of which sees another length; over nothing, over a prefix, and more rows than tokens"""
+    w = World(kind, [200, 777, 60, 150], [200, 180, 60, 170], 1, dim, 16, seed=dim, max_len=777)
+    q, qd = queries(w, 3)
+    want = attend(w, q, 0.1, window=window)
+    close(*run(w, qd, sz.Attention(0.1, window=window)), want)
+    w.seqs = sz.Sequences(*w.dev, max_rows=16, max_len=100)
+    close(*run(w, qd, sz.Attention(0.1, window=window)), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,T", [(64, 64), (128, 64), (128, 16), (256, 5)])
+def test_parts_of_trees(dim, T):
+    """one long sequence in many parts, in every kernel: a random tree at its end"""
+    rng = np.random.default_rng(dim + T)
+    w = World(sz.FP8_E5M2, [T + 2500], [T], 1, dim, 16, seed=3)
+    bits, depth, sees = random_tree(T, rng, 1)
+    q, qd = queries(w, 6)
+    pos = [2500 + d for d in depth]
+    how = sz.Attention(0.08, window=2400, tree=torch.from_numpy(bits).cuda(), positions=torch.tensor(pos, dtype=torch.int32, device="cuda"))
+    want = attend(w, q, 0.08, window=2400, see=lambda s, i, j: sees[i] >> j & 1, positions=pos)
+    first = run(w, qd, how)
+    close(*first, want)
+    for a, b in zip(first, run(w, qd, how)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 30])
+@pytest.mark.parametrize("scale,softcap", [(-0.1, 0.0), (0.0, 0.0), (-0.1, 7.0), (0.1, 5000.0), (0.1, 1e30), (0.3, 1e-20)])
+def test_scales_and_caps(T, scale, softcap):
+    """scales of either sign and none; a cap so wide that it does nothing costs no precision, and one that leaves nothing is no NaN"""
+    w = World(sz.BF16, [300, 40], [T, T], 2, 128, 16, seed=17)
+    q, qd = queries(w, 2)
+    out, lse = run(w, qd, sz.Attention(scale, softcap=softcap))
+    want = list(attend(w, q, scale, softcap=softcap if softcap < 1000 else 0.0))
+    x = abs(scale) * 4 * 128                                              # more than any score here
+    want[3] = np.abs(attend(w, q, abs(scale))[3]) + 4e-7 * min(softcap, x) + (x ** 3 / softcap ** 2 / 3 if softcap >= 1000 else 0.0)
+    close(out, lse, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [2, 40])
+def test_what_all_rows_see_reaches_them(T):
+    """an infinity that every row sees, in 32 tokens of which some rows see a part only, and one in front of them"""
+    w = World(sz.BF16, [100 + T, 400 + T], [T, T], 1, 128, 16, seed=19)
+    q, qd = queries(w, 2)
+    w.set(0, 99, 1, 0, np.where(np.arange(128) == 3, np.inf, 1.0))
+    w.set(0, 100, 1, 0, np.where(np.arange(128) == 70, -np.inf, 1.0))
+    w.set(1, 20, 1, 0, np.where(np.arange(128) == 127, np.nan, 1.0))
+    out = run(w, qd, sz.Attention(0.1))[0].double().cpu().numpy()
+    assert np.isposinf(out[:T, :, 3]).all() and np.isneginf(out[:T, :, 70]).all() and np.isnan(out[T:, :, 127]).all()
+    assert np.isfinite(np.delete(out[:T], [3, 70], 2)).all() and np.isfinite(np.delete(out[T:], 127, 2)).all()
+
+
+@pytest.mark.gpu
+def test_a_pool_beyond_32_bits():
+    """pages more than 4 GiB from the pool's start: written, read, moved and attended to there"""
+    pages = (5 << 30) // (16 * 1024)
+    k, v = (torch.empty(pages, 16, 8, 128, dtype=torch.uint8, device="cuda") for _ in range(2))
+    scales = torch.zeros(2, pages, 8, 16, dtype=torch.uint8, device="cuda")
+    far = sz.KvCache(k, v, sz.FP8_E4M3, scales[0], scales[1])
+    near = sz.KvCache.zeros(8, 16, 8, 128, sz.FP8_E4M3)
+    x = torch.randn(2, 100, 8, 128, device="cuda").to(torch.bfloat16)
+    q = torch.randn(4, 8, 128, device="cuda").to(torch.bfloat16)
+    got = []
+    for cache, first in ((far, pages - 8), (near, 0)):
+        table = torch.arange(first, first + 8, dtype=torch.int32, device="cuda")[None].contiguous()
+        i32 = lambda *y: torch.tensor(y, dtype=torch.int32, device="cuda")   # noqa: E731
+        sz.cache_write(x[0], x[1], cache, sz.Sequences(table, i32(0, 100), i32(100), 100, 100))
+        step = sz.Sequences(table, i32(0, 4), i32(100), 4, 100)
+        sz.cache_move(sz.KvCaches([cache]), step, i32(0, 2, 3)[None].contiguous())
+        back, out = torch.zeros_like(x), torch.zeros_like(q)
+        sz.cache_read(cache, sz.Sequences(table, i32(0, 100), i32(100), 100, 100), back[0], back[1])
+        sz.cache_attention(q, cache, step, out, sz.attention_workspace(cache, step, 4, 8), sz.Attention(0.1))
+        got += [back, out]
+    assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[3]) and got[0].abs().sum() > 0
+
+
+def test_strides_and_caps_beyond_the_limits_are_refused():
+    L, buf = sz.lib(), 1 << 16
+
+    def need(**k):
+        d = dict(k=buf, v=buf, ks=buf, vs=buf, dtype=sz.FP8_E5M2, heads=8, dim=128, page=16, pages=4, res=0, ps=16 * 1024, ts=1024, hs=128, ss=128)
+        d.update(k)
+        c = _CCache(*[d[x] for x in ("k", "v", "ks", "vs", "dtype", "heads", "dim", "page", "pages", "res", "ps", "ts", "hs", "ss")])
+        return L.splitzip_cache_write(c, _CSeqs(buf, buf, buf, 4, 0, 1, 64), buf, 1024, buf, 1024, 0, None)
+
+    assert need() == 0
+    assert need(ts=1 << 28) == 0 and need(ts=(1 << 28) + 16) == -2
+    assert need(ps=(1 << 32) - 16) == 0 and need(ps=1 << 32) == -2
+    assert need(ss=(1 << 32) - 8) == 0 and need(ss=1 << 32) == -2
+    c = _CCache(buf, buf, buf, buf, sz.FP8_E5M2, 8, 128, 16, 4, 0, 16 * 1024, 1024, 128, 128)
+    for cap, rc in ((0.0, 0), (30.0, 0), (-1.0, -1), (math.nan, -1), (math.inf, -1), (1e-40, -1)):
+        how = _CAttention(1.0, cap, None, None, None, 0, 0, 0)
+        assert L.splitzip_cache_attention(c, _CSeqs(buf, buf, buf, 4, 0, 1, 64), how, buf, 1024, buf, 1024, None, 0, 8, None, 0, None) == rc
