@@ -489,7 +489,8 @@ typedef struct {
   uint32_t n_pages;     /* pages in the pool */
   uint32_t reserved;    /* 0 */
   uint64_t page_stride_bytes, token_stride_bytes, head_stride_bytes; /* multiples of 16 */
-  uint64_t scale_page_stride_bytes;                                  /* a multiple of 8 */
+  uint64_t scale_page_stride_bytes;                                  /* a multiple of 8; */
+  /* a token's stride above 2^28, or a page's (of words or scales) from 2^32 on: SPLITZIP_ERR_UNSUPPORTED.  A pool may be of any size. */
 } splitzip_cache;
 
 /* The sequences of a call and the rows it has of each.  Rows d_starts[s] to
@@ -512,7 +513,8 @@ typedef struct {
 /* d_k, d_v: n_rows rows of kv_heads x head_dim BF16 words, k_row_stride and
  * v_row_stride words apart (multiples of 8), 16-byte aligned.  One launch.
  * splitzip_cache_write fills the rows' tokens and nothing else of the pool;
- * splitzip_cache_read rounds word * 2^(b - 127) to BF16. */
+ * splitzip_cache_read rounds word * 2^(b - 127) to BF16 (infinite from 2^128 on,
+ * which no byte that splitzip_cache_write takes for finite rows leads to). */
 int splitzip_cache_write(const splitzip_cache* cache, const splitzip_seqs* seqs, const void* d_k, uint64_t k_row_stride,
                          const void* d_v, uint64_t v_row_stride, uint32_t n_rows, void* stream);
 int splitzip_cache_read(const splitzip_cache* cache, const splitzip_seqs* seqs, void* d_k, uint64_t k_row_stride, void* d_v,
@@ -528,10 +530,10 @@ int splitzip_cache_read(const splitzip_cache* cache, const splitzip_seqs* seqs, 
  * A window w > 0 leaves a row the tokens with pos_row - pos_token < w. */
 typedef struct {
   float scale;                /* x = scale * (q . k) */
-  float softcap;              /* > 0: x = softcap * tanh(x / softcap); 0: none */
+  float softcap;              /* a normal number > 0: x = softcap * tanh(x / softcap); 0: none; else SPLITZIP_ERR_INVALID_ARG */
   const float* d_slopes;      /* q_heads, or NULL: x += slope * (pos_token - pos_row), behind the cap */
   const uint64_t* d_tree;     /* n_rows x tree_words, 8-byte aligned, or NULL */
-  const int32_t* d_positions; /* n_rows, or NULL */
+  const int32_t* d_positions; /* n_rows, from -2^30 to 2^30, or NULL */
   uint32_t tree_words;
   uint32_t window;
   uint64_t reserved;          /* 0 */
@@ -544,12 +546,15 @@ typedef struct {
  * h / (q_heads / kv_heads) of the cache), strides and alignment as above.
  * Statistics and sums are held in 32 bits, the weights are rounded to BF16 in
  * front of the product with V.  A row that sees nothing, or nothing but scores
- * of minus infinity, gets zeros and lse = -infinity.  What a row does not see does
- * not touch it, whatever it holds.  d_workspace: the parts of long sequences until they are joined,
- * splitzip_attention_workspace_bytes (an upper bound for every window; 0 for
- * arguments that a call refuses), 16-byte aligned, no defined value needed;
- * calls that share one must not overlap in time.  One launch, or two.  The
- * result is a pure function of the arguments. */
+ * of minus infinity, gets zeros and lse = -infinity.  What a row does not see
+ * does not touch it, whatever it holds; an infinity or a NaN of V that it sees
+ * reaches it.  d_workspace: the parts of long sequences until they are joined,
+ * splitzip_attention_workspace_bytes of it, 16-byte aligned, no defined value
+ * needed; calls that share one must not overlap in time.  The size depends on
+ * the cache, on n_seqs, max_rows, max_len and table_stride, and on q_heads (0
+ * where no sequence is cut, and for arguments that a call refuses); too
+ * little: SPLITZIP_ERR_CAPACITY.  One launch, and a second one where sequences
+ * are cut.  The result is a pure function of the arguments. */
 size_t splitzip_attention_workspace_bytes(const splitzip_cache* cache, const splitzip_seqs* seqs, uint32_t n_rows, uint32_t q_heads);
 int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* seqs, const splitzip_attention* how, const void* d_q,
                              uint64_t q_row_stride, void* d_out, uint64_t out_row_stride, float* d_lse, uint32_t n_rows,

@@ -493,8 +493,8 @@ __device__ inline bool finite_only(u32x4 (&vt)[N], int t8, int len) {
 __device__ inline float lse_of(float top, float total) { return total != 0.0f ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff(); }
 __device__ inline float one_over(float total) { return total != 0.0f ? 1.0f / total : 0.0f; }   // (a NaN is no 0)
 
-// Up to 16 rows: memory's speed is all that counts.  A wave belongs to one head of the cache; the four of a workgroup take four heads of the
-// same tokens (or two heads, or one, and every second or fourth stage of tokens), so that a token's heads, which lie side by
+// Up to 16 rows: memory's speed is all that counts.  A wave belongs to one head of the cache; the four of a workgroup take two heads (or, of an
+// odd number of heads, one) and every second (or fourth) stage of tokens, so that heads of a token, which lie side by
 // side, are read at the same time.  K and V go from memory straight into a piece of LDS of the wave's own, in whole rows (a load of the
 // matrix operand itself would take 16 bytes from each of 16 rows at a time), from there into registers, and while the wave
 // works on those the next tokens are on their way to the same place: no barrier, 128 KB of a CU's LDS in flight.
@@ -818,7 +818,7 @@ struct Stage {
 };
 
 template <int KIND, int D, int W, int NT, bool PLAIN>
-__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 4 && NT == 1 ? 3 : 2))) attention_rows_kernel(AttentionArgs args) {
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 4 ? 3 : 2))) attention_rows_kernel(AttentionArgs args) {
   using S = Stage<KIND, D, W>;
   constexpr int KS = S::KS, DV = S::DV, kTokens = S::kTokens, kUnits = S::kUnits;
   __shared__ u32x4 lds[2][W * 4 * 64];

@@ -170,27 +170,34 @@ struct AttentionPlan {
   uint32_t shares, block_tokens, least_blocks;
   uint32_t wgs;
 };
-// Sequences of up to so many stages are not cut: what their parts would gain, a little over 1 us a stage, the launch that joins them
-// costs (5 us).
-constexpr uint32_t kUncutStages = 4;
 AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, uint32_t q_heads) {
   AttentionPlan p;
   const uint64_t rows = (uint64_t)(q->max_rows ? q->max_rows : 1) * (q_heads / c->kv_heads);
   p.waves = 0;
   p.nt = 1;
   p.tile_rows = 16;
-  p.heads_across = rows > 16 ? 1u : c->kv_heads % 4 == 0 ? 4u : c->kv_heads % 2 == 0 ? 2u : 1u;
+  // Two heads side by side and two waves for each.  us with one, two and four heads, sequences of eight heads of 128: BF16, one of 4000 tokens
+  // 13.0, 14.3, 15.5, 16 of 4000 49.6, 51.0, 53.3, 64 of 200 14.3, 14.7, 23.1; E5M2 14.9, 13.1, 14.1, 35.9, 35.1, 38.2, 13.0, 12.0, 15.0;
+  // 64 ragged ones of up to 8192 in shuffled pages 192, 181, 186.
+  p.heads_across = rows > 16 || c->kv_heads % 2 ? 1u : 2u;
+  const uint64_t longest = q->max_len < kMostTokens ? q->max_len : kMostTokens, tokens = q->n_seqs * longest;
   if (rows > 16) {
-    p.waves = rows > 128 || c->head_dim == 256 ? 8 : 4;
-    p.nt = rows <= 64 || c->head_dim == 256 ? 1 : 2;
+    // Four waves of 16 rows, three workgroups per CU, or eight of 32 rows, one: these read K and V less often, and have more to start and
+    // to end with.  us the one way and the other, eight heads of 128, BF16: 8 sequences of 300 tokens and 128 rows 24.1 and 30.2, 2 of
+    // 8000 and 256 rows 52 and 58, 8 of 4000 and 128 rows 62.5 and 56.8, 32 of 2000 and 128 rows 98 and 62; E5M2 24.0 and 29.2, 47.6 and 55.5, 55.3 and
+    // 55.8, 82 and 62; 64 rows, 8 of 4000: 52.0 and 48.3, 43.4 and 46.7.  Rows of 256 elements leave a wave room for 16 rows only.
+    const bool wide = rows > 64 && tokens * c->kv_heads >= 768ull * (uint64_t)cu_count();
+    p.waves = wide || c->head_dim == 256 ? 8 : 4;
+    p.nt = wide && c->head_dim != 256 ? 2 : 1;
     p.tile_rows = 16 * p.nt * p.waves;
   }
   const uint64_t tiles = (rows + p.tile_rows - 1) / p.tile_rows;
   p.row_tiles = (uint32_t)(tiles < 1024 ? tiles : 1024);
   p.most_rows = (uint32_t)(rows < (uint64_t)p.row_tiles * p.tile_rows ? rows : (uint64_t)p.row_tiles * p.tile_rows);
   p.kept = (uint32_t)(rows < p.tile_rows ? rows : p.tile_rows);
-  // as many workgroups as the chip holds at a time (two of 64 KB of LDS per CU; one of eight waves)
-  const uint64_t groups = (uint64_t)(c->kv_heads / p.heads_across) * p.row_tiles, slots = (uint64_t)cu_count() * (p.waves == 8 || (p.waves == 0 && c->dtype == SPLITZIP_BF16 && c->head_dim == 256) ? 1 : p.waves == 4 && p.nt == 1 ? 3 : 2);
+  // as many workgroups as the chip holds at a time: two with 64 KB of LDS per CU, one with 128 KB or eight waves, three with 32 KB
+  const bool one_per_cu = p.waves == 8 || (p.waves == 0 && c->dtype == SPLITZIP_BF16 && c->head_dim == 256);
+  const uint64_t groups = (uint64_t)(c->kv_heads / p.heads_across) * p.row_tiles, slots = (uint64_t)cu_count() * (one_per_cu ? 1 : p.waves ? 3 : 2);
   uint64_t shares = (slots + groups - 1) / groups;
   // a block: what the waves of a head stage at a time
   const uint32_t staged = p.waves ? p.waves * 1024u / c->head_dim : 8192u / (c->head_dim * words_bytes(c->dtype));
@@ -198,9 +205,16 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
   // (a sum of blocks is kept in 32 bits)
   const uint64_t most = (uint64_t)q->n_seqs * (q->d_block_table ? (uint64_t)q->table_stride * c->page_tokens : c->page_tokens);
   while (most / p.block_tokens + q->n_seqs > (1ull << 31) && p.block_tokens < (1u << 30)) p.block_tokens *= 2;
-  p.least_blocks = p.waves && p.block_tokens < 256 ? 256 / p.block_tokens : 1;
-  const uint64_t longest = q->max_len < kMostTokens ? q->max_len : kMostTokens;
-  if (longest <= (uint64_t)kUncutStages * p.block_tokens) {   // every sequence is a block
+  // Rows of a tree take at least a sixteenth of all tokens, 64 to 256 of them, since more rows are more to join: us with 64, 128, 256 and 512
+  // tokens, 52 rows of 8 heads, one sequence of 1000 tokens 14.4, 15.3, 16.3, 20.8, four 19.6, 16.9, 17.0, 21.4, one of 4000 22.3, 19.4, 17.7, 22.3.
+  const uint64_t least = tokens / 16 < 64 ? 64 : tokens / 16 > 256 ? 256 : tokens / 16;
+  p.least_blocks = p.waves && p.block_tokens < least ? (uint32_t)(least / p.block_tokens) : 1;
+  // Short sequences are not cut: parts of them would gain less than the launch that joins them costs (5 us, more for many rows).  The longer, the more
+  // there is to do side by side anyway.  us cut and not, E5M2, heads of 64: a sequence of 468 tokens 12.0 and 11.0, of 625 12.0 and 13.2, 64 of
+  // 1000 32.7 and 28.3; of 128: a sequence of 234 11.6 and 10.4, 8 of 468 12.6 and 15.0, 52 rows 8 of 400 19.4 and 15.7, 8 of 800 21.6
+  // and 24.5, 32 of 1000 46 and 34, 256 rows 4 of 300 27 and 14; of 256: a sequence of 117 13.4 and 11.9, 8 of 234 15.5 and 16.3, 256 rows 4 of 300 46 and 22.
+  const uint64_t units = (uint64_t)q->n_seqs * c->kv_heads * ((rows + 15) / 16);
+  if (longest * c->head_dim <= 32768 + 96 * (units < 1024 ? units : 1024)) {   // every sequence is a block
     p.block_tokens = (uint32_t)kMostTokens;
     p.least_blocks = 1;
   }
@@ -219,15 +233,15 @@ struct Attend {
     hipLaunchKernelGGL((attention_rows_kernel<KIND, D, W, NT, PLAIN>), grid, dim3(64 * W), 0, st, *a);
   }
   template <bool PLAIN>
-  static void any(dim3 grid, uint32_t waves, uint32_t nt, hipStream_t st, const AttentionArgs* a) {
+  static void any(dim3 grid, uint32_t waves, hipStream_t st, const AttentionArgs* a) {
     if (!waves) hipLaunchKernelGGL((attention_tokens_kernel<KIND, D, PLAIN>), grid, dim3(kThreads), 0, st, *a);
     else if constexpr (D == 256) rows<8, 1, PLAIN>(grid, st, a);
-    else nt == 1 ? rows<4, 1, PLAIN>(grid, st, a) : waves == 4 ? rows<4, 2, PLAIN>(grid, st, a) : rows<8, 2, PLAIN>(grid, st, a);
+    else waves == 4 ? rows<4, 1, PLAIN>(grid, st, a) : rows<8, 2, PLAIN>(grid, st, a);
   }
-  static int run(dim3 grid, uint32_t waves, uint32_t nt, hipStream_t st, const AttentionArgs* a) {
+  static int run(dim3 grid, uint32_t waves, hipStream_t st, const AttentionArgs* a) {
     // (a scale of 0 times an infinity that is not seen would be a NaN: not plain)
-    if (a->softcap == 0.0f && !a->slopes && a->scale > 0.0f) any<true>(grid, waves, nt, st, a);
-    else any<false>(grid, waves, nt, st, a);
+    if (a->softcap == 0.0f && !a->slopes && a->scale > 0.0f) any<true>(grid, waves, st, a);
+    else any<false>(grid, waves, st, a);
     return launched();
   }
 };
@@ -300,7 +314,7 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   a.block_tokens = p.block_tokens;
   a.least_blocks = p.least_blocks;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  rc = by_kind<Attend>(cache, dim3(p.wgs), p.waves, p.nt, st, (const AttentionArgs*)&a);
+  rc = by_kind<Attend>(cache, dim3(p.wgs), p.waves, st, (const AttentionArgs*)&a);
   if (rc != SPLITZIP_OK || !cuts(p)) return rc;
   const uint64_t outs = (uint64_t)(seqs->max_rows ? seqs->max_rows : 1) * q_heads;
   // a workgroup for each row and head, or, since it takes 256 threads' worth of rows at a time where parts are few, for so many of them
