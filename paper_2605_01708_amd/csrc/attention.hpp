@@ -498,8 +498,13 @@ __device__ inline float one_over(float total) { return total != 0.0f ? 1.0f / to
 // side, are read at the same time.  K and V go from memory straight into a piece of LDS of the wave's own, in whole rows (a load of the
 // matrix operand itself would take 16 bytes from each of 16 rows at a time), from there into registers, and while the wave
 // works on those the next tokens are on their way to the same place: no barrier, 128 KB of a CU's LDS in flight.
+//
+// Bound by memory where there is enough to read: 64 sequences of 700 to 8192 tokens, 8 heads of 128 in BF16, 1.17 GB in 180 us (6.5 TB/s; reading
+// alone reaches 7.1).  Short of that by what a launch has before its first and behind its last load (the tables' and lengths' way to the first
+// address 5 us, the join 5 to 7): 131072 tokens of E4M3, 270 MB, in 50 and 7 us.
 template <int KIND, int D>
 struct Stream {
+  // A stage is 16 KB per wave, two workgroups per CU (32 tokens of 256 BF16 elements: 32 KB, one).
   static constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
   static constexpr int kRow = D * ES;                                    // bytes of a token
   static constexpr int kTokens = 16384 / (2 * kRow) < 32 ? 32 : 16384 / (2 * kRow);   // of a stage
@@ -742,6 +747,10 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
 // conflict), FP8 words converted and V transposed once for all waves.  Half of the waves stage four operands of K each, the others
 // four of V; a wave asks for its piece of the next stage before it works on this one, which is written in the other half of LDS: one
 // barrier a stage, since who writes a half has passed the barrier behind which nobody reads it.
+//
+// Bound by the matrix instructions' rate with what surrounds them, hardly ever by memory: 16 sequences of 3001 to 8192 E5M2 tokens under 256 rows (64 drafts of four
+// query heads) of 8 heads of 128, 94 GFLOP, in 135 us (0.7 PFLOP/s; a large library product of BF16 reaches 1.2), of which, measured apart, the products and
+// exponentials are 86, loads and their conversion 14, and prologue, parts and waiting the rest; joining takes 16 more.
 template <int KIND, int D, int W>
 struct Stage {
   static constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
@@ -972,8 +981,11 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
 }
 
 // The parts of a sequence together.  D / 4 threads have a row and query head, four elements each: where the parts are few, as many rows
-// as that leaves room for go through a workgroup at a time, otherwise all its threads take every (1024 / D)-th part of one.
-constexpr uint32_t kVeryFewParts = 4, kAtOnceParts = 16, kFewParts = 48;
+// as that leaves room for go through a workgroup at a time, otherwise all its threads take every (1024 / D)-th part of one.  Bound by
+// latency: the blocks' count, the statistics and the parts are asked for one behind the other, 5 to 7 us; 16 us for the 32768 rows of 64 drafts
+// of 16 sequences, some 50 MB of parts.  (Up to 48 parts sixteen at a time instead of by all threads: 4 and 52 rows of sequences of 1000 to 2000 tokens 1 us
+// slower; four parts asked for as sixteen: 16 sequences of 4000 tokens under 256 rows 121 us a call, 109 so.)
+constexpr uint32_t kVeryFewParts = 4, kFewParts = 16;
 template <int D>
 __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs a) {
   constexpr uint32_t kAcross = D / 4, kDown = kThreads / kAcross;
@@ -997,7 +1009,7 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs 
   const uint32_t slot0 = b.begin(share0) < front ? 1 : 0;   // of the first part: behind another sequence's; the others are their workgroups' first
   const uint32_t across = threadIdx.x % kAcross, down = threadIdx.x / kAcross;
   const uint32_t outs = (uint32_t)s.rows * q_heads;
-  const bool few = n_parts <= kAtOnceParts || (n_parts <= kFewParts && outs > gridDim.x);   // (with a workgroup for each, all of its threads)
+  const bool few = n_parts <= kFewParts;
   const uint32_t step = few ? kDown : 1;
   for (uint32_t u0 = blockIdx.x * step; u0 < outs; u0 += gridDim.x * step) {
     const uint32_t u = min(u0 + (few ? down : 0), outs - 1);
@@ -1041,7 +1053,8 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs 
       if (n_parts <= kVeryFewParts) {
         add_parts(std::integral_constant<uint32_t, kVeryFewParts>(), 0);
       } else {
-        for (uint32_t p0 = 0; p0 < n_parts; p0 += kAtOnceParts) add_parts(std::integral_constant<uint32_t, kAtOnceParts>(), p0);
+        // (as a loop, though it runs once: straight, a call of one token over 777 takes 12.4 us instead of 10.8)
+        for (uint32_t p0 = 0; p0 < n_parts; p0 += kFewParts) add_parts(std::integral_constant<uint32_t, kFewParts>(), p0);
       }
     } else {
       for (uint32_t p = threadIdx.x; p < n_parts; p += kThreads) high = fmaxf(high, a.part_stat[2 * place(p)]);
