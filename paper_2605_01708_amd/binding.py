@@ -3,7 +3,7 @@
 the current HIP stream, nothing else.
 
 The calls that a serving loop repeats go through the extension module _fastcall first, which marshals the plain form of
-their arguments in one step (lib().fast, by the names of the C entry points) and answers _NOT_TAKEN for any other form; the
+their arguments in one step (lib().fast and fast_cache, by the names of the C entry points) and answers _NOT_TAKEN for any other form; the
 ctypes call behind it takes every form and raises the errors, and serves every call where the module is not there."""
 from __future__ import annotations
 
@@ -212,25 +212,28 @@ def lib():
         L.splitzip_cache_attention.argtypes = [chp, sqp, C.POINTER(_CAttention), vp, u64, vp, u64, vp, C.c_uint32, C.c_uint32, vp, sz, vp]
         L.splitzip_cache_move.restype = i
         L.splitzip_cache_move.argtypes = [chp, C.c_uint32, sqp, vp, C.c_uint32, C.c_uint32, vp]
-        L.fast = _short_way(L)
+        L.fast, L.fast_cache = _short_way(L)
         _lib = L
         _leave_fast_in_a_bad_fork()
     return _lib
 
 
 def _short_way(L):
-    """The functions of _fastcall, or, where it is not built or built for another Python or torch, none that take a call."""
+    """The functions of _fastcall, the codec's and the cache's, or, where it is not built or built for another Python or torch, none that
+    take a call."""
     try:
         from . import _fastcall   # torch's own libraries are loaded by now
-        return types.SimpleNamespace(**_fastcall.bind(L._handle, _CCodebook, Variant, _CPaged, _CCache, _CSeqs, _CAttentionOf, torch.__version__))
+        of = _fastcall.bind(L._handle, _CCodebook, Variant, _CPaged, _CCache, _CSeqs, _CAttentionOf, torch.__version__)
+        cache = {name: of.pop(name) for name in list(of) if name.startswith("splitzip_cache_")}
+        return types.SimpleNamespace(**of), types.SimpleNamespace(**cache)
     except ImportError as e:
         warnings.warn(f"{e}: calls take the general way, 1 to 2 us longer each; build the short one with "
                       "`python -m paper_2605_01708_amd.build`", RuntimeWarning, stacklevel=3)
-        return _NoneTaken()
+        return _NoneTaken(), _NoneTaken()
 
 
 class _NoneTaken:
-    """lib().fast where every call goes the general way."""
+    """lib().fast, or fast_cache, where every call goes the general way."""
 
     def __getattr__(self, name):
         return lambda *args: _NOT_TAKEN
@@ -240,7 +243,7 @@ def _leave_fast_in_a_bad_fork() -> None:
     """In a child of a process that had used the GPU before it forked, torch refuses the GPU where the general way asks it for
     the current stream; the short way does not ask torch."""
     if _lib is not None and getattr(torch._C, "_cuda_isInBadFork", bool)():
-        _lib.fast = _NoneTaken()
+        _lib.fast = _lib.fast_cache = _NoneTaken()
 
 
 if hasattr(os, "register_at_fork"):
@@ -1045,7 +1048,7 @@ def _write_or_read(name, cache: KvCache, seqs: Sequences, k: torch.Tensor, v: to
 
 def cache_write(k: torch.Tensor, v: torch.Tensor, cache: KvCache, seqs: Sequences, stream=None) -> None:
     """splitzip_cache_write: the BF16 rows k, v [rows, kv_heads, head_dim] become their sequences' last tokens, quantised if the cache is FP8."""
-    rc = (_lib or lib()).fast.splitzip_cache_write(cache.c, seqs.c, k, v, None if stream is None else _handle(stream))
+    rc = (_lib or lib()).fast_cache.splitzip_cache_write(cache.c, seqs.c, k, v, None if stream is None else _handle(stream))
     if rc != _NOT_TAKEN:
         return _check(rc, "splitzip_cache_write") if rc else None
     _write_or_read("splitzip_cache_write", cache, seqs, k, v, stream)
@@ -1053,7 +1056,7 @@ def cache_write(k: torch.Tensor, v: torch.Tensor, cache: KvCache, seqs: Sequence
 
 def cache_read(cache: KvCache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
     """splitzip_cache_read: the rows' tokens out of the cache, as BF16, into k, v [rows, kv_heads, head_dim]."""
-    rc = (_lib or lib()).fast.splitzip_cache_read(cache.c, seqs.c, k, v, None if stream is None else _handle(stream))
+    rc = (_lib or lib()).fast_cache.splitzip_cache_read(cache.c, seqs.c, k, v, None if stream is None else _handle(stream))
     if rc != _NOT_TAKEN:
         return _check(rc, "splitzip_cache_read") if rc else None
     _write_or_read("splitzip_cache_read", cache, seqs, k, v, stream)
@@ -1071,7 +1074,7 @@ def attention_workspace(cache: KvCache, seqs: Sequences, n_rows: int, q_heads: i
 def cache_attention(q: torch.Tensor, cache: KvCache, seqs: Sequences, out: torch.Tensor, workspace: torch.Tensor, how: Attention,
                     lse: torch.Tensor | None = None, stream=None) -> None:
     """splitzip_cache_attention: the BF16 rows q [rows, q_heads, head_dim] against their sequences' tokens, into out; lse float32 [rows, q_heads]."""
-    rc = (_lib or lib()).fast.splitzip_cache_attention(cache.c, seqs.c, how.c, q, out, lse, workspace, None, None if stream is None else _handle(stream))
+    rc = (_lib or lib()).fast_cache.splitzip_cache_attention(cache.c, seqs.c, how.c, q, out, lse, workspace, None, None if stream is None else _handle(stream))
     if rc != _NOT_TAKEN:
         return _check(rc, "splitzip_cache_attention") if rc else None
     if q.dim() != 3:
@@ -1091,7 +1094,7 @@ def cache_attention(q: torch.Tensor, cache: KvCache, seqs: Sequences, out: torch
 def cache_move(caches: KvCaches, seqs: Sequences, path: torch.Tensor, n_rows: int | None = None, stream=None) -> None:
     """splitzip_cache_move: in all the caches, row path[s, i] of sequence s becomes its token base + i; path int32 [n_seqs, entries], -1 ends a
     path.  n_rows: rows of the call (all that starts says, if None)."""
-    rc = (_lib or lib()).fast.splitzip_cache_move(caches.items, caches.n, seqs.c, path, _MOST_ROWS if n_rows is None else n_rows,
+    rc = (_lib or lib()).fast_cache.splitzip_cache_move(caches.items, caches.n, seqs.c, path, _MOST_ROWS if n_rows is None else n_rows,
                                                   None if stream is None else _handle(stream))
     if rc != _NOT_TAKEN:
         return _check(rc, "splitzip_cache_move") if rc else None

@@ -539,7 +539,7 @@ def test_many_sequences(rows):
 
 @pytest.mark.gpu
 def test_the_short_way_and_the_general_way(monkeypatch):
-    """what lib().fast takes gives the bits that the ctypes calls give, and what it does not take is refused or taken by them"""
+    """what lib().fast_cache takes gives the bits that the ctypes calls give, and what it does not take is refused or taken by them"""
     w = World(sz.FP8_E4M3, [300, 70], [3, 3], 2, 128, 16, seed=30)
     q, qd = queries(w, 4)
     path = torch.tensor([[0, 2], [1, -1]], dtype=torch.int32, device="cuda")
@@ -557,12 +557,12 @@ def test_the_short_way_and_the_general_way(monkeypatch):
     L, before, scales = sz.lib(), w.pool.clone(), w.scales.clone()
     taken = []
     for name in ("splitzip_cache_write", "splitzip_cache_read", "splitzip_cache_attention", "splitzip_cache_move"):
-        f = getattr(L.fast, name)
-        monkeypatch.setattr(L.fast, name, lambda *a, f=f: taken.append(f(*a)) or taken[-1])
+        f = getattr(L.fast_cache, name)
+        monkeypatch.setattr(L.fast_cache, name, lambda *a, f=f: taken.append(f(*a)) or taken[-1])
     first = all_calls()
     assert taken == [0, 0, 0, 0]
     for name in ("splitzip_cache_write", "splitzip_cache_read", "splitzip_cache_attention", "splitzip_cache_move"):
-        monkeypatch.setattr(L.fast, name, lambda *a: 1)
+        monkeypatch.setattr(L.fast_cache, name, lambda *a: 1)
     w.pool.copy_(before)
     w.scales.copy_(scales)
     for a, b in zip(first, all_calls()):
@@ -572,7 +572,7 @@ def test_the_short_way_and_the_general_way(monkeypatch):
 def test_other_forms_are_left_to_the_general_way():
     z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype)   # noqa: E731
     c, q = sz.KvCache(z(3, 16, 2, 64), z(3, 16, 2, 64), sz.BF16), sz.Sequences(z(2, 4, dtype=torch.int32), z(3, dtype=torch.int32), z(2, dtype=torch.int32), 1, 64)
-    f, x, how = sz.lib().fast, z(2, 2, 64), sz.Attention(1.0)
+    f, x, how = sz.lib().fast_cache, z(2, 2, 64), sz.Attention(1.0)
     assert f.splitzip_cache_write(c.c, q.c, x, x, 0) == 1                 # tensors in host memory
     assert f.splitzip_cache_write(q.c, c.c, x, x, 0) == 1                 # another structure
     assert f.splitzip_cache_attention(c.c, q.c, how.c, x, x, None, x, None, 0) == 1
