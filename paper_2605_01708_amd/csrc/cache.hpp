@@ -317,7 +317,7 @@ struct MoveArgs {
 // the path (a lane each) or eight tokens (a register each).  48 paths of up to 6 tokens in 32 layers of E5M2 (25 MB): 8.6 us.
 __global__ void __launch_bounds__(kThreads) cache_move_kernel(MoveArgs a) {
   constexpr uint32_t kHeld = 8;
-  const uint32_t lane = threadIdx.x % 64;
+  const uint32_t lane = threadIdx.x % 64, first_piece = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x - lane));   // a wave's
   const int32_t* path = a.path + (uint64_t)blockIdx.x * a.path_stride;
   const Seq s = seq_at(a.seqs, blockIdx.x);
   const Pages at_pages(a.cache, a.seqs, blockIdx.x);
@@ -340,12 +340,17 @@ __global__ void __launch_bounds__(kThreads) cache_move_kernel(MoveArgs a) {
     p0 = at_pages.clamped(p0);
     p1 = at_pages.clamped(p1);
     const uint32_t l0 = at_pages.place(t), l1 = at_pages.place(to);
-    for (uint32_t u = threadIdx.x; u < 2 * each; u += kThreads) {
+    // The lanes hold the path's entries, so all 64 of them go through the pieces, also those that have no piece of their own any more:
+    // they take the last one, and do not write it.
+    const uint64_t moving = __ballot(moves);
+    for (uint32_t u0 = first_piece; u0 < 2 * each; u0 += kThreads) {
+      const bool live = u0 + lane < 2 * each;
+      const uint32_t u = min(u0 + lane, 2 * each - 1);
       const bool of_v = u >= each, is_word = u - (of_v ? each : 0) < pieces;
       const uint32_t w = u - (of_v ? each : 0), head = is_word ? w / per_head : w - pieces;
       uint8_t* const words = (of_v ? at.v : at.k) + head * a.cache.head_stride + (is_word ? w - head * per_head : 0) * 16;
       uint8_t* const scales = of_v ? at.v_scales : at.k_scales;
-      for (uint64_t left = __ballot(moves); left;) {
+      for (uint64_t left = moving; left;) {
         u32x4 x[kHeld];
         uint64_t dst[kHeld];
         uint32_t held = 0;
@@ -368,6 +373,7 @@ __global__ void __launch_bounds__(kThreads) cache_move_kernel(MoveArgs a) {
 #pragma unroll
         for (uint32_t j = 0; j < kHeld; ++j) {
           if (j >= held) break;
+          if (!live) continue;
           if (is_word) *reinterpret_cast<u32x4*>(words + dst[j]) = x[j];
           else scales[dst[j]] = (uint8_t)x[j][0];
         }
