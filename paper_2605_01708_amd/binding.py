@@ -84,6 +84,18 @@ class _CAttentionOf(_CAttention):
     _fields_ = [("heads", C.c_int64), ("tree_rows", C.c_int64), ("position_rows", C.c_int64)]
 
 
+class _CCacheElsewhere(_CCache):
+    """of tensors that the GPU does not reach: another type, which the short way does not take"""
+
+
+class _CSeqsElsewhere(_CSeqs):
+    """the same"""
+
+
+class _CAttentionElsewhere(_CAttentionOf):
+    """the same"""
+
+
 class Variant(C.Structure):
     """splitzip_variant: one of the formats of the paper's ablations"""
     _fields_ = [("dtype", C.c_uint32), ("code_bits", C.c_uint32), ("k", C.c_uint32), ("escape_mode", C.c_uint32),
@@ -918,6 +930,18 @@ def _ptr(t: torch.Tensor | None):
     return None if t is None else t.data_ptr()
 
 
+def _reached(*tensors) -> bool:
+    """whether the GPU reaches the tensors (None: none): device memory, and pinned host memory"""
+    return all(t is None or t.is_cuda or t.is_pinned() for t in tensors)
+
+
+def _need_reached(*what) -> None:
+    """for the general way, which takes an address as it is: descriptions (their tensors were looked at when they were made) and tensors"""
+    for x in what:
+        if not (_reached(x) if x is None or isinstance(x, torch.Tensor) else x._reached):
+            raise ValueError("the tensors of a call, and those of its descriptions, must be on the GPU")
+
+
 def _strides(t: torch.Tensor):
     """a tensor's strides, those of dimensions of one element as in a contiguous tensor (there they may be anything)"""
     out = list(t.stride())
@@ -953,8 +977,9 @@ class KvCache:
             scale_stride = _strides(k_scales)[0]
         self.dtype, self.kv_heads, self.head_dim = dtype, heads, dim
         self._keep = (k, v, k_scales, v_scales)
-        self.c = _CCache(k.data_ptr(), v.data_ptr(), _ptr(k_scales), _ptr(v_scales), dtype, heads, dim, tokens, pages, 0,
-                         *(x * es for x in _strides(k)[:3]), scale_stride)
+        self._reached = _reached(*self._keep)
+        self.c = (_CCache if self._reached else _CCacheElsewhere)(k.data_ptr(), v.data_ptr(), _ptr(k_scales), _ptr(v_scales), dtype, heads, dim,
+                         tokens, pages, 0, *(x * es for x in _strides(k)[:3]), scale_stride)
 
     @classmethod
     def zeros(cls, pages: int, page_tokens: int, kv_heads: int, head_dim: int, dtype: int, device="cuda") -> "KvCache":
@@ -986,7 +1011,8 @@ class KvCaches:
     def __init__(self, caches):
         self.n = len(caches)
         self._keep = list(caches)
-        self.items = (_CCache * max(self.n, 1))(*[c.c for c in caches])
+        self._reached = all(c._reached for c in caches)
+        self.items = (_CCache * max(self.n, 1))(*[c.c for c in caches]) if self._reached else None
 
 
 class Sequences:
@@ -1009,7 +1035,8 @@ class Sequences:
                 raise ValueError("block_table must be a contiguous tensor [n_seqs, entries] of 32-bit page indices")
             stride = block_table.shape[1]
         self._keep = (block_table, starts, lens)
-        self.c = _CSeqs(_ptr(block_table), starts.data_ptr(), lens.data_ptr(), stride, n, max_rows, max_len)
+        self._reached = _reached(*self._keep)
+        self.c = (_CSeqs if self._reached else _CSeqsElsewhere)(_ptr(block_table), starts.data_ptr(), lens.data_ptr(), stride, n, max_rows, max_len)
 
 
 class Attention:
@@ -1027,8 +1054,9 @@ class Attention:
         if positions is not None and (positions.element_size() != 4 or not positions.is_contiguous()):
             raise ValueError("positions must be a contiguous tensor of 32-bit integers")
         self._keep = (slopes, tree, positions)
-        self.c = _CAttentionOf(scale, softcap, _ptr(slopes), _ptr(tree), _ptr(positions), 0 if tree is None else tree.shape[1], window, 0,
-                               *(-1 if t is None else t.shape[0] for t in self._keep))
+        self._reached = _reached(*self._keep)
+        self.c = (_CAttentionOf if self._reached else _CAttentionElsewhere)(scale, softcap, _ptr(slopes), _ptr(tree), _ptr(positions),
+                               0 if tree is None else tree.shape[1], window, 0, *(-1 if t is None else t.shape[0] for t in self._keep))
 
 
 def _rows(t: torch.Tensor, heads: int, dim: int, what: str) -> int:
@@ -1043,6 +1071,7 @@ def _write_or_read(name, cache: KvCache, seqs: Sequences, k: torch.Tensor, v: to
     ks, vs = _rows(k, cache.kv_heads, cache.head_dim, "k"), _rows(v, cache.kv_heads, cache.head_dim, "v")
     if k.shape[0] != v.shape[0]:
         raise ValueError("k and v must have the same number of rows")
+    _need_reached(cache, seqs, k, v)
     _check(f(C.byref(cache.c), C.byref(seqs.c), k.data_ptr(), ks, v.data_ptr(), vs, k.shape[0], _stream_ptr(stream)), name)
 
 
@@ -1086,6 +1115,9 @@ def cache_attention(q: torch.Tensor, cache: KvCache, seqs: Sequences, out: torch
     for t, n, what in zip(how._keep, (heads, rows, rows), ("slopes", "tree", "positions")):
         if t is not None and t.shape[0] != n:
             raise ValueError(f"{what} must have {n} entries")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _need_reached(cache, seqs, how, q, out, lse, workspace)
     _check(lib().splitzip_cache_attention(C.byref(cache.c), C.byref(seqs.c), C.byref(how.c), q.data_ptr(), qs, out.data_ptr(), os_, _ptr(lse),
                                           rows, heads, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                           _stream_ptr(stream)), "splitzip_cache_attention")
@@ -1100,6 +1132,7 @@ def cache_move(caches: KvCaches, seqs: Sequences, path: torch.Tensor, n_rows: in
         return _check(rc, "splitzip_cache_move") if rc else None
     if path.dim() != 2 or path.shape[0] != seqs.c.n_seqs or path.element_size() != 4 or not path.is_contiguous():
         raise ValueError("path must be a contiguous tensor [n_seqs, entries] of 32-bit integers")
+    _need_reached(caches, seqs, path)
     _check(lib().splitzip_cache_move(caches.items, caches.n, C.byref(seqs.c), path.data_ptr(), path.shape[1],
                                      _MOST_ROWS if n_rows is None else n_rows, _stream_ptr(stream)), "splitzip_cache_move")
 

@@ -219,7 +219,7 @@ bool run(const Bound& b, PyObject* const* a, Py_ssize_t n_args, int* rc) {
       case 'R': {
         const at::Tensor* t = tensor(o);
         PyObject* cap = *a++;
-        if (!t) return false;
+        if (!t || (cache && !t->is_contiguous())) return false;   // (a workspace of the cache's calls: elements must be bytes that are there)
         if (cap == Py_None) v = static_cast<uint64_t>(t->numel() * t->element_size());
         else if (!integer(cap, &v)) return false;
         word(address(t->data_ptr()));

@@ -1,0 +1,72 @@
+"""What the binding's cache calls refuse before an address reaches the GPU: tensors in host memory and of other types.
+
+The calls here have no rows, so that nothing is launched whatever they say."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2605_01708_amd as sz
+
+I32 = torch.int32
+
+
+def world(device, where=()):
+    """descriptions and tensors of a call without rows, on the device but for those named in `where`, which are in host memory"""
+    def z(name, *shape, dtype=torch.bfloat16):
+        return torch.zeros(*shape, dtype=dtype, device="cpu" if name in where else device)
+
+    u8 = torch.uint8
+    cache = sz.KvCache(z("k", 3, 16, 2, 64, dtype=u8), z("v", 3, 16, 2, 64, dtype=u8), sz.FP8_E5M2, z("k_scales", 3, 2, 16, dtype=u8), z("v_scales", 3, 2, 16, dtype=u8))
+    seqs = sz.Sequences(z("table", 2, 4, dtype=I32), z("starts", 3, dtype=I32), z("lens", 2, dtype=I32), 1, 64)
+    how = sz.Attention(1.0, slopes=z("slopes", 4, dtype=torch.float32), tree=z("tree", 0, 1, dtype=torch.int64), positions=z("positions", 0, dtype=I32))
+    rows = {name: z(name, 0, 2, 64) for name in ("new_k", "new_v")}
+    rows |= {name: z(name, 0, 4, 64) for name in ("q", "out")}
+    return cache, seqs, how, {**rows, "lse": z("lse", 0, 4, dtype=torch.float32), "workspace": z("workspace", 64, dtype=u8), "path": z("path", 2, 3, dtype=I32)}
+
+
+def calls(cache, seqs, how, t):
+    return {"write": lambda: sz.cache_write(t["new_k"], t["new_v"], cache, seqs), "read": lambda: sz.cache_read(cache, seqs, t["new_k"], t["new_v"]),
+            "attention": lambda: sz.cache_attention(t["q"], cache, seqs, t["out"], t["workspace"], how, t["lse"]),
+            "move": lambda: sz.cache_move(sz.KvCaches([cache]), seqs, t["path"], n_rows=0)}
+
+
+SHARED = ("k", "v", "k_scales", "v_scales", "table", "starts", "lens")
+OWN = {"write": ("new_k", "new_v"), "read": ("new_k", "new_v"), "attention": ("slopes", "tree", "positions", "q", "out", "lse", "workspace"), "move": ("path",)}
+
+
+@pytest.mark.parametrize("name", OWN)
+def test_host_memory_is_refused(name):
+    with pytest.raises(ValueError, match="on the GPU"):
+        calls(*world("cpu"))[name]()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", OWN)
+def test_a_single_tensor_in_host_memory_is_refused(name):
+    calls(*world("cuda"))[name]()
+    for what in SHARED + OWN[name]:
+        with pytest.raises(ValueError, match="on the GPU"):
+            calls(*world("cuda", (what,)))[name]()
+
+
+@pytest.mark.gpu
+def test_a_workspace_of_repeated_bytes_is_refused():
+    cache, seqs, how, t = world("cuda")
+    t["workspace"] = torch.zeros(1, dtype=torch.uint8, device="cuda").expand(1 << 20)
+    with pytest.raises(ValueError, match="contiguous"):
+        calls(cache, seqs, how, t)["attention"]()
+
+
+@pytest.mark.gpu
+def test_pinned_memory_is_reached():
+    """what the GPU reaches is taken: a table, starts and lengths in pinned host memory"""
+    i32 = lambda *x: torch.tensor(x, dtype=I32)   # noqa: E731
+    cache = sz.KvCache.zeros(4, 16, 2, 64, sz.BF16)
+    x = torch.randn(2, 21, 2, 64, device="cuda").to(torch.bfloat16)
+    seqs = sz.Sequences(i32(2, 1)[None].pin_memory(), i32(0, 21).pin_memory(), i32(21).pin_memory(), 21, 21)
+    sz.cache_write(x[0], x[1], cache, seqs)
+    y = torch.zeros_like(x)
+    sz.cache_read(cache, seqs, y[0], y[1])
+    torch.cuda.synchronize()
+    assert torch.equal(x, y) and torch.equal(cache.k[2], x[0, :16])
