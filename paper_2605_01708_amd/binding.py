@@ -930,6 +930,11 @@ def _ptr(t: torch.Tensor | None):
     return None if t is None else t.data_ptr()
 
 
+# what may hold a cache's words and rows, which are computed with: the type itself, or integers for bits
+_WORDS = {BF16: (torch.bfloat16, torch.int16, torch.uint16), FP8_E5M2: (torch.float8_e5m2, torch.uint8, torch.int8),
+          FP8_E4M3: (torch.float8_e4m3fn, torch.uint8, torch.int8)}
+
+
 def _reached(*tensors) -> bool:
     """whether the GPU reaches the tensors (None: none): device memory, and pinned host memory"""
     return all(t is None or t.is_cuda or t.is_pinned() for t in tensors)
@@ -954,8 +959,8 @@ def _strides(t: torch.Tensor):
 class KvCache:
     """splitzip_cache: K and V of one layer.
 
-    k, v: device tensors [pages, page_tokens, kv_heads, head_dim] of the dtype's words (any 2-byte dtype for BF16, 1-byte for FP8), of
-    the same strides, head_dim contiguous: views into a pool will do.  k_scales, v_scales (FP8): uint8 [pages, kv_heads, page_tokens]
+    k, v: device tensors [pages, page_tokens, kv_heads, head_dim] of the dtype's words (bfloat16, float8_e5m2 or float8_e4m3fn, or
+    integers of that size), of the same strides, head_dim contiguous: views into a pool will do.  k_scales, v_scales (FP8): uint8 [pages, kv_heads, page_tokens]
     with contiguous pages."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, dtype: int, k_scales: torch.Tensor | None = None,
@@ -963,8 +968,8 @@ class KvCache:
         if k.dim() != 4 or k.shape != v.shape or _strides(k) != _strides(v) or k.stride(3) != 1:
             raise ValueError("k and v must be [pages, page_tokens, kv_heads, head_dim] with the same strides and a contiguous head_dim")
         es = _elem_size(dtype)
-        if k.element_size() != es or v.element_size() != es:
-            raise ValueError("k and v must hold words of the dtype")
+        if dtype not in _WORDS or k.dtype not in _WORDS[dtype] or v.dtype not in _WORDS[dtype]:
+            raise ValueError("k and v must hold words of the dtype, as they are or as integers of their size")
         pages, tokens, heads, dim = k.shape
         scale_stride = 0
         if dtype != BF16:
@@ -1061,8 +1066,8 @@ class Attention:
 
 def _rows(t: torch.Tensor, heads: int, dim: int, what: str) -> int:
     """words from row to row of a tensor [rows, heads, dim] of BF16 words"""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.element_size() != 2 or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
-        raise ValueError(f"{what} must be [rows, {heads}, {dim}] of 2-byte words with contiguous rows")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype not in _WORDS[BF16] or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"{what} must be [rows, {heads}, {dim}] of bfloat16 (or 16-bit integers) with contiguous rows")
     return t.stride(0) if t.shape[0] > 1 else heads * dim
 
 

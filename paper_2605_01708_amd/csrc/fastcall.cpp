@@ -58,7 +58,7 @@ struct Caller<int(A...)> {
 //   C  a codebook: its dtype and its address               K  a codebook: its address alone
 //   V  a format of the variants: its address
 //   c  a cache's description: its address                 q  that of the sequences        h  that of an attention
-//   X  rows of the cache's heads, a tensor [rows, heads, head_dim] of 2-byte words: address, words from row to row
+//   X  rows of the cache's heads, a tensor [rows, heads, head_dim] of BF16 words: address, words from row to row
 //   Q  rows of query heads, the same                      O  as many of the same heads, to be written
 //   L  a float32 tensor [rows, query heads], or None: its address
 //   n  no argument: the rows of the tensors above         e  no argument: their query heads
@@ -160,9 +160,11 @@ struct Views {
 };
 int64_t bytes_per_word(uint64_t dtype) { return dtype == SPLITZIP_BF16 ? 2 : 1; }
 
-// rows of heads of 2-byte words, one behind the other in a row; words from row to row
+// rows of heads of BF16 words, as they are or as integers, one behind the other in a row; words from row to row
 bool rows_of(const at::Tensor* t, int64_t heads, int64_t dim, uint64_t* stride) {
-  if (!t || t->dim() != 3 || t->size(1) != heads || t->size(2) != dim || t->element_size() != 2 || t->stride(2) != 1 || (heads > 1 && t->stride(1) != dim)) return false;
+  if (!t || t->dim() != 3 || t->size(1) != heads || t->size(2) != dim || t->stride(2) != 1 || (heads > 1 && t->stride(1) != dim)) return false;
+  const at::ScalarType type = t->scalar_type();
+  if (type != at::kBFloat16 && type != at::kShort && type != at::kUInt16) return false;
   *stride = static_cast<uint64_t>(t->size(0) > 1 ? t->stride(0) : heads * dim);
   return true;
 }

@@ -1,8 +1,6 @@
 """What the binding's cache calls refuse before an address reaches the GPU: tensors in host memory and of other types.
 
 The calls here have no rows, so that nothing is launched whatever they say."""
-import ctypes as C
-
 import pytest
 import torch
 
@@ -70,3 +68,40 @@ def test_pinned_memory_is_reached():
     sz.cache_read(cache, seqs, y[0], y[1])
     torch.cuda.synchronize()
     assert torch.equal(x, y) and torch.equal(cache.k[2], x[0, :16])
+
+
+# ---- types: the calls compute with the words, so that others of the same size are no words of theirs -----
+
+@pytest.mark.parametrize("dtype,wrong", [(sz.BF16, (torch.float16,)), (sz.FP8_E5M2, (torch.float8_e4m3fn, torch.float8_e5m2fnuz, torch.bool)),
+                                         (sz.FP8_E4M3, (torch.float8_e5m2, torch.float8_e4m3fnuz, torch.bool))])
+def test_words_of_another_type_are_no_cache(dtype, wrong):
+    right = {sz.BF16: (torch.bfloat16, torch.int16, torch.uint16), sz.FP8_E5M2: (torch.float8_e5m2, torch.uint8, torch.int8),
+             sz.FP8_E4M3: (torch.float8_e4m3fn, torch.uint8, torch.int8)}[dtype]
+    scales = torch.zeros(3, 2, 16, dtype=torch.uint8)
+    of = lambda t: torch.zeros(3, 16, 2, 64, dtype=torch.uint8 if t.itemsize == 1 else torch.int16).view(t)   # noqa: E731
+    for t in right:
+        sz.KvCache(of(t), of(t), dtype, scales, scales)
+    for t in wrong:
+        for k, v in ((t, right[0]), (right[0], t)):
+            with pytest.raises(ValueError, match="words of the dtype"):
+                sz.KvCache(of(k), of(v), dtype, scales, scales)
+
+
+def refused_as_rows(device, right, wrong):
+    cache, seqs, how, t = world(device)
+    for name, tensors in (("write", ("new_k", "new_v")), ("read", ("new_k", "new_v")), ("attention", ("q", "out"))):
+        for dtype in right:
+            calls(cache, seqs, how, {**t, **{x: t[x].view(dtype) for x in tensors}})[name]()
+        for x in tensors:
+            for dtype in wrong:
+                with pytest.raises(ValueError, match="bfloat16"):
+                    calls(cache, seqs, how, {**t, x: t[x].to(dtype)})[name]()
+
+
+def test_rows_of_another_type_are_refused_by_the_general_way():
+    refused_as_rows("cpu", (), (torch.float16, torch.float32, torch.uint8))
+
+
+@pytest.mark.gpu
+def test_rows_of_another_type_are_refused():
+    refused_as_rows("cuda", (torch.int16, torch.uint16), (torch.float16, torch.float32, torch.uint8))
