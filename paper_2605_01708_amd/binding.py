@@ -935,6 +935,10 @@ _WORDS = {BF16: (torch.bfloat16, torch.int16, torch.uint16), FP8_E5M2: (torch.fl
           FP8_E4M3: (torch.float8_e4m3fn, torch.uint8, torch.int8)}
 
 
+_INT32, _INT64 = (torch.int32, torch.uint32), (torch.int64, torch.uint64)
+_SCALES = (torch.uint8, torch.int8, torch.float8_e8m0fnu)   # the last one stands for just what a scale byte stands for
+
+
 def _reached(*tensors) -> bool:
     """whether the GPU reaches the tensors (None: none): device memory, and pinned host memory"""
     return all(t is None or t.is_cuda or t.is_pinned() for t in tensors)
@@ -976,7 +980,7 @@ class KvCache:
             if k_scales is None or v_scales is None:
                 raise ValueError("an FP8 cache has scales")
             for s in (k_scales, v_scales):
-                if (tuple(s.shape) != (pages, heads, tokens) or s.element_size() != 1 or _strides(s)[1:] != (tokens, 1)
+                if (tuple(s.shape) != (pages, heads, tokens) or s.dtype not in _SCALES or _strides(s)[1:] != (tokens, 1)
                         or _strides(s)[0] != _strides(k_scales)[0]):
                     raise ValueError("scales must be bytes [pages, kv_heads, page_tokens] with contiguous pages")
             scale_stride = _strides(k_scales)[0]
@@ -1030,13 +1034,13 @@ class Sequences:
     def __init__(self, block_table: torch.Tensor | None, starts: torch.Tensor, lens: torch.Tensor, max_rows: int, max_len: int):
         n = lens.numel()
         for t in (starts, lens):
-            if t.element_size() != 4 or not t.is_contiguous():
+            if t.dtype not in _INT32 or not t.is_contiguous():
                 raise ValueError("starts and lens must be contiguous tensors of 32-bit integers")
         if starts.numel() != n + 1:
             raise ValueError("starts must have an entry more than lens")
         stride = 0
         if block_table is not None:
-            if block_table.dim() != 2 or block_table.shape[0] != n or block_table.element_size() != 4 or not block_table.is_contiguous():
+            if block_table.dim() != 2 or block_table.shape[0] != n or block_table.dtype not in _INT32 or not block_table.is_contiguous():
                 raise ValueError("block_table must be a contiguous tensor [n_seqs, entries] of 32-bit page indices")
             stride = block_table.shape[1]
         self._keep = (block_table, starts, lens)
@@ -1054,9 +1058,9 @@ class Attention:
                  tree: torch.Tensor | None = None, positions: torch.Tensor | None = None):
         if slopes is not None and (slopes.dtype != torch.float32 or not slopes.is_contiguous()):
             raise ValueError("slopes must be contiguous float32")
-        if tree is not None and (tree.dim() != 2 or tree.element_size() != 8 or not tree.is_contiguous()):
+        if tree is not None and (tree.dim() != 2 or tree.dtype not in _INT64 or not tree.is_contiguous()):
             raise ValueError("tree must be a contiguous tensor [n_rows, words] of 64-bit words")
-        if positions is not None and (positions.element_size() != 4 or not positions.is_contiguous()):
+        if positions is not None and (positions.dtype not in _INT32 or not positions.is_contiguous()):
             raise ValueError("positions must be a contiguous tensor of 32-bit integers")
         self._keep = (slopes, tree, positions)
         self._reached = _reached(*self._keep)
@@ -1135,7 +1139,7 @@ def cache_move(caches: KvCaches, seqs: Sequences, path: torch.Tensor, n_rows: in
                                                   None if stream is None else _handle(stream))
     if rc != _NOT_TAKEN:
         return _check(rc, "splitzip_cache_move") if rc else None
-    if path.dim() != 2 or path.shape[0] != seqs.c.n_seqs or path.element_size() != 4 or not path.is_contiguous():
+    if path.dim() != 2 or path.shape[0] != seqs.c.n_seqs or path.dtype not in _INT32 or not path.is_contiguous():
         raise ValueError("path must be a contiguous tensor [n_seqs, entries] of 32-bit integers")
     _need_reached(caches, seqs, path)
     _check(lib().splitzip_cache_move(caches.items, caches.n, C.byref(seqs.c), path.data_ptr(), path.shape[1],

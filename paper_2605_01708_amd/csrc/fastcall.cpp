@@ -310,7 +310,7 @@ bool run(const Bound& b, PyObject* const* a, Py_ssize_t n_args, int* rc) {
       }
       case 'T': {
         const at::Tensor* t = tensor(o);
-        if (!t || t->dim() != 2 || t->element_size() != 4 || !t->is_contiguous() || t->size(0) != static_cast<int64_t>(seqs->n_seqs)) return false;
+        if (!t || t->dim() != 2 || (t->scalar_type() != at::kInt && t->scalar_type() != at::kUInt32) || !t->is_contiguous() || t->size(0) != static_cast<int64_t>(seqs->n_seqs)) return false;
         word(address(t->data_ptr()));
         word(static_cast<uint64_t>(t->size(1)));
         break;

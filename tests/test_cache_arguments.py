@@ -105,3 +105,36 @@ def test_rows_of_another_type_are_refused_by_the_general_way():
 @pytest.mark.gpu
 def test_rows_of_another_type_are_refused():
     refused_as_rows("cuda", (torch.int16, torch.uint16), (torch.float16, torch.float32, torch.uint8))
+
+
+def test_numbers_of_another_type_are_refused():
+    """tables, lengths, starts, positions, paths and masks are whole numbers; 32 or 64 bits of another type are none of them"""
+    i32, f32 = torch.zeros(2, 4, dtype=I32), torch.zeros(2, 4)
+    starts, lens = torch.zeros(3, dtype=I32), torch.zeros(2, dtype=I32)
+    for args in ((f32, starts, lens), (i32, starts.float(), lens), (i32, starts, lens.float())):
+        with pytest.raises(ValueError, match="32-bit"):
+            sz.Sequences(*args, 1, 64)
+    for how in (dict(tree=torch.zeros(2, 1, dtype=torch.float64)), dict(tree=torch.zeros(2, 1, dtype=torch.complex64)), dict(positions=torch.zeros(2))):
+        with pytest.raises(ValueError, match="integers|64-bit words"):
+            sz.Attention(1.0, **how)
+    kv = torch.zeros(3, 16, 2, 64, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="scales"):
+        sz.KvCache(kv, kv, sz.FP8_E5M2, *[torch.zeros(3, 2, 16, dtype=torch.uint8).view(torch.float8_e4m3fn)] * 2)
+    sz.KvCache(kv, kv, sz.FP8_E5M2, *[torch.zeros(3, 2, 16, dtype=torch.uint8).view(torch.float8_e8m0fnu)] * 2)
+    sz.Sequences(i32.view(torch.uint32), starts, lens.view(torch.uint32), 1, 64)
+    sz.Attention(1.0, tree=torch.zeros(2, 1, dtype=torch.uint64), positions=torch.zeros(2, dtype=I32))
+
+
+def path_of_floats(device):
+    cache, seqs, how, t = world(device)
+    with pytest.raises(ValueError, match="32-bit integers"):
+        calls(cache, seqs, how, {**t, "path": t["path"].float()})["move"]()
+
+
+def test_a_path_of_floats_is_refused_by_the_general_way():
+    path_of_floats("cpu")
+
+
+@pytest.mark.gpu
+def test_a_path_of_floats_is_refused():
+    path_of_floats("cuda")
