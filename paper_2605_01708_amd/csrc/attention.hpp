@@ -376,8 +376,8 @@ struct State {
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[n][e / 4][e % 4] = shaped(a, x[n][e / 4][e % 4], bias.slope[n], a.slopes ? (float)(bias.pos[n] - at[e]) : 0.0f);
+#pragma unroll   // (2^30 and -2^30 are 2^31 apart, one more than an integer holds; the one below becomes 2^31 as a float)
+      for (int e = 0; e < 8; ++e) x[n][e / 4][e % 4] = shaped(a, x[n][e / 4][e % 4], bias.slope[n], a.slopes ? (float)__builtin_elementwise_sub_sat(bias.pos[n], at[e]) : 0.0f);
     }
   }
   // without the tokens that a row does not see
