@@ -243,7 +243,7 @@ struct Rows {
     low_edge = -1;
     if (a.window) {
       for (uint32_t r = w.tile * a.tile_rows + 16 * g + m; r < min((w.tile + 1) * a.tile_rows, w.rows); r += 64)
-        low_edge = max(low_edge, (int)min((int64_t)position_of(a, w.s, (int)(r / a.group)) - (int64_t)a.window, (int64_t)w.s.len));
+        low_edge = max(low_edge, (int)max(min((int64_t)position_of(a, w.s, (int)(r / a.group)) - (int64_t)a.window, (int64_t)w.s.len), (int64_t)-1));
 #pragma unroll
       for (int o = 32; o > 0; o /= 2) low_edge = max(low_edge, __shfl_xor(low_edge, o));
     }
