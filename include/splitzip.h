@@ -511,7 +511,8 @@ typedef struct {
 } splitzip_seqs;
 
 /* d_k, d_v: n_rows rows of kv_heads x head_dim BF16 words, k_row_stride and
- * v_row_stride words apart (multiples of 8), 16-byte aligned.  One launch.
+ * v_row_stride words apart (multiples of 8), 16-byte aligned; rows of more than
+ * 2^31 bytes: SPLITZIP_ERR_UNSUPPORTED (queries as well).  One launch.
  * splitzip_cache_write fills the rows' tokens and nothing else of the pool;
  * splitzip_cache_read rounds word * 2^(b - 127) to BF16 (infinite from 2^128 on,
  * which no byte that splitzip_cache_write takes for finite rows leads to). */

@@ -37,6 +37,7 @@ int cu_count() {
 int launched() { return hipGetLastError() == hipSuccess ? SPLITZIP_OK : SPLITZIP_ERR_HIP; }
 
 constexpr uint64_t kMostTokens = 1u << 30;   // of a sequence: token numbers and the steps past them stay in 31 bits
+constexpr uint64_t kMostRow = 1ull << 31;     // bytes of a row of the call's tensors: the place in one is a 32-bit offset
 constexpr uint32_t kMostSeqs = 65535;        // a dimension of a grid
 constexpr uint64_t kStreamed = 96ull << 20;   // bytes that a call moves (figures at the kernels)
 
@@ -145,7 +146,7 @@ int rows_call(const splitzip_cache* c, const splitzip_seqs* q, void* d_k, uint64
   if (rc != SPLITZIP_OK) return rc;
   const uint64_t elems = (uint64_t)c->kv_heads * c->head_dim;
   if (!q->n_seqs || !n_rows) return SPLITZIP_OK;
-  if (n_rows > kMostTokens) return SPLITZIP_ERR_UNSUPPORTED;
+  if (n_rows > kMostTokens || elems * 2 > kMostRow) return SPLITZIP_ERR_UNSUPPORTED;
   if (!rows_ok(d_k, k_stride, elems) || !rows_ok(d_v, v_stride, elems)) return SPLITZIP_ERR_INVALID_ARG;
   RowsArgs a;
   a.cache = device_cache(c, q);
@@ -280,7 +281,7 @@ int splitzip_cache_attention(const splitzip_cache* cache, const splitzip_seqs* s
   if (!aligned(how->d_slopes, 4) || !aligned(how->d_tree, 8) || !aligned(how->d_positions, 4) || (how->d_tree && !how->tree_words)) return SPLITZIP_ERR_INVALID_ARG;
   if (!seqs->n_seqs || !n_rows) return SPLITZIP_OK;
   const uint64_t elems = (uint64_t)q_heads * cache->head_dim;
-  if (n_rows > kMostTokens || elems * 2 > (1ull << 31)) return SPLITZIP_ERR_UNSUPPORTED;
+  if (n_rows > kMostTokens || elems * 2 > kMostRow) return SPLITZIP_ERR_UNSUPPORTED;
   const AttentionPlan p = plan_attention(cache, seqs, q_heads);
   const uint64_t need = workspace_of(p, cache);
   if (workspace_bytes < need) return SPLITZIP_ERR_CAPACITY;

@@ -1,10 +1,13 @@
 """What the binding's cache calls refuse before an address reaches the GPU: tensors in host memory and of other types.
 
 The calls here have no rows, so that nothing is launched whatever they say."""
+import ctypes as C
+
 import pytest
 import torch
 
 import paper_2605_01708_amd as sz
+from paper_2605_01708_amd.binding import _CAttention, _CCache, _CSeqs
 
 I32 = torch.int32
 
@@ -138,3 +141,15 @@ def test_a_path_of_floats_is_refused_by_the_general_way():
 @pytest.mark.gpu
 def test_a_path_of_floats_is_refused():
     path_of_floats("cuda")
+
+
+@pytest.mark.parametrize("heads,rc", [((1 << 24) - 1, -1), (1 << 24, -1), ((1 << 24) + 1, -2), (1 << 25, -2)])
+def test_rows_that_offsets_of_32_bits_do_not_span_are_refused(heads, rc):
+    """(the calls have no tensors, which is what rows of up to 2^31 bytes are refused for)"""
+    L, buf = sz.lib(), 1 << 16
+    c = _CCache(buf, buf, buf, buf, sz.FP8_E5M2, heads, 64, 8, 1, 0, 8 * 64, 64, 8 * 64, 8 * heads)
+    q = _CSeqs(buf, buf, buf, 1, 1, 1, 8)
+    for f in (L.splitzip_cache_write, L.splitzip_cache_read):
+        assert f(C.byref(c), C.byref(q), None, 64 * heads, None, 64 * heads, 1, None) == rc
+    how = _CAttention(1.0, 0.0, None, None, None, 0, 0, 0)
+    assert L.splitzip_cache_attention(C.byref(c), C.byref(q), C.byref(how), None, 64 * heads, None, 64 * heads, None, 1, heads, None, 0, None) == rc
