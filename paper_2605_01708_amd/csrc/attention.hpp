@@ -68,22 +68,53 @@ __device__ inline int position_of(const AttentionArgs& a, const Seq& s, int i) {
   return a.positions ? a.positions[s.start + i] : s.base + i;
 }
 
-// The first token that any row of the sequence may see, a multiple of 32: with a window, the one that the row at the lowest
+// A sequence and the first token that any row of it may see, a multiple of 32: with a window, the one that the row at the lowest
 // position sees.  The sequence's blocks count from it.
-__device__ inline int first_token(const AttentionArgs& a, const Seq& s) {
-  if (!a.window) return 0;
-  int low = s.base;   // without positions: the first row's
-  if (a.positions) {
-    low = 0x7fffffff;
-    for (int i = 0; i < s.rows; ++i) low = min(low, position_of(a, s, i));
+struct Span : Seq {
+  int first;
+};
+// The lowest position of `rows` rows from `start` on; `each` lanes (a power of two) side by side take them, this one being number `of`.
+// Eight at a time: one by one, a call of 16 trees of 64 rows waited 35 us for its positions, one of a prompt of 2048 rows 250.
+__device__ inline int lowest(const AttentionArgs& a, int start, int rows, int of, int each) {
+  int low = 0x7fffffff;
+  for (int i = of; i < rows; i += 8 * each) {
+    int at[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) at[k] = a.positions[start + min(i + k * each, rows - 1)];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) low = min(low, at[k]);
   }
+  for (int o = each / 2; o > 0; o /= 2) low = min(low, __shfl_xor(low, o));
+  return low;
+}
+// low: the lowest position of the sequence's rows
+__device__ inline int first_from(const AttentionArgs& a, const Seq& s, int low) {
+  if (!a.window) return 0;
   const int64_t first = (int64_t)low - (int64_t)a.window + 1;
   const int64_t most = max(min(s.base, s.len), 0);   // drafted tokens lie where their positions say, not where they are stored
   return (int)(max(min(first, most), (int64_t)0) & ~(int64_t)(kStep - 1));
 }
+// All lanes of a wave together: sequence `seq`, the same for all of them, and sequence at + lane (no rows where there is none).
+__device__ inline Span span_at(const AttentionArgs& a, uint32_t lane, uint32_t seq) {
+  Span s{seq_at(a.seqs, seq), 0};
+  s.first = first_from(a, s, a.window && a.positions ? __builtin_amdgcn_readfirstlane(lowest(a, s.start, s.rows, (int)lane, 64)) : s.base);
+  return s;
+}
+__device__ inline Span spans_at(const AttentionArgs& a, uint32_t lane, uint32_t at) {
+  Span s{Seq{0, 0, 0, 0}, 0};
+  if (at + lane < a.seqs.n_seqs) static_cast<Seq&>(s) = seq_at(a.seqs, at + lane);
+  int low = s.base;
+  if (a.window && a.positions) {   // as many lanes for each sequence as there are
+    const uint32_t n = min(a.seqs.n_seqs - at, 64u), shift = n > 1 ? (uint32_t)__builtin_clz(n - 1) - 26u : 6u, of = lane >> shift;
+    low = lowest(a, __shfl(s.start, (int)of), __shfl(s.rows, (int)of), (int)(lane & ((1u << shift) - 1u)), 1 << shift);
+    low = __shfl(low, (int)(lane << shift));
+  }
+  s.first = first_from(a, s, low);
+  return s;
+}
 // One at least where there are rows: somebody has to write their zeros.
-__device__ inline uint32_t blocks_of(const AttentionArgs& a, const Seq& s, int first) {
-  return s.rows ? max(((uint32_t)(s.len - first) + a.block_tokens - 1) / a.block_tokens, 1u) : 0u;
+__device__ inline uint32_t blocks_of(const AttentionArgs& a, const Span& s) {
+  return s.rows ? max(((uint32_t)(s.len - s.first) + a.block_tokens - 1) / a.block_tokens, 1u) : 0u;
 }
 
 // The blocks of all sequences, one sequence behind the other, are dealt out evenly to a.shares workgroups (per heads and tile of
@@ -98,31 +129,21 @@ struct Blocks {
     const uint32_t longer = odd * (each + 1);
     return block < longer ? block / (each + 1) : odd + (block - longer) / each;
   }
-  // blocks of sequence seq, and the sequence, a lane each
-  static __device__ uint32_t blocks_of_seq(const AttentionArgs& a, uint32_t seq, Seq& s) {
-    if (seq >= a.seqs.n_seqs) return 0;
-    s = seq_at(a.seqs, seq);
-    return blocks_of(a, s, first_token(a, s));
-  }
-  // own, own_seq: of sequence `lane`
-  __device__ void count(const AttentionArgs& a, uint32_t lane, uint32_t& own, Seq& own_seq) {
-    own_seq = Seq{0, 0, 0, 0};
-    own = blocks_of_seq(a, lane, own_seq);
-    uint32_t total = wave_last(wave_incl_scan(own));
-    for (uint32_t at = 64; at < a.seqs.n_seqs; at += 64) {
-      Seq s;
-      total += wave_last(wave_incl_scan(blocks_of_seq(a, at + lane, s)));
-    }
+  // mine: sequence `lane`
+  __device__ void count(const AttentionArgs& a, uint32_t lane, Span& mine) {
+    mine = spans_at(a, lane, 0);
+    uint32_t total = wave_last(wave_incl_scan(blocks_of(a, mine)));
+    for (uint32_t at = 64; at < a.seqs.n_seqs; at += 64) total += wave_last(wave_incl_scan(blocks_of(a, spans_at(a, lane, at))));
     shares = min(a.shares, (total + a.least_blocks - 1) / a.least_blocks);
     each = total / max(shares, 1u);
     odd = total - each * shares;
   }
   // the sequence that has this block, and the number of its first block
-  __device__ void find(const AttentionArgs& a, uint32_t lane, uint32_t own, const Seq& own_seq, uint32_t block, uint32_t& seq, uint32_t& front, Seq& s) const {
+  __device__ void find(const AttentionArgs& a, uint32_t lane, Span mine, uint32_t block, uint32_t& seq, uint32_t& front, Span& s) const {
     uint32_t before = 0;
     for (uint32_t at = 0;; at += 64) {
-      Seq mine = own_seq;
-      const uint32_t n = at == 0 ? own : blocks_of_seq(a, at + lane, mine), upto = before + wave_incl_scan(n);
+      if (at) mine = spans_at(a, lane, at);
+      const uint32_t n = blocks_of(a, mine), upto = before + wave_incl_scan(n);
       const uint64_t beyond = __ballot(upto > block);
       if (beyond) {
         const int l = __builtin_ctzll(beyond);
@@ -134,17 +155,18 @@ struct Blocks {
       before = wave_last(upto);
     }
   }
-  static __device__ Seq of_lane(const Seq& s, int l) {
-    return Seq{__builtin_amdgcn_readlane(s.start, l), __builtin_amdgcn_readlane(s.rows, l), __builtin_amdgcn_readlane(s.len, l), __builtin_amdgcn_readlane(s.base, l)};
+  static __device__ Span of_lane(const Span& s, int l) {
+    return Span{Seq{__builtin_amdgcn_readlane(s.start, l), __builtin_amdgcn_readlane(s.rows, l), __builtin_amdgcn_readlane(s.len, l), __builtin_amdgcn_readlane(s.base, l)},
+                __builtin_amdgcn_readlane(s.first, l)};
   }
 };
 
 // What a workgroup is to do: segment after segment of its blocks, each a piece of one sequence, for heads from `head` on and the rows of
 // tile `tile`.
 struct Share {
-  Seq s;
+  Span s;
   uint32_t seq, head, tile, rows;   // rows: of the matrix product, the sequence's times the group's query heads
-  int first, begin, end;            // the sequence's first token, the segment's tokens
+  int begin, end;                   // the segment's tokens
   uint32_t block, blocks, left;     // the segment's first block in the sequence, the sequence's blocks, the workgroup's from here on
   uint32_t slot, wg;                // where the segment's part is kept
   bool whole;                       // the segment is all of the sequence: no part
@@ -159,38 +181,37 @@ struct Share {
     const uint32_t unit = of * 8 + wg % 8, share = unit / groups;
     head = unit % groups * a.heads_across;
     Blocks b;
-    Seq own_seq;
-    uint32_t own, front;
-    b.count(a, lane, own, own_seq);
+    Span mine;
+    uint32_t front;
+    b.count(a, lane, mine);
     if (share >= b.shares) return false;
     const uint32_t from = b.begin(share);
     left = b.begin(share + 1) - from;
-    b.find(a, lane, own, own_seq, from, seq, front, s);
+    b.find(a, lane, mine, from, seq, front, s);
     later = 0;
     take(a, from - front);
     return true;
   }
   __device__ void take(const AttentionArgs& a, uint32_t at) {
-    first = first_token(a, s);
-    blocks = blocks_of(a, s, first);
+    blocks = blocks_of(a, s);
     rows = (uint32_t)s.rows * a.group;
     block = at;
     if (!blocks) return;
     const uint32_t mine = min(blocks - at, left);
-    begin = first + (int)(at * a.block_tokens);
+    begin = s.first + (int)(at * a.block_tokens);
     end = at + mine < blocks ? begin + (int)(mine * a.block_tokens) : s.len;
     whole = at == 0 && mine == blocks;
     slot = later ? 1u : 0u;
   }
   // to the next segment
-  __device__ bool next() {
+  __device__ bool next(uint32_t lane) {
     const AttentionArgs a = args_again();
     left -= min(blocks - block, left);
     ++later;
     do {
       if (!left) return false;
       seq = (uint32_t)__builtin_amdgcn_readfirstlane((int)(seq + 1));
-      s = seq_at(a.seqs, seq);
+      s = span_at(a, lane, seq);
       take(a, 0);
     } while (!blocks);
     return true;
@@ -202,7 +223,7 @@ struct Share {
     tile = wg / 8 % a.row_tiles;
     if (rows > a.most_rows) {
       if (block) return false;
-      begin = first;
+      begin = s.first;
       end = s.len;
       whole = true;
     }
@@ -289,10 +310,21 @@ struct Rows {
     }
     if (a.window) {
       const int pos = position_of(a, w.s, row[n]);
+      if (a.positions && j0 > -8) {
 #pragma unroll 1
-      for (int e = 0; e < 8; ++e) {
-        const int j = j0 + e, at = j >= 0 && t8 + e < w.s.len ? position_of(a, w.s, j) : t8 + e;
-        if ((int64_t)pos - (int64_t)at >= (int64_t)a.window) bits &= ~(1u << e);
+        for (int e0 = 0; e0 < 8; e0 += 4) {   // four positions at a time (that prompt 163 us, 186 one by one; eight cost all calls registers)
+          int at[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) at[e] = a.positions[w.s.start + min(max(j0 + e0 + e, 0), w.s.rows - 1)];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = j0 + e0 + e;
+            if ((int64_t)pos - (int64_t)(j >= 0 && j < w.s.rows ? at[e] : t8 + e0 + e) >= (int64_t)a.window) bits &= ~(1u << (e0 + e));
+          }
+        }
+      } else {   // tokens lie where they are stored: those of the eight up to pos - window are behind it
+        const int64_t behind_it = (int64_t)pos - (int64_t)a.window - (int64_t)t8 + 1;
+        bits &= ~0u << (int)min(max(behind_it, (int64_t)0), (int64_t)8);
       }
     }
     return bits;
@@ -739,7 +771,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
         }
       }
     } while (w.more_rows());
-  } while (w.next());
+  } while (w.next(lane));
 }
 
 // More rows: the W waves of a workgroup take 16 NT rows each of the same tokens.  Those are staged in LDS, 4 KB per wave at a time, as the
@@ -977,32 +1009,32 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
         }
       }
     } while (w.more_rows());
-  } while (w.next());
+  } while (w.next(lane));
 }
 
 // The parts of a sequence together.  D / 4 threads have a row and query head, four elements each: where the parts are few, as many rows
 // as that leaves room for go through a workgroup at a time, otherwise all its threads take every (1024 / D)-th part of one.  Bound by
 // latency: the blocks' count, the statistics and the parts are asked for one behind the other, 5 to 7 us; 16 us for the 32768 rows of 64 drafts
 // of 16 sequences, some 50 MB of parts.  (Up to 48 parts sixteen at a time instead of by all threads: 4 and 52 rows of sequences of 1000 to 2000 tokens 1 us
-// slower; four parts asked for as sixteen: 16 sequences of 4000 tokens under 256 rows 121 us a call, 109 so.)
+// slower; four parts asked for as sixteen: 16 sequences of 4000 tokens under 256 rows 121 us a call, 109 so.  Four waves per SIMD: with a few
+// registers too many for that 17 us where it takes 15.)
 constexpr uint32_t kVeryFewParts = 4, kFewParts = 16;
 template <int D>
-__global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs a) {
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) attention_join_kernel(AttentionArgs a) {
   constexpr uint32_t kAcross = D / 4, kDown = kThreads / kAcross;
   __shared__ f32x4 lds_out[kThreads];
   __shared__ float lds_sum[kDown], lds_top[kWaves];
   const uint32_t lane = threadIdx.x % 64, q_heads = a.cache.heads * a.group, groups = a.cache.heads / a.heads_across;
   Blocks b;
-  Seq own_seq;
-  uint32_t own, front = 0;
-  b.count(a, lane, own, own_seq);
+  Span mine;
+  uint32_t front = 0;
+  b.count(a, lane, mine);
   for (uint32_t at = 0; at < blockIdx.y; at += 64) {
-    Seq other;
-    const uint32_t n = at == 0 ? own : Blocks::blocks_of_seq(a, at + lane, other);
+    const uint32_t n = blocks_of(a, at ? spans_at(a, lane, at) : mine);
     front += wave_last(wave_incl_scan(at + lane < blockIdx.y ? n : 0));
   }
-  const Seq s = blockIdx.y < 64 ? Blocks::of_lane(own_seq, (int)blockIdx.y) : seq_at(a.seqs, blockIdx.y);
-  const uint32_t blocks = blocks_of(a, s, first_token(a, s));
+  const Span s = blockIdx.y < 64 ? Blocks::of_lane(mine, (int)blockIdx.y) : span_at(a, lane, blockIdx.y);
+  const uint32_t blocks = blocks_of(a, s);
   if (blocks < 2 || (uint64_t)s.rows * a.group > a.most_rows) return;   // written already
   const uint32_t share0 = b.owner(front), n_parts = b.owner(front + blocks - 1) + 1 - share0;
   if (n_parts == 1) return;

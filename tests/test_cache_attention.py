@@ -34,3 +34,45 @@ def test_a_window_wider_than_any_sequence_is_none(T, window):
     assert not torch.isfinite(out[:T, :, 9]).any() and torch.isfinite(out[T:]).all()
     again, lse2 = run(w, qd, sz.Attention(0.5, window=window))
     assert torch.equal(torch.isnan(out), torch.isnan(again)) and torch.equal(out.nan_to_num(), again.nan_to_num()) and torch.equal(lse, lse2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,T", [(1, 1), (1, 200), (2, 70), (3, 9), (5, 33), (16, 17), (33, 3), (64, 2), (70, 1), (130, 4)])
+@pytest.mark.parametrize("hint", [None, 5000])
+def test_positions_under_a_window(n, T, hint):
+    """the row at the lowest position, wherever it is among a sequence's rows and whatever number of lanes looks for it, decides where the
+    sequence begins; some sequences have no rows, more than 64 are counted in turns, and a hint of long ones cuts short ones into parts"""
+    rng = np.random.default_rng(n + T)
+    rows = [T if k % 4 != 3 else int(rng.integers(0, T + 1)) for k in range(n)]
+    lens = [r + int(rng.integers(0, 300 if n < 64 else 200)) for r in rows]
+    w = World(sz.FP8_E4M3 if n % 2 else sz.BF16, lens, rows, 1, 64, 16, seed=n, max_len=hint)
+    pos = np.concatenate([[max(0, L - r) + rng.permutation(r)] for L, r in zip(lens, rows)], axis=None).astype(np.int64)
+    for s in range(n):   # one row far in front of the others
+        if rows[s] > 2:
+            pos[w.starts[s] + int(rng.integers(rows[s]))] -= 60
+    q, qd = queries(w, 2)
+    how = sz.Attention(0.1, window=40, positions=torch.from_numpy(pos.astype(np.int32)).cuda())
+    close(*run(w, qd, how), attend(w, q, 0.1, window=40, positions=pos))
+
+
+@pytest.mark.gpu
+def test_positions_of_a_prompt_do_not_wait_for_one_another():
+    """a piece of a prompt of 2048 rows with positions and a window takes less than two and a half times what it takes without (four times
+    if the positions were looked at one by one)"""
+    T = 2048
+    cache = sz.KvCache.zeros(T // 16, 16, 8, 128, sz.BF16)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")   # noqa: E731
+    seqs = sz.Sequences(torch.arange(T // 16, dtype=torch.int32, device="cuda")[None], i32(0, T), i32(T), T, T)
+    q = torch.randn(T, 32, 128, device="cuda").to(torch.bfloat16)
+    out, workspace = torch.empty_like(q), sz.attention_workspace(cache, seqs, T, 32)
+    hows = [sz.Attention(0.1), sz.Attention(0.1, window=1 << 20, positions=torch.arange(T, dtype=torch.int32, device="cuda"))]
+    took = [[], []]
+    for k in range(20):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(5):
+            sz.cache_attention(q, cache, seqs, out, workspace, hows[k % 2])
+        b.record()
+        torch.cuda.synchronize()
+        took[k % 2].append(a.elapsed_time(b))
+    assert min(took[1]) < 2.5 * min(took[0]), took
