@@ -863,7 +863,9 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
   using S = Stage<KIND, D, W>;
   constexpr int KS = S::KS, DV = S::DV, kTokens = S::kTokens, kUnits = S::kUnits;
   __shared__ u32x4 lds[2][W * 4 * 64];
-  __shared__ uint32_t lds_odd;   // words of V were left out
+  // The workgroup's last tile of rows (of the even ones, and of the odd ones) in whose stages words of V were left out.  They are counted from 1:
+  // what a tile finds here is its own, since a place is written again by the second tile after it, two barriers on.
+  __shared__ uint32_t lds_odd[2];
   const uint32_t lane = threadIdx.x % 64, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), m = lane % 16, g = lane / 16;
   Share w;
   if (!w.start(lane)) return;
@@ -877,12 +879,14 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
   const uint8_t* const base = of_k ? c.k + w.head * c.head_stride + (uint64_t)(m % 4) * c.token_stride + 16 * g
                                    : c.v + w.head * c.head_stride + S::ES * (64 * (piece % (D / 64)) + 4 * m);
   const uint32_t group = of_k ? S::k_group(piece, m) : S::v_group(piece, g);   // the lane's eight tokens of a stage
-  if (threadIdx.x == 0) lds_odd = 0;
+  if (threadIdx.x < 2) lds_odd[threadIdx.x] = 0;
   lds_barrier();
+  uint32_t turn = 0;
 
   do {
     if (!w.first_rows()) continue;
     do {
+      ++turn;
       int from, to;
       w.tokens(from, to, kTokens);
       const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
@@ -907,7 +911,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
         if (t0 >= to) return;
         u32x4* to = lds[buf] + 64 * (of_k ? 4 * piece : S::kV + 4 * piece) + lane;
         if (of_k) stage.store_k(to, piece, m);
-        else if (__builtin_expect(stage.store_v(to, !r.see_all(w, t0, kTokens), t0 + (int)group, w.s.len), 0)) lds_odd = 1;
+        else if (__builtin_expect(stage.store_v(to, !r.see_all(w, t0, kTokens), t0 + (int)group, w.s.len), 0)) lds_odd[turn % 2] = turn;
       };
       // the scores of 32 tokens, unit u of a stage
       const auto scores = [&](f32x4 (&x)[NT][2], const u32x4* at) {
@@ -967,7 +971,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
         }
       }
       lds_barrier();   // the next tile of rows writes where these tokens are
-      if (__builtin_expect(lds_odd, 0)) st.add_odd(w, r, from, to, kTokens, [&](int j, int i) { return 64 * (j / 4) + 16 * g + 4 * i + j % 4; });
+      if (__builtin_expect(lds_odd[turn % 2] == turn, 0)) st.add_odd(w, r, from, to, kTokens, [&](int j, int i) { return 64 * (j / 4) + 16 * g + 4 * i + j % 4; });
 
       // lane (m, g) has elements 64 b + 16 g + 4 i + j of row m in acc[4 b + j][i]
       const AttentionArgs a = args_again();

@@ -76,3 +76,36 @@ def test_positions_of_a_prompt_do_not_wait_for_one_another():
         torch.cuda.synchronize()
         took[k % 2].append(a.elapsed_time(b))
     assert min(took[1]) < 2.5 * min(took[0]), took
+
+
+@pytest.mark.gpu
+def test_an_infinity_is_looked_for_in_its_own_rows_alone():
+    """one infinity of V in the first of the sequences that a workgroup takes costs what it does in the last one (seven times that, if
+    the sequences behind it were searched as well), and touches no other sequence"""
+    n, T = 4096, 200
+    cache = sz.KvCache.zeros(n * 25, 8, 1, 64, sz.BF16)
+    table = torch.arange(n * 25, dtype=torch.int32, device="cuda").view(n, 25)
+    starts = torch.arange(n + 1, dtype=torch.int32, device="cuda") * T
+    seqs = sz.Sequences(table, starts, torch.full((n,), T, dtype=torch.int32, device="cuda"), T, T)
+    x = torch.randn(3, n * T, 1, 64, device="cuda").to(torch.bfloat16)
+    sz.cache_write(x[0], x[1], cache, seqs)
+    out, workspace, how = torch.empty_like(x[2]), sz.attention_workspace(cache, seqs, n * T, 1), sz.Attention(0.1)
+    took, outs = [[], []], []
+    for k in range(12):
+        odd = (0, n - 1)[k % 2]
+        was = cache.v[odd * 25, 3, 0, 5].clone()
+        cache.v[odd * 25, 3, 0, 5] = float("inf")
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(5):
+            sz.cache_attention(x[2], cache, seqs, out, workspace, how)
+        b.record()
+        torch.cuda.synchronize()
+        took[k % 2].append(a.elapsed_time(b))
+        outs.append(out.clone())
+        cache.v[odd * 25, 3, 0, 5] = was
+    first, last = outs[-2].view(n, T, 64), outs[-1].view(n, T, 64)
+    assert torch.isposinf(first[0, 3:, 5]).all() and torch.isfinite(first[1:]).all() and torch.isfinite(first[0, :3]).all()
+    assert torch.isposinf(last[-1, 3:, 5]).all() and torch.isfinite(last[:-1]).all()
+    assert torch.equal(first[1:-1], last[1:-1])
+    assert min(took[0]) < 2 * min(took[1]), took
