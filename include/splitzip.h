@@ -545,9 +545,11 @@ typedef struct {
  * lse = ln sum e^x (nullable).  d_q and d_out: n_rows rows of q_heads x head_dim
  * BF16 words (q_heads a multiple of kv_heads; query head h reads head
  * h / (q_heads / kv_heads) of the cache), strides and alignment as above.
- * Statistics and sums are held in 32 bits, the weights are rounded to BF16 in
- * front of the product with V.  A row that sees nothing, or nothing but scores
- * of minus infinity, gets zeros and lse = -infinity.  What a row does not see
+ * Statistics and sums are held in 32 bits.  In the product with V a weight is
+ * 2^-15 of itself off at most where a head of the cache has up to 16 rows
+ * (max_rows times its query heads), and rounded to BF16 (2^-8) where it has
+ * more.  A row that sees nothing, or nothing but scores of minus infinity,
+ * gets zeros and lse = -infinity.  What a row does not see
  * does not touch it, whatever it holds; an infinity or a NaN of V that it sees
  * reaches it.  d_workspace: the parts of long sequences until they are joined,
  * splitzip_attention_workspace_bytes of it, 16-byte aligned, no defined value

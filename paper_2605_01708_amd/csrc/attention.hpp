@@ -18,9 +18,12 @@
 //
 // The running maximum is one that is at most 2^8 short: it is raised (and what was summed rescaled) only when a score would be
 // beyond that, which a wave finds with one comparison and a ballot; weights up to 256 cost nothing in a floating format.  Statistics,
-// outputs and the sums over waves and over the parts of a long sequence are held in 32 bits.  P goes into the second product as
-// BF16, as V does (relative error 2^-8 per token, as that of the BF16 result); its sum is taken before that rounding, since lse is a
-// result in 32 bits.
+// outputs and the sums over waves and over the parts of a long sequence are held in 32 bits.  V goes into the second product as BF16, and so
+// do the weights: up to 16 rows in two parts, which loses nothing that the BF16 result shows (memory's time hides the second product: 64
+// sequences of 700 to 8192 tokens 181.1 us, 180.7 with one part; 131072 tokens of E4M3 57.8 and 56.8); of more rows rounded (2^-8 of a weight, as the
+// result's own rounding; the error of the result against 64 bits is 0.0021 of it in place of 0.0017), since these kernels are bound by their
+// instructions: 16 trees of 64 rows over E5M2 136 us, 161 with two parts, a prompt of 2048 rows 112 and 121.  Their sum is taken before any
+// rounding, since lse is a result in 32 bits.
 //
 // Two kernels: attention_tokens_kernel for up to 16 rows, whose waves take different tokens (memory's speed is all that
 // counts), and attention_rows_kernel, whose waves take different rows of the same tokens, staged in LDS.
@@ -371,6 +374,10 @@ __device__ inline float larger(float x, float y) { return __builtin_amdgcn_fmed3
 __device__ inline f32x4 mfma(const bf16x8& x, const bf16x8& y, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
 __device__ inline bf16x8 as_bf16(const u32x4& x) { return __builtin_bit_cast(bf16x8, x); }
 
+// bytes of a pair of tokens' elements 2 i, 2 i + 1 (BF16) into the pair of element 2 i and that of 2 i + 1
+__device__ inline uint32_t evens(uint32_t t0, uint32_t t1) { return byte_perm(t1, t0, 0x05040100u); }
+__device__ inline uint32_t odds(uint32_t t0, uint32_t t1) { return byte_perm(t1, t0, 0x07060302u); }
+
 // Nothing is fetched ahead across this: on the ways that are rarely taken, registers count, which the usual way needs.
 __device__ inline void one_at_a_time() { asm volatile("" ::: "memory"); }
 
@@ -444,15 +451,27 @@ struct State {
       }
     }
   }
-  // The weights of the lane's eight tokens and their sum; powers of two are the scores times c.
-  __device__ void weigh(float c, const f32x4 (&x)[NT][2], bf16x8 (&p)[NT]) {
+  // The weights of the lane's eight tokens and their sum; powers of two are the scores times c.  N = 1: weights rounded to BF16.  N = 2: each
+  // in two parts of BF16, 2^-15 of it short at most; the first is cut from a little less than the weight, so that both are above 0
+  // where the weight is, and an infinity of V stays one in either product.
+  template <int N>
+  __device__ void weigh(float c, const f32x4 (&x)[NT][2], bf16x8 (&p)[N][NT]) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       float e[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i / 4][i % 4], c, -top[n]));
       sum[n] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-      p[n] = as_bf16(u32x4{bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7])});
+      if constexpr (N == 2) {
+        uint32_t first[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          first[i] = __float_as_uint(e[i] * (1.0f - 0x1p-9f));
+          e[i] -= __uint_as_float(first[i] & 0xffff0000u);
+        }
+        p[1][n] = as_bf16(u32x4{odds(first[0], first[1]), odds(first[2], first[3]), odds(first[4], first[5]), odds(first[6], first[7])});
+      }
+      p[0][n] = as_bf16(u32x4{bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7])});
     }
   }
 
@@ -460,9 +479,12 @@ struct State {
     const float x = sum[n] + __shfl_xor(sum[n], 16);
     return x + __shfl_xor(x, 32);
   }
-  __device__ void add(int j, const bf16x8& v, const bf16x8 (&p)[NT]) {
+  template <int N>
+  __device__ void add(int j, const bf16x8& v, const bf16x8 (&p)[N][NT]) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n][j] = mfma(v, p[n], acc[n][j]);
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) acc[n][j] = mfma(v, p[k][n], acc[n][j]);
   }
   // A token that some row does not see may hold anything, and 0 times an infinity or a NaN is no 0: where there are such tokens, V goes
   // into the product without these words (finite_only), and what rows do see of them is added here, from memory, when the
@@ -500,9 +522,6 @@ struct State {
   }
 };
 
-// bytes of a pair of tokens' elements 2 i, 2 i + 1 (BF16) into the pair of element 2 i and that of 2 i + 1
-__device__ inline uint32_t evens(uint32_t t0, uint32_t t1) { return byte_perm(t1, t0, 0x05040100u); }
-__device__ inline uint32_t odds(uint32_t t0, uint32_t t1) { return byte_perm(t1, t0, 0x07060302u); }
 // halves of a pair of tokens that are among the sequence's
 __device__ inline uint32_t inside(int t, int len) { return (t < len ? 0xffffu : 0u) | (t + 1 < len ? 0xffff0000u : 0u); }
 // zeros for the infinities and NaN of N registers of V (element j of the eight tokens from t8 on in vt[j]); whether a token of the sequence had one
@@ -683,7 +702,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
           if constexpr (!PLAIN) st.shape(w, bias, x, t8);
           if (__builtin_expect(!all, 0)) st.mask(w, r, x, t8);
           st.raise({st.highest(x[0]) * scale});
-          bf16x8 p[1];
+          bf16x8 p[2][1];
           st.weigh(scale, x, p);
           u32x4 vt[DV];   // element j of the eight tokens
   #pragma unroll
@@ -964,7 +983,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
         st.raise(high);
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-          bf16x8 p[NT];
+          bf16x8 p[1][NT];
           st.weigh(scale, x[u], p);
 #pragma unroll
           for (int j = 0; j < DV; ++j) st.add(j, as_bf16(at[64 * (S::kV + u * DV + j)]), p);

@@ -109,3 +109,24 @@ def test_an_infinity_is_looked_for_in_its_own_rows_alone():
     assert torch.isposinf(last[-1, 3:, 5]).all() and torch.isfinite(last[:-1]).all()
     assert torch.equal(first[1:-1], last[1:-1])
     assert min(took[0]) < 2 * min(took[1]), took
+
+
+def exactly(got, got_lse, want, tokens):
+    """as `close`, with weights that are 2^-15 of themselves off at most in place of 2^-8, and sums over so many tokens in 32 bits"""
+    out, lse, mean, dx = want
+    got = got.double().cpu().numpy()
+    bound = 2.0 ** -8 * 1.01 * np.abs(out) + (2.0 ** -15 * 1.01 + 2.5 * dx[..., None] + 2.0 ** -20 + 2.0 ** -23 * tokens[:, None, None]) * mean
+    worst = np.abs(got - out) - bound
+    assert (worst <= 0).all(), (worst.max(), (worst > 0).mean())
+    assert (np.abs(got_lse.double().cpu().numpy() - lse) <= dx + 2.0 ** -20 * (1 + np.abs(lse))).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [sz.BF16, sz.FP8_E5M2, sz.FP8_E4M3])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("group,T", [(1, 1), (4, 4), (16, 1)])
+def test_weights_of_few_rows_keep_their_bits(kind, dim, group, T):
+    """up to 16 rows of a head of the cache: the result's own rounding to BF16 is the only one that shows; whole sequences, and parts"""
+    w = World(kind, [T + 30, T + 61, T + 900], [T] * 3, 1, dim, 16, seed=dim + T, max_len=9000)
+    q, qd = queries(w, group)
+    exactly(*run(w, qd, sz.Attention(0.01)), attend(w, q, 0.01), np.repeat(w.lens, w.rows))
