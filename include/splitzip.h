@@ -514,8 +514,9 @@ typedef struct {
  * v_row_stride words apart (multiples of 8), 16-byte aligned; rows of more than
  * 2^31 bytes: SPLITZIP_ERR_UNSUPPORTED (queries as well).  One launch.
  * splitzip_cache_write fills the rows' tokens and nothing else of the pool;
- * splitzip_cache_read rounds word * 2^(b - 127) to BF16 (infinite from 2^128 on,
- * which no byte that splitzip_cache_write takes for finite rows leads to). */
+ * splitzip_cache_read rounds word * 2^(b - 127) to BF16, infinite from 2^128 on:
+ * of finite rows, magnitudes from 1.875 * 2^127 (E5M2) or 1.9375 * 2^127 (E4M3)
+ * on, which a word is 2^128 for. */
 int splitzip_cache_write(const splitzip_cache* cache, const splitzip_seqs* seqs, const void* d_k, uint64_t k_row_stride,
                          const void* d_v, uint64_t v_row_stride, uint32_t n_rows, void* stream);
 int splitzip_cache_read(const splitzip_cache* cache, const splitzip_seqs* seqs, void* d_k, uint64_t k_row_stride, void* d_v,
@@ -544,8 +545,11 @@ typedef struct {
  * drafted tokens, or a piece of a prompt -- over the cache: out = softmax(x) v,
  * lse = ln sum e^x (nullable).  d_q and d_out: n_rows rows of q_heads x head_dim
  * BF16 words (q_heads a multiple of kv_heads; query head h reads head
- * h / (q_heads / kv_heads) of the cache), strides and alignment as above.
- * Statistics and sums are held in 32 bits.  In the product with V a weight is
+ * h / (q_heads / kv_heads) of the cache), strides and alignment as above.  K and
+ * V are what splitzip_cache_read makes of the words.
+ * Statistics and sums are held in 32 bits; they are divided at the end, and a
+ * weight may be 2^8 until then, so that the tokens of a row with values of V
+ * near 2^120 and above may sum up to an infinity.  In the product with V a weight is
  * 2^-15 of itself off at most where a head of the cache has up to 16 rows
  * (max_rows times its query heads), and rounded to BF16 (2^-8) where it has
  * more.  A row that sees nothing, or nothing but scores of minus infinity,
