@@ -43,7 +43,7 @@ __device__ inline Seq seq_at(const Seqs& q, uint32_t s) {
   Seq r;
   const int a = q.starts[s], b = q.starts[s + 1], n = q.lens[s];
   r.start = min(max(a, 0), (int)q.n_rows);
-  r.rows = max(min(b, (int)q.n_rows) - r.start, 0);
+  r.rows = max(min(b, (int)q.n_rows), r.start) - r.start;   // (the difference is taken last: b may be any number)
   r.len = min(max(n, 0), (int)q.capacity);
   r.base = r.len - r.rows;
   return r;
