@@ -34,6 +34,9 @@ def tree_of(rows: int, branches: int = 3):
 def step(tokens: int = 2000, sequences: int = 4, layers: int = 4, drafts: int = 13, device: str = "cuda"):
     """Runs the step; returns the attention's outputs per layer, the accepted sequences' lengths, the codec's ratio and whether what arrived
     is what was sent."""
+    if sequences < 1 or layers < 1 or not 1 <= drafts <= 64 or tokens <= 37 * (sequences - 1):
+        raise ValueError("a step has a sequence and a layer at least, 1 to 64 drafts (the bits of a word), and more tokens than the 37 by which each "
+                         "prompt is shorter than the one before it")
     i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=device)   # noqa: E731
     gen = torch.Generator(device=device)
     gen.manual_seed(0)
@@ -111,7 +114,10 @@ def main() -> None:
     p.add_argument("--layers", type=int, default=4)
     p.add_argument("--drafts", type=int, default=13)
     a = p.parse_args()
-    outs, lens, ratio, same = step(a.tokens, a.sequences, a.layers, a.drafts)
+    try:
+        outs, lens, ratio, same = step(a.tokens, a.sequences, a.layers, a.drafts)
+    except ValueError as e:
+        p.error(str(e))
     torch.cuda.synchronize()
     print(f"{len(outs)} layers, outputs {tuple(outs[0].shape)}; sequences of {lens} tokens after the accepted path; "
           f"one of them sent at a ratio of {ratio:.3f}, {'as it was' if same else 'CHANGED'}")

@@ -153,3 +153,20 @@ def test_rows_that_offsets_of_32_bits_do_not_span_are_refused(heads, rc):
         assert f(C.byref(c), C.byref(q), None, 64 * heads, None, 64 * heads, 1, None) == rc
     how = _CAttention(1.0, 0.0, None, None, None, 0, 0, 0)
     assert L.splitzip_cache_attention(C.byref(c), C.byref(q), C.byref(how), None, 64 * heads, None, 64 * heads, None, 1, heads, None, 0, None) == rc
+
+
+@pytest.mark.parametrize("args", [dict(drafts=65), dict(drafts=0), dict(tokens=111, sequences=4), dict(sequences=0), dict(layers=0)])
+def test_the_example_says_what_it_takes(args):
+    from paper_2605_01708_amd import tree_decode
+
+    with pytest.raises(ValueError, match="64 drafts"):
+        tree_decode.step(**args)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("args", [dict(tokens=40, sequences=2, layers=1, drafts=64), dict(tokens=1, sequences=1, layers=1, drafts=1)])
+def test_the_example_takes_its_extremes(args):
+    from paper_2605_01708_amd import tree_decode
+
+    outs, lens, ratio, same = tree_decode.step(**args)
+    assert same and all(torch.isfinite(o).all() for o in outs)
