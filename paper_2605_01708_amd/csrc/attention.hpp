@@ -732,35 +732,33 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
         for (int t = w.begin + (int)turn * S::kTokens; t < w.end; t += stride) st.add_odd(w, r, t, min(t + S::kTokens, w.end), (int)kStep, element);
       }
 
-      // the waves of a head together, where there are several; lane (m, g) has elements DV (4 g + i) + j of row m in acc[j][i]
+      // the waves of a head (two or four) together; lane (m, g) has elements DV (4 g + i) + j of row m in acc[j][i]
       float total = st.total(0);
-      if (tw > 1) {
-        if (g == 0) {
-          lds_stat[wave][m][0] = st.top[0];
-          lds_stat[wave][m][1] = total;
-        }
-        f32x4* out = reinterpret_cast<f32x4*>(mine) + lane;
-  #pragma unroll
-        for (int j = 0; j < DV; ++j) out[64 * j] = st.acc[0][j];
-        lds_barrier();
-        if (turn == 0) {
-          float high = st.top[0];
-          for (uint32_t v = 1; v < tw; ++v) high = fmaxf(high, lds_stat[wave + v * hw][m][0]);
-          const float f0 = __builtin_amdgcn_exp2f(st.top[0] - high);
-          st.top[0] = high;
-          total *= f0;
-  #pragma unroll
-          for (int j = 0; j < DV; ++j) st.acc[0][j] *= f0;
-          for (uint32_t v = 1; v < tw; ++v) {
-            const float f = __builtin_amdgcn_exp2f(lds_stat[wave + v * hw][m][0] - high);
-            total += f * lds_stat[wave + v * hw][m][1];
-            const f32x4* from = reinterpret_cast<const f32x4*>(lds_all[wave + v * hw]) + lane;
-  #pragma unroll
-            for (int j = 0; j < DV; ++j) st.acc[0][j] += f * from[64 * j];
-          }
-        }
-        lds_barrier();   // (the next tile of rows writes there)
+      if (g == 0) {
+        lds_stat[wave][m][0] = st.top[0];
+        lds_stat[wave][m][1] = total;
       }
+      f32x4* out = reinterpret_cast<f32x4*>(mine) + lane;
+  #pragma unroll
+      for (int j = 0; j < DV; ++j) out[64 * j] = st.acc[0][j];
+      lds_barrier();
+      if (turn == 0) {
+        float high = st.top[0];
+        for (uint32_t v = 1; v < tw; ++v) high = fmaxf(high, lds_stat[wave + v * hw][m][0]);
+        const float f0 = __builtin_amdgcn_exp2f(st.top[0] - high);
+        st.top[0] = high;
+        total *= f0;
+  #pragma unroll
+        for (int j = 0; j < DV; ++j) st.acc[0][j] *= f0;
+        for (uint32_t v = 1; v < tw; ++v) {
+          const float f = __builtin_amdgcn_exp2f(lds_stat[wave + v * hw][m][0] - high);
+          total += f * lds_stat[wave + v * hw][m][1];
+          const f32x4* from = reinterpret_cast<const f32x4*>(lds_all[wave + v * hw]) + lane;
+  #pragma unroll
+          for (int j = 0; j < DV; ++j) st.acc[0][j] += f * from[64 * j];
+        }
+      }
+      lds_barrier();   // (the next tile of rows writes there)
       const uint32_t at = w.tile * 16 + m;
       if (turn == 0 && at < w.rows) {
         const AttentionArgs a = args_again();
