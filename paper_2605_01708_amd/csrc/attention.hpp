@@ -552,7 +552,7 @@ __device__ inline float one_over(float total) { return total != 0.0f ? 1.0f / to
 //
 // Bound by memory where there is enough to read: 64 sequences of 700 to 8192 tokens, 8 heads of 128 in BF16, 1.17 GB in 180 us (6.5 TB/s; reading
 // alone reaches 7.1).  Short of that by what a launch has before its first and behind its last load (the tables' and lengths' way to the first
-// address 5 us, the join 5 to 7): 131072 tokens of E4M3, 270 MB, in 50 and 7 us.
+// address 5 us, the join 5 to 7): 131072 tokens of E4M3, 270 MB, in 51 and 6 us.
 template <int KIND, int D>
 struct Stream {
   // A stage is 16 KB per wave, two workgroups per CU (32 tokens of 256 BF16 elements: 32 KB, one).
@@ -798,7 +798,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
 // barrier a stage, since who writes a half has passed the barrier behind which nobody reads it.
 //
 // Bound by the matrix instructions' rate with what surrounds them, hardly ever by memory: 16 sequences of 3001 to 8192 E5M2 tokens under 256 rows (64 drafts of four
-// query heads) of 8 heads of 128, 94 GFLOP, in 135 us (0.7 PFLOP/s; a large library product of BF16 reaches 1.2), of which, measured apart, the products and
+// query heads) of 8 heads of 128, 94 GFLOP, in 134 us (0.7 PFLOP/s; a large library product of BF16 reaches 1.2), of which, measured apart, the products and
 // exponentials are 86, loads and their conversion 14, and prologue, parts and waiting the rest; joining takes 16 more.
 template <int KIND, int D, int W>
 struct Stage {
@@ -1035,7 +1035,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
 
 // The parts of a sequence together.  D / 4 threads have a row and query head, four elements each: where the parts are few, as many rows
 // as that leaves room for go through a workgroup at a time, otherwise all its threads take every (1024 / D)-th part of one.  Bound by
-// latency: the blocks' count, the statistics and the parts are asked for one behind the other, 5 to 7 us; 16 us for the 32768 rows of 64 drafts
+// latency: the blocks' count, the statistics and the parts are asked for one behind the other, 4 to 6 us; 15 us for the 32768 rows of 64 drafts
 // of 16 sequences, some 50 MB of parts.  (Up to 48 parts sixteen at a time instead of by all threads: 4 and 52 rows of sequences of 1000 to 2000 tokens 1 us
 // slower; four parts asked for as sixteen: 16 sequences of 4000 tokens under 256 rows 121 us a call, 109 so.  Four waves per SIMD: with a few
 // registers too many for that 17 us where it takes 15.)
