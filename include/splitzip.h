@@ -51,8 +51,9 @@ extern "C" {
 typedef enum {
   SPLITZIP_BF16 = 0,     /* 16-bit words: 1 sign, 8 exponent, 7 mantissa bits */
   SPLITZIP_FP8_E5M2 = 1, /* 8-bit words: 1 sign, 5 exponent, 2 mantissa bits (paper appendix "SplitZip on FP8") */
-  SPLITZIP_FP8_E4M3 = 2  /* 8-bit words: 1 sign, 4 exponent, 3 mantissa bits; accepted by the splitzip_variant_* calls only
+  SPLITZIP_FP8_E4M3 = 2, /* 8-bit words: 1 sign, 4 exponent, 3 mantissa bits; accepted by the splitzip_variant_* calls only
                             (a 4-bit code cannot shrink a 4-bit exponent, same appendix) */
+  SPLITZIP_FP4_E2M1 = 16 /* 4-bit words: 1 sign, 2 exponent, 1 mantissa bits; the splitzip_cache_* calls only */
 } splitzip_dtype;
 
 typedef enum {
@@ -454,9 +455,9 @@ int splitzip_variant_decompress(const void* d_comp, size_t comp_bytes, uint64_t 
 /* ---- A KV cache in pages: writing it, reading it, attention over it ------------------------------
  *
  * What a serving program does with the caches that the calls above pack for
- * the way: new tokens are written into the pages -- rounded to FP8 as they
- * are, if the cache holds FP8 words --, every step attends to what is there,
- * and sequences are read back as BF16.  The words lie as splitzip_paged
+ * the way: new tokens are written into the pages -- rounded to FP8 or to 4
+ * bits as they are, if the cache holds such words --, every step attends to what is there,
+ * and sequences are read back as BF16.  BF16 and FP8 words lie as splitzip_paged
  * describes them, so splitzip_compress_batch_paged and its reverse move such
  * caches as they are (the scales, one byte per token and head, travel beside
  * the streams).
@@ -468,6 +469,14 @@ int splitzip_variant_decompress(const void* d_comp, size_t comp_bytes, uint64_t 
  * even.  Infinities stay infinities in E5M2 and become NaN in E4M3, which has
  * none; they and NaN do not count for b.
  *
+ * A cache of 4-bit words (SPLITZIP_FP4_E2M1: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and
+ * their negatives) has such a byte for every 32 elements of a token and head,
+ * the least b for which their largest magnitude fits 6 * 2^(b - 127).  The
+ * format has neither infinities nor NaN: 32 elements that hold one get the
+ * byte 255, under which all of them are NaN, whatever their words.  These
+ * caches are about a quarter of BF16's size as they are; the codec, which
+ * works on exponent fields, takes no 4-bit words.
+ *
  * Nothing that device memory holds (tables, lengths, starts, paths) leads
  * outside the buffers that the descriptions give; where it is inconsistent
  * the results are undefined.  No call allocates, synchronises or reads device
@@ -475,13 +484,14 @@ int splitzip_variant_decompress(const void* d_comp, size_t comp_bytes, uint64_t 
  * other tables, lengths and starts in the same buffers. */
 
 /* K and V of one layer.  Token t of a page, head h: d_k + page * page_stride_bytes
- * + t * token_stride_bytes + h * head_stride_bytes, head_dim words; V in the
+ * + t * token_stride_bytes + h * head_stride_bytes, head_dim words (two 4-bit
+ * words a byte, the even element in the low half); V in the
  * same way from d_v (pages of both, or K and V side by side in a page). */
 typedef struct {
   void* d_k;            /* 16-byte aligned */
   void* d_v;
   uint8_t* d_k_scales;  /* FP8: byte [page][head][token of the page], pages scale_page_stride_bytes apart, 8-byte aligned; */
-  uint8_t* d_v_scales;  /* BF16: not looked at */
+  uint8_t* d_v_scales;  /* 4-bit words: byte [page][head][head_dim / 32][token of the page]; BF16: not looked at */
   uint32_t dtype;       /* splitzip_dtype of the words */
   uint32_t kv_heads;
   uint32_t head_dim;    /* 64, 128 or 256 (others: SPLITZIP_ERR_UNSUPPORTED) */
@@ -516,7 +526,7 @@ typedef struct {
  * splitzip_cache_write fills the rows' tokens and nothing else of the pool;
  * splitzip_cache_read rounds word * 2^(b - 127) to BF16, infinite from 2^128 on:
  * of finite rows, magnitudes from 1.875 * 2^127 (E5M2) or 1.9375 * 2^127 (E4M3)
- * on, which a word is 2^128 for. */
+ * on, or 1.75 * 2^127 (E2M1), which a word is 2^128 for. */
 int splitzip_cache_write(const splitzip_cache* cache, const splitzip_seqs* seqs, const void* d_k, uint64_t k_row_stride,
                          const void* d_v, uint64_t v_row_stride, uint32_t n_rows, void* stream);
 int splitzip_cache_read(const splitzip_cache* cache, const splitzip_seqs* seqs, void* d_k, uint64_t k_row_stride, void* d_v,

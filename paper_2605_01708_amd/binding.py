@@ -16,7 +16,8 @@ import torch
 
 BF16 = 0
 FP8_E5M2 = 1
-FP8_E4M3 = 2   # accepted by the variant_* calls only
+FP8_E4M3 = 2   # accepted by the variant_* and the cache_* calls only
+FP4_E2M1 = 16  # by the cache_* calls only
 ESC_POS, ESC_SENTINEL, ESC_ABS32 = 0, 1, 2
 
 STATUS_OVERFLOW = 1
@@ -932,7 +933,8 @@ def _ptr(t: torch.Tensor | None):
 
 # what may hold a cache's words and rows, which are computed with: the type itself, or integers for bits
 _WORDS = {BF16: (torch.bfloat16, torch.int16, torch.uint16), FP8_E5M2: (torch.float8_e5m2, torch.uint8, torch.int8),
-          FP8_E4M3: (torch.float8_e4m3fn, torch.uint8, torch.int8)}
+          FP8_E4M3: (torch.float8_e4m3fn, torch.uint8, torch.int8), FP4_E2M1: (torch.float4_e2m1fn_x2, torch.uint8, torch.int8)}
+_GROUP = 32   # 4-bit words that share a scale
 
 
 _INT32, _INT64 = (torch.int32, torch.uint32), (torch.int64, torch.uint64)
@@ -965,7 +967,8 @@ class KvCache:
 
     k, v: device tensors [pages, page_tokens, kv_heads, head_dim] of the dtype's words (bfloat16, float8_e5m2 or float8_e4m3fn, or
     integers of that size), of the same strides, head_dim contiguous: views into a pool will do.  k_scales, v_scales (FP8): uint8 [pages, kv_heads, page_tokens]
-    with contiguous pages."""
+    with contiguous pages.  FP4_E2M1: bytes of two words, the even element in the low half, [pages, page_tokens, kv_heads, head_dim / 2]
+    (float4_e2m1fn_x2 or 8-bit integers), and scales uint8 [pages, kv_heads, head_dim / 32, page_tokens]."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, dtype: int, k_scales: torch.Tensor | None = None,
                  v_scales: torch.Tensor | None = None):
@@ -975,14 +978,21 @@ class KvCache:
         if dtype not in _WORDS or k.dtype not in _WORDS[dtype] or v.dtype not in _WORDS[dtype]:
             raise ValueError("k and v must hold words of the dtype, as they are or as integers of their size")
         pages, tokens, heads, dim = k.shape
+        scale_shape = (pages, heads, tokens)
+        if dtype == FP4_E2M1:
+            dim *= 2
+            scale_shape = (pages, heads, dim // _GROUP, tokens)
+        inner = [1]   # strides of a page's scales
+        for n in scale_shape[:1:-1]:
+            inner.insert(0, inner[0] * n)
         scale_stride = 0
         if dtype != BF16:
             if k_scales is None or v_scales is None:
-                raise ValueError("an FP8 cache has scales")
+                raise ValueError("an FP8 cache has scales" if dtype != FP4_E2M1 else "a cache of 4-bit words has scales")
             for s in (k_scales, v_scales):
-                if (tuple(s.shape) != (pages, heads, tokens) or s.dtype not in _SCALES or _strides(s)[1:] != (tokens, 1)
+                if (tuple(s.shape) != scale_shape or s.dtype not in _SCALES or _strides(s)[1:] != tuple(inner)
                         or _strides(s)[0] != _strides(k_scales)[0]):
-                    raise ValueError("scales must be bytes [pages, kv_heads, page_tokens] with contiguous pages")
+                    raise ValueError(f"scales must be bytes [pages, kv_heads, {'' if dtype != FP4_E2M1 else 'head_dim / 32, '}page_tokens] with contiguous pages")
             scale_stride = _strides(k_scales)[0]
         self.dtype, self.kv_heads, self.head_dim = dtype, heads, dim
         self._keep = (k, v, k_scales, v_scales)
@@ -993,8 +1003,9 @@ class KvCache:
     @classmethod
     def zeros(cls, pages: int, page_tokens: int, kv_heads: int, head_dim: int, dtype: int, device="cuda") -> "KvCache":
         """A cache of its own memory, zeros."""
-        kv = [torch.zeros((pages, page_tokens, kv_heads, head_dim), dtype=torch.bfloat16 if dtype == BF16 else torch.uint8, device=device) for _ in range(2)]
-        scales = [None if dtype == BF16 else torch.zeros((pages, kv_heads, page_tokens), dtype=torch.uint8, device=device) for _ in range(2)]
+        row, groups = (head_dim // 2, (head_dim // _GROUP,)) if dtype == FP4_E2M1 else (head_dim, ())
+        kv = [torch.zeros((pages, page_tokens, kv_heads, row), dtype=torch.bfloat16 if dtype == BF16 else torch.uint8, device=device) for _ in range(2)]
+        scales = [None if dtype == BF16 else torch.zeros((pages, kv_heads, *groups, page_tokens), dtype=torch.uint8, device=device) for _ in range(2)]
         return cls(*kv, dtype, *scales)
 
     @property
@@ -1085,7 +1096,7 @@ def _write_or_read(name, cache: KvCache, seqs: Sequences, k: torch.Tensor, v: to
 
 
 def cache_write(k: torch.Tensor, v: torch.Tensor, cache: KvCache, seqs: Sequences, stream=None) -> None:
-    """splitzip_cache_write: the BF16 rows k, v [rows, kv_heads, head_dim] become their sequences' last tokens, quantised if the cache is FP8."""
+    """splitzip_cache_write: the BF16 rows k, v [rows, kv_heads, head_dim] become their sequences' last tokens, quantised if the cache is not BF16."""
     rc = (_lib or lib()).fast_cache.splitzip_cache_write(cache.c, seqs.c, k, v, None if stream is None else _handle(stream))
     if rc != _NOT_TAKEN:
         return _check(rc, "splitzip_cache_write") if rc else None

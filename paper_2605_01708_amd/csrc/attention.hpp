@@ -13,8 +13,8 @@
 // the first product in the layout in which the second takes them: lane group g = l / 16 has tokens 4 g .. 4 g + 3 of a
 // 16-token tile, and with the tile's row m standing for token 8 (m / 4) + m % 4 of the 32 (and + 4 in the second
 // tile) these are tokens 8 g .. 8 g + 7, the lane's eight elements of the second product's K dimension.  No score moves between lanes.
-// K is loaded as rows, V as eight tokens times a few elements per lane, transposed in registers by byte permutes.  FP8 words become BF16
-// on the way, their scale with them.
+// K is loaded as rows, V as eight tokens times a few elements per lane, transposed in registers by byte permutes.  FP8 and 4-bit words become BF16
+// on the way, their scale with them: 16 bytes of a row of 4-bit words are 32 elements, which share one.
 //
 // The running maximum is one that is at most 2^8 short: it is raised (and what was summed rescaled) only when a score would be
 // beyond that, which a wave finds with one comparison and a ballot; weights up to 256 cost nothing in a floating format.  Statistics,
@@ -281,8 +281,9 @@ struct Rows {
       const uint8_t* at = a.q + (uint64_t)(uint32_t)(w.s.start + max(row[n], 0)) * a.q_stride + 2 * (uint64_t)h * D;
 #pragma unroll
       for (int t = 0; t < D / 32; ++t) {
-        // FP8 rows are loaded 16 bytes, two steps, at a time: the same order here
-        const uint32_t d = KIND == SPLITZIP_BF16 ? 32 * t + 8 * g : 64 * (t / 2) + 16 * g + 8 * (t % 2);
+        // rows are loaded 16 bytes at a time (32 bytes of 4-bit words 8): one step of BF16, two of FP8, four of 4-bit words.  The same order here.
+        constexpr int kSteps = KIND == SPLITZIP_BF16 ? 1 : KIND == SPLITZIP_FP4_E2M1 && D > 64 ? 4 : 2;
+        const uint32_t d = 32 * kSteps * (t / kSteps) + 8 * kSteps * g + 8 * (t % kSteps);
         u32x4 x = {0, 0, 0, 0};
         if (have) x = *reinterpret_cast<const u32x4*>(at + 2 * d) ^ a.flip_q;
         q[n][t] = __builtin_bit_cast(bf16x8, x);
@@ -500,8 +501,9 @@ struct State {
       for (int t = t0; t < min(t0 + step, min(end, w.s.len)); ++t) {
         const uint32_t page = pages.page((uint32_t)t), place = pages.place((uint32_t)t);
         const uint8_t* at = a.cache.v + token_offset(a.cache, page, place) + w.head * a.cache.head_stride;
+        const auto scale = [&](uint32_t group) { return (uint32_t)a.cache.v_scales[scale_offset(a.cache, page, place, w.head * kGroups<KIND, D> + group)]; };
         uint32_t byte = 0;
-        if constexpr (KIND != SPLITZIP_BF16) byte = a.cache.v_scales[scale_offset(a.cache, page, place, w.head)];
+        if constexpr (kBits<KIND> == 8) byte = scale(0);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const bool mine = r.seen(w, n, t & ~7) >> (t & 7) & 1;
@@ -510,8 +512,10 @@ struct State {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               uint32_t v;
-              if constexpr (KIND == SPLITZIP_BF16) v = reinterpret_cast<const uint16_t*>(at)[element(j, i)];
-              else v = fp8_pair_to_bf16<KIND, false>(at[element(j, i)], byte) & 0xffffu;
+              const uint32_t e = (uint32_t)element(j, i);
+              if constexpr (KIND == SPLITZIP_BF16) v = reinterpret_cast<const uint16_t*>(at)[e];
+              else if constexpr (KIND == SPLITZIP_FP4_E2M1) v = fp4_pair_to_bf16(at[e / 2], scale(e / kGroup4), 0) >> (16 * (e % 2)) & 0xffffu;
+              else v = fp8_pair_to_bf16<KIND, false>(at[e], byte) & 0xffffu;
               acc[n][j][i] += mine && (v & 0x7f80u) == 0x7f80u ? __uint_as_float(v << 16) : 0.0f;
             }
             one_at_a_time();
@@ -553,29 +557,39 @@ __device__ inline float one_over(float total) { return total != 0.0f ? 1.0f / to
 // Bound by memory where there is enough to read: 64 sequences of 700 to 8192 tokens, 8 heads of 128 in BF16, 1.17 GB in 180 us (6.5 TB/s; reading
 // alone reaches 7.1).  Short of that by what a launch has before its first and behind its last load (the tables' and lengths' way to the first
 // address 5 us, the join 5 to 7): 131072 tokens of E4M3, 270 MB, in 51 and 6 us.
+constexpr uint32_t stage_tokens(uint32_t dtype, uint32_t row_bytes) {
+  return 8192 / row_bytes < 32 ? 32 : dtype == SPLITZIP_FP4_E2M1 ? 64 : 8192 / row_bytes;
+}
 template <int KIND, int D>
 struct Stream {
-  // A stage is 16 KB per wave, two workgroups per CU (32 tokens of 256 BF16 elements: 32 KB, one).
-  static constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
-  static constexpr int kRow = D * ES;                                    // bytes of a token
-  static constexpr int kTokens = 16384 / (2 * kRow) < 32 ? 32 : 16384 / (2 * kRow);   // of a stage
+  // A stage is 16 KB per wave, two workgroups per CU (32 tokens of 256 BF16 elements: 32 KB, one), of 4-bit words 64 tokens.
+  static constexpr int kRow = D * kBits<KIND> / 8;                       // bytes of a token
+  static constexpr int kTokens = (int)stage_tokens(KIND, kRow);                // of a stage
   static constexpr int kHalf = kTokens * kRow;                           // bytes of K, or V, of a stage
   static constexpr int kSteps = kTokens / (int)kStep;
   static constexpr int kUnits = kRow / 16;                               // 16-byte units of a row
   static constexpr int KS = D / 32, DV = D / 16;
-  static constexpr int KW = KS * ES / 2;                                 // units of a row of K per lane
-  static constexpr int VB = DV * ES;                                     // bytes of a token of V per lane
-  static constexpr int VW = VB / 4;
+  static constexpr int KB = kRow / 4 < 16 ? kRow / 4 : 16;               // bytes of a row of K that a lane takes at a time, and how often
+  static constexpr int KW = kRow / 4 / KB;
+  static constexpr int VB = kRow / 16;                                   // bytes of a token of V per lane
+  static constexpr int VW = (VB + 3) / 4;
+  typedef typename std::conditional<KB == 16, u32x4, u32x2>::type KPart;
+  // scales of a token of K per lane: the lane's bytes of a row are of KG groups (FP8: the row's one), and which group they are of
+  static constexpr int KG = KIND == SPLITZIP_FP4_E2M1 ? KW : 1;
+  __device__ static uint32_t k_group(int i, uint32_t g) { return KIND == SPLITZIP_FP4_E2M1 ? (KB == 16 ? 4 * i + g : g / 2) : 0; }
+  __device__ static uint32_t v_group(uint32_t m) { return KIND == SPLITZIP_FP4_E2M1 ? m * DV / kGroup4 : 0; }
 
   // Rows of K lie in the order of the tokens, their units permuted so that the 16 rows of an operand (of the tile's row m: token
-  // 8 (m / 4) + m % 4, the other tile's 4 further) lie in 16 different units of the banks.
+  // 8 (m / 4) + m % 4, the other tile's 4 further) lie in 16 different units of the banks.  Rows of 32 bytes: eight of them are all banks, so
+  // that those of the second and fourth eight change places four by four.
   __device__ static uint32_t k_key(uint32_t token) {
     const uint32_t mi = token / 8 % 4 * 4 + token % 4;
     return kUnits >= 16 ? mi : mi / (16 / kUnits);
   }
-  // Rows of V: those of the second and fourth eight in pairs the other way round where four of them (one of each eight) are read at a time
-  // and a row is half of the banks.
-  __device__ static uint32_t v_row(uint32_t token) { return kUnits == 8 ? token ^ (token / 8 & 1) : token; }
+  __device__ static uint32_t k_row(uint32_t token) { return kUnits == 2 ? token ^ (token / 8 & 1) * 4 : token; }
+  // Rows of V, four of which (one of each eight) are read at a time: those of the second and fourth eight in pairs the other way round where a row
+  // is half of the banks, of each eight in another order where it is a quarter or less.
+  __device__ static uint32_t v_row(uint32_t token) { return kUnits == 8 ? token ^ (token / 8 & 1) : KIND == SPLITZIP_FP4_E2M1 ? token ^ (token / 8 & 3) : token; }
 
   // asks for the stage from token t0 on; pages: lane l has the page of its 8 l-th token
   __device__ static void ask(const Cache& c, const Pages& at_pages, const uint8_t* k_base, const uint8_t* v_base, uint32_t pages, int t0,
@@ -589,7 +603,7 @@ struct Stream {
       if constexpr (kUnits >= 8) page = (uint32_t)__builtin_amdgcn_readlane((int)pages, i * 64 / kUnits / 8);
       else page = (uint32_t)__shfl((int)pages, (int)(row / 8));
       const uint64_t from = token_offset(c, page, at_pages.place(min((uint32_t)t0 + 8 * eight, last8)));
-      const uint32_t k_off = row % 8 * c.token_stride + (at ^ k_key(row)) * 16;
+      const uint32_t k_off = k_row(row) % 8 * c.token_stride + (at ^ k_key(k_row(row))) * 16;
       const uint32_t v_off = v_row(row) % 8 * c.token_stride + at * 16;
       load_to_lds(k_base + from + k_off, lds + i * 1024);
       load_to_lds(v_base + from + v_off, lds + kHalf + i * 1024);
@@ -600,7 +614,8 @@ struct Stream {
 template <int KIND, int D, bool PLAIN>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Stream<KIND, D>::kHalf > 8192 ? 1 : 2))) attention_tokens_kernel(AttentionArgs args) {
   using S = Stream<KIND, D>;
-  constexpr int ES = S::ES, KS = S::KS, DV = S::DV, KW = S::KW, VW = S::VW;
+  constexpr int KS = S::KS, DV = S::DV, KW = S::KW, VW = S::VW, KG = S::KG;
+  typedef typename S::KPart KPart;
   __shared__ __attribute__((aligned(1024))) uint8_t lds_all[kWaves][2 * S::kHalf];
   __shared__ float lds_stat[kWaves][16][2];
   const uint32_t lane = threadIdx.x % 64, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), m = lane % 16, g = lane / 16;
@@ -620,15 +635,17 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
       const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
       const Pages at_pages(c, args.seqs, w.seq);
       const auto ask_pages = [&](int t0) { return at_pages.entry(min((uint32_t)t0 + 8 * (lane % (S::kTokens / 8)), last8)); };
-      u32x2 k_scales[S::kSteps], v_scales[S::kSteps];
+      u32x2 k_scales[S::kSteps][KG], v_scales[S::kSteps];
       const auto ask_scales = [&](uint32_t pages, int t0) {
-        if constexpr (ES == 1) {
+        if constexpr (KIND != SPLITZIP_BF16) {
   #pragma unroll
           for (int u = 0; u < S::kSteps; ++u) {
             const uint32_t k4 = 4 * u + m / 4, v4 = 4 * u + g;
             const uint32_t k_place = at_pages.place(min((uint32_t)t0 + 8 * k4, last8)), v_place = at_pages.place(min((uint32_t)t0 + 8 * v4, last8));
-            k_scales[u] = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, (uint32_t)__shfl((int)pages, (int)k4), k_place, w.head));
-            v_scales[u] = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, (uint32_t)__shfl((int)pages, (int)v4), v_place, w.head));
+            const uint32_t k_page = (uint32_t)__shfl((int)pages, (int)k4), v_page = (uint32_t)__shfl((int)pages, (int)v4), row = w.head * kGroups<KIND, D>;
+  #pragma unroll
+            for (int i = 0; i < KG; ++i) k_scales[u][i] = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, k_page, k_place, row + S::k_group(i, g)));
+            v_scales[u] = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, v_page, v_place, row + S::v_group(m)));
           }
         }
       };
@@ -651,7 +668,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
   #pragma unroll 1
       for (; t0 < w.end; t0 += stride) {
         memory_arrived();
-        u32x4 k[S::kSteps][2][KW];
+        KPart k[S::kSteps][2][KW];
         uint32_t v[S::kSteps][8][VW];
   #pragma unroll
         for (int u = 0; u < S::kSteps; ++u) {
@@ -660,16 +677,20 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
   #pragma unroll
             for (int i = 0; i < KW; ++i) {
               const uint32_t token = 32 * u + 8 * (m / 4) + 4 * b + m % 4;
-              k[u][b][i] = *reinterpret_cast<const u32x4*>(mine + token * S::kRow + ((4 * i + g) ^ S::k_key(token)) * 16);
+              const uint32_t unit = S::KB == 16 ? 4 * i + g : g / 2, half = S::KB == 16 ? 0 : g % 2 * 8;
+              k[u][b][i] = *reinterpret_cast<const KPart*>(mine + S::k_row(token) * S::kRow + (unit ^ S::k_key(token)) * 16 + half);
             }
   #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            __builtin_memcpy(v[u][e], __builtin_assume_aligned(mine + S::kHalf + S::v_row(32 * u + 8 * g + e) * S::kRow + S::VB * m, S::VB < 16 ? S::VB : 16), S::VB);
+          for (int e = 0; e < 8; ++e) {
+            if constexpr (S::VB < 4) v[u][e][0] = *reinterpret_cast<const uint16_t*>(mine + S::kHalf + S::v_row(32 * u + 8 * g + e) * S::kRow + S::VB * m);
+            else __builtin_memcpy(v[u][e], __builtin_assume_aligned(mine + S::kHalf + S::v_row(32 * u + 8 * g + e) * S::kRow + S::VB * m, S::VB < 16 ? S::VB : 16), S::VB);
+          }
         }
-        u32x2 ks[S::kSteps], vs[S::kSteps];
+        u32x2 ks[S::kSteps][KG], vs[S::kSteps];
   #pragma unroll
         for (int u = 0; u < S::kSteps; ++u) {
-          ks[u] = k_scales[u];
+  #pragma unroll
+          for (int i = 0; i < KG; ++i) ks[u][i] = k_scales[u][i];
           vs[u] = v_scales[u];
         }
         lds_read();   // into registers: the place is free
@@ -689,11 +710,14 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
             x[0][b] = f32x4{0, 0, 0, 0};
   #pragma unroll
             for (int t = 0; t < KS; ++t) {
-              if constexpr (ES == 2) {
+              if constexpr (kBits<KIND> == 16) {
                 x[0][b] = mfma(as_bf16(k[u][b][t]), r.q[0][t], x[0][b]);
-              } else {
+              } else if constexpr (kBits<KIND> == 8) {
                 const u32x2 words = {k[u][b][t / 2][t % 2 * 2], k[u][b][t / 2][t % 2 * 2 + 1]};
-                x[0][b] = mfma(as_bf16(from_fp8<KIND>(words, ks[u][b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
+                x[0][b] = mfma(as_bf16(from_fp8<KIND>(words, ks[u][0][b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
+              } else {
+                constexpr int kEach = S::KB / 4;   // steps of a part
+                x[0][b] = mfma(as_bf16(from_fp4(k[u][b][t / kEach][t % kEach], ks[u][t / kEach][b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
               }
             }
           }
@@ -710,11 +734,14 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
   #pragma unroll
             for (int j = 0; j < DV; j += 2) {
               uint32_t w0, w1;
-              if constexpr (ES == 2) {
+              const uint32_t b0 = vs[u][i / 2] >> (16 * (i % 2)) & 0xffu, b1 = vs[u][i / 2] >> (16 * (i % 2) + 8) & 0xffu;
+              if constexpr (kBits<KIND> == 16) {
                 w0 = v[u][2 * i][j / 2];
                 w1 = v[u][2 * i + 1][j / 2];
+              } else if constexpr (kBits<KIND> == 4) {
+                w0 = fp4_pair_to_bf16(v[u][2 * i][j / 8], b0, j % 8 / 2);
+                w1 = fp4_pair_to_bf16(v[u][2 * i + 1][j / 8], b1, j % 8 / 2);
               } else {
-                const uint32_t b0 = vs[u][i / 2] >> (16 * (i % 2)) & 0xffu, b1 = vs[u][i / 2] >> (16 * (i % 2) + 8) & 0xffu;
                 w0 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[u][2 * i][j / 4], b0) : fp8_pair_to_bf16<KIND, false>(v[u][2 * i][j / 4], b0);
                 w1 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[u][2 * i + 1][j / 4], b1) : fp8_pair_to_bf16<KIND, false>(v[u][2 * i + 1][j / 4], b1);
               }
@@ -802,46 +829,62 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
 // exponentials are 86, loads and their conversion 14, and prologue, parts and waiting the rest; joining takes 16 more.
 template <int KIND, int D, int W>
 struct Stage {
-  static constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
+  static constexpr int kB = kBits<KIND>;
   static constexpr int KS = D / 32, DV = D / 16;
   static constexpr int kTokens = W * 1024 / D, kUnits = kTokens / (int)kStep;
   static constexpr int kV = 2 * W;   // operands of K, and of V behind them
   static_assert(kTokens >= (int)kStep, "a stage has 32 tokens at least");
-  uint32_t w[8 * ES];   // K: 16-byte runs of rows, operands 4 s .. 4 s + 3 (two of them in 16 bytes of FP8); V: four elements of eight tokens
+  uint32_t w[kB == 16 ? 16 : 8];   // K: 16-byte runs of rows, operands 4 s .. 4 s + 3 (two of them in 16 bytes of FP8, all in those of 4-bit words); V: four elements of eight tokens
   u32x2 scales;
 
   // piece s of K: operand f = 4 s + i is step f % KS of the tile f / KS of 16 tokens
   __device__ static uint32_t k_group(uint32_t s, uint32_t m) { return 4 * s / KS / 2 * 32 + 8 * (m / 4); }
-  // (base: of the head, the lane's token of eight and its 16 bytes)
-  __device__ void load_k(const Cache& c, const uint8_t* base, uint32_t page, uint32_t place, uint32_t head, uint32_t s) {
+  // byte of a lane's part in a row, and its scale: rows of 64 4-bit words have 8 bytes for each of the lanes' four groups
+  __device__ static uint32_t k_bytes(uint32_t g) { return kB == 4 && D == 64 ? 8 * g : 16 * g; }
+  __device__ static uint32_t k_scale(uint32_t s, uint32_t g) { return kB != 4 ? 0 : D == 64 ? g / 2 : 4 * s % KS + g; }
+  __device__ static uint32_t v_bytes(uint32_t s, uint32_t m) { return kB * (64 * (s % (D / 64)) + 4 * m) / 8; }
+  __device__ static uint32_t v_scale(uint32_t s, uint32_t m) { return kB != 4 ? 0 : (64 * (s % (D / 64)) + 4 * m) / kGroup4; }
+  // (base: of the head, the lane's token of eight and its 16 bytes; row: of its scale)
+  __device__ void load_k(const Cache& c, const uint8_t* base, uint32_t page, uint32_t place, uint32_t row, uint32_t s) {
     const uint8_t* at = base + token_offset(c, page, place);
+    if constexpr (kB == 4 && D == 64) {   // two steps of a tile are 8 bytes
 #pragma unroll
-    for (int i = 0; i < 2 * ES; ++i) {
-      const uint32_t f = 4 * s + (ES == 2 ? i : 2 * i);
-      const u32x4 x = *reinterpret_cast<const u32x4*>(at + (uint64_t)(f / KS % 2 * 4) * c.token_stride + (ES == 2 ? f % KS : f % KS / 2) * 64);
+      for (int i = 0; i < 2; ++i) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(at + (uint64_t)(i * 4) * c.token_stride);
+        w[2 * i] = x[0];
+        w[2 * i + 1] = x[1];
+      }
+    } else {
+      constexpr int kEach = 16 / kB;   // operands of 16 bytes
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
+      for (int i = 0; i < 4 / kEach; ++i) {
+        const uint32_t f = 4 * s + kEach * i;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(at + (uint64_t)(f / KS % 2 * 4) * c.token_stride + f % KS / kEach * 64);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
+      }
     }
-    if constexpr (ES == 1) scales = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, page, place, head));
+    if constexpr (kB != 16) scales = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, page, place, row));
   }
   __device__ void store_k(u32x4* to, uint32_t s, uint32_t m) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if constexpr (ES == 2) {
-        to[64 * i] = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
-      } else {
-        const uint32_t pair = (4 * s + i) / KS % 2 ? scales[1] : scales[0];
-        to[64 * i] = from_fp8<KIND>(u32x2{w[2 * i], w[2 * i + 1]}, pair >> (8 * (m % 4)) & 0xffu);
-      }
+      const uint32_t pair = (4 * s + i) / KS % 2 ? scales[1] : scales[0], byte = pair >> (8 * (m % 4)) & 0xffu;
+      if constexpr (kB == 16) to[64 * i] = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+      else if constexpr (kB == 8) to[64 * i] = from_fp8<KIND>(u32x2{w[2 * i], w[2 * i + 1]}, byte);
+      else to[64 * i] = from_fp4(w[i], byte);
     }
   }
   // piece s of V: 64 elements (block s % (D / 64)) of 32 tokens; a lane has elements 4 m .. 4 m + 3 of them of tokens 8 g ..
   __device__ static uint32_t v_group(uint32_t s, uint32_t g) { return s / (D / 64) * 32 + 8 * g; }
-  __device__ void load_v(const Cache& c, const uint8_t* base, uint32_t page, uint32_t place, uint32_t head) {
+  __device__ void load_v(const Cache& c, const uint8_t* base, uint32_t page, uint32_t place, uint32_t row) {
     const uint8_t* at = base + token_offset(c, page, place);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) __builtin_memcpy(w + ES * e, __builtin_assume_aligned(at + (uint64_t)e * c.token_stride, 4 * ES), 4 * ES);
-    if constexpr (ES == 1) scales = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, page, place, head));
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (kB == 4) w[e] = *reinterpret_cast<const uint16_t*>(at + (uint64_t)e * c.token_stride);
+      else __builtin_memcpy(w + kB / 8 * e, __builtin_assume_aligned(at + (uint64_t)e * c.token_stride, kB / 2), kB / 2);
+    }
+    if constexpr (kB != 16) scales = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, page, place, row));
   }
   // guarded: without infinities and NaN; true if there were some
   __device__ bool store_v(u32x4* to, bool guarded, int t8, int len) const {
@@ -849,13 +892,19 @@ struct Stage {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t x0[2], x1[2];
-      if constexpr (ES == 2) {
+      const uint32_t b0 = scales[i / 2] >> (16 * (i % 2)) & 0xffu, b1 = scales[i / 2] >> (16 * (i % 2) + 8) & 0xffu;
+      if constexpr (kB == 16) {
         x0[0] = w[4 * i];
         x0[1] = w[4 * i + 1];
         x1[0] = w[4 * i + 2];
         x1[1] = w[4 * i + 3];
+      } else if constexpr (kB == 4) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          x0[j] = fp4_pair_to_bf16(w[2 * i], b0, j);
+          x1[j] = fp4_pair_to_bf16(w[2 * i + 1], b1, j);
+        }
       } else {
-        const uint32_t b0 = scales[i / 2] >> (16 * (i % 2)) & 0xffu, b1 = scales[i / 2] >> (16 * (i % 2) + 8) & 0xffu;
         x0[0] = fp8_pair_to_bf16<KIND, false>(w[2 * i], b0);
         x0[1] = fp8_pair_to_bf16<KIND, true>(w[2 * i], b0);
         x1[0] = fp8_pair_to_bf16<KIND, false>(w[2 * i + 1], b1);
@@ -893,8 +942,9 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
   if (W == 8 && wave >= 4) __builtin_amdgcn_s_setprio(1);
   const bool of_k = wave < W / 2;
   const uint32_t piece = wave % (W / 2);
-  const uint8_t* const base = of_k ? c.k + w.head * c.head_stride + (uint64_t)(m % 4) * c.token_stride + 16 * g
-                                   : c.v + w.head * c.head_stride + S::ES * (64 * (piece % (D / 64)) + 4 * m);
+  const uint8_t* const base = of_k ? c.k + w.head * c.head_stride + (uint64_t)(m % 4) * c.token_stride + S::k_bytes(g)
+                                   : c.v + w.head * c.head_stride + S::v_bytes(piece, m);
+  const uint32_t scale_row = w.head * kGroups<KIND, D> + (of_k ? S::k_scale(piece, g) : S::v_scale(piece, m));
   const uint32_t group = of_k ? S::k_group(piece, m) : S::v_group(piece, g);   // the lane's eight tokens of a stage
   if (threadIdx.x < 2) lds_odd[threadIdx.x] = 0;
   lds_barrier();
@@ -921,8 +971,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W =
         if (t0 >= to) return;
         const uint32_t place = at_pages.place(min((uint32_t)t0 + group, last8));
         const uint32_t in_pool = at_pages.clamped(page);
-        if (of_k) stage.load_k(c, base, in_pool, place, w.head, piece);
-        else stage.load_v(c, base, in_pool, place, w.head);
+        if (of_k) stage.load_k(c, base, in_pool, place, scale_row, piece);
+        else stage.load_v(c, base, in_pool, place, scale_row);
       };
       const auto store = [&](int t0, int buf) {
         if (t0 >= to) return;

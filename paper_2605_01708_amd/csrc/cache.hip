@@ -41,17 +41,19 @@ constexpr uint64_t kMostRow = 1ull << 31;     // bytes of a row of the call's te
 constexpr uint32_t kMostSeqs = 65535;        // a dimension of a grid
 constexpr uint64_t kStreamed = 96ull << 20;   // bytes that a call moves (figures at the kernels)
 
-int words_bytes(uint32_t dtype) { return dtype == SPLITZIP_BF16 ? 2 : 1; }
+uint32_t word_bits(uint32_t dtype) { return dtype == SPLITZIP_BF16 ? 16 : dtype == SPLITZIP_FP4_E2M1 ? 4 : 8; }
+uint32_t row_bytes(const splitzip_cache* c) { return c->head_dim * word_bits(c->dtype) / 8; }   // of a token and head
+uint32_t scales_of(const splitzip_cache* c) { return c->dtype == SPLITZIP_BF16 ? 0 : c->dtype == SPLITZIP_FP4_E2M1 ? c->head_dim / kGroup4 : 1; }
 
 // a geometry's rules; the addresses of the words are looked at where a call has them
 int check_cache(const splitzip_cache* c, bool pointers) {
-  if (!c || c->dtype > SPLITZIP_FP8_E4M3 || c->reserved) return SPLITZIP_ERR_INVALID_ARG;
+  if (!c || (c->dtype > SPLITZIP_FP8_E4M3 && c->dtype != SPLITZIP_FP4_E2M1) || c->reserved) return SPLITZIP_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return SPLITZIP_ERR_UNSUPPORTED;
   if (!c->kv_heads || !c->n_pages || c->page_tokens < 8 || c->page_tokens > kMostTokens) return SPLITZIP_ERR_INVALID_ARG;
   if (!aligned16(c->page_stride_bytes) || !aligned16(c->token_stride_bytes) || !aligned16(c->head_stride_bytes)) return SPLITZIP_ERR_INVALID_ARG;
   // eight tokens are a 32-bit offset, and so is a page
   if (c->token_stride_bytes > (1ull << 28) || c->page_stride_bytes >> 32 || c->scale_page_stride_bytes >> 32) return SPLITZIP_ERR_UNSUPPORTED;
-  const uint64_t row = (uint64_t)c->head_dim * words_bytes(c->dtype);
+  const uint64_t row = row_bytes(c);
   if (c->token_stride_bytes < row || c->head_stride_bytes < row) return SPLITZIP_ERR_INVALID_ARG;
   if (c->dtype != SPLITZIP_BF16 && (c->scale_page_stride_bytes & 7u || c->page_tokens & 7u)) return SPLITZIP_ERR_INVALID_ARG;
   if (!pointers) return SPLITZIP_OK;
@@ -118,6 +120,7 @@ int by_kind(const splitzip_cache* c, A... args) {
   SPLITZIP_KIND(SPLITZIP_BF16)
   SPLITZIP_KIND(SPLITZIP_FP8_E5M2)
   SPLITZIP_KIND(SPLITZIP_FP8_E4M3)
+  SPLITZIP_KIND(SPLITZIP_FP4_E2M1)
 #undef SPLITZIP_KIND
   return SPLITZIP_ERR_INVALID_ARG;
 }
@@ -159,7 +162,7 @@ int rows_call(const splitzip_cache* c, const splitzip_seqs* q, void* d_k, uint64
   uint64_t wgs = (pairs + per - 1) / per;
   const uint64_t most = (uint64_t)cu_count() * 32;
   if (wgs > most) wgs = most;
-  const uint64_t bytes = 2 * n_rows * elems * (2 + words_bytes(c->dtype));
+  const uint64_t bytes = 2 * n_rows * elems * (16 + word_bits(c->dtype)) / 8;
   return by_kind<F>(c, dim3((unsigned)wgs, q->n_seqs), bytes >= kStreamed, static_cast<hipStream_t>(stream), (const RowsArgs*)&a);
 }
 
@@ -201,8 +204,8 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
   const uint64_t groups = (uint64_t)(c->kv_heads / p.heads_across) * p.row_tiles, slots = (uint64_t)cu_count() * (one_per_cu ? 1 : p.waves ? 3 : 2);
   uint64_t shares = (slots + groups - 1) / groups;
   // a block: what the waves of a head stage at a time
-  const uint32_t staged = p.waves ? p.waves * 1024u / c->head_dim : 8192u / (c->head_dim * words_bytes(c->dtype));
-  p.block_tokens = p.waves ? staged : (staged < 32 ? 32 : staged) * (kWaves / p.heads_across);
+  const uint32_t staged = p.waves ? p.waves * 1024u / c->head_dim : stage_tokens(c->dtype, row_bytes(c));
+  p.block_tokens = p.waves ? staged : staged * (kWaves / p.heads_across);
   // (a sum of blocks is kept in 32 bits)
   const uint64_t most = (uint64_t)q->n_seqs * (q->d_block_table ? (uint64_t)q->table_stride * c->page_tokens : c->page_tokens);
   while (most / p.block_tokens + q->n_seqs > (1ull << 31) && p.block_tokens < (1u << 30)) p.block_tokens *= 2;
@@ -352,7 +355,8 @@ int splitzip_cache_move(const splitzip_cache* caches, uint32_t n_caches, const s
   a.seqs = device_seqs(caches, seqs, n_rows);
   a.path = d_path;
   a.path_stride = path_stride;
-  a.row_bytes = caches->head_dim * (uint32_t)words_bytes(caches->dtype);
+  a.row_bytes = row_bytes(caches);
+  a.groups = scales_of(caches);
   for (uint32_t at = 0; at < n_caches; at += kMoveMax) {
     const uint32_t n = n_caches - at < kMoveMax ? n_caches - at : kMoveMax;
     for (uint32_t k = 0; k < n; ++k) {

@@ -7,6 +7,10 @@
 // their subnormal range; x 2^-e is exact, so a word is rounded once; and the words' exponents lie in the same place in
 // every tensor, which is what the codec's codebooks count on.  Sums are not taken anywhere here: a largest magnitude and
 // products with powers of two are exact in 32 bits.
+//
+// A cache of 4-bit words (E2M1: 0, 1/2, 1, 3/2, 2, 3, 4 and 6, and their negatives) keeps such a scale for every 32 elements, since three
+// bits of magnitude reach only from 1/2 to 6: the least e with max |x| <= 6 * 2^e.  The format has neither infinities nor NaN; a group that
+// holds one gets the byte 255, under which all of its words are NaN, as the conversion instructions have it.
 #ifndef SPLITZIP_CACHE_HPP
 #define SPLITZIP_CACHE_HPP
 
@@ -14,7 +18,18 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kTopE5m2 = 15, kTopE4m3 = 8;
+// the words of a cache: bits of one; elements that share a scale (of a head of D elements)
+template <int KIND>
+constexpr int kBits = KIND == SPLITZIP_BF16 ? 16 : KIND == SPLITZIP_FP4_E2M1 ? 4 : 8;
+constexpr int kGroup4 = 32;
+template <int KIND, int D>
+constexpr uint32_t kGroups = KIND == SPLITZIP_FP4_E2M1 ? D / kGroup4 : 1;   // scales of a token and head
+
+// a format's largest finite word: m * 2^X, and m's bits behind the point as those of a float
+template <int KIND>
+constexpr int kTop = KIND == SPLITZIP_FP8_E5M2 ? 15 : KIND == SPLITZIP_FP8_E4M3 ? 8 : 2;
+template <int KIND>
+constexpr uint32_t kTopMantissa = KIND == SPLITZIP_FP4_E2M1 ? 0x400000u : 0x600000u;   // 1.5, 1.75
 
 // the words of K and V and their scales; a page is where the table says, or, without a table, sequence s is page s
 struct Cache {
@@ -68,9 +83,9 @@ struct Pages {
 __device__ inline uint64_t token_offset(const Cache& c, uint32_t page, uint32_t place) {
   return (uint64_t)page * c.page_stride + (uint64_t)place * c.token_stride;
 }
-// byte of its scale: [heads][tokens of a page], so that the scales of eight tokens of a head are one load
-__device__ inline uint64_t scale_offset(const Cache& c, uint32_t page, uint32_t place, uint32_t head) {
-  return (uint64_t)page * c.scale_page_stride + (uint64_t)head * c.page_tokens + place;
+// byte of its scale: [heads][groups of a head][tokens of a page], so that the scales of eight tokens are one load; row: head * groups + group
+__device__ inline uint64_t scale_offset(const Cache& c, uint32_t page, uint32_t place, uint32_t row) {
+  return (uint64_t)page * c.scale_page_stride + (uint64_t)row * c.page_tokens + place;
 }
 
 // 16 bytes per lane from memory straight into LDS: the wave's lanes one behind the other from `to` on, which is the wave's.  They are
@@ -103,10 +118,9 @@ __device__ inline uint32_t largest8(const u32x4& w) {
   return m;
 }
 
-// the scale byte for a largest magnitude of these BF16 bits
-template <int TOP>
-__device__ inline int scale_byte(uint32_t bits) {
-  const uint32_t f = bits << 16;
+// the scale byte for a largest finite magnitude of these bits (of a float)
+template <int KIND>
+__device__ inline int scale_byte(uint32_t f) {
   int e = (int)(f >> 23) - 127;
   uint32_t mant = f & 0x7fffffu;
   if (!(f >> 23)) {   // a subnormal: shifted up to its first bit
@@ -114,8 +128,8 @@ __device__ inline int scale_byte(uint32_t bits) {
     e = -126 - up;
     mant = (mant << up) & 0x7fffffu;
   }
-  e = e - TOP + (mant > 0x600000u ? 1 : 0);
-  return bits && e > -127 ? e + 127 : 0;
+  e = e - kTop<KIND> + (mant > kTopMantissa<KIND> ? 1 : 0);
+  return f && e > -127 ? e + 127 : 0;
 }
 
 // 8 BF16 words times 2^(127 - byte), rounded to FP8: 8 bytes.  2^(127 - byte) as two factors, each a normal number.
@@ -164,6 +178,76 @@ __device__ inline u32x4 from_fp8(const u32x2& w, uint32_t byte) {
   return u32x4{fp8_pair_to_bf16<KIND, false>(w[0], byte), fp8_pair_to_bf16<KIND, true>(w[0], byte), fp8_pair_to_bf16<KIND, false>(w[1], byte),
                fp8_pair_to_bf16<KIND, true>(w[1], byte)};
 }
+
+// The same for the pair of 4-bit words in byte `of` of a register (a constant once loops are unrolled).  Two significant bits at most: results from
+// 2^128 on become infinite, below BF16's normal numbers they are exact down to 2^-128.  Byte 255: NaN.
+__device__ inline uint32_t fp4_pair_to_bf16(uint32_t w, uint32_t byte, int of) {
+  const float power = __uint_as_float(byte << 23);
+  switch (of) {
+    case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 0));
+    case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 1));
+    case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 2));
+    default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 3));
+  }
+}
+__device__ inline u32x4 from_fp4(uint32_t w, uint32_t byte) {
+  return u32x4{fp4_pair_to_bf16(w, byte, 0), fp4_pair_to_bf16(w, byte, 1), fp4_pair_to_bf16(w, byte, 2), fp4_pair_to_bf16(w, byte, 3)};
+}
+
+// 8 BF16 words times 2^(127 - byte), rounded once to 4-bit words, to nearest, ties to even; the even element in a byte's low half.  The
+// instruction divides by the power in its exponent field; what a group without infinities and NaN holds fits the format.
+__device__ inline uint32_t to_fp4(const u32x4& w, int byte) {
+  const float power = __uint_as_float((uint32_t)byte << 23);
+  const auto pair = [&](int i) {
+    const uint32_t x = w[i];   // (__builtin_bit_cast of a vector's element itself reads the first)
+    return __builtin_bit_cast(bf16x2, x);
+  };
+  uint32_t d = 0;
+  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, pair(0), power, 0);
+  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, pair(1), power, 1);
+  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, pair(2), power, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(d, pair(3), power, 3);
+}
+
+// 8 elements of a lane as they lie in memory
+template <int KIND>
+using Lane8 = typename std::conditional<kBits<KIND> == 16, u32x4, typename std::conditional<kBits<KIND> == 8, u32x2, uint32_t>::type>::type;
+
+// The largest magnitude among the lanes that share a scale, all of a head's (FP8) or four (4-bit words), from each lane's own, as bits.
+template <int KIND, int D>
+__device__ inline uint32_t largest_of_group(uint32_t m) {
+#pragma unroll
+  for (int o = D / 16 / (int)kGroups<KIND, D>; o > 0; o /= 2) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+  return m;
+}
+// 8 BF16 words of a lane as words of the cache, and the byte of the lane's scale
+template <int KIND, int D>
+__device__ inline Lane8<KIND> quantised(const u32x4& w, int& byte) {
+  if constexpr (KIND == SPLITZIP_BF16) {
+    return w;
+  } else if constexpr (KIND == SPLITZIP_FP4_E2M1) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max(m, max(w[i] << 16 & 0x7fff0000u, w[i] & 0x7fff0000u));
+    m = largest_of_group<KIND, D>(m);
+    byte = m >= 0x7f800000u ? 255 : scale_byte<KIND>(m);
+    return to_fp4(w, byte);
+  } else {
+    byte = scale_byte<KIND>(largest_of_group<KIND, D>(largest8(w)) << 16);
+    return to_fp8<KIND>(w, byte);
+  }
+}
+template <int KIND>
+__device__ inline u32x4 dequantised(const Lane8<KIND>& w, uint32_t byte) {
+  if constexpr (KIND == SPLITZIP_BF16) return w;
+  else if constexpr (KIND == SPLITZIP_FP4_E2M1) return from_fp4(w, byte);
+  else return from_fp8<KIND>(w, byte);
+}
+// whether the lane writes its scale, the first of those that share it, and the scale's row
+template <int KIND, int D>
+__device__ inline bool has_scale(uint32_t lane) { return lane % (D / 8 / kGroups<KIND, D>) == 0; }
+template <int KIND, int D>
+__device__ inline uint32_t scale_row(uint32_t head, uint32_t lane) { return head * kGroups<KIND, D> + lane / (D / 8 / kGroups<KIND, D>); }
 
 // Rows into the cache, and back.  A row of a head is taken by D / 8 lanes, eight elements each; a workgroup belongs to one
 // sequence (blockIdx.y) and takes kAtOnce (row, head) pairs per lane at a time, K and V of a pair together: all of their words are asked for before
@@ -225,22 +309,12 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(RowsArgs a) {
       if (!have[j]) continue;
       const uint32_t in = p.pages.clamped(page[j]), place = p.pages.place((uint32_t)p.token[j]);
       const uint64_t word = token_offset(a.cache, in, place) + p.heads[j] * a.cache.head_stride;
-      if constexpr (KIND == SPLITZIP_BF16) {
-        *reinterpret_cast<u32x4*>(a.cache.k + word + lane * 16) = k[j];
-        *reinterpret_cast<u32x4*>(a.cache.v + word + lane * 16) = v[j];
-      } else {
-        uint32_t mk = largest8(k[j]), mv = largest8(v[j]);
-#pragma unroll
-        for (int o = Pairs<D>::kLanes / 2; o > 0; o /= 2) {
-          mk = max(mk, (uint32_t)__shfl_xor((int)mk, o));
-          mv = max(mv, (uint32_t)__shfl_xor((int)mv, o));
-        }
-        constexpr int kTop = KIND == SPLITZIP_FP8_E5M2 ? kTopE5m2 : kTopE4m3;
-        const int bk = scale_byte<kTop>(mk), bv = scale_byte<kTop>(mv);
-        *reinterpret_cast<u32x2*>(a.cache.k + word + lane * 8) = to_fp8<KIND>(k[j], bk);
-        *reinterpret_cast<u32x2*>(a.cache.v + word + lane * 8) = to_fp8<KIND>(v[j], bv);
-        if (lane == 0) {
-          const uint64_t scale = scale_offset(a.cache, in, place, p.heads[j]);
+      int bk = 0, bv = 0;
+      *reinterpret_cast<Lane8<KIND>*>(a.cache.k + word + lane * kBits<KIND>) = quantised<KIND, D>(k[j], bk);
+      *reinterpret_cast<Lane8<KIND>*>(a.cache.v + word + lane * kBits<KIND>) = quantised<KIND, D>(v[j], bv);
+      if constexpr (KIND != SPLITZIP_BF16) {
+        if (has_scale<KIND, D>(lane)) {
+          const uint64_t scale = scale_offset(a.cache, in, place, scale_row<KIND, D>(p.heads[j], lane));
           a.cache.k_scales[scale] = (uint8_t)bk;
           a.cache.v_scales[scale] = (uint8_t)bv;
         }
@@ -251,14 +325,13 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(RowsArgs a) {
 
 template <int KIND, int D, bool STREAM>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(RowsArgs a) {
-  constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
-  typedef typename std::conditional<ES == 2, u32x4, u32x2>::type Words;
+  typedef Lane8<KIND> Words;
   Pairs<D> p(a);
   const uint32_t lane = threadIdx.x % Pairs<D>::kLanes;
   for (uint32_t p0 = blockIdx.x * Pairs<D>::kStepPairs; p0 < p.n; p0 += gridDim.x * Pairs<D>::kStepPairs) {
     bool have[kAtOnce];
     Words k[kAtOnce], v[kAtOnce];
-    uint32_t page[kAtOnce], bk[kAtOnce], bv[kAtOnce];
+    uint32_t page[kAtOnce], bk[kAtOnce] = {}, bv[kAtOnce] = {};
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
       have[j] = p.at(a, p0, j);
@@ -267,11 +340,11 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(RowsArgs a) {
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
       const uint32_t in = p.pages.clamped(page[j]), place = p.pages.place((uint32_t)max(p.token[j], 0));
-      const uint64_t word = token_offset(a.cache, in, place) + p.heads[j] * a.cache.head_stride + lane * 8 * ES;
+      const uint64_t word = token_offset(a.cache, in, place) + p.heads[j] * a.cache.head_stride + lane * kBits<KIND>;
       k[j] = ld_row<STREAM, Words>(a.cache.k + word);
       v[j] = ld_row<STREAM, Words>(a.cache.v + word);
-      if constexpr (ES == 1) {
-        const uint64_t scale = scale_offset(a.cache, in, place, p.heads[j]);
+      if constexpr (KIND != SPLITZIP_BF16) {
+        const uint64_t scale = scale_offset(a.cache, in, place, scale_row<KIND, D>(p.heads[j], lane));
         bk[j] = a.cache.k_scales[scale];
         bv[j] = a.cache.v_scales[scale];
       }
@@ -280,14 +353,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(RowsArgs a) {
     for (int j = 0; j < kAtOnce; ++j) {
       if (!have[j]) continue;
       const uint32_t at = 2 * (p.heads[j] * D + lane * 8);
-      u32x4 ko, vo;
-      if constexpr (ES == 2) {
-        ko = k[j];
-        vo = v[j];
-      } else {
-        ko = from_fp8<KIND>(k[j], bk[j]);
-        vo = from_fp8<KIND>(v[j], bv[j]);
-      }
+      u32x4 ko = dequantised<KIND>(k[j], bk[j]), vo = dequantised<KIND>(v[j], bv[j]);
       if (p.token[j] < 0) ko = vo = u32x4{0, 0, 0, 0};   // a row in front of the sequence's first token
       u32x4 *const k_to = reinterpret_cast<u32x4*>(a.k + p.row[j] * a.k_stride + at), *const v_to = reinterpret_cast<u32x4*>(a.v + p.row[j] * a.v_stride + at);
       if constexpr (STREAM) {
@@ -310,7 +376,7 @@ struct MoveArgs {
   Cache cache;             // the geometry all of them share
   Seqs seqs;
   const int32_t* path;
-  uint32_t path_stride, row_bytes;   // entries per sequence; bytes of a token and head
+  uint32_t path_stride, row_bytes, groups;   // entries per sequence; bytes and scales of a token and head
   struct { uint8_t *k, *v, *k_scales, *v_scales; } at[kMoveMax];
 };
 // Bound by latency: the starts, the path, the table and the tokens are asked for one behind the other, each of them once for 64 entries of
@@ -322,7 +388,7 @@ __global__ void __launch_bounds__(kThreads) cache_move_kernel(MoveArgs a) {
   const Seq s = seq_at(a.seqs, blockIdx.x);
   const Pages at_pages(a.cache, a.seqs, blockIdx.x);
   const auto& at = a.at[blockIdx.y];
-  const uint32_t per_head = a.row_bytes / 16, pieces = per_head * a.cache.heads, each = pieces + (at.k_scales ? a.cache.heads : 0);   // of K, and of V
+  const uint32_t per_head = a.row_bytes / 16, pieces = per_head * a.cache.heads, each = pieces + a.groups * a.cache.heads;   // of K, and of V
   int before = -1;
   for (uint32_t i0 = 0; i0 < a.path_stride; i0 += 64) {
     // the entries of the path that are part of it, a lane each
@@ -347,7 +413,7 @@ __global__ void __launch_bounds__(kThreads) cache_move_kernel(MoveArgs a) {
       const bool live = u0 + lane < 2 * each;
       const uint32_t u = min(u0 + lane, 2 * each - 1);
       const bool of_v = u >= each, is_word = u - (of_v ? each : 0) < pieces;
-      const uint32_t w = u - (of_v ? each : 0), head = is_word ? w / per_head : w - pieces;
+      const uint32_t w = u - (of_v ? each : 0), head = is_word ? w / per_head : w - pieces;   // (a scale's row, if it is one)
       uint8_t* const words = (of_v ? at.v : at.k) + head * a.cache.head_stride + (is_word ? w - head * per_head : 0) * 16;
       uint8_t* const scales = of_v ? at.v_scales : at.k_scales;
       for (uint64_t left = moving; left;) {

@@ -1,0 +1,463 @@
+"""The cache calls over 4-bit words (FP4_E2M1, a power of two for each 32 elements) against their formulas in 64 bits.
+
+Words and scale bytes are exact, as those of FP8 are.  A word times its power of two is a BF16 number (two significant bits), so that attention's
+tolerance is the other formats': the result's rounding and, beyond 16 rows of a head, that of the weights (2^-8 each), and what a score is off."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_01708_amd as sz
+from paper_2605_01708_amd.binding import _CAttention, _CCache, _CSeqs
+from test_cache_guards import Guarded
+from test_cache_ops import World, attend, close, queries, random_tree, rounded, run, special_rows
+
+I32 = torch.int32
+GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+WORDS = np.concatenate([GRID, -GRID])
+
+
+def quantised4(x):
+    """x [..., dim] in 64 bits: nibbles, scale bytes [..., dim / 32] and the values they stand for"""
+    g = x.reshape(*x.shape[:-1], -1, 32)
+    finite = np.isfinite(g).all(-1)
+    top = np.abs(np.where(finite[..., None], g, 0)).max(-1)
+    fits = top[..., None] <= 6 * np.exp2(np.arange(255.0) - 127)
+    byte = np.where(finite, fits.argmax(-1), 255)
+    assert (fits.any(-1) | ~finite).all()
+    with np.errstate(invalid="ignore"):
+        y = np.abs(g) * np.exp2(127.0 - np.minimum(byte, 254))[..., None]
+    far = np.abs(np.where(finite[..., None], y, 0)[..., None] - GRID)                # nearest; of two as near, the even one
+    near = far == far.min(-1, keepdims=True)
+    code = np.where(near[..., ::2].any(-1), near[..., ::2].argmax(-1) * 2, near.argmax(-1))
+    nibble = code + 8 * np.signbit(g)
+    value = WORDS[nibble] * np.exp2(byte - 127.0)[..., None]
+    value[~finite] = np.nan
+    return nibble.reshape(x.shape), byte.astype(np.uint8), value.reshape(x.shape)
+
+
+def packed(nibble):
+    return torch.from_numpy((nibble[..., ::2] | nibble[..., 1::2] << 4).astype(np.uint8))
+
+
+class World4(World):
+    """World of 4-bit words"""
+
+    def __init__(self, lens, rows, heads=2, dim=128, page=16, layout="nhd", seed=0, max_rows=None, max_len=None):
+        rng = np.random.default_rng(seed)
+        self.kind, self.lens, self.rows, self.heads, self.dim, self.page = sz.FP4_E2M1, lens, rows, heads, dim, page
+        n = len(lens)
+        if layout == "flat":
+            page = self.page = max(8, -(-max(lens, default=1) // 8) * 8)
+            self.pages, table = max(n, 1), None
+        else:
+            used = [-(-x // page) for x in lens]
+            self.pages = sum(used) + 2
+            order = rng.permutation(self.pages)
+            table, at = np.full((n, max(max(used, default=1), 1)), 1 << 30, np.int32), 0
+            for s, u in enumerate(used):
+                table[s, :u] = order[at:at + u]
+                at += u
+        self.table = table
+        x = rng.standard_normal((2, self.pages, page, heads, dim)) * np.exp(0.5 * rng.standard_normal((2, 1, 1, heads, dim)))
+        nibble, byte, self.value = quantised4(x)
+        owned = np.zeros((self.pages, page), bool)
+        for s in range(n):
+            for t in range(lens[s]):
+                owned[self.slot(s, t)] = True
+        byte[:, ~owned] = 255                                                       # what belongs to no token is NaN
+        raw = packed(nibble)
+        self.scales = torch.from_numpy(byte).permute(0, 1, 3, 4, 2).contiguous().cuda()
+        if layout == "hnd":
+            pool = raw.permute(0, 1, 3, 2, 4).contiguous().cuda()
+            k, v = pool[0].transpose(1, 2), pool[1].transpose(1, 2)
+        elif layout == "side":
+            pool = raw.permute(1, 0, 2, 3, 4).contiguous().cuda()
+            k, v = pool[:, 0], pool[:, 1]
+        else:
+            pool = raw.cuda()
+            k, v = pool[0], pool[1]
+        self.owned, self.pool = owned, pool
+        self.cache = sz.KvCache(k, v, sz.FP4_E2M1, *self.scales)
+        starts = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+        self.starts, self.n_rows = starts, int(starts[-1])
+        self.dev = [None if table is None else torch.from_numpy(table).cuda(), torch.from_numpy(starts).cuda(), torch.tensor(lens, dtype=I32, device="cuda")]
+        self.seqs = sz.Sequences(*self.dev, max_rows=max(rows, default=0) if max_rows is None else max_rows, max_len=max(lens, default=0) if max_len is None else max_len)
+
+    def set_byte(self, s, t, which, head, group, byte):
+        p, a = self.slot(s, t)
+        self.scales[which, p, head, group, a] = byte
+
+
+# ---- what is refused -----------------------------------------------------------------------------------
+
+def test_descriptions_are_checked():
+    L, buf = sz.lib(), 1 << 16
+
+    def write(**k):
+        d = dict(k=buf, v=buf, ks=buf, vs=buf, dtype=sz.FP4_E2M1, heads=8, dim=128, page=16, pages=4, res=0, ps=16 * 512, ts=512, hs=64, ss=512)
+        d.update(k)
+        c = _CCache(*[d[x] for x in ("k", "v", "ks", "vs", "dtype", "heads", "dim", "page", "pages", "res", "ps", "ts", "hs", "ss")])
+        q, how = _CSeqs(buf, buf, buf, 4, 2, 1, 64), _CAttention(1.0, 0.0, None, None, None, 0, 0, 0)
+        rc = L.splitzip_cache_write(C.byref(c), C.byref(q), buf, 1024, buf, 1024, 0, None)
+        assert L.splitzip_cache_attention(C.byref(c), C.byref(q), C.byref(how), buf, 4096, buf, 4096, None, 0, 4 * d["heads"], None, 0, None) == rc
+        assert L.splitzip_cache_move(C.byref(c), 1, C.byref(q), buf, 4, 0, None) == rc
+        return rc
+
+    assert write() == 0 and write(dim=64, hs=32, ts=256) == 0
+    for k, rc in ((dict(dtype=15), -1), (dict(dtype=17), -1), (dict(dtype=3), -1), (dict(dim=96), -2), (dict(dim=32), -2), (dict(hs=48), -1), (dict(ts=48), -1),
+                  (dict(ks=None), -1), (dict(vs=buf + 4), -1), (dict(ss=4), -1), (dict(page=4), -1), (dict(hs=56), -1)):
+        assert write(**k) == rc, k
+
+
+def test_the_codec_takes_no_4_bit_words():
+    L, buf = sz.lib(), 1 << 16
+    for f in (L.splitzip_fixed_bytes, L.splitzip_compress_bound, L.splitzip_workspace_bytes):
+        assert f(1024, sz.FP4_E2M1) == 0
+    assert L.splitzip_histogram(buf, 16, sz.FP4_E2M1, buf, None) == -1
+    with pytest.raises(sz.SplitZipError):
+        sz.codebook_from_dec(range(16), sz.FP4_E2M1)
+
+
+def test_python_side_checks():
+    z = lambda *s, dtype=torch.uint8: torch.zeros(*s, dtype=dtype)   # noqa: E731
+    kv, scales = z(3, 16, 2, 64), z(3, 2, 4, 16)
+    c = sz.KvCache(kv, kv, sz.FP4_E2M1, scales, scales)
+    assert (c.head_dim, c.kv_heads) == (128, 2) and c.c.token_stride_bytes == 128 and c.c.scale_page_stride_bytes == 128
+    sz.KvCache(kv.view(torch.float4_e2m1fn_x2), kv.view(torch.int8), sz.FP4_E2M1, scales, scales)
+    sz.KvCache(kv, kv, sz.FP4_E2M1, z(3, 5, 4, 16)[:, :2], z(3, 5, 4, 16)[:, :2])            # pages further apart
+    for args in ((kv, kv, sz.FP4_E2M1), (kv, kv, sz.FP4_E2M1, scales, z(3, 2, 16)), (kv, kv, sz.FP4_E2M1, z(3, 2, 2, 16), scales),
+                 (kv, kv, sz.FP4_E2M1, z(3, 2, 16, 4).transpose(2, 3), scales), (kv, kv, sz.FP4_E2M1, z(3, 4, 2, 16).transpose(1, 2), scales),
+                 (kv.view(torch.float8_e4m3fn), kv, sz.FP4_E2M1, scales, scales), (kv, kv, sz.FP4_E2M1, scales, scales.view(torch.float8_e4m3fn)),
+                 (z(3, 16, 2, 64, dtype=torch.int16), kv, sz.FP4_E2M1, scales, scales)):
+        with pytest.raises(ValueError):
+            sz.KvCache(*args)
+    with pytest.raises(ValueError):                                                          # rows are of elements, not of bytes
+        x = z(2, 2, 64, dtype=torch.bfloat16)
+        sz.cache_write(x, x, c, sz.Sequences(z(2, 4, dtype=I32), z(3, dtype=I32), z(2, dtype=I32), 1, 64))
+
+
+# ---- writing and reading -------------------------------------------------------------------------------
+
+def special_groups(n, heads, dim, seed):
+    """special_rows, and groups of 32 with what can go wrong in one of them alone: infinities, NaN, zeros of both signs, ties, borders of the scale"""
+    rng = np.random.default_rng(seed)
+    x = special_rows(n, heads, dim, seed)
+    for g in x.reshape(-1, 32)[1::2]:
+        what = int(rng.integers(0, 8))
+        e = 2.0 ** int(rng.integers(-100, 100))
+        if what == 0:
+            g[rng.integers(0, 32)] = np.inf
+        elif what == 1:
+            g[rng.integers(0, 32)] = np.nan
+        elif what == 2:
+            g[:] = np.where(rng.integers(0, 2, 32), 0.0, -0.0)
+        elif what == 3:
+            g[:] = e * np.resize([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 6, -0.25, -0.75, -1.25, -1.75, -2.5, -3.5, -5, -6], 32)
+        elif what == 4:
+            g[:] = e * (6.0 + (g > 0) * 2.0 ** -5)                                           # the largest word, and the next BF16 number
+        elif what == 5:
+            g[:] = 2.0 ** -133 * rng.integers(-127, 128, 32)
+        elif what == 6:
+            g[:] = rounded(np.sign(g + 0.5) * 2.0 ** 127 * rng.uniform(1.5, 1.99, 32), sz.BF16)
+    return x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,heads,page,layout", [(128, 2, 16, "nhd"), (64, 3, 8, "hnd"), (256, 1, 32, "side"), (128, 8, 16, "flat")])
+def test_write_and_read_are_exact(dim, heads, page, layout):
+    lens, rows = [37, 1, 0, 100, 16, 5], [37, 1, 0, 13, 0, 7]           # (7 rows of 5 tokens: the first two are nowhere)
+    w = World4(lens, rows, heads, dim, page, layout, seed=3)
+    x = [special_groups(w.n_rows, heads, dim, seed) for seed in (1, 2)]
+    both = torch.from_numpy(np.stack(x, 1)).to(torch.bfloat16).cuda()    # K and V as parts of one tensor
+    was = [t.clone() for t in (w.cache.k, w.cache.v, *w.scales)]
+    sz.cache_write(both[:, 0], both[:, 1], w.cache, w.seqs)
+    back = torch.full((w.n_rows, 2, heads, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    sz.cache_read(w.cache, w.seqs, back[:, 0], back[:, 1])
+    back = back.double().cpu().numpy()
+    now = [t.clone() for t in (w.cache.k, w.cache.v, *w.scales)]
+    fresh = torch.zeros(w.pages, w.page, dtype=torch.bool)
+    for s in range(len(lens)):
+        for i in range(rows[s]):
+            t, row = lens[s] - rows[s] + i, int(w.starts[s]) + i
+            if t < 0:
+                assert (back[row] == 0).all()
+                continue
+            p, a = w.slot(s, t)
+            fresh[p, a] = True
+            for which in range(2):
+                nibble, byte, value = quantised4(x[which][row])
+                assert np.array_equal(now[2 + which][p, :, :, a].cpu().numpy(), byte)
+                held = now[which][p, a].cpu().numpy()
+                unpacked = np.stack([held & 15, held >> 4], -1).reshape(nibble.shape)
+                fine = np.repeat(byte < 255, 32, -1)
+                assert np.array_equal(unpacked[fine], nibble[fine])
+                assert np.array_equal(back[row, which], rounded(value, sz.BF16), equal_nan=True)
+    for a, b in zip(now[:2], was[:2]):
+        assert torch.equal(a[~fresh.cuda()], b[~fresh.cuda()])
+    for a, b in zip(now[2:], was[2:]):
+        assert torch.equal(a.movedim(-1, 1)[~fresh.cuda()], b.movedim(-1, 1)[~fresh.cuda()])
+
+
+@pytest.mark.gpu
+def test_read_every_word_under_every_scale():
+    """all pairs of words times all scale bytes, rounded to BF16 once; 255 is NaN"""
+    k = torch.arange(256, dtype=torch.uint8).view(1, 1, 2, 128).expand(1, 256, 2, 128).contiguous()      # a token for each byte
+    scales = torch.arange(256, dtype=torch.uint8).expand(1, 2, 8, 256).contiguous()
+    c = sz.KvCache(k.cuda(), k.cuda(), sz.FP4_E2M1, scales.cuda(), scales.cuda())
+    q = sz.Sequences(None, torch.tensor([0, 256], dtype=I32, device="cuda"), torch.tensor([256], dtype=I32, device="cuda"), 256, 256)
+    out = [torch.zeros(256, 2, 256, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    sz.cache_read(c, q, *out)
+    byte = np.arange(256)
+    value = np.stack([WORDS[byte & 15], WORDS[byte >> 4]], -1).reshape(1, 2, 256) * np.exp2(np.arange(256) - 127.0)[:, None, None]
+    value = rounded(value, sz.BF16)
+    value[255] = np.nan
+    for o in out:
+        assert np.array_equal(o.double().cpu().numpy(), value, equal_nan=True)
+
+
+# ---- attention -----------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("group,T", [(1, 1), (4, 1), (5, 3), (16, 1), (8, 3), (3, 21), (4, 33)])
+def test_chains(dim, group, T):
+    lens = [T, T + 1, 40 + T, 129, 0, 300 + T, 31 + T]
+    w = World4(lens, [T, T, T, T, 0, max(T - 1, 1), T], 2, dim, 16, seed=T)
+    q, qd = queries(w, group)
+    close(*run(w, qd, sz.Attention(dim ** -0.5)), attend(w, q, dim ** -0.5))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("page,layout", [(8, "nhd"), (16, "hnd"), (64, "side"), (128, "nhd"), (16, "flat")])
+@pytest.mark.parametrize("group", [2, 20])
+def test_layouts(dim, page, layout, group):
+    w = World4([1, 7, 8, 9, 63, 64, 65, 200], [1] * 8, 3, dim, page, layout, seed=7)
+    q, qd = queries(w, group)
+    close(*run(w, qd, sz.Attention(0.1)), attend(w, q, 0.1))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,words", [(13, 1), (64, 1), (130, 3)])
+def test_trees(T, words):
+    rng = np.random.default_rng(T)
+    lens, rows = [T, T + 77, 300 + T], [T, T - 3, T]
+    w = World4(lens, rows, 1, 128, 16, seed=2)
+    bits, pos, sees = [], [], []
+    for n, r in zip(lens, rows):
+        b, d, s = random_tree(r, rng, words)
+        bits.append(b)
+        pos += [n - r + x for x in d]
+        sees.append(s)
+    q, qd = queries(w, 4)
+    slopes = np.array([0.5, 0.25, 0.125, 0.0625])
+    how = sz.Attention(0.09, slopes=torch.tensor(slopes, dtype=torch.float32, device="cuda"), tree=torch.from_numpy(np.concatenate(bits)).cuda(),
+                       positions=torch.tensor(pos, dtype=I32, device="cuda"))
+    close(*run(w, qd, how), attend(w, q, 0.09, slopes=slopes, see=lambda s, i, j: sees[s][i] >> j & 1, positions=pos))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("softcap,window,bias,T", [(30.0, 0, False, 1), (0.0, 50, False, 1), (5.0, 33, True, 4), (0.0, 1, False, 3), (20.0, 0, True, 40)])
+def test_capped_windowed_biased(dim, softcap, window, bias, T):
+    w = World4([T, 64 + T, 257, 1500], [T] * 4, 2, dim, 32, seed=9)
+    q, qd = queries(w, 3)
+    q, qd = q * 4, qd * 4
+    slopes = 2.0 ** -np.arange(1, 7) if bias else None
+    how = sz.Attention(0.088, softcap=softcap, window=window, slopes=None if slopes is None else torch.tensor(slopes, dtype=torch.float32, device="cuda"))
+    close(*run(w, qd, how), attend(w, q, 0.088, softcap=softcap, window=window, slopes=slopes))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_long_sequences_in_parts(dim):
+    """parts, their join, and hints that are too small or too large"""
+    w = World4([3001, 1, 2000, 700], [2, 1, 9, 9], 1, dim, 16, seed=11)
+    q, qd = queries(w, 4)
+    want = attend(w, q, 0.1)
+    close(*run(w, qd, sz.Attention(0.1)), want)
+    for rows, most in ((1, 3001), (9, 300), (0, 0), (100, 100000)):
+        w.seqs = sz.Sequences(*w.dev, max_rows=rows, max_len=most)
+        close(*run(w, qd, sz.Attention(0.1)), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 100])
+def test_pieces_of_prompts(dim, window):
+    w = World4([200, 777, 60, 150], [200, 180, 60, 170], 1, dim, 16, seed=dim, max_len=777)
+    q, qd = queries(w, 3)
+    close(*run(w, qd, sz.Attention(0.1, window=window)), attend(w, q, 0.1, window=window))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 40])
+def test_many_sequences(rows):
+    rng = np.random.default_rng(rows)
+    lens = [int(x) for x in rng.integers(0, 90, 150)] + [900, 0, 500]
+    w = World4(lens, [min(rows, n) if k % 5 else 0 for k, n in enumerate(lens)], 1, 64, 16, seed=rows)
+    q, qd = queries(w, 2)
+    close(*run(w, qd, sz.Attention(0.1)), attend(w, q, 0.1))
+
+
+@pytest.mark.gpu
+def test_rows_that_see_nothing():
+    w = World4([5, 9, 70], [5, 5, 70], 2, 64, 8, seed=4)
+    tree = torch.zeros(80, 1, dtype=torch.int64, device="cuda")
+    tree[2] = 0b10100
+    tree[79] = -1
+    sees = lambda s, i, j: (s == 0 and i == 2 and j in (2, 4)) or (s == 2 and i == 69 and j < 64)   # noqa: E731
+    q, qd = queries(w, 2)
+    out, lse = run(w, qd, sz.Attention(0.1, tree=tree))
+    close(out, lse, attend(w, q, 0.1, see=sees))
+    assert (out[0] == 0).all() and (out[78] == 0).all() and torch.isneginf(lse[0]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("T", [2, 40])
+def test_groups_of_nan_and_of_infinities(dim, T):
+    """a group under the byte 255 is NaN, under 254 words from 2 on are infinite: unseen they touch no row, seen they reach it, in their elements alone"""
+    w = World4([100 + T, 260 + T], [T, T], 1, dim, 16, seed=13)
+    q, qd = queries(w, 2)
+    clean = attend(w, q, 0.1)
+    last, groups = T - 1, dim // 32
+    w.set_byte(0, 100 + last, 0, 0, 0, 255)                          # K of the last row
+    w.set_byte(1, 260 + last, 1, 0, groups - 1, 255)                 # V of the other sequence's last
+    out, lse = run(w, qd, sz.Attention(0.1))
+    fine = np.ones(2 * T, bool)
+    fine[[last, T + last]] = False
+    close(out[torch.from_numpy(fine)], lse[torch.from_numpy(fine)], tuple(x[fine] for x in clean))
+    assert torch.isnan(out[last]).all() and torch.isnan(lse[last]).all()
+    assert torch.isnan(out[T + last, :, -32:]).all() and torch.isfinite(out[T + last, :, :-32]).all() and torch.isfinite(lse[T + last]).all()
+    # behind a window, in front of everything, and seen by all: an infinity
+    w = World4([200 + T], [T], 1, dim, 16, seed=14)
+    w.set_byte(0, 3, 0, 0, 0, 255)
+    w.set_byte(0, 150, 1, 0, 1, 255)
+    p, a = w.slot(0, 199)
+    w.cache.v[p, a, 0, :16] = 0x21                                   # 1/2 and 1 ...
+    w.cache.v[p, a, 0, 0] = 0x2e                                     # ... but for an infinity of -4 2^127, and 1
+    w.set_byte(0, 199, 1, 0, 0, 254)
+    q, qd = queries(w, 2)
+    out, lse = run(w, qd, sz.Attention(0.1, window=44))
+    assert torch.isfinite(lse).all() and torch.isneginf(out[:, :, 0]).all() and not torch.isnan(out).any()
+    assert torch.isfinite(out[:, :, 32:]).all()
+
+
+@pytest.mark.gpu
+def test_strided_rows_other_streams_graphs_and_repeats():
+    w = World4([2000, 400, 33], [2, 2, 2], 2, 128, 16, seed=16)
+    q, qd = queries(w, 4)
+    wide = torch.full((w.n_rows, 3, 8, 128), 9.0, dtype=torch.bfloat16, device="cuda")
+    wide[:, 1] = qd
+    how = sz.Attention(0.1)
+    first, lse1 = run(w, wide[:, 1], how, out=wide[:, 2])
+    close(first, lse1, attend(w, q, 0.1))
+    assert (wide[:, 0] == 9).all()
+    out, lse = torch.zeros_like(qd), torch.zeros(qd.shape[:2], device="cuda")
+    ws = sz.attention_workspace(w.cache, w.seqs, w.n_rows, 8)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    sz.cache_attention(qd, w.cache, w.seqs, out, ws, how, lse, stream=side)
+    side.synchronize()
+    assert torch.equal(out, first) and torch.equal(lse, lse1)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sz.cache_attention(qd, w.cache, w.seqs, out, ws, how, lse)
+    for lens in ([2000, 400, 33], [1500, 2, 20], [5, 400, 33], [2000, 400, 33]):
+        w.dev[2].copy_(torch.tensor(lens, dtype=I32))
+        out.fill_(1.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        w.lens = lens
+        close(out, lse, attend(w, q, 0.1))
+    assert torch.equal(out, first)
+
+
+# ---- moving, far pages, guards -------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,layout,layers", [(64, "nhd", 1), (128, "side", 3), (256, "nhd", 66)])
+def test_move(dim, layout, layers):
+    lens, rows = [64, 13, 40, 9, 7, 90], [13, 13, 20, 9, 9, 30]
+    paths = [[0, 2, 5, 9, 12, -1], [1, 3, 4, 11, -1, -1], [0, 1, 2, 3, 4, 19], [-1, 3, 4, -1, -1, -1], [3, 4, 6, 8, -1, -1], [5, 8, 7, 20, 29, 30]]
+    valid = [[0, 2, 5, 9, 12], [1, 3, 4, 11], [0, 1, 2, 3, 4, 19], [], [3, 4, 6, 8], [5, 8]]
+    w = World4(lens, rows, 2, dim, 8, layout, seed=20)
+    caches, tensors = [], []
+    for layer in range(layers):
+        gen = torch.Generator("cuda").manual_seed(layer)
+        pool = torch.randint(0, 256, w.pool.shape, dtype=I32, device="cuda", generator=gen).to(torch.uint8)
+        scales = torch.randint(0, 255, w.scales.shape, device="cuda", generator=gen).to(torch.uint8)
+        k, v = (pool[:, 0], pool[:, 1]) if layout == "side" else (pool[0], pool[1])
+        caches.append(sz.KvCache(k, v, sz.FP4_E2M1, *scales))
+        tensors.append((k, v, scales))
+    want = []
+    for k, v, b in tensors:
+        new, old = [t.cpu().clone() for t in (k, v, b)], [t.cpu() for t in (k, v, b)]
+        for s, path in enumerate(valid):
+            base = lens[s] - rows[s]
+            for i, a in enumerate(path):
+                if base + i >= 0:
+                    (p0, t0), (p1, t1) = w.slot(s, base + a), w.slot(s, base + i)
+                    new[0][p1, t1], new[1][p1, t1], new[2][:, p1, :, :, t1] = old[0][p0, t0], old[1][p0, t0], old[2][:, p0, :, :, t0]
+        want.append(new)
+    sz.cache_move(sz.KvCaches(caches), w.seqs, torch.tensor(paths, dtype=I32, device="cuda"))
+    torch.cuda.synchronize()
+    for got, new in zip(tensors, want):
+        assert all(torch.equal(a.cpu(), b) for a, b in zip(got, new))
+
+
+@pytest.mark.gpu
+def test_a_pool_beyond_32_bits():
+    """pages more than 4 GiB from the pool's start, and scales too: written, read, moved and attended to there"""
+    pages = (5 << 30) // (16 * 512)
+    k, v = (torch.empty(pages, 16, 8, 64, dtype=torch.uint8, device="cuda") for _ in range(2))
+    stride = 8448                                                                            # pages of scales further apart than they are large
+    room = torch.empty(2 * pages * stride, dtype=torch.uint8, device="cuda")
+    scales = [torch.as_strided(room, (pages, 8, 4, 16), (stride, 64, 16, 1), i * pages * stride) for i in range(2)]
+    far = sz.KvCache(k, v, sz.FP4_E2M1, *scales)
+    near = sz.KvCache.zeros(8, 16, 8, 128, sz.FP4_E2M1)
+    x = torch.randn(2, 100, 8, 128, device="cuda").to(torch.bfloat16)
+    q = torch.randn(4, 8, 128, device="cuda").to(torch.bfloat16)
+    got = []
+    for cache, first in ((far, pages - 8), (near, 0)):
+        table = torch.arange(first, first + 8, dtype=I32, device="cuda")[None].contiguous()
+        i32 = lambda *y: torch.tensor(y, dtype=I32, device="cuda")   # noqa: E731
+        sz.cache_write(x[0], x[1], cache, sz.Sequences(table, i32(0, 100), i32(100), 100, 100))
+        step = sz.Sequences(table, i32(0, 4), i32(100), 4, 100)
+        sz.cache_move(sz.KvCaches([cache]), step, i32(0, 2, 3)[None].contiguous())
+        back, out = torch.zeros_like(x), torch.zeros_like(q)
+        sz.cache_read(cache, sz.Sequences(table, i32(0, 100), i32(100), 100, 100), back[0], back[1])
+        sz.cache_attention(q, cache, step, out, sz.attention_workspace(cache, step, 4, 8), sz.Attention(0.1))
+        got += [back, out]
+    assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[3]) and got[0].abs().sum() > 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,rows", [(64, 2), (128, 2), (256, 2), (64, 20), (128, 20), (256, 20)])
+@pytest.mark.parametrize("lens,starts,table", [((40, 50), (0, 1, 1), None), ((1 << 30, -5), (0, 1, 1), None), ((40, 50), (-3, 1, 1 << 20), None), ((40, 50), (0, 1, 1), -1)])
+def test_calls_stay_in_their_buffers(dim, rows, lens, starts, table):
+    """whatever lengths, starts and table entries say, what lies around the buffers stays as it is"""
+    g, heads, page, pages = Guarded(), 2, 16, 5
+    n = 2 * rows
+    k, v = (g(pages, page, heads, dim // 2, dtype=torch.uint8, fill=torch.randint(0, 256, (pages, page, heads, dim // 2))) for _ in range(2))
+    scales = [g(pages, heads, dim // 32, page, dtype=torch.uint8, fill=torch.full((pages, heads, dim // 32, page), 120)) for _ in range(2)]
+    cache = sz.KvCache(k, v, sz.FP4_E2M1, *scales)
+    i32 = lambda *x: g(len(x), dtype=I32, fill=torch.tensor(x, dtype=I32))   # noqa: E731
+    starts = [s * rows if abs(s) < 3 else s for s in (0, *starts[1:])] if starts[0] == 0 else list(starts)
+    seqs = sz.Sequences(g(2, 4, dtype=I32, fill=torch.full((2, 4), table) if table else torch.tensor([[0, 1, 2, 3], [4, 3, 2, 1]])), i32(*starts), i32(*lens), rows, 64)
+    new, back = ([g(n, heads, dim, dtype=torch.bfloat16, fill=torch.randn(n, heads, dim)) for _ in range(2)] for _ in range(2))
+    q, out = (g(n, 3 * heads, dim, dtype=torch.bfloat16, fill=torch.randn(n, 3 * heads, dim)) for _ in range(2))
+    sz.cache_write(*new, cache, seqs)
+    assert g.intact()
+    sz.cache_read(cache, seqs, *back)
+    assert g.intact()
+    for window in (0, 9):
+        workspace = g(sz.attention_workspace_bytes(cache, seqs, n, 3 * heads), dtype=torch.uint8)
+        sz.cache_attention(q, cache, seqs, out, workspace, sz.Attention(0.1, window=window), g(n, 3 * heads, dtype=torch.float32))
+        assert g.intact()
+    sz.cache_move(sz.KvCaches([cache]), seqs, g(2, 3, dtype=I32, fill=torch.tensor([[0, 1, 7], [1, 0, -1]])), n_rows=n)
+    assert g.intact()
