@@ -520,6 +520,48 @@ typedef struct {
   uint32_t max_len;              /* Larger ones in device memory are right, and slower. */
 } splitzip_seqs;
 
+/* The pages of a pool that no sequence has: a stack, d_free[0] to
+ * d_free[free - 1], the next one to be taken on top.  A program that starts
+ * fills it with all pages' numbers, and sets free to n_pages. */
+typedef struct {
+  int32_t free;     /* in and out; the others are what the last call did: */
+  int32_t status;   /* splitzip_allot_status, 0: taken as asked for */
+  int32_t lacking;  /* pages that there were too few of (SPLITZIP_ALLOT_PAGES) */
+  int32_t rows, max_rows, max_len;   /* rows of the step, the most of a sequence, and the longest sequence after it */
+  int32_t taken, given;              /* pages out of the pool, and back into it */
+} splitzip_pool_state;
+typedef enum {
+  SPLITZIP_ALLOT_PAGES = 1,  /* too few free pages */
+  SPLITZIP_ALLOT_ROWS = 2,   /* more than n_rows rows */
+  SPLITZIP_ALLOT_LENGTH = 4, /* a sequence longer than its row of the table, or than 2^30 */
+  SPLITZIP_ALLOT_POOL = 8    /* more pages than the pool has, or fewer than none */
+} splitzip_allot_status;
+typedef struct {
+  uint32_t* d_free;             /* n_pages */
+  splitzip_pool_state* d_state; /* both 4-byte aligned */
+  uint32_t n_pages;             /* below 2^31 */
+  uint32_t page_tokens;         /* a power of two, at least 8 */
+  uint64_t reserved;            /* 0 */
+} splitzip_pool;
+
+/* What the other calls of a step need, from what its requests ask for: sequence
+ * s keeps min(d_keep[s], d_lens[s]) of its tokens (all of them without d_keep;
+ * below 0: none) and gets d_rows[s] new ones (below 0: none).  Written are, in
+ * the buffers that seqs names: d_lens; d_starts; the table's entries for the
+ * pages that a sequence did not have -- pages that it no longer needs go back
+ * first, the first of them (by sequence, then by place) on top, and then pages
+ * are taken from the top in the same order, so that a step's pages go back as they
+ * lay --; and, for each of the step's rows, in n_rows entries each
+ * (nullable): d_slots, page * page_tokens + the place in the page, of its token;
+ * d_row_seqs, its sequence; d_positions, its token's number.  Entries behind
+ * the last row become -1.  A page belongs to one sequence.
+ * A step that cannot be taken (status) changes neither lengths, table nor pool;
+ * d_starts is all 0 then, so that the step's other calls have no rows.
+ * seqs needs a block table; its max_rows and max_len are not looked at.  One
+ * launch up to 4096 rows, else two. */
+int splitzip_cache_allot(const splitzip_pool* pool, const splitzip_seqs* seqs, const int32_t* d_rows, const int32_t* d_keep,
+                         int64_t* d_slots, int32_t* d_row_seqs, int32_t* d_positions, uint32_t n_rows, void* stream);
+
 /* d_k, d_v: n_rows rows of kv_heads x head_dim BF16 words, k_row_stride and
  * v_row_stride words apart (multiples of 8), 16-byte aligned; rows of more than
  * 2^31 bytes: SPLITZIP_ERR_UNSUPPORTED (queries as well).  One launch.
@@ -531,6 +573,42 @@ int splitzip_cache_write(const splitzip_cache* cache, const splitzip_seqs* seqs,
                          const void* d_v, uint64_t v_row_stride, uint32_t n_rows, void* stream);
 int splitzip_cache_read(const splitzip_cache* cache, const splitzip_seqs* seqs, void* d_k, uint64_t k_row_stride, void* d_v,
                         uint64_t v_row_stride, uint32_t n_rows, void* stream);
+
+/* Norms of the heads of Q and K and their rotation.  A head x of a row at
+ * position p, in 32 bits (the angle in 64) and rounded once:
+ *   norm:     x = x / sqrt(mean of x^2 + eps) * (weight + weight_offset)
+ *             (no weights: nothing is multiplied; magnitudes up to 2^60, as
+ *             their squares are summed in 32 bits)
+ *   rotation: the pairs (x[a], x[b]) of the first rotary_dim elements become
+ *             (x[a] c - x[b] s, x[b] c + x[a] s), c and s the cosine and sine
+ *             of p * d_freqs[i], times scaling; a = i, b = i + rotary_dim / 2,
+ *             or, interleaved, a = 2 i, b = 2 i + 1 */
+typedef struct {
+  const float* d_freqs;       /* rotary_dim / 2, radians per position */
+  const void* d_q_weight;     /* head_dim weights, BF16 or (weights_f32) float, 16-byte aligned, or NULL */
+  const void* d_k_weight;
+  const int32_t* d_positions; /* n_rows, from -2^30 to 2^30, or NULL: row i of a sequence is at d_lens[s] - T + i */
+  float scaling;
+  float eps;                  /* with norm a normal number > 0 */
+  float weight_offset;
+  uint32_t rotary_dim;        /* 0 to head_dim, a multiple of 16 */
+  uint32_t interleaved;       /* 0 or 1, as the next two */
+  uint32_t norm;
+  uint32_t weights_f32;
+  uint32_t reserved;          /* 0 */
+} splitzip_rotation;
+
+/* A step's projections, in one launch: Q is normed and rotated into d_q_out, K
+ * likewise into the cache (and, with d_k_out, as BF16 rows), V into the cache as
+ * it is: what splitzip_cache_write does, but that K is rounded to the cache's
+ * words from 32 bits.  Rows, strides and alignment are as there; q_heads is any
+ * number (0: no Q; then d_q and d_q_out are not looked at).  d_q_out may be d_q
+ * and d_k_out d_k, with the same stride; other overlaps are not allowed.  Rows in front of token 0 get their Q
+ * (and BF16 K) and are not written to the cache. */
+int splitzip_cache_append(const splitzip_cache* cache, const splitzip_seqs* seqs, const splitzip_rotation* how, const void* d_q,
+                          uint64_t q_row_stride, void* d_q_out, uint64_t q_out_row_stride, const void* d_k, uint64_t k_row_stride,
+                          const void* d_v, uint64_t v_row_stride, void* d_k_out, uint64_t k_out_row_stride, uint32_t n_rows,
+                          uint32_t q_heads, void* stream);
 
 /* What a row sees, and how scores are shaped.  With base = d_lens[s] - T:
  * tokens below base are seen by all rows of the sequence; token base + j by

@@ -24,6 +24,8 @@ STATUS_OVERFLOW = 1
 STATUS_BAD_STREAM = 2
 STATUS_INTERNAL = 4
 
+ALLOT_PAGES, ALLOT_ROWS, ALLOT_LENGTH, ALLOT_POOL = 1, 2, 4, 8   # what a step's status may have (splitzip_allot_status)
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
 
@@ -75,6 +77,21 @@ class _CSeqs(C.Structure):
                 ("n_seqs", C.c_uint32), ("max_rows", C.c_uint32), ("max_len", C.c_uint32)]
 
 
+class _CRotation(C.Structure):
+    _fields_ = [("d_freqs", C.c_void_p), ("d_q_weight", C.c_void_p), ("d_k_weight", C.c_void_p), ("d_positions", C.c_void_p),
+                ("scaling", C.c_float), ("eps", C.c_float), ("weight_offset", C.c_float), ("rotary_dim", C.c_uint32),
+                ("interleaved", C.c_uint32), ("norm", C.c_uint32), ("weights_f32", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class _CRotationOf(_CRotation):
+    """and how many elements its weights have and how many rows its positions (-1: none), which the calls compare with their tensors"""
+    _fields_ = [("dim", C.c_int64), ("position_rows", C.c_int64)]
+
+
+class _CPool(C.Structure):
+    _fields_ = [("d_free", C.c_void_p), ("d_state", C.c_void_p), ("n_pages", C.c_uint32), ("page_tokens", C.c_uint32), ("reserved", C.c_uint64)]
+
+
 class _CAttention(C.Structure):
     _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("d_slopes", C.c_void_p), ("d_tree", C.c_void_p),
                 ("d_positions", C.c_void_p), ("tree_words", C.c_uint32), ("window", C.c_uint32), ("reserved", C.c_uint64)]
@@ -94,6 +111,14 @@ class _CSeqsElsewhere(_CSeqs):
 
 
 class _CAttentionElsewhere(_CAttentionOf):
+    """the same"""
+
+
+class _CRotationElsewhere(_CRotationOf):
+    """the same"""
+
+
+class _CPoolElsewhere(_CPool):
     """the same"""
 
 
@@ -223,6 +248,10 @@ def lib():
         L.splitzip_attention_workspace_bytes.argtypes = [chp, sqp, C.c_uint32, C.c_uint32]
         L.splitzip_cache_attention.restype = i
         L.splitzip_cache_attention.argtypes = [chp, sqp, C.POINTER(_CAttention), vp, u64, vp, u64, vp, C.c_uint32, C.c_uint32, vp, sz, vp]
+        L.splitzip_cache_append.restype = i
+        L.splitzip_cache_append.argtypes = [chp, sqp, C.POINTER(_CRotation), *[vp, u64] * 5, C.c_uint32, C.c_uint32, vp]
+        L.splitzip_cache_allot.restype = i
+        L.splitzip_cache_allot.argtypes = [C.POINTER(_CPool), sqp, vp, vp, vp, vp, vp, C.c_uint32, vp]
         L.splitzip_cache_move.restype = i
         L.splitzip_cache_move.argtypes = [chp, C.c_uint32, sqp, vp, C.c_uint32, C.c_uint32, vp]
         L.fast, L.fast_cache = _short_way(L)
@@ -236,7 +265,7 @@ def _short_way(L):
     take a call."""
     try:
         from . import _fastcall   # torch's own libraries are loaded by now
-        of = _fastcall.bind(L._handle, _CCodebook, Variant, _CPaged, _CCache, _CSeqs, _CAttentionOf, torch.__version__)
+        of = _fastcall.bind(L._handle, _CCodebook, Variant, _CPaged, _CCache, _CSeqs, _CAttentionOf, _CRotationOf, _CPool, torch.__version__)
         cache = {name: of.pop(name) for name in list(of) if name.startswith("splitzip_cache_")}
         return types.SimpleNamespace(**of), types.SimpleNamespace(**cache)
     except ImportError as e:
@@ -1079,6 +1108,73 @@ class Attention:
                                0 if tree is None else tree.shape[1], window, 0, *(-1 if t is None else t.shape[0] for t in self._keep))
 
 
+class Rotation:
+    """splitzip_rotation: norms of the heads of Q and K (with eps) and their rotation by position (with freqs).
+
+    freqs: float32 [rotary_dim / 2], radians per position; q_weight, k_weight: [head_dim], both bfloat16 or both float32 (None: ones);
+    positions: int32 [n_rows] (contiguous, on the device; None: a row's token's number)."""
+
+    def __init__(self, freqs: torch.Tensor | None = None, interleaved: bool = False, scaling: float = 1.0, eps: float | None = None,
+                 q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, weight_offset: float = 0.0,
+                 positions: torch.Tensor | None = None):
+        if freqs is not None and (freqs.dim() != 1 or freqs.dtype != torch.float32 or not freqs.is_contiguous()):
+            raise ValueError("freqs must be contiguous float32 [rotary_dim / 2]")
+        weights = [w for w in (q_weight, k_weight) if w is not None]
+        if weights and eps is None:
+            raise ValueError("weights are a norm's, which has an eps")
+        if any(w.dim() != 1 or w.dtype not in (torch.bfloat16, torch.float32) or not w.is_contiguous() or w.shape != weights[0].shape
+               or w.dtype != weights[0].dtype for w in weights):
+            raise ValueError("weights must be contiguous [head_dim], both bfloat16 or both float32")
+        if positions is not None and (positions.dtype not in _INT32 or not positions.is_contiguous()):
+            raise ValueError("positions must be a contiguous tensor of 32-bit integers")
+        self._keep = (freqs, q_weight, k_weight, positions)
+        self._reached = _reached(*self._keep)
+        self.c = (_CRotationOf if self._reached else _CRotationElsewhere)(
+            *(_ptr(t) for t in self._keep), scaling, 0.0 if eps is None else eps, weight_offset, 0 if freqs is None else 2 * freqs.shape[0],
+            int(interleaved), int(eps is not None), int(bool(weights) and weights[0].dtype == torch.float32), 0,
+            weights[0].shape[0] if weights else -1, -1 if positions is None else positions.shape[0])
+
+
+class PagePool:
+    """splitzip_pool: the pages that no sequence has.
+
+    free: int32 [pages], the stack's entries; state: int32 [8], a splitzip_pool_state (POOL_STATE has its fields' names); both contiguous,
+    on the device."""
+
+    def __init__(self, free: torch.Tensor, state: torch.Tensor, page_tokens: int):
+        for t in (free, state):
+            if t.dim() != 1 or t.dtype not in _INT32 or not t.is_contiguous():
+                raise ValueError("free and state must be contiguous tensors of 32-bit integers")
+        if state.numel() != len(POOL_STATE):
+            raise ValueError(f"state must have {len(POOL_STATE)} entries")
+        self._keep = (free, state)
+        self._reached = _reached(*self._keep)
+        self.c = (_CPool if self._reached else _CPoolElsewhere)(free.data_ptr(), state.data_ptr(), free.numel(), page_tokens, 0)
+
+    @classmethod
+    def full(cls, pages: int, page_tokens: int, device="cuda") -> "PagePool":
+        """A pool that has all of its pages, page 0 on top."""
+        state = torch.zeros(len(POOL_STATE), dtype=torch.int32, device=device)
+        state[:1].fill_(pages)
+        return cls(torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device), state, page_tokens)
+
+    @property
+    def free(self) -> torch.Tensor:
+        return self._keep[0]
+
+    @property
+    def state(self) -> torch.Tensor:
+        return self._keep[1]
+
+
+POOL_STATE = ("free", "status", "lacking", "rows", "max_rows", "max_len", "taken", "given")
+
+
+def read_pool_state(pool: PagePool) -> dict:
+    """The pool's state on the host (waits for the device)."""
+    return dict(zip(POOL_STATE, pool.state.tolist()))
+
+
 def _rows(t: torch.Tensor, heads: int, dim: int, what: str) -> int:
     """words from row to row of a tensor [rows, heads, dim] of BF16 words"""
     if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype not in _WORDS[BF16] or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
@@ -1109,6 +1205,51 @@ def cache_read(cache: KvCache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor
     if rc != _NOT_TAKEN:
         return _check(rc, "splitzip_cache_read") if rc else None
     _write_or_read("splitzip_cache_read", cache, seqs, k, v, stream)
+
+
+def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, cache: KvCache, seqs: Sequences, how: Rotation,
+                 q_out: torch.Tensor | None, k_out: torch.Tensor | None = None, stream=None) -> None:
+    """splitzip_cache_append: the BF16 rows k [rows, kv_heads, head_dim], normed and rotated, and v become their sequences' last tokens;
+    q [rows, q_heads, head_dim] (None: none), normed and rotated, goes into q_out, which may be q itself, and k as BF16 into k_out."""
+    rc = (_lib or lib()).fast_cache.splitzip_cache_append(cache.c, seqs.c, how.c, q, q_out, k, v, k_out, None if stream is None else _handle(stream))
+    if rc != _NOT_TAKEN:
+        return _check(rc, "splitzip_cache_append") if rc else None
+    rows, heads, dim = k.shape[0], cache.kv_heads, cache.head_dim
+    ks, vs = _rows(k, heads, dim, "k"), _rows(v, heads, dim, "v")
+    kos = _rows(k_out, heads, dim, "k_out") if k_out is not None else 0
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None and q.dim() != 3:
+        raise ValueError("q must be [rows, q_heads, head_dim]")
+    q_heads = 0 if q is None else q.shape[1]
+    qs, qos = (0, 0) if q is None else (_rows(q, q_heads, dim, "q"), _rows(q_out, q_heads, dim, "q_out"))
+    if any(t is not None and t.shape[0] != rows for t in (q, q_out, v, k_out)):
+        raise ValueError("q, q_out, k, v and k_out must have the same number of rows")
+    if how.c.dim not in (-1, dim) or how.c.position_rows not in (-1, rows):
+        raise ValueError(f"weights must have {dim} entries, positions {rows}")
+    _need_reached(cache, seqs, how, q, q_out, k, v, k_out)
+    _check(lib().splitzip_cache_append(C.byref(cache.c), C.byref(seqs.c), C.byref(how.c), _ptr(q), qs, _ptr(q_out), qos, k.data_ptr(), ks, v.data_ptr(), vs,
+                                       _ptr(k_out), kos, rows, q_heads, _stream_ptr(stream)), "splitzip_cache_append")
+
+
+def cache_allot(pool: PagePool, seqs: Sequences, rows: torch.Tensor, keep: torch.Tensor | None = None, slots: torch.Tensor | None = None,
+                row_seqs: torch.Tensor | None = None, positions: torch.Tensor | None = None, stream=None) -> None:
+    """splitzip_cache_allot: sequence s keeps keep[s] tokens (None: all) and gets rows[s] more (int32 [n_seqs]); the block table, starts and
+    lens that seqs was made of are written, and for each row of the step its slot (int64), sequence and position (int32; [n_rows] all, None: not
+    wanted).  The pool's state says what became of it."""
+    rc = (_lib or lib()).fast_cache.splitzip_cache_allot(pool.c, seqs.c, rows, keep, slots, row_seqs, positions, None if stream is None else _handle(stream))
+    if rc != _NOT_TAKEN:
+        return _check(rc, "splitzip_cache_allot") if rc else None
+    for t, what in ((rows, "rows"), (keep, "keep")):
+        if t is not None and (t.dim() != 1 or t.shape[0] != seqs.c.n_seqs or t.dtype not in _INT32 or not t.is_contiguous()):
+            raise ValueError(f"{what} must be a contiguous tensor [n_seqs] of 32-bit integers")
+    n_rows = {t.shape[0] for t in (slots, row_seqs, positions) if t is not None and t.dim() == 1}
+    for t, types in ((slots, _INT64), (row_seqs, _INT32), (positions, _INT32)):
+        if t is not None and (t.dim() != 1 or t.dtype not in types or not t.is_contiguous() or len(n_rows) != 1):
+            raise ValueError("slots must be a contiguous tensor [n_rows] of 64-bit integers, row_seqs and positions as many of 32 bits")
+    _need_reached(pool, seqs, rows, keep, slots, row_seqs, positions)
+    _check(lib().splitzip_cache_allot(C.byref(pool.c), C.byref(seqs.c), rows.data_ptr(), _ptr(keep), _ptr(slots), _ptr(row_seqs), _ptr(positions),
+                                      n_rows.pop() if n_rows else _MOST_ROWS, _stream_ptr(stream)), "splitzip_cache_allot")
 
 
 def attention_workspace_bytes(cache: KvCache, seqs: Sequences, n_rows: int, q_heads: int) -> int:

@@ -2,6 +2,8 @@
 // written, and attention over it -- and the host side of their kernels.  The kernels live in the headers included below:
 //   common.hpp      byte permutes and vector types shared with the codec
 //   cache.hpp       where the words of a token are; writing, reading back, moving an accepted path
+//   allot.hpp       pages for a step's rows: tables, lengths and slots by what its requests ask for
+//   append.hpp      norms and rotation of Q and K on the way there
 //   attention.hpp   attention of a step's rows, one token or a tree of drafted ones, over everything cached
 #include <float.h>
 #include <hip/hip_runtime.h>
@@ -16,6 +18,8 @@ namespace {
 
 #include "common.hpp"
 #include "cache.hpp"
+#include "allot.hpp"
+#include "append.hpp"
 #include "attention.hpp"
 
 bool aligned16(uint64_t x) { return (x & 15u) == 0; }
@@ -166,6 +170,15 @@ int rows_call(const splitzip_cache* c, const splitzip_seqs* q, void* d_k, uint64
   return by_kind<F>(c, dim3((unsigned)wgs, q->n_seqs), bytes >= kStreamed, static_cast<hipStream_t>(stream), (const RowsArgs*)&a);
 }
 
+template <int KIND, int D>
+struct Append {
+  static int run(dim3 grid, bool several, hipStream_t st, const AppendArgs* a) {
+    if (several) hipLaunchKernelGGL((cache_append_kernel<KIND, D, kAppendHeads>), grid, dim3(kThreads), 0, st, *a);
+    else hipLaunchKernelGGL((cache_append_kernel<KIND, D, 1>), grid, dim3(kThreads), 0, st, *a);
+    return launched();
+  }
+};
+
 // How an attention call is cut: which kernel, the rows of a (sequence, head of the cache) into tiles, the tokens of all sequences
 // into blocks and these into shares.
 struct AttentionPlan {
@@ -267,6 +280,93 @@ int splitzip_cache_write(const splitzip_cache* cache, const splitzip_seqs* seqs,
 int splitzip_cache_read(const splitzip_cache* cache, const splitzip_seqs* seqs, void* d_k, uint64_t k_row_stride, void* d_v, uint64_t v_row_stride,
                         uint32_t n_rows, void* stream) {
   return rows_call<Read>(cache, seqs, d_k, k_row_stride, d_v, v_row_stride, n_rows, stream);
+}
+
+int splitzip_cache_allot(const splitzip_pool* pool, const splitzip_seqs* seqs, const int32_t* d_rows, const int32_t* d_keep, int64_t* d_slots,
+                         int32_t* d_row_seqs, int32_t* d_positions, uint32_t n_rows, void* stream) {
+  if (!pool || pool->reserved || !pool->d_free || !pool->d_state || !aligned(pool->d_free, 4) || !aligned(pool->d_state, 4)) return SPLITZIP_ERR_INVALID_ARG;
+  if (!pool->n_pages || pool->page_tokens < 8 || pool->page_tokens > kMostTokens || (pool->page_tokens & (pool->page_tokens - 1))) return SPLITZIP_ERR_INVALID_ARG;
+  if (!seqs || !seqs->n_seqs) return seqs ? SPLITZIP_OK : SPLITZIP_ERR_INVALID_ARG;
+  if (seqs->n_seqs > kMostSeqs || n_rows > kMostTokens || pool->n_pages >> 31) return SPLITZIP_ERR_UNSUPPORTED;
+  if (!seqs->d_block_table || !seqs->table_stride || !seqs->d_starts || !seqs->d_lens || !d_rows) return SPLITZIP_ERR_INVALID_ARG;
+  if (!aligned(seqs->d_block_table, 4) || !aligned(seqs->d_starts, 4) || !aligned(seqs->d_lens, 4) || !aligned(d_rows, 4) || !aligned(d_keep, 4)) return SPLITZIP_ERR_INVALID_ARG;
+  if (!aligned(d_slots, 8) || !aligned(d_row_seqs, 4) || !aligned(d_positions, 4)) return SPLITZIP_ERR_INVALID_ARG;
+  AllotArgs a;
+  a.table = const_cast<uint32_t*>(seqs->d_block_table);
+  a.starts = const_cast<int32_t*>(seqs->d_starts);
+  a.lens = const_cast<int32_t*>(seqs->d_lens);
+  a.rows = d_rows;
+  a.keep = d_keep;
+  a.stack = pool->d_free;
+  a.state = reinterpret_cast<int32_t*>(pool->d_state);
+  a.slots = d_slots;
+  a.row_seqs = d_row_seqs;
+  a.positions = d_positions;
+  a.table_stride = seqs->table_stride;
+  a.n_seqs = seqs->n_seqs;
+  const uint64_t reach = (uint64_t)seqs->table_stride * pool->page_tokens;
+  a.capacity = (uint32_t)(reach < kMostTokens ? reach : kMostTokens);
+  a.n_pages = pool->n_pages;
+  a.n_rows = n_rows;
+  a.page_shift = 31u - (uint32_t)__builtin_clz(pool->page_tokens);
+  const bool fills = n_rows && (d_slots || d_row_seqs || d_positions);
+  a.fill = fills && n_rows <= kRowsHere;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(cache_allot_kernel, dim3(1), dim3(kAllotThreads), 0, st, a);
+  if (fills && !a.fill) hipLaunchKernelGGL(cache_allot_fill_kernel, dim3((n_rows + kFillRows - 1) / kFillRows), dim3(kThreads), 0, st, a);
+  return launched();
+}
+
+int splitzip_cache_append(const splitzip_cache* cache, const splitzip_seqs* seqs, const splitzip_rotation* how, const void* d_q, uint64_t q_row_stride,
+                          void* d_q_out, uint64_t q_out_row_stride, const void* d_k, uint64_t k_row_stride, const void* d_v, uint64_t v_row_stride,
+                          void* d_k_out, uint64_t k_out_row_stride, uint32_t n_rows, uint32_t q_heads, void* stream) {
+  int rc = check_cache(cache, true);
+  if (rc == SPLITZIP_OK) rc = check_seqs(cache, seqs);
+  if (rc != SPLITZIP_OK) return rc;
+  if (!how || how->interleaved > 1 || how->norm > 1 || how->weights_f32 > 1 || how->reserved) return SPLITZIP_ERR_INVALID_ARG;
+  if (how->rotary_dim > cache->head_dim || how->rotary_dim % 16 || (how->rotary_dim && (!how->d_freqs || !aligned(how->d_freqs, 4)))) return SPLITZIP_ERR_INVALID_ARG;
+  if (how->norm && !(how->eps >= FLT_MIN && how->eps <= FLT_MAX)) return SPLITZIP_ERR_INVALID_ARG;
+  if (!aligned16(how->d_q_weight) || !aligned16(how->d_k_weight) || !aligned(how->d_positions, 4)) return SPLITZIP_ERR_INVALID_ARG;
+  if (!seqs->n_seqs || !n_rows) return SPLITZIP_OK;
+  const uint64_t elems = (uint64_t)cache->kv_heads * cache->head_dim, q_elems = (uint64_t)q_heads * cache->head_dim;
+  if (n_rows > kMostTokens || elems * 2 > kMostRow || q_elems * 2 > kMostRow) return SPLITZIP_ERR_UNSUPPORTED;
+  if (!rows_ok(d_k, k_row_stride, elems) || !rows_ok(d_v, v_row_stride, elems) || (d_k_out && !rows_ok(d_k_out, k_out_row_stride, elems))) return SPLITZIP_ERR_INVALID_ARG;
+  if (q_heads && (!rows_ok(d_q, q_row_stride, q_elems) || !rows_ok(d_q_out, q_out_row_stride, q_elems))) return SPLITZIP_ERR_INVALID_ARG;
+  if ((d_q == d_q_out && q_heads && q_row_stride != q_out_row_stride) || (d_k == d_k_out && k_row_stride != k_out_row_stride)) return SPLITZIP_ERR_INVALID_ARG;
+  AppendArgs a;
+  a.cache = device_cache(cache, seqs);
+  a.seqs = device_seqs(cache, seqs, n_rows);
+  a.q = static_cast<const uint8_t*>(d_q);
+  a.k = static_cast<const uint8_t*>(d_k);
+  a.v = static_cast<const uint8_t*>(d_v);
+  a.q_out = static_cast<uint8_t*>(d_q_out);
+  a.k_out = static_cast<uint8_t*>(d_k_out);
+  a.q_stride = 2 * q_row_stride;
+  a.k_stride = 2 * k_row_stride;
+  a.v_stride = 2 * v_row_stride;
+  a.q_out_stride = 2 * q_out_row_stride;
+  a.k_out_stride = 2 * k_out_row_stride;
+  a.freqs = how->d_freqs;
+  a.q_weight = how->d_q_weight;
+  a.k_weight = how->d_k_weight;
+  a.positions = how->d_positions;
+  a.scaling = how->scaling;
+  a.eps = how->eps;
+  a.weight_offset = how->weight_offset;
+  a.q_heads = q_heads;
+  a.rotary = how->rotary_dim;
+  a.interleaved = how->interleaved;
+  a.norm = how->norm;
+  a.weights_f32 = how->weights_f32;
+  // a workgroup for every 16 heads of 128 of a row, or, where that is more of them than the chip holds, for four times as many
+  const uint64_t rows = !seqs->max_rows ? 1 : seqs->max_rows < n_rows ? seqs->max_rows : n_rows, cus = (uint64_t)cu_count(), per = 8 * kThreads / cache->head_dim;
+  const uint64_t heads = (uint64_t)q_heads + 2 * (uint64_t)cache->kv_heads, single = (heads + per - 1) / per;
+  const bool several = rows * single * seqs->n_seqs > 8 * cus && single > 1;
+  const uint64_t chunks = several ? (single + kAppendHeads - 1) / kAppendHeads : single;
+  const uint64_t most = (8 * cus + seqs->n_seqs - 1) / seqs->n_seqs;   // of a sequence
+  const uint64_t across = rows * chunks <= most ? rows : most <= chunks ? 1 : most / chunks;
+  a.chunks = (uint32_t)chunks;
+  return by_kind<Append>(cache, dim3((unsigned)(across * chunks), seqs->n_seqs), several, static_cast<hipStream_t>(stream), (const AppendArgs*)&a);
 }
 
 size_t splitzip_attention_workspace_bytes(const splitzip_cache* cache, const splitzip_seqs* seqs, uint32_t n_rows, uint32_t q_heads) {

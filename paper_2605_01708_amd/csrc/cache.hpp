@@ -132,16 +132,16 @@ __device__ inline int scale_byte(uint32_t f) {
   return f && e > -127 ? e + 127 : 0;
 }
 
-// 8 BF16 words times 2^(127 - byte), rounded to FP8: 8 bytes.  2^(127 - byte) as two factors, each a normal number.
+// 8 numbers times 2^(127 - byte), rounded to FP8: 8 bytes.  2^(127 - byte) as two factors, each a normal number.  (What the first of them takes
+// below 32 bits' normal numbers is far below FP8's least.)
 template <int KIND>
-__device__ inline u32x2 to_fp8(const u32x4& w, int byte) {
+__device__ inline u32x2 to_fp8(const float (&y)[8], int byte) {
   const int up = 127 - byte, half = up / 2;
   const float a = __uint_as_float((uint32_t)(127 + half) << 23), b = __uint_as_float((uint32_t)(127 + up - half) << 23);
   u32x2 out;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const float x0 = __uint_as_float(w[2 * i] << 16) * a * b, x1 = __uint_as_float(w[2 * i] & 0xffff0000u) * a * b;
-    const float x2 = __uint_as_float(w[2 * i + 1] << 16) * a * b, x3 = __uint_as_float(w[2 * i + 1] & 0xffff0000u) * a * b;
+    const float x0 = y[4 * i] * a * b, x1 = y[4 * i + 1] * a * b, x2 = y[4 * i + 2] * a * b, x3 = y[4 * i + 3] * a * b;
     int d = 0;
     if constexpr (KIND == SPLITZIP_FP8_E5M2) {
       d = __builtin_amdgcn_cvt_pk_bf8_f32(x0, x1, d, false);
@@ -153,6 +153,13 @@ __device__ inline u32x2 to_fp8(const u32x4& w, int byte) {
     out[i] = (uint32_t)d;
   }
   return out;
+}
+__device__ inline void floats_of(const u32x4& w, float (&y)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[2 * i] = __uint_as_float(w[i] << 16);
+    y[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
 }
 
 // The words of a pair of bytes (the low or the high two of a register) times 2^(byte - 127), rounded to BF16.  The instruction takes the
@@ -194,8 +201,17 @@ __device__ inline u32x4 from_fp4(uint32_t w, uint32_t byte) {
   return u32x4{fp4_pair_to_bf16(w, byte, 0), fp4_pair_to_bf16(w, byte, 1), fp4_pair_to_bf16(w, byte, 2), fp4_pair_to_bf16(w, byte, 3)};
 }
 
-// 8 BF16 words times 2^(127 - byte), rounded once to 4-bit words, to nearest, ties to even; the even element in a byte's low half.  The
+// 8 numbers times 2^(127 - byte), rounded once to 4-bit words, to nearest, ties to even; the even element in a byte's low half.  The
 // instruction divides by the power in its exponent field; what a group without infinities and NaN holds fits the format.
+__device__ inline uint32_t to_fp4(const float (&y)[8], int byte) {
+  const float power = __uint_as_float((uint32_t)byte << 23);
+  uint32_t d = 0;
+  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, y[0], y[1], power, 0);
+  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, y[2], y[3], power, 1);
+  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, y[4], y[5], power, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, y[6], y[7], power, 3);
+}
+// the same of 8 BF16 words
 __device__ inline uint32_t to_fp4(const u32x4& w, int byte) {
   const float power = __uint_as_float((uint32_t)byte << 23);
   const auto pair = [&](int i) {
@@ -234,7 +250,9 @@ __device__ inline Lane8<KIND> quantised(const u32x4& w, int& byte) {
     return to_fp4(w, byte);
   } else {
     byte = scale_byte<KIND>(largest_of_group<KIND, D>(largest8(w)) << 16);
-    return to_fp8<KIND>(w, byte);
+    float y[8];
+    floats_of(w, y);
+    return to_fp8<KIND>(y, byte);
   }
 }
 template <int KIND>

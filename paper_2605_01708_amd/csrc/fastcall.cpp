@@ -61,14 +61,18 @@ struct Caller<int(A...)> {
 //   X  rows of the cache's heads, a tensor [rows, heads, head_dim] of BF16 words: address, words from row to row
 //   Q  rows of query heads, the same                      O  as many of the same heads, to be written
 //   L  a float32 tensor [rows, query heads], or None: its address
-//   n  no argument: the rows of the tensors above         e  no argument: their query heads
+//   x  rows of the cache's heads, or None: the same, or two nulls
+//   n  no argument: the rows of the tensors above, 2^30 if there are none         e  no argument: their query heads
+//   r  a rotation's description: its address              p  that of a pool
+//   U  32-bit integers, a tensor [sequences]: its address               u  the same, or None: null
+//   M  64-bit integers, a tensor [rows], or None: its address           m  the same of 32-bit integers
 //   T  a path, a tensor [sequences, entries] of 32-bit integers: address, entries
 //   S  a stream's handle, or None: the current one
 constexpr bool in(const char* set, char c) { return *set && (*set == c || in(set + 1, c)); }
 constexpr int count(const char* spec, const char* twice, const char* never = "") {
   return *spec ? (in(twice, *spec) ? 2 : in(never, *spec) ? 0 : 1) + count(spec + 1, twice, never) : 0;
 }
-constexpr bool known(const char* spec) { return !*spec || (in("WPZzRYINDAGCKVScqhXQOLneT", *spec) && known(spec + 1)); }
+constexpr bool known(const char* spec) { return !*spec || (in("WPZzRYINDAGCKVScqhXQOLneTxrpUuMm", *spec) && known(spec + 1)); }
 struct Entry {
   const char* name;
   const char* spec;
@@ -99,19 +103,21 @@ constexpr Entry kEntries[] = {
     ENTRY(splitzip_cache_read, "cqXXnS"),
     ENTRY(splitzip_cache_attention, "cqhQOLneRS"),
     ENTRY(splitzip_cache_move, "AIqTIS"),
+    ENTRY(splitzip_cache_append, "cqrQOXXxneS"),
+    ENTRY(splitzip_cache_allot, "pqUuMmmnS"),
 };
 #undef ENTRY
 constexpr bool fit(size_t k) {
-  return k == 0 || (known(kEntries[k - 1].spec) && count(kEntries[k - 1].spec, "WRCXQOT") == kEntries[k - 1].n_words && fit(k - 1));
+  return k == 0 || (known(kEntries[k - 1].spec) && count(kEntries[k - 1].spec, "WRCXQOTx") == kEntries[k - 1].n_words && fit(k - 1));
 }
 static_assert(fit(sizeof kEntries / sizeof kEntries[0]), "a letter for every argument of the library's functions");
 
 // the binding's ctypes structures, as bind was given them
 struct Types {
-  PyObject *codebook, *variant, *paged, *cache, *seqs, *attention;
+  PyObject *codebook, *variant, *paged, *cache, *seqs, *attention, *rotation, *pool;
   template <typename F>
   void each(F f) const {
-    for (PyObject* t : {codebook, variant, paged, cache, seqs, attention}) f(t);
+    for (PyObject* t : {codebook, variant, paged, cache, seqs, attention, rotation, pool}) f(t);
   }
 };
 // the binding's description of an attention goes on behind the library's: how many entries its slopes, its tree and its positions have,
@@ -119,6 +125,11 @@ struct Types {
 struct Attention {
   splitzip_attention how;
   int64_t heads, tree_rows, position_rows;
+};
+// that of a rotation: elements of its weights, rows of its positions
+struct Rotation {
+  splitzip_rotation how;
+  int64_t dim, position_rows;
 };
 struct Bound {
   void* fn;
@@ -180,12 +191,13 @@ bool run(const Bound& b, PyObject* const* a, Py_ssize_t n_args, int* rc) {
   const splitzip_cache* cache = nullptr;
   const splitzip_seqs* seqs = nullptr;
   const Attention* how = nullptr;
-  int64_t rows = -1, heads = 0;   // of the tensors of rows
+  const Rotation* rotation = nullptr;
+  int64_t rows = -1, heads = 0;   // of the tensors of rows: rows, query heads
   const auto word = [&](uint64_t x) { w[n++] = x; };
   const auto address = [](const void* p) { return static_cast<uint64_t>(reinterpret_cast<uintptr_t>(p)); };
   for (const char* s = b.entry->spec; *s; ++s) {
     if (*s == 'n' || *s == 'e') {
-      word(static_cast<uint64_t>(*s == 'n' ? rows : heads));
+      word(static_cast<uint64_t>(*s == 'e' ? heads : rows >= 0 ? rows : int64_t(1) << 30));
       continue;
     }
     PyObject* o = *a++;
@@ -284,15 +296,60 @@ bool run(const Bound& b, PyObject* const* a, Py_ssize_t n_args, int* rc) {
         word(address(how));
         break;
       }
+      case 'r': {
+        rotation = static_cast<const Rotation*>(views.of(o, b.types.rotation, sizeof(Rotation)));
+        if (!rotation || (rotation->dim >= 0 && rotation->dim != static_cast<int64_t>(cache->head_dim))) return false;
+        word(address(rotation));
+        break;
+      }
+      case 'p': {
+        const void* p = views.of(o, b.types.pool, sizeof(splitzip_pool));
+        if (!p) return false;
+        word(address(p));
+        break;
+      }
+      case 'U':
+      case 'u': {
+        if (*s == 'u' && o == Py_None) {
+          word(0);
+          break;
+        }
+        const at::Tensor* t = tensor(o);
+        if (!t || t->dim() != 1 || (t->scalar_type() != at::kInt && t->scalar_type() != at::kUInt32) || !t->is_contiguous() || t->size(0) != static_cast<int64_t>(seqs->n_seqs)) return false;
+        word(address(t->data_ptr()));
+        break;
+      }
+      case 'M':
+      case 'm': {
+        if (o == Py_None) {
+          word(0);
+          break;
+        }
+        const at::Tensor* t = tensor(o);
+        if (!t || t->dim() != 1 || !t->is_contiguous() || (rows >= 0 && t->size(0) != rows)) return false;
+        const at::ScalarType type = t->scalar_type();
+        if (*s == 'M' ? type != at::kLong && type != at::kUInt64 : type != at::kInt && type != at::kUInt32) return false;
+        rows = t->size(0);
+        word(address(t->data_ptr()));
+        break;
+      }
+      case 'x':
+        if (o == Py_None) {
+          word(0);
+          word(0);
+          break;
+        }
+        [[fallthrough]];
       case 'X':
       case 'Q':
       case 'O': {
         const at::Tensor* t = tensor(o);
-        if (*s == 'X') heads = cache->kv_heads;
-        else if (*s == 'Q' && t && t->dim() == 3) heads = t->size(1);
-        if (!rows_of(t, heads, cache->head_dim, &v) || (rows >= 0 && t->size(0) != rows)) return false;
+        const bool of_cache = *s == 'X' || *s == 'x';
+        if (*s == 'Q' && t && t->dim() == 3) heads = t->size(1);
+        if (!rows_of(t, of_cache ? static_cast<int64_t>(cache->kv_heads) : heads, cache->head_dim, &v) || (rows >= 0 && t->size(0) != rows)) return false;
         rows = t->size(0);
-        if (*s == 'Q' && ((how->heads >= 0 && how->heads != heads) || (how->tree_rows >= 0 && how->tree_rows != rows) ||
+        if (*s == 'Q' && rotation && rotation->position_rows >= 0 && rotation->position_rows != rows) return false;
+        if (*s == 'Q' && how && ((how->heads >= 0 && how->heads != heads) || (how->tree_rows >= 0 && how->tree_rows != rows) ||
                           (how->position_rows >= 0 && how->position_rows != rows))) return false;
         word(address(t->data_ptr()));
         word(v);
@@ -349,14 +406,15 @@ void forget(PyObject* capsule) {
   delete b;
 }
 
-// bind(handle, codebook, variant, paged, cache, seqs, attention, torch): the entry points of the library that ctypes holds by this handle, name ->
+// bind(handle, codebook, variant, paged, cache, seqs, attention, rotation, pool, torch): the entry points of the library that ctypes holds by this handle, name ->
 // function, for the binding's structures of these types; an ImportError if the torch of this version is not the one that
 // this was built for (torch's headers read the fields of its tensors)
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject* handle = nullptr;
   Types types;
   const char* torch_version = nullptr;
-  if (!PyArg_ParseTuple(args, "OOOOOOOs", &handle, &types.codebook, &types.variant, &types.paged, &types.cache, &types.seqs, &types.attention, &torch_version))
+  if (!PyArg_ParseTuple(args, "OOOOOOOOOs", &handle, &types.codebook, &types.variant, &types.paged, &types.cache, &types.seqs, &types.attention, &types.rotation,
+                        &types.pool, &torch_version))
     return nullptr;
   if (strcmp(torch_version, BUILT_FOR_TORCH) != 0) {
     PyErr_Format(PyExc_ImportError, "_fastcall was built for torch %s, this is %s", BUILT_FOR_TORCH, torch_version);
@@ -393,7 +451,7 @@ PyObject* bind(PyObject*, PyObject* args) {
   return out;
 }
 
-PyMethodDef kMethods[] = {{"bind", bind, METH_VARARGS, "bind(handle, codebook, variant, paged, cache, seqs, attention, torch): {name: function} for a libsplitzip.so that is loaded"}, {nullptr, nullptr, 0, nullptr}};
+PyMethodDef kMethods[] = {{"bind", bind, METH_VARARGS, "bind(handle, codebook, variant, paged, cache, seqs, attention, rotation, pool, torch): {name: function} for a libsplitzip.so that is loaded"}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
