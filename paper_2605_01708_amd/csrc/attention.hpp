@@ -557,39 +557,29 @@ __device__ inline float one_over(float total) { return total != 0.0f ? 1.0f / to
 // Bound by memory where there is enough to read: 64 sequences of 700 to 8192 tokens, 8 heads of 128 in BF16, 1.17 GB in 180 us (6.5 TB/s; reading
 // alone reaches 7.1).  Short of that by what a launch has before its first and behind its last load (the tables' and lengths' way to the first
 // address 5 us, the join 5 to 7): 131072 tokens of E4M3, 270 MB, in 51 and 6 us.
-constexpr uint32_t stage_tokens(uint32_t dtype, uint32_t row_bytes) {
-  return 8192 / row_bytes < 32 ? 32 : dtype == SPLITZIP_FP4_E2M1 ? 64 : 8192 / row_bytes;
-}
 template <int KIND, int D>
 struct Stream {
-  // A stage is 16 KB per wave, two workgroups per CU (32 tokens of 256 BF16 elements: 32 KB, one), of 4-bit words 64 tokens.
-  static constexpr int kRow = D * kBits<KIND> / 8;                       // bytes of a token
-  static constexpr int kTokens = (int)stage_tokens(KIND, kRow);                // of a stage
+  // A stage is 16 KB per wave, two workgroups per CU (32 tokens of 256 BF16 elements: 32 KB, one).
+  static constexpr int ES = KIND == SPLITZIP_BF16 ? 2 : 1;
+  static constexpr int kRow = D * ES;                                    // bytes of a token
+  static constexpr int kTokens = 16384 / (2 * kRow) < 32 ? 32 : 16384 / (2 * kRow);   // of a stage
   static constexpr int kHalf = kTokens * kRow;                           // bytes of K, or V, of a stage
   static constexpr int kSteps = kTokens / (int)kStep;
   static constexpr int kUnits = kRow / 16;                               // 16-byte units of a row
   static constexpr int KS = D / 32, DV = D / 16;
-  static constexpr int KB = kRow / 4 < 16 ? kRow / 4 : 16;               // bytes of a row of K that a lane takes at a time, and how often
-  static constexpr int KW = kRow / 4 / KB;
-  static constexpr int VB = kRow / 16;                                   // bytes of a token of V per lane
-  static constexpr int VW = (VB + 3) / 4;
-  typedef typename std::conditional<KB == 16, u32x4, u32x2>::type KPart;
-  // scales of a token of K per lane: the lane's bytes of a row are of KG groups (FP8: the row's one), and which group they are of
-  static constexpr int KG = KIND == SPLITZIP_FP4_E2M1 ? KW : 1;
-  __device__ static uint32_t k_group(int i, uint32_t g) { return KIND == SPLITZIP_FP4_E2M1 ? (KB == 16 ? 4 * i + g : g / 2) : 0; }
-  __device__ static uint32_t v_group(uint32_t m) { return KIND == SPLITZIP_FP4_E2M1 ? m * DV / kGroup4 : 0; }
+  static constexpr int KW = KS * ES / 2;                                 // units of a row of K per lane
+  static constexpr int VB = DV * ES;                                     // bytes of a token of V per lane
+  static constexpr int VW = VB / 4;
 
   // Rows of K lie in the order of the tokens, their units permuted so that the 16 rows of an operand (of the tile's row m: token
-  // 8 (m / 4) + m % 4, the other tile's 4 further) lie in 16 different units of the banks.  Rows of 32 bytes: eight of them are all banks, so
-  // that those of the second and fourth eight change places four by four.
+  // 8 (m / 4) + m % 4, the other tile's 4 further) lie in 16 different units of the banks.
   __device__ static uint32_t k_key(uint32_t token) {
     const uint32_t mi = token / 8 % 4 * 4 + token % 4;
     return kUnits >= 16 ? mi : mi / (16 / kUnits);
   }
-  __device__ static uint32_t k_row(uint32_t token) { return kUnits == 2 ? token ^ (token / 8 & 1) * 4 : token; }
-  // Rows of V, four of which (one of each eight) are read at a time: those of the second and fourth eight in pairs the other way round where a row
-  // is half of the banks, of each eight in another order where it is a quarter or less.
-  __device__ static uint32_t v_row(uint32_t token) { return kUnits == 8 ? token ^ (token / 8 & 1) : KIND == SPLITZIP_FP4_E2M1 ? token ^ (token / 8 & 3) : token; }
+  // Rows of V: those of the second and fourth eight in pairs the other way round where four of them (one of each eight) are read at a time
+  // and a row is half of the banks.
+  __device__ static uint32_t v_row(uint32_t token) { return kUnits == 8 ? token ^ (token / 8 & 1) : token; }
 
   // asks for the stage from token t0 on; pages: lane l has the page of its 8 l-th token
   __device__ static void ask(const Cache& c, const Pages& at_pages, const uint8_t* k_base, const uint8_t* v_base, uint32_t pages, int t0,
@@ -603,7 +593,7 @@ struct Stream {
       if constexpr (kUnits >= 8) page = (uint32_t)__builtin_amdgcn_readlane((int)pages, i * 64 / kUnits / 8);
       else page = (uint32_t)__shfl((int)pages, (int)(row / 8));
       const uint64_t from = token_offset(c, page, at_pages.place(min((uint32_t)t0 + 8 * eight, last8)));
-      const uint32_t k_off = k_row(row) % 8 * c.token_stride + (at ^ k_key(k_row(row))) * 16;
+      const uint32_t k_off = row % 8 * c.token_stride + (at ^ k_key(row)) * 16;
       const uint32_t v_off = v_row(row) % 8 * c.token_stride + at * 16;
       load_to_lds(k_base + from + k_off, lds + i * 1024);
       load_to_lds(v_base + from + v_off, lds + kHalf + i * 1024);
@@ -611,11 +601,71 @@ struct Stream {
   }
 };
 
+// The waves of a head (two or four of the workgroup's) together, and what they have of their rows to where it goes.  Lane (m, g) has elements
+// D / 16 (4 g + i) + j of row m in acc[j][i].  room: 4 D bytes times 16 of LDS for each wave, room_bytes apart.
+template <int D>
+__device__ inline void finish_tokens(const Share& w, State<D, 1>& st, uint8_t* room, uint32_t room_bytes, float (*stat)[16][2], uint32_t wave, uint32_t lane, uint32_t hw) {
+  constexpr int DV = D / 16;
+  const uint32_t tw = kWaves / hw, turn = wave / hw, m = lane % 16, g = lane / 16;
+  float total = st.total(0);
+  if (g == 0) {
+    stat[wave][m][0] = st.top[0];
+    stat[wave][m][1] = total;
+  }
+  f32x4* out = reinterpret_cast<f32x4*>(room + wave * room_bytes) + lane;
+#pragma unroll
+  for (int j = 0; j < DV; ++j) out[64 * j] = st.acc[0][j];
+  lds_barrier();
+  if (turn == 0) {
+    float high = st.top[0];
+    for (uint32_t v = 1; v < tw; ++v) high = fmaxf(high, stat[wave + v * hw][m][0]);
+    const float f0 = __builtin_amdgcn_exp2f(st.top[0] - high);
+    st.top[0] = high;
+    total *= f0;
+#pragma unroll
+    for (int j = 0; j < DV; ++j) st.acc[0][j] *= f0;
+    for (uint32_t v = 1; v < tw; ++v) {
+      const float f = __builtin_amdgcn_exp2f(stat[wave + v * hw][m][0] - high);
+      total += f * stat[wave + v * hw][m][1];
+      const f32x4* from = reinterpret_cast<const f32x4*>(room + (wave + v * hw) * room_bytes) + lane;
+#pragma unroll
+      for (int j = 0; j < DV; ++j) st.acc[0][j] += f * from[64 * j];
+    }
+  }
+  lds_barrier();   // (the next tile of rows writes there)
+  const uint32_t at = w.tile * 16 + m;
+  if (turn != 0 || at >= w.rows) return;
+  const AttentionArgs a = args_again();
+  const uint32_t q_heads = a.cache.heads * a.group, h = w.head * a.group + at % a.group;
+  const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(at / a.group));
+  if (w.whole) {
+    const float f = one_over(total);
+    uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + 4 * DV * g);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < DV; j += 4)
+        *reinterpret_cast<u32x2*>(to + 2 * (DV * i + j)) = u32x2{bf16_pair(st.acc[0][j][i] * f, st.acc[0][j + 1][i] * f), bf16_pair(st.acc[0][j + 2][i] * f, st.acc[0][j + 3][i] * f)};
+    if (g == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(st.top[0], total);
+  } else {
+    const uint64_t place = w.place(a, wave % hw, m);
+    float* to = a.part_out + place * D + 4 * DV * g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < DV; j += 4)
+        *reinterpret_cast<f32x4*>(to + DV * i + j) = f32x4{st.acc[0][j][i], st.acc[0][j + 1][i], st.acc[0][j + 2][i], st.acc[0][j + 3][i]};
+    if (g == 0) {
+      a.part_stat[2 * place] = st.top[0];
+      a.part_stat[2 * place + 1] = total;
+    }
+  }
+}
+
 template <int KIND, int D, bool PLAIN>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Stream<KIND, D>::kHalf > 8192 ? 1 : 2))) attention_tokens_kernel(AttentionArgs args) {
   using S = Stream<KIND, D>;
-  constexpr int KS = S::KS, DV = S::DV, KW = S::KW, VW = S::VW, KG = S::KG;
-  typedef typename S::KPart KPart;
+  constexpr int ES = S::ES, KS = S::KS, DV = S::DV, KW = S::KW, VW = S::VW;
   __shared__ __attribute__((aligned(1024))) uint8_t lds_all[kWaves][2 * S::kHalf];
   __shared__ float lds_stat[kWaves][16][2];
   const uint32_t lane = threadIdx.x % 64, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), m = lane % 16, g = lane / 16;
@@ -635,17 +685,15 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
       const uint32_t last8 = (uint32_t)(w.s.len - 1) & ~7u;   // tokens behind the sequence's end are read at its last eight
       const Pages at_pages(c, args.seqs, w.seq);
       const auto ask_pages = [&](int t0) { return at_pages.entry(min((uint32_t)t0 + 8 * (lane % (S::kTokens / 8)), last8)); };
-      u32x2 k_scales[S::kSteps][KG], v_scales[S::kSteps];
+      u32x2 k_scales[S::kSteps], v_scales[S::kSteps];
       const auto ask_scales = [&](uint32_t pages, int t0) {
-        if constexpr (KIND != SPLITZIP_BF16) {
+        if constexpr (ES == 1) {
   #pragma unroll
           for (int u = 0; u < S::kSteps; ++u) {
             const uint32_t k4 = 4 * u + m / 4, v4 = 4 * u + g;
             const uint32_t k_place = at_pages.place(min((uint32_t)t0 + 8 * k4, last8)), v_place = at_pages.place(min((uint32_t)t0 + 8 * v4, last8));
-            const uint32_t k_page = (uint32_t)__shfl((int)pages, (int)k4), v_page = (uint32_t)__shfl((int)pages, (int)v4), row = w.head * kGroups<KIND, D>;
-  #pragma unroll
-            for (int i = 0; i < KG; ++i) k_scales[u][i] = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, k_page, k_place, row + S::k_group(i, g)));
-            v_scales[u] = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, v_page, v_place, row + S::v_group(m)));
+            k_scales[u] = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, (uint32_t)__shfl((int)pages, (int)k4), k_place, w.head));
+            v_scales[u] = *reinterpret_cast<const u32x2*>(c.v_scales + scale_offset(c, (uint32_t)__shfl((int)pages, (int)v4), v_place, w.head));
           }
         }
       };
@@ -668,7 +716,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
   #pragma unroll 1
       for (; t0 < w.end; t0 += stride) {
         memory_arrived();
-        KPart k[S::kSteps][2][KW];
+        u32x4 k[S::kSteps][2][KW];
         uint32_t v[S::kSteps][8][VW];
   #pragma unroll
         for (int u = 0; u < S::kSteps; ++u) {
@@ -677,20 +725,16 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
   #pragma unroll
             for (int i = 0; i < KW; ++i) {
               const uint32_t token = 32 * u + 8 * (m / 4) + 4 * b + m % 4;
-              const uint32_t unit = S::KB == 16 ? 4 * i + g : g / 2, half = S::KB == 16 ? 0 : g % 2 * 8;
-              k[u][b][i] = *reinterpret_cast<const KPart*>(mine + S::k_row(token) * S::kRow + (unit ^ S::k_key(token)) * 16 + half);
+              k[u][b][i] = *reinterpret_cast<const u32x4*>(mine + token * S::kRow + ((4 * i + g) ^ S::k_key(token)) * 16);
             }
   #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if constexpr (S::VB < 4) v[u][e][0] = *reinterpret_cast<const uint16_t*>(mine + S::kHalf + S::v_row(32 * u + 8 * g + e) * S::kRow + S::VB * m);
-            else __builtin_memcpy(v[u][e], __builtin_assume_aligned(mine + S::kHalf + S::v_row(32 * u + 8 * g + e) * S::kRow + S::VB * m, S::VB < 16 ? S::VB : 16), S::VB);
-          }
+          for (int e = 0; e < 8; ++e)
+            __builtin_memcpy(v[u][e], __builtin_assume_aligned(mine + S::kHalf + S::v_row(32 * u + 8 * g + e) * S::kRow + S::VB * m, S::VB < 16 ? S::VB : 16), S::VB);
         }
-        u32x2 ks[S::kSteps][KG], vs[S::kSteps];
+        u32x2 ks[S::kSteps], vs[S::kSteps];
   #pragma unroll
         for (int u = 0; u < S::kSteps; ++u) {
-  #pragma unroll
-          for (int i = 0; i < KG; ++i) ks[u][i] = k_scales[u][i];
+          ks[u] = k_scales[u];
           vs[u] = v_scales[u];
         }
         lds_read();   // into registers: the place is free
@@ -710,14 +754,11 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
             x[0][b] = f32x4{0, 0, 0, 0};
   #pragma unroll
             for (int t = 0; t < KS; ++t) {
-              if constexpr (kBits<KIND> == 16) {
+              if constexpr (ES == 2) {
                 x[0][b] = mfma(as_bf16(k[u][b][t]), r.q[0][t], x[0][b]);
-              } else if constexpr (kBits<KIND> == 8) {
-                const u32x2 words = {k[u][b][t / 2][t % 2 * 2], k[u][b][t / 2][t % 2 * 2 + 1]};
-                x[0][b] = mfma(as_bf16(from_fp8<KIND>(words, ks[u][0][b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
               } else {
-                constexpr int kEach = S::KB / 4;   // steps of a part
-                x[0][b] = mfma(as_bf16(from_fp4(k[u][b][t / kEach][t % kEach], ks[u][t / kEach][b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
+                const u32x2 words = {k[u][b][t / 2][t % 2 * 2], k[u][b][t / 2][t % 2 * 2 + 1]};
+                x[0][b] = mfma(as_bf16(from_fp8<KIND>(words, ks[u][b] >> (8 * (m % 4)) & 0xffu)), r.q[0][t], x[0][b]);
               }
             }
           }
@@ -734,14 +775,11 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
   #pragma unroll
             for (int j = 0; j < DV; j += 2) {
               uint32_t w0, w1;
-              const uint32_t b0 = vs[u][i / 2] >> (16 * (i % 2)) & 0xffu, b1 = vs[u][i / 2] >> (16 * (i % 2) + 8) & 0xffu;
-              if constexpr (kBits<KIND> == 16) {
+              if constexpr (ES == 2) {
                 w0 = v[u][2 * i][j / 2];
                 w1 = v[u][2 * i + 1][j / 2];
-              } else if constexpr (kBits<KIND> == 4) {
-                w0 = fp4_pair_to_bf16(v[u][2 * i][j / 8], b0, j % 8 / 2);
-                w1 = fp4_pair_to_bf16(v[u][2 * i + 1][j / 8], b1, j % 8 / 2);
               } else {
+                const uint32_t b0 = vs[u][i / 2] >> (16 * (i % 2)) & 0xffu, b1 = vs[u][i / 2] >> (16 * (i % 2) + 8) & 0xffu;
                 w0 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[u][2 * i][j / 4], b0) : fp8_pair_to_bf16<KIND, false>(v[u][2 * i][j / 4], b0);
                 w1 = j % 4 ? fp8_pair_to_bf16<KIND, true>(v[u][2 * i + 1][j / 4], b1) : fp8_pair_to_bf16<KIND, false>(v[u][2 * i + 1][j / 4], b1);
               }
@@ -759,61 +797,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(S
         for (int t = w.begin + (int)turn * S::kTokens; t < w.end; t += stride) st.add_odd(w, r, t, min(t + S::kTokens, w.end), (int)kStep, element);
       }
 
-      // the waves of a head (two or four) together; lane (m, g) has elements DV (4 g + i) + j of row m in acc[j][i]
-      float total = st.total(0);
-      if (g == 0) {
-        lds_stat[wave][m][0] = st.top[0];
-        lds_stat[wave][m][1] = total;
-      }
-      f32x4* out = reinterpret_cast<f32x4*>(mine) + lane;
-  #pragma unroll
-      for (int j = 0; j < DV; ++j) out[64 * j] = st.acc[0][j];
-      lds_barrier();
-      if (turn == 0) {
-        float high = st.top[0];
-        for (uint32_t v = 1; v < tw; ++v) high = fmaxf(high, lds_stat[wave + v * hw][m][0]);
-        const float f0 = __builtin_amdgcn_exp2f(st.top[0] - high);
-        st.top[0] = high;
-        total *= f0;
-  #pragma unroll
-        for (int j = 0; j < DV; ++j) st.acc[0][j] *= f0;
-        for (uint32_t v = 1; v < tw; ++v) {
-          const float f = __builtin_amdgcn_exp2f(lds_stat[wave + v * hw][m][0] - high);
-          total += f * lds_stat[wave + v * hw][m][1];
-          const f32x4* from = reinterpret_cast<const f32x4*>(lds_all[wave + v * hw]) + lane;
-  #pragma unroll
-          for (int j = 0; j < DV; ++j) st.acc[0][j] += f * from[64 * j];
-        }
-      }
-      lds_barrier();   // (the next tile of rows writes there)
-      const uint32_t at = w.tile * 16 + m;
-      if (turn == 0 && at < w.rows) {
-        const AttentionArgs a = args_again();
-        const uint32_t q_heads = a.cache.heads * a.group, h = w.head * a.group + at % a.group;
-        const uint64_t out_row = (uint64_t)(uint32_t)(w.s.start + (int)(at / a.group));
-        if (w.whole) {
-          const float f = one_over(total);
-          uint8_t* to = a.out + out_row * a.out_stride + 2 * ((uint64_t)h * D + 4 * DV * g);
-  #pragma unroll
-          for (int i = 0; i < 4; ++i)
-  #pragma unroll
-            for (int j = 0; j < DV; j += 4)
-              *reinterpret_cast<u32x2*>(to + 2 * (DV * i + j)) = u32x2{bf16_pair(st.acc[0][j][i] * f, st.acc[0][j + 1][i] * f), bf16_pair(st.acc[0][j + 2][i] * f, st.acc[0][j + 3][i] * f)};
-          if (g == 0 && a.lse) a.lse[out_row * q_heads + h] = lse_of(st.top[0], total);
-        } else {
-          const uint64_t place = w.place(a, wave % hw, m);
-          float* to = a.part_out + place * D + 4 * DV * g;
-  #pragma unroll
-          for (int i = 0; i < 4; ++i)
-  #pragma unroll
-            for (int j = 0; j < DV; j += 4)
-              *reinterpret_cast<f32x4*>(to + DV * i + j) = f32x4{st.acc[0][j][i], st.acc[0][j + 1][i], st.acc[0][j + 2][i], st.acc[0][j + 3][i]};
-          if (g == 0) {
-            a.part_stat[2 * place] = st.top[0];
-            a.part_stat[2 * place + 1] = total;
-          }
-        }
-      }
+      finish_tokens<D>(w, st, lds_all[0], 2 * S::kHalf, lds_stat, wave, lane, hw);
     } while (w.more_rows());
   } while (w.next(lane));
 }

@@ -21,6 +21,7 @@ namespace {
 #include "allot.hpp"
 #include "append.hpp"
 #include "attention.hpp"
+#include "attention4.hpp"
 
 bool aligned16(uint64_t x) { return (x & 15u) == 0; }
 bool aligned16(const void* p) { return aligned16((uint64_t)reinterpret_cast<uintptr_t>(p)); }
@@ -181,6 +182,10 @@ struct Append {
 
 // How an attention call is cut: which kernel, the rows of a (sequence, head of the cache) into tiles, the tokens of all sequences
 // into blocks and these into shares.
+uint32_t stage4_tokens(uint32_t head_dim, uint32_t heads) {
+  return head_dim == 256 ? Stage4<256, 1>::kTokens : head_dim == 128 ? (heads == 2 ? Stage4<128, 2>::kTokens : Stage4<128, 1>::kTokens)
+         : heads == 4 ? Stage4<64, 4>::kTokens : heads == 2 ? Stage4<64, 2>::kTokens : Stage4<64, 1>::kTokens;
+}
 struct AttentionPlan {
   uint32_t waves, nt;   // waves 0: attention_tokens_kernel; else attention_rows_kernel with so many waves of 16 nt rows
   uint32_t heads_across, tile_rows, row_tiles, most_rows, kept;
@@ -197,6 +202,11 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
   // 13.0, 14.3, 15.5, 16 of 4000 49.6, 51.0, 53.3, 64 of 200 14.3, 14.7, 23.1; E5M2 14.9, 13.1, 14.1, 35.9, 35.1, 38.2, 13.0, 12.0, 15.0;
   // 64 ragged ones of up to 8192 in shuffled pages 192, 181, 186.
   p.heads_across = rows > 16 || c->kv_heads % 2 ? 1u : 2u;
+  const bool fp4 = c->dtype == SPLITZIP_FP4_E2M1;
+  if (fp4 && rows <= 16) {   // as many as make up a cache line
+    p.heads_across = 256 / c->head_dim;
+    while (c->kv_heads % p.heads_across) p.heads_across /= 2;
+  }
   const uint64_t longest = q->max_len < kMostTokens ? q->max_len : kMostTokens, tokens = q->n_seqs * longest;
   if (rows > 16) {
     // Four waves of 16 rows, three workgroups per CU, or eight of 32 rows, one: these read K and V less often, and have more to start and
@@ -212,13 +222,13 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
   p.row_tiles = (uint32_t)(tiles < 1024 ? tiles : 1024);
   p.most_rows = (uint32_t)(rows < (uint64_t)p.row_tiles * p.tile_rows ? rows : (uint64_t)p.row_tiles * p.tile_rows);
   p.kept = (uint32_t)(rows < p.tile_rows ? rows : p.tile_rows);
-  // as many workgroups as the chip holds at a time: two with 64 KB of LDS per CU, one with 128 KB or eight waves, three with 32 KB
+  // as many workgroups as the chip holds at a time: two with 64 KB of LDS per CU, one with 128 KB or eight waves, three with 32 KB and a few more
   const bool one_per_cu = p.waves == 8 || (p.waves == 0 && c->dtype == SPLITZIP_BF16 && c->head_dim == 256);
-  const uint64_t groups = (uint64_t)(c->kv_heads / p.heads_across) * p.row_tiles, slots = (uint64_t)cu_count() * (one_per_cu ? 1 : p.waves ? 3 : 2);
+  const uint64_t groups = (uint64_t)(c->kv_heads / p.heads_across) * p.row_tiles, slots = (uint64_t)cu_count() * (one_per_cu ? 1 : p.waves ? 3 : fp4 && c->head_dim != 256 ? 3 : 2);
   uint64_t shares = (slots + groups - 1) / groups;
   // a block: what the waves of a head stage at a time
-  const uint32_t staged = p.waves ? p.waves * 1024u / c->head_dim : stage_tokens(c->dtype, row_bytes(c));
-  p.block_tokens = p.waves ? staged : staged * (kWaves / p.heads_across);
+  const uint32_t staged = p.waves ? p.waves * 1024u / c->head_dim : 8192u / row_bytes(c);
+  p.block_tokens = p.waves ? staged : fp4 ? stage4_tokens(c->head_dim, p.heads_across) : (staged < 32 ? 32 : staged) * (kWaves / p.heads_across);
   // (a sum of blocks is kept in 32 bits)
   const uint64_t most = (uint64_t)q->n_seqs * (q->d_block_table ? (uint64_t)q->table_stride * c->page_tokens : c->page_tokens);
   while (most / p.block_tokens + q->n_seqs > (1ull << 31) && p.block_tokens < (1u << 30)) p.block_tokens *= 2;
@@ -249,10 +259,22 @@ struct Attend {
   static void rows(dim3 grid, hipStream_t st, const AttentionArgs* a) {
     hipLaunchKernelGGL((attention_rows_kernel<KIND, D, W, NT, PLAIN>), grid, dim3(64 * W), 0, st, *a);
   }
+  template <int H, bool PLAIN>
+  static void heads4(dim3 grid, hipStream_t st, const AttentionArgs* a) {
+    hipLaunchKernelGGL((attention_tokens4_kernel<D, H, PLAIN>), grid, dim3(kThreads), 0, st, *a);
+  }
+  template <bool PLAIN>
+  static void tokens4(dim3 grid, hipStream_t st, const AttentionArgs* a) {
+    if (D == 64 && a->heads_across == 4) heads4<D == 64 ? 4 : 1, PLAIN>(grid, st, a);
+    else if (D < 256 && a->heads_across == 2) heads4<D < 256 ? 2 : 1, PLAIN>(grid, st, a);
+    else heads4<1, PLAIN>(grid, st, a);
+  }
   template <bool PLAIN>
   static void any(dim3 grid, uint32_t waves, hipStream_t st, const AttentionArgs* a) {
-    if (!waves) hipLaunchKernelGGL((attention_tokens_kernel<KIND, D, PLAIN>), grid, dim3(kThreads), 0, st, *a);
-    else if constexpr (D == 256) rows<8, 1, PLAIN>(grid, st, a);
+    if (!waves) {
+      if constexpr (KIND == SPLITZIP_FP4_E2M1) tokens4<PLAIN>(grid, st, a);
+      else hipLaunchKernelGGL((attention_tokens_kernel<KIND, D, PLAIN>), grid, dim3(kThreads), 0, st, *a);
+    } else if constexpr (D == 256) rows<8, 1, PLAIN>(grid, st, a);
     else waves == 4 ? rows<4, 1, PLAIN>(grid, st, a) : rows<8, 2, PLAIN>(grid, st, a);
   }
   static int run(dim3 grid, uint32_t waves, hipStream_t st, const AttentionArgs* a) {
