@@ -9,9 +9,14 @@
 // once, to what is written; t in 64 bits, in turns, of which the whole ones are dropped before sine and cosine: positions go up to 2^30,
 // where 32 bits of an angle would leave nothing of it.
 //
-// A row's sines and cosines are the same for all of its heads: a workgroup belongs to one row at a time, its first R / 2 threads make an angle
-// each while the heads' words are on their way, and all lanes read their eight elements' from LDS.  D / 8 lanes take a head, eight elements each, as in
-// cache_write_kernel; what a lane's elements are turned with lies in another lane of the same head.
+// A row's sines and cosines are the same for all of its heads: a workgroup makes those of a few rows at a time, an angle per thread, and all
+// lanes read their eight elements' from LDS.  D / 8 lanes take a head, eight elements each, as in cache_write_kernel; what a lane's elements
+// are turned with lies in another lane of the same head.
+//
+// Bound by memory for long calls, by the launch for short ones.  16384 rows of 32 + 8 + 8 heads of 128 into E4M3, 369 MB: 68.4 us (5.4 TB/s; a plain
+// copy of that mix of reads and writes 5.6); streamed loads alone 73.3, streamed stores alone 70.2, neither 72.8.  The next row's words are asked for
+// before this one's are worked on, and a workgroup keeps its heads: a row at a time with all of its heads, 123 us.  Workgroups: 6 per CU 78.7, 12 78.5,
+// 24 73.9, 48 71.3, 96 as 48.
 #ifndef SPLITZIP_APPEND_HPP
 #define SPLITZIP_APPEND_HPP
 
@@ -27,7 +32,7 @@ struct AppendArgs {
   float scaling, eps, weight_offset;
   uint32_t q_heads, rotary;
   uint32_t interleaved, norm, weights_f32;
-  uint32_t chunks;                                                 // workgroups of a row
+  uint32_t chunks, each;                                           // workgroups of a row; rows that one takes at a time
 };
 
 // eight elements of a lane, in 32 bits, as words of the cache, and the byte of the lane's scale
@@ -70,113 +75,105 @@ __device__ inline void load_weights(const AppendArgs& a, const void* at, uint32_
   for (int e = 0; e < 8; ++e) w[e] += a.weight_offset;
 }
 
-// N: heads of each lane at a time
-constexpr int kAppendHeads = 4;
-template <int KIND, int D, int N>
+// A lane's eight elements turned; cosines and sines of the row, `half` each.
+template <int D>
+__device__ inline void turn(const AppendArgs& a, const float (*turns)[D / 2], uint32_t lane, uint32_t half, float (&y)[8]) {
+  const bool turned = 8 * lane < a.rotary;
+  if (a.interleaved) {
+    const uint32_t f = turned ? 4 * lane : 0;
+    const f32x4 c = *reinterpret_cast<const f32x4*>(turns[0] + f), s = *reinterpret_cast<const f32x4*>(turns[1] + f);
+    if (!turned) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float u = y[2 * e], v = y[2 * e + 1];
+      y[2 * e] = u * c[e] - v * s[e];
+      y[2 * e + 1] = v * c[e] + u * s[e];
+    }
+    return;
+  }
+  const bool upper = 8 * lane >= half;
+  float z[8];   // the pairs' other halves
+  if (D == 128 && half == 64) {   // eight lanes on, in rows of sixteen
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(y[e]), 0x128, 0xf, 0xf, false));
+  } else {
+    const int from = (int)(threadIdx.x + (!upper ? half / 8 : turned ? 0u - half / 8 : 0u));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], from);
+  }
+  const uint32_t f = turned ? 8 * lane - (upper ? half : 0) : 0;
+  const f32x4 *const cs = reinterpret_cast<const f32x4*>(turns[0] + f), *const sn = reinterpret_cast<const f32x4*>(turns[1] + f);
+  const f32x4 c[2] = {cs[0], cs[1]}, s[2] = {sn[0], sn[1]};
+  if (!turned) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = y[e] * c[e / 4][e % 4] + z[e] * (upper ? s[e / 4][e % 4] : -s[e / 4][e % 4]);
+}
+
+template <int D>
+constexpr uint32_t kAppendRows = 2 * kThreads / D;   // of which a workgroup makes the angles at a time: one per thread
+
+template <int KIND, int D, bool STREAM>
 __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
   constexpr uint32_t kLanes = D / 8, kHeads = kThreads / kLanes;
-  __shared__ float turns[2][2][D / 2];   // of the even and of the odd rows that the workgroup takes: cosines, sines
+  __shared__ __attribute__((aligned(16))) float turns[2][kAppendRows<D>][2][D / 2];   // of the even and of the odd times: of a row cosines, sines
   const uint32_t lane = threadIdx.x % kLanes, half = a.rotary / 2;
   const Seq s = seq_at(a.seqs, blockIdx.y);
   const Pages pages(a.cache, a.seqs, blockIdx.y);
-  const uint32_t heads = a.q_heads + 2 * a.cache.heads;   // those of Q, of K, of V
-  const uint32_t first = blockIdx.x % a.chunks * N * kHeads + threadIdx.x / kLanes;
-  const uint32_t step = gridDim.x / a.chunks;
-  float q_weight[8], k_weight[8];
-  if (a.norm) {
-    load_weights(a, a.q_weight, lane, q_weight);
-    load_weights(a, a.k_weight, lane, k_weight);
-  }
+  // the lane's head: one of Q, of K, of V (the last one once more where there are no more)
+  const uint32_t kv = a.cache.heads, heads = a.q_heads + 2 * kv, chunk = blockIdx.x % a.chunks * kHeads, here = chunk + threadIdx.x / kLanes, h = min(here, heads - 1);
+  const bool of_q = h < a.q_heads, of_k = !of_q && h < a.q_heads + kv, rotates = a.rotary && chunk < a.q_heads + kv;   // (rotates: one of the workgroup's)
+  const uint32_t head = of_q ? h : h - a.q_heads - (of_k ? 0 : kv);
+  const uint64_t stride = of_q ? a.q_stride : of_k ? a.k_stride : a.v_stride;
+  const uint8_t* const from = as_global(of_q ? a.q : of_k ? a.k : a.v) + 2 * ((uint64_t)head * D + 8 * lane);
+  float weight[8];
+  if (a.norm && (of_q || of_k)) load_weights(a, of_q ? a.q_weight : a.k_weight, lane, weight);
+  const uint32_t first = blockIdx.x / a.chunks * a.each, step = gridDim.x / a.chunks * a.each, rows = (uint32_t)s.rows;
+  const auto load = [&](uint32_t i) { return ld_row<STREAM, u32x4>(from + (uint64_t)((uint32_t)s.start + i) * stride); };
+  u32x4 next = {0, 0, 0, 0};
+  if (first < rows) next = load(first);
   uint32_t parity = 0;
-  for (uint32_t i = blockIdx.x / a.chunks; i < (uint32_t)s.rows; i += step, parity ^= 1) {
-    const uint64_t row = (uint32_t)s.start + i;
-    const int token = s.base + (int)i;
-    u32x4 x[N];
-#pragma unroll
-    for (int n = 0; n < N; ++n) {   // (the last head once more where there are no more: no load stands behind a condition)
-      const uint32_t h = min(first + n * kHeads, heads - 1);
-      const uint8_t* const at = h < a.q_heads ? a.q + row * a.q_stride + 2 * (uint64_t)h * D
-                                : h < a.q_heads + a.cache.heads ? a.k + row * a.k_stride + 2 * (uint64_t)(h - a.q_heads) * D
-                                                                : a.v + row * a.v_stride + 2 * (uint64_t)(h - a.q_heads - a.cache.heads) * D;
-      x[n] = *reinterpret_cast<const u32x4*>(as_global(at) + 16 * lane);
-    }
-    const uint32_t page = pages.page((uint32_t)max(token, 0)), place = pages.place((uint32_t)max(token, 0));
-    if (threadIdx.x < half) {
-      const int position = a.positions ? a.positions[row] : token;
-      const double turn = (double)position * ((double)a.freqs[threadIdx.x] * 0.15915494309189533577);
-      float sine, cosine;
-      sincospif(2.0f * (float)(turn - rint(turn)), &sine, &cosine);
-      turns[parity][0][threadIdx.x] = cosine * a.scaling;
-      turns[parity][1][threadIdx.x] = sine * a.scaling;
-    }
-    lds_barrier();   // (a place is written again by the second row after this one, a barrier on)
-    // the lane's elements times `same`, the others of their pairs times `other`
-    float same[8], other[8];
-    const bool turned = 8 * lane < a.rotary;
-    if (turned) {
-      if (a.interleaved) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float c = turns[parity][0][4 * lane + e], sn = turns[parity][1][4 * lane + e];
-          same[2 * e] = same[2 * e + 1] = c;
-          other[2 * e] = -sn;
-          other[2 * e + 1] = sn;
-        }
-      } else {
-        const bool upper = 8 * lane >= half;
-        const uint32_t f = 8 * lane - (upper ? half : 0);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          same[e] = turns[parity][0][f + e];
-          other[e] = upper ? turns[parity][1][f + e] : -turns[parity][1][f + e];
-        }
+  for (uint32_t i0 = first; i0 < rows; i0 += step, parity ^= 1) {
+    if (rotates) {
+      const uint32_t r = threadIdx.x / (D / 2), f = threadIdx.x % (D / 2);
+      if (r < a.each && i0 + r < rows && f < half) {
+        const int position = a.positions ? a.positions[(uint32_t)s.start + i0 + r] : s.base + (int)(i0 + r);
+        const double turn = (double)position * ((double)a.freqs[f] * 0.15915494309189533577);
+        float sine, cosine;
+        sincospif(2.0f * (float)(turn - rint(turn)), &sine, &cosine);
+        turns[parity][r][0][f] = cosine * a.scaling;
+        turns[parity][r][1][f] = sine * a.scaling;
       }
+      lds_barrier();   // (a place is written again two times on, a barrier after everybody has read it)
     }
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const uint32_t h = first + n * kHeads;
-      if (h >= heads) continue;
-      const bool of_q = h < a.q_heads, of_k = !of_q && h < a.q_heads + a.cache.heads;
+    for (uint32_t r = 0; r < a.each && i0 + r < rows; ++r) {
+      const uint32_t i = i0 + r, after = r + 1 < a.each && i + 1 < rows ? i + 1 : i0 + step;
+      const uint64_t row = (uint32_t)s.start + i;
+      const int token = s.base + (int)i;
       float y[8];
-      floats_of(x[n], y);
+      floats_of(next, y);
+      if (after < rows) next = load(after);
       if (of_q || of_k) {
         if (a.norm) {
           float sum = 0.0f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) sum += y[e] * y[e];
-#pragma unroll
-          for (uint32_t o = kLanes / 2; o > 0; o /= 2) sum += __shfl_xor(sum, (int)o);
+          sum = __uint_as_float(of_lanes<(int)kLanes>(__float_as_uint(sum), [](uint32_t u, uint32_t v) { return __float_as_uint(__uint_as_float(u) + __uint_as_float(v)); }));
           const float over = rsqrtf(sum * (1.0f / D) + a.eps);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = y[e] * over * (of_q ? q_weight[e] : k_weight[e]);
+          for (int e = 0; e < 8; ++e) y[e] = y[e] * over * weight[e];
         }
-        if (a.rotary) {
-          float z[8];
-          if (a.interleaved) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = y[e ^ 1];
-          } else {
-            const int from = (int)(threadIdx.x + (8 * lane < half ? half / 8 : turned ? 0u - half / 8 : 0u));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], from);
-          }
-          if (turned) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = y[e] * same[e] + z[e] * other[e];
-          }
-        }
+        if (a.rotary) turn<D>(a, turns[parity][r], lane, half, y);
       }
-      if (of_q) {
+      if (here >= heads) continue;
+      if (of_q || (of_k && a.k_out)) {
         int none;
-        *reinterpret_cast<u32x4*>(a.q_out + row * a.q_out_stride + 2 * ((uint64_t)h * D + 8 * lane)) = quantised<SPLITZIP_BF16, D>(y, none);
-        continue;
+        uint8_t* const to = of_q ? a.q_out + row * a.q_out_stride : a.k_out + row * a.k_out_stride;
+        const u32x4 words = quantised<SPLITZIP_BF16, D>(y, none);
+        if constexpr (STREAM) st_stream(reinterpret_cast<u32x4*>(to + 2 * ((uint64_t)head * D + 8 * lane)), words);
+        else *reinterpret_cast<u32x4*>(to + 2 * ((uint64_t)head * D + 8 * lane)) = words;
       }
-      const uint32_t head = h - a.q_heads - (of_k ? 0 : a.cache.heads);
-      if (of_k && a.k_out) {
-        int none;
-        *reinterpret_cast<u32x4*>(a.k_out + row * a.k_out_stride + 2 * ((uint64_t)head * D + 8 * lane)) = quantised<SPLITZIP_BF16, D>(y, none);
-      }
-      if (token < 0) continue;
+      if (of_q || token < 0) continue;
+      const uint32_t page = pages.page((uint32_t)token), place = pages.place((uint32_t)token);
       int byte = 0;
       const Lane8<KIND> words = quantised<KIND, D>(y, byte);
       const uint64_t at = token_offset(a.cache, page, place) + head * a.cache.head_stride + lane * kBits<KIND>;

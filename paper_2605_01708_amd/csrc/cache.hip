@@ -173,9 +173,9 @@ int rows_call(const splitzip_cache* c, const splitzip_seqs* q, void* d_k, uint64
 
 template <int KIND, int D>
 struct Append {
-  static int run(dim3 grid, bool several, hipStream_t st, const AppendArgs* a) {
-    if (several) hipLaunchKernelGGL((cache_append_kernel<KIND, D, kAppendHeads>), grid, dim3(kThreads), 0, st, *a);
-    else hipLaunchKernelGGL((cache_append_kernel<KIND, D, 1>), grid, dim3(kThreads), 0, st, *a);
+  static int run(dim3 grid, bool stream, hipStream_t st, const AppendArgs* a) {
+    if (stream) hipLaunchKernelGGL((cache_append_kernel<KIND, D, true>), grid, dim3(kThreads), 0, st, *a);
+    else hipLaunchKernelGGL((cache_append_kernel<KIND, D, false>), grid, dim3(kThreads), 0, st, *a);
     return launched();
   }
 };
@@ -380,15 +380,16 @@ int splitzip_cache_append(const splitzip_cache* cache, const splitzip_seqs* seqs
   a.interleaved = how->interleaved;
   a.norm = how->norm;
   a.weights_f32 = how->weights_f32;
-  // a workgroup for every 16 heads of 128 of a row, or, where that is more of them than the chip holds, for four times as many
+  // a workgroup for every 16 heads of 128 of a row, or, where that is more of them than the chip holds, of a few rows
   const uint64_t rows = !seqs->max_rows ? 1 : seqs->max_rows < n_rows ? seqs->max_rows : n_rows, cus = (uint64_t)cu_count(), per = 8 * kThreads / cache->head_dim;
-  const uint64_t heads = (uint64_t)q_heads + 2 * (uint64_t)cache->kv_heads, single = (heads + per - 1) / per;
-  const bool several = rows * single * seqs->n_seqs > 8 * cus && single > 1;
-  const uint64_t chunks = several ? (single + kAppendHeads - 1) / kAppendHeads : single;
-  const uint64_t most = (8 * cus + seqs->n_seqs - 1) / seqs->n_seqs;   // of a sequence
-  const uint64_t across = rows * chunks <= most ? rows : most <= chunks ? 1 : most / chunks;
+  const uint64_t heads = (uint64_t)q_heads + 2 * (uint64_t)cache->kv_heads, chunks = (heads + per - 1) / per;
+  constexpr uint64_t kPerCu = 48;
+  a.each = rows * chunks * seqs->n_seqs > kPerCu * cus ? 2 * kThreads / cache->head_dim : 1;
+  const uint64_t most = (kPerCu * cus + seqs->n_seqs - 1) / seqs->n_seqs, groups = (rows + a.each - 1) / a.each;   // workgroups of a sequence
+  const uint64_t across = groups * chunks <= most ? groups : most <= chunks ? 1 : most / chunks;
   a.chunks = (uint32_t)chunks;
-  return by_kind<Append>(cache, dim3((unsigned)(across * chunks), seqs->n_seqs), several, static_cast<hipStream_t>(stream), (const AppendArgs*)&a);
+  const uint64_t bytes = n_rows * (4 * q_elems + 2 * elems * (16 + word_bits(cache->dtype)) / 8);
+  return by_kind<Append>(cache, dim3((unsigned)(across * chunks), seqs->n_seqs), bytes >= kStreamed, static_cast<hipStream_t>(stream), (const AppendArgs*)&a);
 }
 
 size_t splitzip_attention_workspace_bytes(const splitzip_cache* cache, const splitzip_seqs* seqs, uint32_t n_rows, uint32_t q_heads) {

@@ -229,12 +229,21 @@ __device__ inline uint32_t to_fp4(const u32x4& w, int byte) {
 template <int KIND>
 using Lane8 = typename std::conditional<kBits<KIND> == 16, u32x4, typename std::conditional<kBits<KIND> == 8, u32x2, uint32_t>::type>::type;
 
+// What the lanes of a group of N (4 to 32, side by side) have, put together by `both`; the same in all of them.  Up to 16 without LDS: lanes
+// change places inside fours, then fours (or eights) all of whose lanes have the same are mirrored.
+template <int N, typename F>
+__device__ inline uint32_t of_lanes(uint32_t x, const F& both) {
+  x = both(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false));              // quad_perm 1 0 3 2
+  x = both(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, false));              // quad_perm 2 3 0 1
+  if constexpr (N >= 8) x = both(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));    // row_half_mirror
+  if constexpr (N >= 16) x = both(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false));   // row_mirror
+  if constexpr (N >= 32) x = both(x, (uint32_t)__shfl_xor((int)x, 16));
+  return x;
+}
 // The largest magnitude among the lanes that share a scale, all of a head's (FP8) or four (4-bit words), from each lane's own, as bits.
 template <int KIND, int D>
 __device__ inline uint32_t largest_of_group(uint32_t m) {
-#pragma unroll
-  for (int o = D / 16 / (int)kGroups<KIND, D>; o > 0; o /= 2) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-  return m;
+  return of_lanes<D / 8 / (int)kGroups<KIND, D>>(m, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 // 8 BF16 words of a lane as words of the cache, and the byte of the lane's scale
 template <int KIND, int D>
