@@ -17,6 +17,7 @@
 constexpr uint32_t kAllotThreads = 1024, kAllotWaves = kAllotThreads / 64;
 constexpr uint32_t kRowsHere = 4096;     // rows that the first launch fills in itself
 constexpr uint32_t kFillRows = 1024;     // rows of a workgroup of the second
+constexpr uint32_t kPages = 8;           // pages that a thread moves at a time
 
 struct AllotArgs {
   uint32_t* table;
@@ -48,16 +49,18 @@ struct Wanted {
   __device__ uint32_t takes() const { return need > held ? need - held : 0; }
 };
 
-template <typename T>
-__device__ inline T wave_sum(T x) {
-#pragma unroll
-  for (int o = 32; o > 0; o /= 2) x += __shfl_xor(x, o);
-  return x;
+// of 64 numbers below 2^38 each (sums of up to 64 of 32 bits), the sum; their halves' sums stay in 32 bits
+__device__ inline uint64_t wave_sum(uint64_t x) {
+  return wave_last(wave_incl_scan((uint32_t)x & 0xffffu)) + ((uint64_t)wave_last(wave_incl_scan((uint32_t)(x >> 16))) << 16);
 }
-__device__ inline uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int o = 32; o > 0; o /= 2) x = max(x, (uint32_t)__shfl_xor((int)x, o));
-  return x;
+__device__ inline uint32_t wave_max(uint32_t v) {   // as wave_incl_scan
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
+  return wave_last(v);
 }
 
 // the last of entries [0, n] of ascending starts (starts[0] = 0) that is not above i, i below starts[n]: the sequence that has row i
@@ -198,13 +201,35 @@ __global__ void __launch_bounds__(kAllotThreads) cache_allot_kernel(AllotArgs a)
         }
       }
       __syncthreads();
-      for (uint32_t p = threadIdx.x; p < all_pages; p += kAllotThreads) {
-        const uint32_t of = owner_of(moved, kAllotThreads, p);
-        uint32_t* const entry = a.table + (uint64_t)(s0 + of) * a.table_stride + column[of] + (p - moved[of]);
-        uint32_t* const place = a.stack + (top - 1 - (before_pages + p));
-        if (round) *entry = *place;
-        else *place = *entry;
-      }
+      // several pages of a thread at a time, since each goes through what a search and a load take
+      const auto move = [&](auto pages_at_a_time, uint32_t p0) {
+        constexpr uint32_t N = decltype(pages_at_a_time)::value;
+        // (the last one once more where there are no more: the same word to the same place)
+        uint32_t p[N], low[N], page[N];
+        uint32_t *entry[N], *place[N];
+#pragma unroll
+        for (uint32_t k = 0; k < N; ++k) {
+          p[k] = min(p0 + k * kAllotThreads, all_pages - 1);
+          low[k] = 0;
+        }
+#pragma unroll 1
+        for (uint32_t step = kAllotThreads / 2; step > 0; step /= 2) {   // the last sequence that no more than p pages are moved before
+#pragma unroll
+          for (uint32_t k = 0; k < N; ++k) low[k] += moved[low[k] + step] <= p[k] ? step : 0;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < N; ++k) {
+          entry[k] = a.table + (uint64_t)(s0 + low[k]) * a.table_stride + column[low[k]] + (p[k] - moved[low[k]]);
+          place[k] = a.stack + (top - 1 - (before_pages + p[k]));
+          page[k] = round ? *place[k] : *entry[k];
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < N; ++k) *(round ? entry[k] : place[k]) = page[k];
+      };
+      uint32_t p0 = threadIdx.x;
+      if (all_pages > kAllotThreads)
+        for (; p0 < all_pages; p0 += kPages * kAllotThreads) move(std::integral_constant<uint32_t, kPages>(), p0);
+      else if (p0 < all_pages) move(std::integral_constant<uint32_t, 1>(), p0);
       before_rows += all_rows;
       before_pages += all_pages;
     }
@@ -225,16 +250,42 @@ __global__ void __launch_bounds__(kAllotThreads) cache_allot_kernel(AllotArgs a)
   }
 }
 
-// Many rows: 1024 of them per workgroup.
+// the same by all lanes of a wave for one row: 64 entries are looked at at a time
+__device__ inline uint32_t owner_by_wave(const int32_t* starts, uint32_t n, uint32_t i, uint32_t lane) {
+  uint32_t low = 0, high = n;
+  while (high - low > 1) {
+    const uint32_t step = (high - low + 63) / 64, at = low + lane * step;
+    const uint32_t upto = (uint32_t)__popcll(__ballot(at < high && (uint32_t)starts[min(at, high - 1)] <= i));   // the first `upto` lanes, the first at least
+    low += (upto - 1) * step;
+    high = min(high, low + step);
+  }
+  return low;
+}
+
+// Many rows: 1024 of them per workgroup, which looks their sequences' starts up first.
 __global__ void __launch_bounds__(kThreads) cache_allot_fill_kernel(AllotArgs a) {
-  const uint32_t n_rows = (uint32_t)a.starts[a.n_seqs];
+  __shared__ uint32_t part[kFillRows + 1];
+  const uint32_t lane = threadIdx.x % 64, first = blockIdx.x * kFillRows, n_rows = (uint32_t)a.starts[a.n_seqs];
+  uint32_t low = 0, n = 0;
+  if (first < n_rows) {
+    low = owner_by_wave(a.starts, a.n_seqs, first, lane);
+    n = owner_by_wave(a.starts, a.n_seqs, min(first + kFillRows, n_rows) - 1, lane) + 1 - low;
+    // (sequences without rows may be more than that)
+    if (n <= kFillRows)
+      for (uint32_t k = threadIdx.x; k <= n; k += kThreads) part[k] = (uint32_t)a.starts[low + k];
+  }
+  __syncthreads();
+#pragma unroll
   for (uint32_t k = 0; k < kFillRows; k += kThreads) {
-    const uint32_t i = blockIdx.x * kFillRows + k + threadIdx.x;
-    if (i >= a.n_rows) return;
+    const uint32_t i = first + k + threadIdx.x;
+    if (i >= a.n_rows) continue;
     if (i >= n_rows) {
       no_row(a, i);
+    } else if (n <= kFillRows) {
+      const uint32_t s = owner_of(part, n, i);
+      fill_row(a, i, low + s, part[s], part[s + 1]);
     } else {
-      const uint32_t s = owner_of(a.starts, a.n_seqs, i);
+      const uint32_t s = low + owner_of(a.starts + low, n, i);
       fill_row(a, i, s, (uint32_t)a.starts[s], (uint32_t)a.starts[s + 1]);
     }
   }

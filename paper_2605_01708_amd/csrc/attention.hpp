@@ -848,12 +848,15 @@ struct Stage {
         for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
       }
     }
+    if constexpr (kB == 4)   // (load_v fills eight: without these its last and the last of four become one store, to an address, and w memory: 164 us for 64 drafts that take ...)
+      for (int j = 4; j < 8; ++j) w[j] = 0;
     if constexpr (kB != 16) scales = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, page, place, row));
   }
   __device__ void store_k(u32x4* to, uint32_t s, uint32_t m) const {
+    const uint32_t low = scales[0], high = scales[1];   // (as they are, the compiler makes an index of the question, and memory of the two)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t pair = (4 * s + i) / KS % 2 ? scales[1] : scales[0], byte = pair >> (8 * (m % 4)) & 0xffu;
+      const uint32_t byte = ((4 * s + i) / KS % 2 ? high : low) >> (8 * (m % 4)) & 0xffu;
       if constexpr (kB == 16) to[64 * i] = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
       else if constexpr (kB == 8) to[64 * i] = from_fp8<KIND>(u32x2{w[2 * i], w[2 * i + 1]}, byte);
       else to[64 * i] = from_fp4(w[i], byte);
