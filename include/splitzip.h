@@ -552,9 +552,11 @@ typedef struct {
  * first, the first of them (by sequence, then by place) on top, and then pages
  * are taken from the top in the same order, so that a step's pages go back as they
  * lay --; and, for each of the step's rows, in n_rows entries each
- * (nullable): d_slots, page * page_tokens + the place in the page, of its token;
- * d_row_seqs, its sequence; d_positions, its token's number.  Entries behind
- * the last row become -1.  A page belongs to one sequence.
+ * (nullable; n_rows is the most that the step may have in any case): d_slots,
+ * page * page_tokens + the place in the page, of its token; d_row_seqs, its
+ * sequence; d_positions, its token's number.  Entries behind the last row
+ * become -1.  A page belongs to one sequence.  Calls that share a pool or
+ * sequences must not overlap in time, nor calls that read those sequences with this one.
  * A step that cannot be taken (status) changes neither lengths, table nor pool;
  * d_starts is all 0 then, so that the step's other calls have no rows.
  * seqs needs a block table; its max_rows and max_len are not looked at.  One
