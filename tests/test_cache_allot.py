@@ -256,6 +256,27 @@ def test_what_a_program_leaves_out_and_other_streams():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n", [5, 1500])
+def test_lengths_may_be_what_is_kept(n):
+    """keep is the tensor of the lengths itself; the most rows hold also where none of the outputs is wanted"""
+    h = Host(n, 6, 8, 5 * n, seed=6)
+    d = Device(h)
+    rows = np.arange(n) % 13
+    for _ in range(2):
+        want = h.step(rows, h.lens.copy(), 20000)
+        got = outputs(20000)
+        sz.cache_allot(d.pool, d.seqs, i32(rows), d.lens, *got)
+        d.same(h)
+        compare(got, want, 20000)
+    L, zero = sz.lib(), h.step(np.full(n, 1), None, n - 1)
+    assert zero is None
+    rows = i32(np.full(n, 1))
+    assert L.splitzip_cache_allot(C.byref(d.pool.c), C.byref(d.seqs.c), rows.data_ptr(), None, None, None, None, n - 1, None) == 0
+    torch.cuda.synchronize()
+    d.same(h)
+
+
+@pytest.mark.gpu
 def test_captured_steps():
     """a step captured once and replayed with other rows, its lengths going on from replay to replay"""
     h = Host(6, 20, 8, 90, seed=5)

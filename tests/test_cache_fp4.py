@@ -240,6 +240,19 @@ def test_layouts(dim, page, layout, group):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dim,heads", [(64, 4), (64, 8), (64, 6), (128, 4), (128, 8), (256, 4)])
+@pytest.mark.parametrize("layout", ["nhd", "hnd", "side"])
+def test_heads_of_a_cache_line(dim, heads, layout):
+    """as many heads of a workgroup as make up a line, or as divide them; heads apart from one another; parts, windows and a tile of rows of two tokens"""
+    w = World4([1, 33, 64, 700, 1300], [1, 2, 1, 2, 2], heads, dim, 16, layout, seed=heads)
+    q, qd = queries(w, 3)
+    close(*run(w, qd, sz.Attention(0.1)), attend(w, q, 0.1))
+    close(*run(w, qd, sz.Attention(0.1, window=100)), attend(w, q, 0.1, window=100))
+    w.seqs = sz.Sequences(*w.dev, max_rows=2, max_len=20000)         # cut into parts
+    close(*run(w, qd, sz.Attention(0.1)), attend(w, q, 0.1))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T,words", [(13, 1), (64, 1), (130, 3)])
 def test_trees(T, words):
     rng = np.random.default_rng(T)
