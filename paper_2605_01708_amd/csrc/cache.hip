@@ -236,9 +236,6 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
   // tokens, 52 rows of 8 heads, one sequence of 1000 tokens 14.4, 15.3, 16.3, 20.8, four 19.6, 16.9, 17.0, 21.4, one of 4000 22.3, 19.4, 17.7, 22.3.
   const uint64_t least = tokens / 16 < 64 ? 64 : tokens / 16 > 256 ? 256 : tokens / 16;
   p.least_blocks = p.waves && p.block_tokens < least ? (uint32_t)(least / p.block_tokens) : 1;
-  // So does a workgroup over 4-bit words, whose blocks are small: up to eight.  us with one, four and eight at least: a sequence of 8192 tokens 15.9, 15.1, 18.0, of
-  // 32768 22.0, 20.2, 19.0, of 131072 (four heads) 31.0, 31.0, 28.5, 16 of 4096 27.7, 27.6, 24.3.
-  if (fp4 && !p.waves) p.least_blocks = tokens < 4096 ? 1 : tokens < 16384 ? (uint32_t)(tokens / 2048) : 8;
   // Short sequences are not cut: parts of them would gain less than the launch that joins them costs (5 us, more for many rows).  The longer, the more
   // there is to do side by side anyway.  us cut and not, E5M2, heads of 64: a sequence of 468 tokens 12.0 and 11.0, of 625 12.0 and 13.2, 64 of
   // 1000 32.7 and 28.3; of 128: a sequence of 234 11.6 and 10.4, 8 of 468 12.6 and 15.0, 52 rows 8 of 400 19.4 and 15.7, 8 of 800 21.6
@@ -248,8 +245,12 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
     p.block_tokens = (uint32_t)kMostTokens;
     p.least_blocks = 1;
   }
+  // Over 4-bit words, whose blocks are small, a call is cut for up to eight of them each.  us with one, four and eight: a sequence of 8192 tokens 15.9, 15.1, 18.0, of
+  // 32768 22.0, 20.2, 19.0, of 131072 (four heads) 31.0, 31.0, 28.5, 16 of 4096 27.7, 27.6, 24.3.  (A bound on the workgroups, and none on what each takes: where a
+  // window leaves few blocks, they take one each.)
+  const uint32_t each = !fp4 || p.waves || p.block_tokens == kMostTokens ? p.least_blocks : tokens < 4096 ? 1 : tokens < 16384 ? (uint32_t)(tokens / 2048) : 8;
   const uint64_t blocks = q->n_seqs * (longest ? (longest + p.block_tokens - 1) / p.block_tokens : 1);   // by what the call says
-  if (shares > (blocks + p.least_blocks - 1) / p.least_blocks) shares = (blocks + p.least_blocks - 1) / p.least_blocks;
+  if (shares > (blocks + each - 1) / each) shares = (blocks + each - 1) / each;
   if (shares < 1) shares = 1;
   p.shares = (uint32_t)shares;
   p.wgs = (uint32_t)((shares * (c->kv_heads / p.heads_across) + 7) / 8 * 8 * p.row_tiles);
