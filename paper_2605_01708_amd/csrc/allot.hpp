@@ -11,6 +11,9 @@
 // Nothing here is much work: lengths, counts and page numbers, 32 bits each, and 16 bytes a row.  It is bound by latency, of the sums over
 // the sequences, which all else waits for.  One workgroup makes them, and what follows from them for lengths, starts, stack and tables; few rows are filled in by
 // it as well, many by a second launch.
+//
+// Bound by latency.  48 sequences with up to 5 rows each: 4.6 us.  1000 sequences that give 16 000 pages back, or take them: 11.9 us with eight pages at a time per
+// thread (four 12.2, sixteen 11.8; one at a time, and sums without DPP, 19.1); the entries of 250 000 rows 6.2 us (9.4 with every row's sequence looked for among all).
 #ifndef SPLITZIP_ALLOT_HPP
 #define SPLITZIP_ALLOT_HPP
 

@@ -26,7 +26,8 @@
 // rounding, since lse is a result in 32 bits.
 //
 // Two kernels: attention_tokens_kernel for up to 16 rows, whose waves take different tokens (memory's speed is all that
-// counts), and attention_rows_kernel, whose waves take different rows of the same tokens, staged in LDS.
+// counts), and attention_rows_kernel, whose waves take different rows of the same tokens, staged in LDS.  (Up to 16 rows over 4-bit words have a third,
+// attention_tokens4_kernel in attention4.hpp.)
 #ifndef SPLITZIP_ATTENTION_HPP
 #define SPLITZIP_ATTENTION_HPP
 
@@ -848,8 +849,9 @@ struct Stage {
         for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
       }
     }
-    if constexpr (kB == 4)   // (load_v fills eight: without these its last and the last of four become one store, to an address, and w memory: 164 us for 64 drafts that take ...)
-      for (int j = 4; j < 8; ++j) w[j] = 0;
+    if constexpr (kB == 4) {   // (load_v fills eight: without these its last and the last of four become one store, to an address, and w memory: 64 drafts of 16 sequences
+      for (int j = 4; j < 8; ++j) w[j] = 0;   // 168.6 us, 134.9 so)
+    }
     if constexpr (kB != 16) scales = *reinterpret_cast<const u32x2*>(c.k_scales + scale_offset(c, page, place, row));
   }
   __device__ void store_k(u32x4* to, uint32_t s, uint32_t m) const {

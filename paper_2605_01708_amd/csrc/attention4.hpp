@@ -6,6 +6,10 @@
 // many heads as make up a line (4 of 64 elements, 2 of 128, 1 of 256), its four waves bring whole lines of a stage's tokens into LDS, a quarter
 // each, and then work on a head and a part of the tokens each.  A stage is written into one half of LDS while the other is
 // worked on: one barrier a stage.
+//
+// Bound by memory and, behind it, by instructions: 64 sequences of 501 to 12000 tokens, 8 heads of 128, 437 MB in 82 us (5.3 TB/s); the same work on the first stage's
+// tokens alone, without further loads, 59.  131072 tokens of 4 heads: 19.5 us, 17 without further loads.  Three waves per SIMD: with the join 85.9 us
+// for the 64 sequences, two 86.9, four, with 35 to 39 registers in memory, 125 to 129.
 #ifndef SPLITZIP_ATTENTION4_HPP
 #define SPLITZIP_ATTENTION4_HPP
 

@@ -5,6 +5,7 @@
 //   allot.hpp       pages for a step's rows: tables, lengths and slots by what its requests ask for
 //   append.hpp      norms and rotation of Q and K on the way there
 //   attention.hpp   attention of a step's rows, one token or a tree of drafted ones, over everything cached
+//   attention4.hpp  the same for few rows over 4-bit words
 #include <float.h>
 #include <hip/hip_runtime.h>
 #include <stddef.h>
@@ -180,14 +181,16 @@ struct Append {
   }
 };
 
-// How an attention call is cut: which kernel, the rows of a (sequence, head of the cache) into tiles, the tokens of all sequences
-// into blocks and these into shares.
+// tokens of a stage of attention_tokens4_kernel
 uint32_t stage4_tokens(uint32_t head_dim, uint32_t heads) {
   return head_dim == 256 ? Stage4<256, 1>::kTokens : head_dim == 128 ? (heads == 2 ? Stage4<128, 2>::kTokens : Stage4<128, 1>::kTokens)
          : heads == 4 ? Stage4<64, 4>::kTokens : heads == 2 ? Stage4<64, 2>::kTokens : Stage4<64, 1>::kTokens;
 }
+
+// How an attention call is cut: which kernel, the rows of a (sequence, head of the cache) into tiles, the tokens of all sequences
+// into blocks and these into shares.
 struct AttentionPlan {
-  uint32_t waves, nt;   // waves 0: attention_tokens_kernel; else attention_rows_kernel with so many waves of 16 nt rows
+  uint32_t waves, nt;   // waves 0: attention_tokens_kernel, or over 4-bit words attention_tokens4_kernel; else attention_rows_kernel with so many waves of 16 nt rows
   uint32_t heads_across, tile_rows, row_tiles, most_rows, kept;
   uint32_t shares, block_tokens, least_blocks;
   uint32_t wgs;
