@@ -105,3 +105,36 @@ def test_steps_against_the_formulas(graph):
             top = np.repeat(np.abs(want).reshape(total, heads, -1, 32).max(-1), 32, -1)
             assert (np.abs(flat[which] - want) <= top / 3 * 1.01).all()           # (a step is 2 of 6 at the top, and the power up to twice what it need be)
         close(out, lse, attend(held, q_out.double().cpu().numpy(), 0.09))
+
+
+@pytest.mark.parametrize("pages", [-1, 0, 1])
+def test_a_pool_that_no_request_fits_is_refused(pages):
+    """16 tokens, one more by the captured step and one behind it: two pages"""
+    from paper_2605_01708_amd import decode_step
+
+    with pytest.raises(ValueError, match="needs 2 pages"):
+        decode_step.serve(sequences=1, tokens=16, steps=1, layers=1, pages=pages)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("args,dry", [(dict(sequences=8, tokens=300, steps=5, layers=2), False), (dict(sequences=1, tokens=16, steps=1, layers=1, pages=2), False),
+                                      (dict(sequences=5, tokens=200, steps=20, layers=1, pages=48), True), (dict(sequences=4, tokens=64, steps=40, layers=2, pages=16), True),
+                                      (dict(sequences=6, tokens=90, steps=33, layers=1, pages=8), True)])
+def test_no_step_is_lost_when_pages_run_out(args, dry):
+    """the oldest request has a token of every step, a request its prompt and a token of each step that it was in, one that waits nothing; what the last step
+    returns is attention over what the cache holds"""
+    from paper_2605_01708_amd import decode_step
+
+    outs, lens, waited, batch = decode_step.serve(**args)
+    torch.cuda.synchronize()
+    assert (waited > 0) == dry
+    assert lens[0] == args["tokens"] + args["steps"] + 1
+    if not dry:
+        assert lens == [n + (1 if s % 2 else args["steps"] + 1) for s, n in enumerate(batch.prompts)]
+    assert lens == [batch.prompts[s] + batch.decoded[s] if s in batch.running else 0 for s in range(batch.n)]
+    rows = [int(s in batch.running) for s in range(batch.n)]
+    for cache, q, out in zip(batch.caches, batch.queries, outs):
+        held = Held(cache, batch.table, lens, rows, decode_step.DIM, decode_step.PAGE)
+        assert out.shape == q.shape == (sum(rows), decode_step.KV_HEADS * decode_step.GROUP, decode_step.DIM)
+        want, lse, mean, dx = attend(held, q.double().cpu().numpy(), decode_step.DIM ** -0.5)
+        close(out, torch.from_numpy(lse), (want, lse, mean, dx))                    # (the program does not ask for lse)
