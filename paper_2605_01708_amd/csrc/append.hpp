@@ -157,8 +157,9 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
           float sum = 0.0f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) sum += y[e] * y[e];
+          sum *= 1.0f / D;   // (in front of the lanes' sum: 256 squares of 2^60 are 2^128)
           sum = __uint_as_float(of_lanes<(int)kLanes>(__float_as_uint(sum), [](uint32_t u, uint32_t v) { return __float_as_uint(__uint_as_float(u) + __uint_as_float(v)); }));
-          const float over = rsqrtf(sum * (1.0f / D) + a.eps);
+          const float over = rsqrtf(sum + a.eps);
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e] = y[e] * over * weight[e];
         }

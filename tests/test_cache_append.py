@@ -352,3 +352,20 @@ def test_calls_stay_in_their_buffers(kind, lens, starts, table):
     w = g(64, dtype=torch.float32, fill=torch.rand(64))
     call(st, sz.Rotation(freqs, False, 1.0, 1e-6, w, w, positions=g(40, dtype=I32, fill=torch.arange(40))), k_out=st.k_out)
     assert g.intact()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("kind", [sz.BF16, sz.FP8_E4M3])
+def test_norms_of_the_largest_magnitudes(kind, dim):
+    """elements of 2^60, all of them, some of them, and of what is next to nothing beside them"""
+    st = Step(kind, [20], [5], 3, 2, dim, seed=9)
+    big = 2.0 ** 60 * torch.where(torch.randn(st.qkv.shape, device="cuda", generator=torch.Generator("cuda").manual_seed(9)) > 0, 1.0, -1.0)
+    big[1, :, 1::2] = 0.0
+    big[2, :, 1:] = 2.0 ** -60
+    big[3] *= 2.0 ** -9
+    st.qkv.copy_(big)
+    st.qkv0 = st.qkv.clone()
+    for eps in (1e-6, 2.0 ** -126):
+        call(st, sz.Rotation(eps=eps), k_out=st.k_out)
+        check(st, st.q_out, st.k_out, (None, None), 0.0, eps, None, False, 1.0)
