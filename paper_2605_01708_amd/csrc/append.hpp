@@ -176,7 +176,11 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
       if (of_q || token < 0) continue;
       const uint32_t page = pages.page((uint32_t)token), place = pages.place((uint32_t)token);
       int byte = 0;
-      const Lane8<KIND> words = quantised<KIND, D>(y, byte);
+      Lane8<KIND> words = quantised<KIND, D>(y, byte);
+      if constexpr (KIND == SPLITZIP_BF16) {   // V as it came: rounding makes signalling NaN quiet
+#pragma unroll
+        for (int e = 0; e < 4; ++e) words[e] = of_k ? words[e] : byte_perm(__float_as_uint(y[2 * e + 1]), __float_as_uint(y[2 * e]), 0x07060302u);
+      }
       const uint64_t at = token_offset(a.cache, page, place) + head * a.cache.head_stride + lane * kBits<KIND>;
       *reinterpret_cast<Lane8<KIND>*>((of_k ? a.cache.k : a.cache.v) + at) = words;
       if constexpr (KIND != SPLITZIP_BF16) {

@@ -369,3 +369,24 @@ def test_norms_of_the_largest_magnitudes(kind, dim):
     for eps in (1e-6, 2.0 ** -126):
         call(st, sz.Rotation(eps=eps), k_out=st.k_out)
         check(st, st.q_out, st.k_out, (None, None), 0.0, eps, None, False, 1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_v_is_written_as_it_is(kind):
+    """every BF16 word: what cache_write makes of it, bit for bit, whatever K's norm and rotation are"""
+    a, b = (Step(kind, [200], [160], 3, 4, 128, seed=10) for _ in range(2))
+    words = torch.arange(65536, dtype=I32, device="cuda")
+    rows = torch.cat([words.view(128, 4, 128), words.view(-1, 128).T.reshape(-1)[:32 * 512].view(32, 4, 128)]).to(torch.int16)   # alike in size, and mixed
+    for st in (a, b):
+        st.v.view(torch.int16).copy_(rows)
+    call(a, sz.Rotation(freqs_of(64), eps=1e-6))
+    sz.cache_write(b.k, b.v, b.cache, b.seqs)
+    torch.cuda.synchronize()
+    x, y = a.kv[1], b.kv[1]
+    if kind != sz.BF16:
+        assert torch.equal(a.scales[1], b.scales[1])
+    if kind == sz.FP4_E2M1:                                          # (words under the byte 255 are not looked at)
+        fine = (a.scales[1] != 255).movedim(-1, 1).repeat_interleave(16, -1)
+        x, y = x[fine], y[fine]
+    assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
