@@ -1125,8 +1125,8 @@ class Rotation:
         if any(w.dim() != 1 or w.dtype not in (torch.bfloat16, torch.float32) or not w.is_contiguous() or w.shape != weights[0].shape
                or w.dtype != weights[0].dtype for w in weights):
             raise ValueError("weights must be contiguous [head_dim], both bfloat16 or both float32")
-        if positions is not None and (positions.dtype not in _INT32 or not positions.is_contiguous()):
-            raise ValueError("positions must be a contiguous tensor of 32-bit integers")
+        if positions is not None and (positions.dim() != 1 or positions.dtype not in _INT32 or not positions.is_contiguous()):
+            raise ValueError("positions must be a contiguous tensor [n_rows] of 32-bit integers")
         self._keep = (freqs, q_weight, k_weight, positions)
         self._reached = _reached(*self._keep)
         self.c = (_CRotationOf if self._reached else _CRotationElsewhere)(

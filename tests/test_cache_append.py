@@ -390,3 +390,9 @@ def test_v_is_written_as_it_is(kind):
         fine = (a.scales[1] != 255).movedim(-1, 1).repeat_interleave(16, -1)
         x, y = x[fine], y[fine]
     assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+def test_positions_are_one_for_each_row():
+    for t in (torch.zeros(5, 2, dtype=I32), torch.zeros((), dtype=I32)):
+        with pytest.raises(ValueError, match="positions"):
+            sz.Rotation(positions=t)
