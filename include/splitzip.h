@@ -641,8 +641,8 @@ typedef struct {
  * weight may be 2^8 until then, so that the tokens of a row with values of V
  * near 2^120 and above may sum up to an infinity.  In the product with V a weight is
  * 2^-15 of itself off at most where a head of the cache has up to 16 rows
- * (max_rows times its query heads) and words of 16 or 8 bits, and rounded to
- * BF16 (2^-8) where it has more rows, or words of 4 bits.  A row that sees nothing, or nothing but scores of minus infinity,
+ * (max_rows times its query heads), and rounded to BF16 (2^-8) where it has
+ * more.  A row that sees nothing, or nothing but scores of minus infinity,
  * gets zeros and lse = -infinity.  What a row does not see
  * does not touch it, whatever it holds; an infinity or a NaN of V that it sees
  * reaches it.  d_workspace: the parts of long sequences until they are joined,

@@ -7,9 +7,11 @@
 // each, and then work on a head and a part of the tokens each.  A stage is written into one half of LDS while the other is
 // worked on: one barrier a stage.
 //
-// Bound by memory and, behind it, by instructions: 64 sequences of 501 to 12000 tokens, 8 heads of 128, 437 MB in 82 us (5.3 TB/s); the same work on the first stage's
-// tokens alone, without further loads, 59.  131072 tokens of 4 heads: 19.5 us, 17 without further loads.  Three waves per SIMD: with the join 85.9 us
-// for the 64 sequences, two 86.9, four, with 35 to 39 registers in memory, 125 to 129.
+// Bound by memory and, behind it, by instructions: 64 sequences of 501 to 12000 tokens, 8 heads of 128, 437 MB in 84 us (5.2 TB/s); the same
+// work on the first stage's tokens alone, without further loads, 67.  131072 tokens of 4 heads: 20.7 us, 18.5 without further loads.  Three
+// waves per SIMD: with the join 87.2 us for the 64 sequences, two 90.8, four, with 36 registers in memory, 132.  Weights in two parts, as over
+// other words (attention.hpp); rounded to BF16 those 64 sequences take 86.3 us and 131072 tokens 27.5 for 28.5, and the result is 0.0021 of
+// itself off in place of its own rounding's 0.0016.  One head of 128, two of 64: 4 and 2 registers in memory (6 and none with caps or slopes).
 #ifndef SPLITZIP_ATTENTION4_HPP
 #define SPLITZIP_ATTENTION4_HPP
 
@@ -188,7 +190,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D
           if constexpr (!PLAIN) st.shape(w, bias, x, t8);
           if (__builtin_expect(!all, 0)) st.mask(w, r, x, t8);
           st.raise({st.highest(x[0]) * scale});
-          bf16x8 p[1][1];   // (rounded to BF16: words of V have two significant bits.  In two parts, as over other words, decode of 64 sequences 90.1 us for 85.9)
+          bf16x8 p[2][1];
           st.weigh(scale, x, p);
           uint32_t byte[8];
 #pragma unroll

@@ -474,3 +474,37 @@ def test_calls_stay_in_their_buffers(dim, rows, lens, starts, table):
         assert g.intact()
     sz.cache_move(sz.KvCaches([cache]), seqs, g(2, 3, dtype=I32, fill=torch.tensor([[0, 1, 7], [1, 0, -1]])), n_rows=n)
     assert g.intact()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,heads", [(64, 1), (64, 2), (64, 4), (128, 1), (128, 2), (256, 1)])
+@pytest.mark.parametrize("plain", [True, False])
+def test_weights_of_few_rows_keep_their_bits(dim, heads, plain):
+    """A token of weight 1 and zeros of V, the others of the weight (1 + 2^-8) 2^-k, which half a step of BF16 is short of or beyond: the result is what a
+    BF16 number can be nearest to the formula's, but for weights 2^-15 off, and as much of sums of up to 700 terms in 32 bits and 2^-18 of their
+    scores and powers: 2^-13."""
+    lens = [9, 17, 25, 30, 70, 300, 700]
+    w = World4(lens, [1] * len(lens), heads, dim, 16, seed=1)
+    group = 16
+    k, v = w.cache.k, w.cache.v
+    k.zero_()
+    k[..., 0] = 2                                                    # 1 in the first element
+    v.copy_(torch.tensor([0x21, 0x43, 0x65, 0x77, 0xa1, 0x7c], dtype=torch.uint8, device="cuda").repeat(43)[:dim // 2].expand_as(v))
+    w.scales.copy_(torch.where(w.scales == 255, 255, 127))
+    for s in range(len(lens)):
+        p, a = w.slot(s, 0)
+        k[p, a] = 0
+        v[p, a] = 0
+    byte = np.array([0x21, 0x43, 0x65, 0x77, 0xa1, 0x7c] * 43)[:dim // 2]
+    value = np.stack([WORDS[byte & 15], WORDS[byte >> 4]], -1).ravel()
+    q = torch.zeros(len(lens), heads * group, dim, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = -1
+    for power in range(1, 9):
+        scale = float(np.float32(power * np.log(2) - np.log1p(2.0 ** -8)))
+        out, lse = run(w, q, sz.Attention(scale) if plain else sz.Attention(scale, slopes=torch.zeros(heads * group, device="cuda")))
+        for s, n in enumerate(lens):
+            total = (n - 1) * np.exp(-scale)
+            want = value * total / (1 + total)
+            step = np.exp2(np.floor(np.log2(np.abs(want))) - 7)
+            assert (np.abs(out[s].double().cpu().numpy() - want) <= step / 2 + 2.0 ** -13 * np.abs(want)).all()
+            assert np.abs(lse[s].double().cpu().numpy() - np.log1p(total)).max() < 1e-5
