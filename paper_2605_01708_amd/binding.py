@@ -1147,6 +1147,8 @@ class PagePool:
                 raise ValueError("free and state must be contiguous tensors of 32-bit integers")
         if state.numel() != len(POOL_STATE):
             raise ValueError(f"state must have {len(POOL_STATE)} entries")
+        if free.numel() >> 31 or page_tokens >> 31:
+            raise ValueError("free must have less than 2^31 entries, page_tokens must be less and above 0")
         self._keep = (free, state)
         self._reached = _reached(*self._keep)
         self.c = (_CPool if self._reached else _CPoolElsewhere)(free.data_ptr(), state.data_ptr(), free.numel(), page_tokens, 0)
@@ -1247,6 +1249,8 @@ def cache_allot(pool: PagePool, seqs: Sequences, rows: torch.Tensor, keep: torch
     for t, types in ((slots, _INT64), (row_seqs, _INT32), (positions, _INT32)):
         if t is not None and (t.dim() != 1 or t.dtype not in types or not t.is_contiguous() or len(n_rows) != 1):
             raise ValueError("slots must be a contiguous tensor [n_rows] of 64-bit integers, row_seqs and positions as many of 32 bits")
+    if any(n >> 32 for n in n_rows):   # (the library's word for them has 32 bits; from 2^30 on it refuses them)
+        raise ValueError("slots, row_seqs and positions must have less than 2^32 entries")
     _need_reached(pool, seqs, rows, keep, slots, row_seqs, positions)
     _check(lib().splitzip_cache_allot(C.byref(pool.c), C.byref(seqs.c), rows.data_ptr(), _ptr(keep), _ptr(slots), _ptr(row_seqs), _ptr(positions),
                                       n_rows.pop() if n_rows else _MOST_ROWS, _stream_ptr(stream)), "splitzip_cache_allot")

@@ -326,7 +326,7 @@ bool run(const Bound& b, PyObject* const* a, Py_ssize_t n_args, int* rc) {
           break;
         }
         const at::Tensor* t = tensor(o);
-        if (!t || t->dim() != 1 || !t->is_contiguous() || (rows >= 0 && t->size(0) != rows)) return false;
+        if (!t || t->dim() != 1 || !t->is_contiguous() || (rows >= 0 && t->size(0) != rows) || t->size(0) >> 32) return false;   // (the library's word for them has 32 bits)
         const at::ScalarType type = t->scalar_type();
         if (*s == 'M' ? type != at::kLong && type != at::kUInt64 : type != at::kInt && type != at::kUInt32) return false;
         rows = t->size(0);

@@ -314,3 +314,16 @@ def test_calls_stay_in_their_buffers(lens, keep, free, n_rows, rows):
     got = outputs(n_rows, g)
     sz.cache_allot(d.pool, d.seqs, g(2, dtype=I32, fill=torch.tensor(rows, dtype=I32)), None if keep is None else g(2, dtype=I32, fill=torch.tensor(keep, dtype=I32)), *got)
     assert g.intact()
+
+
+def test_sizes_that_32_bits_do_not_hold_are_refused():
+    """(tensors without memory: nothing looks at more than their sizes)"""
+    large = lambda dtype: torch.empty((1 << 32) + 5, dtype=dtype, device="meta")   # noqa: E731
+    for k in (dict(slots=large(I64), row_seqs=None, positions=None), dict(slots=None, row_seqs=large(I32), positions=None), dict(slots=None, row_seqs=None, positions=large(I32)),
+              dict(free=torch.empty((1 << 32) + 4, dtype=I32, device="meta"))):
+        with pytest.raises(ValueError, match="must have"):
+            of_host("cpu", **k)()
+    z = torch.zeros(8, dtype=I32)
+    for page in ((1 << 32) + 16, -16):
+        with pytest.raises(ValueError, match="must be"):
+            sz.PagePool(z, z, page)
