@@ -508,3 +508,62 @@ def test_weights_of_few_rows_keep_their_bits(dim, heads, plain):
             step = np.exp2(np.floor(np.log2(np.abs(want))) - 7)
             assert (np.abs(out[s].double().cpu().numpy() - want) <= step / 2 + 2.0 ** -13 * np.abs(want)).all()
             assert np.abs(lse[s].double().cpu().numpy() - np.log1p(total)).max() < 1e-5
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,heads", [(64, 1), (64, 2), (64, 4), (128, 1), (128, 2), (128, 6), (256, 1), (256, 2)])
+@pytest.mark.parametrize("T,group,window,bias", [(4, 4, 0, False), (3, 5, 60, True), (8, 2, 37, False), (5, 3, 0, True), (16, 1, 9, True)])
+def test_trees_of_few_rows(dim, heads, T, group, window, bias):
+    """up to 16 rows of a head: trees with positions, under windows and slopes, a row that sees nothing among them"""
+    rng = np.random.default_rng(T + dim)
+    lens, rows = [T, T + 77, 300 + T, 1000 + T, 40], [T, T, max(T - 2, 1), T, 0]
+    w = World4(lens, rows, heads, dim, 16, seed=T)
+    bits, pos, sees = [], [], []
+    for s, (n, r) in enumerate(zip(lens, rows)):
+        if not r:
+            sees.append([])
+            continue
+        b, d, see = random_tree(r, rng, 1)
+        if s == 0:                                                   # (nothing lies in front of it)
+            b[-1], see[-1] = 0, 0
+        bits.append(b)
+        pos += [n - r + x for x in d]
+        sees.append(see)
+    q, qd = queries(w, group)
+    slopes = 2.0 ** -np.arange(1, heads * group + 1) if bias else None
+    how = sz.Attention(0.09, window=window, slopes=None if slopes is None else torch.tensor(slopes, dtype=torch.float32, device="cuda"),
+                       tree=torch.from_numpy(np.concatenate(bits)).cuda(), positions=torch.tensor(pos, dtype=I32, device="cuda"))
+    want = attend(w, q, 0.09, window=window, slopes=slopes, see=lambda s, i, j: sees[s][i] >> j & 1, positions=pos)
+    out, lse = run(w, qd, how)
+    close(out, lse, want)
+    assert (out[T - 1] == 0).all() and torch.isneginf(lse[T - 1]).all()
+    w.seqs = sz.Sequences(*w.dev, max_rows=T, max_len=30000)         # cut into parts
+    close(*run(w, qd, how), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,heads", [(64, 1), (64, 2), (64, 4), (128, 1), (128, 2), (128, 4), (256, 1), (256, 3)])
+@pytest.mark.parametrize("T,offset", [(2, 2), (2, 13), (5, 0), (5, 30), (8, 7)])
+def test_an_infinity_of_a_head_is_that_heads(dim, heads, T, offset):
+    """in the last tokens of each sequence, where rows see some and others not: it reaches the rows of its head that see it, in its element, and nothing else"""
+    lens = [n + T for n in (33, 64, 70, 100, 127, 160, 260, 705)]
+    w = World4(lens, [T] * len(lens), heads, dim, 16, seed=offset)
+    group, bad = 2, heads - 1
+    for s, n in enumerate(lens):
+        p, a = w.slot(s, n - 1 - offset)
+        w.cache.v[p, a, bad, 16:32] = 0x21                           # 1/2 and 1 ...
+        w.cache.v[p, a, bad, 16] = 0x2e                              # ... but for an infinity of -4 2^127, and 1
+        w.set_byte(s, n - 1 - offset, 1, bad, 1, 254)
+    q, qd = queries(w, group)
+    want = attend(w, q, 0.1)
+    out, lse = run(w, qd, sz.Attention(0.1))
+    sees = torch.tensor([i >= T - 1 - offset for _ in lens for i in range(T)], device="cuda")
+    mine = out[:, bad * group:]
+    assert torch.isneginf(mine[sees][..., 32]).all() and not torch.isnan(out).any()
+    out = out.clone()
+    out[..., bad * group:, 32:64][sees] = torch.from_numpy(want[0][:, bad * group:, 32:64]).to(torch.bfloat16).cuda()[sees]
+    # (the group's other elements are of other tokens' size there where the row does not see it)
+    hidden = ~sees.cpu().numpy()
+    clean = attend(w, q, 0.1)
+    close(out, lse, clean)
+    assert torch.isfinite(mine[~sees]).all() and hidden.sum() == (~sees).sum()
