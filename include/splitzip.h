@@ -559,7 +559,8 @@ typedef struct {
  * sequences must not overlap in time, nor calls that read those sequences with this one.
  * A step that cannot be taken (status) changes neither lengths, table nor pool;
  * d_starts is all 0 then, so that the step's other calls have no rows.
- * seqs needs a block table; its max_rows and max_len are not looked at.  One
+ * seqs needs a block table; its max_rows and max_len are not looked at.  A call
+ * without sequences (n_seqs 0) writes nothing, the state included.  One
  * launch up to 4096 rows, else two. */
 int splitzip_cache_allot(const splitzip_pool* pool, const splitzip_seqs* seqs, const int32_t* d_rows, const int32_t* d_keep,
                          int64_t* d_slots, int32_t* d_row_seqs, int32_t* d_positions, uint32_t n_rows, void* stream);

@@ -13,10 +13,11 @@
 // lanes read their eight elements' from LDS.  D / 8 lanes take a head, eight elements each, as in cache_write_kernel; what a lane's elements
 // are turned with lies in another lane of the same head.
 //
-// Bound by memory for long calls, by the launch for short ones.  16384 rows of 32 + 8 + 8 heads of 128 into E4M3, 369 MB: 68.4 us (5.4 TB/s; a plain
-// copy of that mix of reads and writes 5.6); streamed loads alone 73.3, streamed stores alone 70.2, neither 72.8.  The next row's words are asked for
-// before this one's are worked on, and a workgroup keeps its heads: a row at a time with all of its heads, 123 us.  Workgroups: 6 per CU 78.7, 12 78.5,
-// 24 73.9, 48 71.3, 96 as 48.
+// Bound by memory for long calls, by the launch for short ones.  16384 rows of 32 + 8 + 8 heads of 128 into E4M3, 369 MB: 68.3 us (5.4 TB/s; a plain
+// copy of that mix of reads and writes 5.6); streamed loads alone 73.4, streamed stores alone 70.6, neither 73.0; workgroups: 6 per CU 74.6, 12 73.4,
+// 24 70.2, 48 as it is, 96 68.4.  The next row's words are asked for before this one's are worked on, and a workgroup keeps its heads: the first form,
+// a row at a time with all of its heads, took 123.  A workgroup's lanes hold 16 heads of 128: of fewer heads the others do the last one's work once more
+// (42 sequences of 1660 rows, 4 + 2 heads of 128, E4M3: 78 us for 197 MB).
 #ifndef SPLITZIP_APPEND_HPP
 #define SPLITZIP_APPEND_HPP
 

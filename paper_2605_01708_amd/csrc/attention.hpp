@@ -20,7 +20,7 @@
 // beyond that, which a wave finds with one comparison and a ballot; weights up to 256 cost nothing in a floating format.  Statistics,
 // outputs and the sums over waves and over the parts of a long sequence are held in 32 bits.  V goes into the second product as BF16, and so
 // do the weights: up to 16 rows in two parts, which loses nothing that the BF16 result shows (memory's time hides the second product: 64
-// sequences of 700 to 8192 tokens 181.1 us, 180.7 with one part; 131072 tokens of E4M3 57.8 and 56.8); of more rows rounded (2^-8 of a weight, as the
+// sequences of 700 to 8192 tokens 181.1 us, 180.7 with one part; 131072 tokens of E4M3 57.8 and 56.8; over 4-bit words, where it does not hide all of it, see attention4.hpp); of more rows rounded (2^-8 of a weight, as the
 // result's own rounding; the error of the result against 64 bits is 0.0021 of it in place of 0.0017), since these kernels are bound by their
 // instructions: 16 trees of 64 rows over E5M2 136 us, 161 with two parts, a prompt of 2048 rows 112 and 121.  Their sum is taken before any
 // rounding, since lse is a result in 32 bits.
@@ -602,7 +602,7 @@ struct Stream {
   }
 };
 
-// The waves of a head (two or four of the workgroup's) together, and what they have of their rows to where it goes.  Lane (m, g) has elements
+// The waves of a head (one, two or four of the workgroup's) together, and what they have of their rows to where it goes.  Lane (m, g) has elements
 // D / 16 (4 g + i) + j of row m in acc[j][i].  room: 4 D bytes times 16 of LDS for each wave, room_bytes apart.
 template <int D>
 __device__ inline void finish_tokens(const Share& w, State<D, 1>& st, uint8_t* room, uint32_t room_bytes, float (*stat)[16][2], uint32_t wave, uint32_t lane, uint32_t hw) {

@@ -248,9 +248,14 @@ AttentionPlan plan_attention(const splitzip_cache* c, const splitzip_seqs* q, ui
     p.block_tokens = (uint32_t)kMostTokens;
     p.least_blocks = 1;
   }
-  // Over 4-bit words, whose blocks are small, a call is cut for up to eight of them each.  us with one, four and eight: a sequence of 8192 tokens 15.9, 15.1, 18.0, of
-  // 32768 22.0, 20.2, 19.0, of 131072 (four heads) 31.0, 31.0, 28.5, 16 of 4096 27.7, 27.6, 24.3.  (A bound on the workgroups, and none on what each takes: where a
-  // window leaves few blocks, they take one each.)
+  // Over 4-bit words, whose blocks are small, a call is cut for up to eight of them each, by its tokens.  us as cut here, and for one, four and eight of them; heads of 128:
+  //   a sequence of                8192 tokens, one head  13.9  11.8 14.0 17.6    eight heads 14.5  15.5 14.6 18.0
+  //   a sequence of               32768                   18.1  15.8 14.8 18.0                19.1  21.3 20.1 19.1
+  //   a sequence of              131072                   20.1  29.5 19.0 20.1                39.0  38.4 39.1 37.6
+  //   16 of 4096                                          18.4  14.1 14.8 18.4                25.1  28.1 28.2 25.1
+  //   8 of 2265                                           21.1  12.0 17.8 21.2                21.5  16.7 17.3 21.5
+  // Eight are right where they leave the chip full; with few heads, or sequences of a few blocks, they leave workgroups out that the call has work for: heads are
+  // not counted here.  (A bound on the workgroups, and none on what each takes: where a window leaves few blocks, they take one each.)
   const uint32_t each = !fp4 || p.waves || p.block_tokens == kMostTokens ? p.least_blocks : tokens < 4096 ? 1 : tokens < 16384 ? (uint32_t)(tokens / 2048) : 8;
   const uint64_t blocks = q->n_seqs * (longest ? (longest + p.block_tokens - 1) / p.block_tokens : 1);   // by what the call says
   if (shares > (blocks + each - 1) / each) shares = (blocks + each - 1) / each;
